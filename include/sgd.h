@@ -367,6 +367,24 @@ SGD_API int sgd_step_profile(sgd_ctx* ctx, const void* state_in_dev, void* out_d
 SGD_API int sgd_sampler_update(float* z_dev, const float* eps_dev, float alpha, float beta, int64_t n,
                        void* stream);
 
+/*
+ * sgd_sampler_reveal — the sampler update of a masked-token model (SGD_STEM_EMBED): of every
+ * sample's positions with ids == mask_id, inside its window, the n_reveal[b] with the best scores
+ * take their candidates; every other position of ids_out is that of ids.  Asynchronous on `stream`.
+ * ids, ids_out int32 [batch, n_tokens] (ids_out may be ids; no other output may overlap an input);
+ * cand int32 and score fp32: position n of sample b at [(b n_tokens + n) stride] (stride >= 1: a
+ * column of sgd_kernel_logprobs' [rows, top_k] outputs).  Best is largest, or smallest with lowest
+ * != 0 (entropies); equal scores (-0 and +0 are equal) go to the lower position, NaN is worse than all others.
+ * n_reveal int32 [batch] on the device: below 0 is 0, more than there are takes all.  window int32
+ * [batch, 2] (first and end position, cut to [0, n_tokens]; NULL: the whole sample).  n_left int32
+ * [batch] (may be NULL): positions of ids_out that were masked and were not chosen.
+ * n_tokens <= 49152 (else SGD_ERR_SHAPE).
+ */
+SGD_API int sgd_sampler_reveal(const int32_t* ids_dev, const int32_t* cand_dev, int64_t cand_stride,
+                       const float* score_dev, int64_t score_stride, int lowest, const int32_t* n_reveal_dev,
+                       const int32_t* window_dev, int32_t* ids_out_dev, int32_t* n_left_dev, int batch,
+                       int n_tokens, int mask_id, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

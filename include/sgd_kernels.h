@@ -203,6 +203,66 @@ SGD_API int sgd_kernel_norm(const float* h, void* out, int rows, int d, int kind
 SGD_API int sgd_kernel_frozen_run(float* h, const void* const* caches_host, int n_caches, int64_t n,
                           void* stream);
 
+/* Element type of a row of logits or of its gradient. */
+typedef enum { SGD_F16 = 0, SGD_BF16 = 1, SGD_F32 = 2 } sgd_dtype;
+
+/*
+ * Log-probabilities of given tokens, entropy and the likeliest tokens of rows of logits (such as a
+ * step of a SGD_HEAD_LOGITS model writes).  With p = softmax(scale * logits[r, :]), ln p
+ * computed in fp32 whatever the logits' type:
+ *   token_logprobs fp32 [rows, n_tokens] = ln p of tokens int32 [rows, n_tokens]; 0 where the token is
+ *     negative (padding), NaN where it is not below vocab;
+ *   entropy fp32 [rows] = - sum p ln p (0 ln 0 = 0);
+ *   top_ids int32 [rows, top_k], top_logprobs fp32 [rows, top_k]: the tokens of the largest logits, in
+ *     descending order, equal logits (-0 and +0 are equal) in the order of the token.
+ * Any of the outputs may be NULL (tokens with n_tokens = 0), but not all.
+ * logits [rows, vocab] of type dtype, rows ld elements apart, aligned to their elements alone.
+ * scale > 0 (1 / temperature).  row_ids int32 [rows]: where given, only rows with row_ids[r] == row_id
+ * (positions that are still masked, say) are read, and what the others' outputs held stays.
+ * -inf masks a token: its ln p is -inf.  A row of -inf alone has ln p = -inf, entropy 0 and the
+ * top tokens 0, 1, ...; a row that holds NaN or +inf has NaN for every ln p and for the entropy,
+ * and NaN ranks with -inf.
+ * 0 <= top_k <= 64 and <= vocab; vocab * element size <= 3 MiB (else SGD_ERR_SHAPE).  No workspace:
+ * calls on several streams and replays of captured ones may overlap.  Results are the same on
+ * every run.
+ */
+SGD_API int sgd_kernel_logprobs(const void* logits, int dtype, int64_t ld, int rows, int vocab, float scale,
+                                const int32_t* row_ids, int row_id, const int32_t* tokens, int n_tokens,
+                                float* token_logprobs, float* entropy, int top_k, int32_t* top_ids,
+                                float* top_logprobs, void* stream);
+
+/* What a teacher's list says of the tokens that are not in it (sgd_kernel_distill). */
+typedef enum {
+  SGD_TAIL_RENORM = 0,  /* nothing: the list's probabilities are divided by their sum          */
+  SGD_TAIL_BUCKET = 1   /* together they have what is left of 1: one more outcome, "any other" */
+} sgd_tail_kind;
+
+/*
+ * Divergence of rows of logits from a teacher's likeliest tokens, with its gradient (the full
+ * model's lists from sgd_kernel_logprobs against a scheduled model's logits, say).  With
+ * p = softmax(scale * logits[r, :]), the list's tokens S and q_i = exp(teacher_logprobs_i), Q = sum q_i:
+ *   SGD_TAIL_RENORM: L = sum_S (q_i / Q) (ln (q_i / Q) - ln p_i);
+ *   SGD_TAIL_BUCKET: L = sum_S q_i (ln q_i - ln p_i) + q_T (ln q_T - ln p_T), q_T = max(0, 1 - Q),
+ *                    p_T = sum of p outside S; the second term is left out where q_T or p_T is 0;
+ *   loss fp32 [rows] = w_r L;  grad [rows, vocab] = w_r dL / dlogits (NULL: the loss alone).
+ * top_k = 1 with teacher_logprobs 0 and SGD_TAIL_RENORM is the cross entropy of the listed token.
+ * logits [rows, vocab] of type dtype, rows ld elements apart; teacher_ids int32 and teacher_logprobs
+ * fp32 [rows, top_k].  An id outside [0, vocab) pads the list; of ids that are equal the first counts.
+ * row_weight fp32 [rows] (NULL: 1): the logits of rows of weight 0 are not read, their loss and
+ * gradient are 0; so are those of a row whose list has no token (SGD_TAIL_RENORM: or Q = 0).
+ * -inf masks a token (p = 0): the loss is +inf where the list gives it weight, the gradient finite.
+ * NaN in a row, or +inf, makes its loss and gradient NaN.
+ * grad of type grad_dtype, rows ld_grad elements apart, each value rounded once from fp32 (out of
+ * fp16's range: inf).  grad may be logits itself (same type and ld); it must not overlap it
+ * otherwise (SGD_ERR_ARG).  1 <= top_k <= 64; vocab * element size of logits <= 3 MiB (else SGD_ERR_SHAPE).
+ * No workspace: calls on several streams and replays of captured ones may overlap.  Results are
+ * the same on every run.
+ */
+SGD_API int sgd_kernel_distill(const void* logits, int dtype, int64_t ld, int rows, int vocab, float scale,
+                               const int32_t* teacher_ids, const float* teacher_logprobs, int top_k,
+                               const float* row_weight, int tail, float* loss, void* grad, int grad_dtype,
+                               int64_t ld_grad, void* stream);
+
 /* Device status word shared by all kernels (bounded-wait expiry); returns and clears it. */
 SGD_API int sgd_kernel_status(int* status_host);
 

@@ -56,9 +56,13 @@ EXPORTED = [
     "sgd_set_exec_mode", "sgd_step_host_async", "sgd_host_wait", "sgd_kernel_gemm_static_ws",
     "sgd_set_policy", "sgd_get_drift", "sgd_selftest_wait_timeout", "sgd_kernel_f16_clamped",
     "sgd_kernel_gemm_stat_slots", "sgd_kernel_attention_hs", "sgd_kernel_dependent_launches", "sgd_kernel_gemm_tile",
+    "sgd_kernel_logprobs", "sgd_kernel_distill", "sgd_sampler_reveal",
 ]
 EXEC_JAGGED_GRAPH, EXEC_EAGER, EXEC_PADDED_GRAPH = 0, 1, 2
 POLICY_STATIC, POLICY_DRIFT = 0, 1
+DTYPE_NAMES = {"torch.float16": 0, "torch.bfloat16": 1, "torch.float32": 2}  # sgd_dtype
+TAIL_RENORM, TAIL_BUCKET = 0, 1
+TAIL = {"renorm": TAIL_RENORM, "bucket": TAIL_BUCKET}
 
 
 class sgd_model_desc(C.Structure):
@@ -157,6 +161,9 @@ def lib() -> C.CDLL:
             "sgd_set_policy": (i, [vp, i]),
             "sgd_selftest_wait_timeout": (i, [vp]),
             "sgd_get_drift": (i, [vp, i, vp, i]),
+            "sgd_kernel_logprobs": (i, [vp, i, i64, i, i, f, vp, i, vp, i, vp, vp, i, vp, vp, vp]),
+            "sgd_kernel_distill": (i, [vp, i, i64, i, i, f, vp, vp, i, vp, i, vp, vp, i, i64, vp]),
+            "sgd_sampler_reveal": (i, [vp, vp, i64, vp, i64, i, vp, vp, vp, vp, i, i, i, vp]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)
@@ -283,6 +290,138 @@ def sgd_kernel_f16_clamped() -> int:
 def sgd_sampler_update(z, eps, alpha, beta, stream=None):
     return check(lib().sgd_sampler_update(_ptr(z), _ptr(eps), alpha, beta, z.numel(),
                                           _stream(stream)), "sgd_sampler_update")
+
+
+# The operators on a token model's logits take tensors whose sizes are checked here, as the C side
+# sees only pointers: shapes, types and devices (TypeError / ValueError), before anything is launched.
+
+def _tensor(t, name, dtype, shape, device):
+    """`t` (or None): a dense tensor of this type, shape and device."""
+    if t is None:
+        return None
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _rows(t, name):
+    """(type, row stride) of a [rows, vocab] tensor on a CUDA device with dense rows."""
+    kind = DTYPE_NAMES.get(str(t.dtype))
+    if kind is None:
+        raise TypeError(f"{name} must be float16, bfloat16 or float32, not {t.dtype}")
+    if t.dim() != 2 or not t.is_cuda:
+        raise ValueError(f"{name} must be a 2-d tensor on a CUDA device")
+    rows, vocab = t.shape
+    ld, step = t.stride()
+    if step != 1 and vocab > 1:
+        raise ValueError(f"the rows of {name} must be dense")
+    return kind, ld if rows > 1 else max(ld, vocab)
+
+
+def _call_on(device, name, stream, *args):
+    """The library launches on the current device: that of the tensors, for the time of the call."""
+    import torch
+    if torch.cuda.current_device() == device.index:
+        return check(getattr(lib(), name)(*args, _stream(stream)), name)
+    with torch.cuda.device(device):
+        return check(getattr(lib(), name)(*args, _stream(stream)), name)
+
+
+def sgd_kernel_logprobs(logits, tokens=None, token_logprobs=None, entropy=None, top_ids=None, top_logprobs=None,
+                        scale=1.0, row_ids=None, row_id=0, stream=None):
+    """Log-probabilities of given tokens, entropy and likeliest tokens of logits [rows, vocab] (any row
+    stride), into the output tensors that are given: token_logprobs float32 [rows, n] for tokens int32
+    [rows, n], entropy float32 [rows], top_ids int32 and top_logprobs float32 [rows, k].  With row_ids
+    (int32 [rows]) only rows whose entry is row_id are read and written."""
+    import torch
+    kind, ld = _rows(logits, "logits")
+    rows, vocab = logits.shape
+    device, i32, f32 = logits.device, torch.int32, torch.float32
+    if (tokens is None) != (token_logprobs is None):
+        raise ValueError("tokens and token_logprobs go together")
+    n = 0
+    if tokens is not None:
+        if tokens.dim() != 2:
+            raise ValueError("tokens must have the shape [rows, n]")
+        n = tokens.shape[1]
+    top = top_ids if top_ids is not None else top_logprobs
+    k = 0
+    if top is not None:
+        if top.dim() != 2:
+            raise ValueError("top_ids and top_logprobs must have the shape [rows, k]")
+        k = top.shape[1]
+    return _call_on(device, "sgd_kernel_logprobs", stream, logits.data_ptr(), kind, ld, rows, vocab, scale,
+                    _tensor(row_ids, "row_ids", i32, (rows,), device), row_id,
+                    _tensor(tokens, "tokens", i32, (rows, n), device), n,
+                    _tensor(token_logprobs, "token_logprobs", f32, (rows, n), device),
+                    _tensor(entropy, "entropy", f32, (rows,), device), k,
+                    _tensor(top_ids, "top_ids", i32, (rows, k), device),
+                    _tensor(top_logprobs, "top_logprobs", f32, (rows, k), device))
+
+
+def sgd_kernel_distill(logits, teacher_ids, teacher_logprobs, loss, grad=None, row_weight=None, tail=TAIL_BUCKET,
+                       scale=1.0, stream=None):
+    """Divergence of logits [rows, vocab] from the teacher's lists [rows, k] (sgd_kernel_logprobs' top_ids and
+    top_logprobs), into loss float32 [rows] and, where given, its gradient [rows, vocab] of any of the
+    three types (or logits itself)."""
+    import torch
+    kind, ld = _rows(logits, "logits")
+    rows, vocab = logits.shape
+    device = logits.device
+    if teacher_ids.dim() != 2:
+        raise ValueError("teacher_ids must have the shape [rows, k]")
+    k = teacher_ids.shape[1]
+    gkind = ldg = 0
+    if grad is not None:
+        gkind, ldg = _rows(grad, "grad")
+        if grad.shape != logits.shape or grad.device != device:
+            raise ValueError("grad must have the shape and the device of logits")
+    return _call_on(device, "sgd_kernel_distill", stream, logits.data_ptr(), kind, ld, rows, vocab, scale,
+                    _tensor(teacher_ids, "teacher_ids", torch.int32, (rows, k), device),
+                    _tensor(teacher_logprobs, "teacher_logprobs", torch.float32, (rows, k), device), k,
+                    _tensor(row_weight, "row_weight", torch.float32, (rows,), device), tail,
+                    _tensor(loss, "loss", torch.float32, (rows,), device),
+                    None if grad is None else grad.data_ptr(), gkind, ldg)
+
+
+def _column(t, name, dtype, shape, device):
+    """(pointer, stride) of a [batch, n_tokens] tensor whose positions are evenly spaced (a column of a
+    [batch, n_tokens, k] one, say)."""
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
+    if t.shape != shape or t.device != device:
+        raise ValueError(f"{name} must have the shape {tuple(shape)} and be on {device}")
+    a, b = t.stride()
+    if shape[1] <= 1:
+        b = a
+    if shape[0] > 1 and a != b * shape[1]:
+        raise ValueError(f"the positions of {name} must be evenly spaced")
+    return t.data_ptr(), max(b, 1)
+
+
+def sgd_sampler_reveal(ids, cand, score, n_reveal, ids_out, mask_id, lowest=False, window=None, n_left=None,
+                       stream=None):
+    """The masked positions of ids int32 [batch, n_tokens] with the best scores (n_reveal int32 [batch] of them;
+    window int32 [batch, 2]: between these positions) take their candidates in ids_out (which may
+    be ids); n_left int32 [batch]: masked positions that remain."""
+    import torch
+    if ids.dim() != 2 or not ids.is_cuda:
+        raise ValueError("ids must be a 2-d tensor on a CUDA device")
+    device, shape, i32 = ids.device, ids.shape, torch.int32
+    batch, n = shape
+    pc, sc = _column(cand, "cand", i32, shape, device)
+    ps, ss = _column(score, "score", torch.float32, shape, device)
+    return _call_on(device, "sgd_sampler_reveal", stream, _tensor(ids, "ids", i32, shape, device), pc, sc, ps, ss,
+                    int(lowest), _tensor(n_reveal, "n_reveal", i32, (batch,), device),
+                    _tensor(window, "window", i32, (batch, 2), device),
+                    _tensor(ids_out, "ids_out", i32, shape, device),
+                    _tensor(n_left, "n_left", i32, (batch,), device), batch, n, mask_id)
 
 
 def make_desc(cfg, flags: int = 0) -> sgd_model_desc:

@@ -79,6 +79,7 @@ struct Op {
   std::function<cudaError_t(cudaStream_t)> run;
 };
 
+bool al4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 bool al16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 int validate_schedule(int T, int n_units, const int32_t* S, const int32_t* groups,
@@ -1710,6 +1711,23 @@ int sgd_sampler_update(float* z, const float* eps, float alpha, float beta, int6
   return SGD_OK;
 }
 
+int sgd_sampler_reveal(const int32_t* ids, const int32_t* cand, int64_t cand_stride, const float* score,
+                       int64_t score_stride, int lowest, const int32_t* n_reveal, const int32_t* window,
+                       int32_t* ids_out, int32_t* n_left, int batch, int n_tokens, int mask_id, void* stream) {
+  if (!ids || !cand || !score || !n_reveal || !ids_out) return fail(SGD_ERR_ARG, "reveal: null argument");
+  if (batch < 0 || n_tokens < 0 || cand_stride < 1 || score_stride < 1)
+    return fail(SGD_ERR_ARG, "reveal: negative size, or a stride below 1");
+  if (!al4(ids) || !al4(cand) || !al4(score) || !al4(n_reveal) || !al4(window) || !al4(ids_out) || !al4(n_left))
+    return fail(SGD_ERR_ARG, "reveal: pointers must be 4-byte aligned");
+  if (n_tokens > kRevealMaxTokens)
+    return fail(SGD_ERR_SHAPE, "reveal: n_tokens is above " + std::to_string(kRevealMaxTokens));
+  if (batch == 0 || (n_tokens == 0 && !n_left)) return SGD_OK;
+  const RevealParams p{ids, cand, cand_stride, score, score_stride, lowest, n_reveal, window, ids_out, n_left,
+                       batch, n_tokens, mask_id};
+  CUDA_TRY(reveal_launch(p, static_cast<cudaStream_t>(stream)));
+  return SGD_OK;
+}
+
 // ----- kernel-level entry points (include/sgd_kernels.h) -----
 
 namespace {
@@ -1932,6 +1950,76 @@ int sgd_kernel_frozen_run(float* h, const void* const* caches, int n_caches, int
     p.caches[i] = H16(caches[i]);
   }
   CUDA_TRY(frozen_launch(p, static_cast<cudaStream_t>(stream)));
+  return SGD_OK;
+}
+
+namespace {
+
+int elem_size(int dtype) { return dtype == SGD_F32 ? 4 : 2; }
+
+// What the two operators on rows of logits ask of them.
+int check_rows(const char* name, const void* logits, int dtype, int64_t ld, int rows, int vocab, float scale) {
+  const std::string n = std::string(name) + ": ";
+  if (!logits) return fail(SGD_ERR_ARG, n + "null logits");
+  if (dtype < SGD_F16 || dtype > SGD_F32) return fail(SGD_ERR_ARG, n + "unknown element type");
+  if (rows < 0 || vocab < 1 || ld < vocab) return fail(SGD_ERR_ARG, n + "rows >= 0, vocab >= 1 and ld >= vocab are needed");
+  if (!(scale > 0.f) || !std::isfinite(scale)) return fail(SGD_ERR_ARG, n + "scale must be positive and finite");
+  if (reinterpret_cast<uintptr_t>(logits) % elem_size(dtype)) return fail(SGD_ERR_ARG, n + "misaligned logits");
+  if (static_cast<int64_t>(vocab) * elem_size(dtype) > kMaxRowBytes)
+    return fail(SGD_ERR_SHAPE, n + "a row of more than 3 MiB");
+  if (rows > kMaxRows) return fail(SGD_ERR_SHAPE, n + "more than " + std::to_string(kMaxRows) + " rows");
+  return SGD_OK;
+}
+
+}  // namespace
+
+int sgd_kernel_logprobs(const void* logits, int dtype, int64_t ld, int rows, int vocab, float scale,
+                        const int32_t* row_ids, int row_id, const int32_t* tokens, int n_tokens,
+                        float* token_logprobs, float* entropy, int top_k, int32_t* top_ids, float* top_logprobs,
+                        void* stream) {
+  const int rc = check_rows("logprobs", logits, dtype, ld, rows, vocab, scale);
+  if (rc) return rc;
+  if (n_tokens < 0 || (n_tokens > 0) != (tokens && token_logprobs))
+    return fail(SGD_ERR_ARG, "logprobs: n_tokens, tokens and token_logprobs go together");
+  if (top_k < 0 || top_k > kMaxTop || top_k > vocab)
+    return fail(SGD_ERR_ARG, "logprobs: top_k must be in 0..64 and at most vocab");
+  if ((top_k > 0) != (top_ids || top_logprobs))
+    return fail(SGD_ERR_ARG, "logprobs: top_k goes with top_ids or top_logprobs");
+  if (!n_tokens && !entropy && !top_k) return fail(SGD_ERR_ARG, "logprobs: no output asked for");
+  if (!al4(row_ids) || !al4(tokens) || !al4(token_logprobs) || !al4(entropy) || !al4(top_ids) || !al4(top_logprobs))
+    return fail(SGD_ERR_ARG, "logprobs: pointers must be 4-byte aligned");
+  if (rows == 0) return SGD_OK;
+  const LogprobsParams p{logits, dtype, ld, rows, vocab, scale, row_ids, row_id, tokens, n_tokens,
+                         token_logprobs, entropy, top_k, top_ids, top_logprobs};
+  CUDA_TRY(logprobs_launch(p, static_cast<cudaStream_t>(stream)));
+  return SGD_OK;
+}
+
+int sgd_kernel_distill(const void* logits, int dtype, int64_t ld, int rows, int vocab, float scale,
+                       const int32_t* teacher_ids, const float* teacher_logprobs, int top_k,
+                       const float* row_weight, int tail, float* loss, void* grad, int grad_dtype,
+                       int64_t ld_grad, void* stream) {
+  const int rc = check_rows("distill", logits, dtype, ld, rows, vocab, scale);
+  if (rc) return rc;
+  if (!teacher_ids || !teacher_logprobs || !loss) return fail(SGD_ERR_ARG, "distill: null argument");
+  if (top_k < 1 || top_k > kMaxTop) return fail(SGD_ERR_ARG, "distill: top_k must be in 1..64");
+  if (tail != SGD_TAIL_RENORM && tail != SGD_TAIL_BUCKET) return fail(SGD_ERR_ARG, "distill: unknown kind of tail");
+  if (!al4(teacher_ids) || !al4(teacher_logprobs) || !al4(row_weight) || !al4(loss))
+    return fail(SGD_ERR_ARG, "distill: pointers must be 4-byte aligned");
+  if (grad) {
+    if (grad_dtype < SGD_F16 || grad_dtype > SGD_F32) return fail(SGD_ERR_ARG, "distill: unknown type of the gradient");
+    if (ld_grad < vocab || reinterpret_cast<uintptr_t>(grad) % elem_size(grad_dtype))
+      return fail(SGD_ERR_ARG, "distill: ld_grad < vocab, or a misaligned gradient");
+    const uintptr_t a = reinterpret_cast<uintptr_t>(logits), g = reinterpret_cast<uintptr_t>(grad);
+    const uintptr_t an = (static_cast<uintptr_t>(rows ? rows - 1 : 0) * ld + vocab) * elem_size(dtype);
+    const uintptr_t gn = (static_cast<uintptr_t>(rows ? rows - 1 : 0) * ld_grad + vocab) * elem_size(grad_dtype);
+    if (!(a == g && dtype == grad_dtype && ld == ld_grad) && a < g + gn && g < a + an)
+      return fail(SGD_ERR_ARG, "distill: the gradient overlaps the logits without being them");
+  }
+  if (rows == 0) return SGD_OK;
+  const DistillParams p{logits, dtype, ld, rows, vocab, scale, teacher_ids, teacher_logprobs, top_k, row_weight, tail,
+                        loss, grad, grad_dtype, ld_grad};
+  CUDA_TRY(distill_launch(p, static_cast<cudaStream_t>(stream)));
   return SGD_OK;
 }
 

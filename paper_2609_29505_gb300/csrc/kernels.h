@@ -304,4 +304,65 @@ cudaError_t rowdot_bf16_launch(const bf16* w, const bf16* x, int64_t rows, int K
 cudaError_t sampler_launch(float* z, const float* eps, float alpha, float beta, int64_t n,
                            cudaStream_t s);
 
+// Limits of the operators on rows of logits: a row is held by a cluster of at most 16 CTAs (the grid has
+// one per row), 192 KB each.
+constexpr int64_t kMaxRowBytes = 3ll << 20;
+constexpr int kMaxRows = 0x7FFFFFFF / 16;
+constexpr int kMaxTop = 64;
+
+// Rows of logits (sgd_kernel_logprobs).  dtype: sgd_dtype.
+struct LogprobsParams {
+  const void* logits;
+  int dtype;
+  int64_t ld;
+  int rows, vocab;
+  float scale;
+  const int32_t* row_ids;
+  int row_id;
+  const int32_t* tokens;
+  int n_tokens;
+  float* token_logprobs;
+  float* entropy;
+  int top_k;
+  int32_t* top_ids;
+  float* top_logprobs;
+};
+cudaError_t logprobs_launch(const LogprobsParams& p, cudaStream_t s);
+
+// Loss and gradient against another model's likeliest tokens (sgd_kernel_distill).
+struct DistillParams {
+  const void* logits;
+  int dtype;
+  int64_t ld;
+  int rows, vocab;
+  float scale;
+  const int32_t* ids;
+  const float* logq;
+  int k;
+  const float* weight;
+  int tail;
+  float* loss;
+  void* grad;
+  int grad_dtype;
+  int64_t ld_grad;
+};
+cudaError_t distill_launch(const DistillParams& p, cudaStream_t s);
+
+// Reveal step of the masked-token sampler (sgd_sampler_reveal).
+constexpr int kRevealMaxTokens = 49152;  // a sample's keys in shared memory: 192 KB
+struct RevealParams {
+  const int32_t* ids;
+  const int32_t* cand;
+  int64_t cand_stride;
+  const float* score;
+  int64_t score_stride;
+  int lowest;
+  const int32_t* n_reveal;
+  const int32_t* window;
+  int32_t* ids_out;
+  int32_t* n_left;
+  int batch, n_tokens, mask_id;
+};
+cudaError_t reveal_launch(const RevealParams& p, cudaStream_t s);
+
 }  // namespace sgd
