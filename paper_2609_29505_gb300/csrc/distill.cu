@@ -128,8 +128,7 @@ __global__ void __launch_bounds__(kThreads, 3) distill_kernel(const Params p) {
   __shared__ float list_z[kMaxList];  // leader: the list's logits
   __shared__ double loss_sum[2];
   const int rank = cluster_rank();
-  uint32_t n_ctas;
-  asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(n_ctas));
+  const uint32_t n_ctas = cluster_ctas();
   const int64_t r = blockIdx.x / n_ctas;
   const T* row = static_cast<const T*>(p.logits) + r * p.ld;
   const Slice<T> sl(row, p.vocab, rank, n_ctas);
@@ -209,13 +208,7 @@ __global__ void __launch_bounds__(kThreads, 3) distill_kernel(const Params p) {
 
   const float c = p.scale * kLog2e;
   Stat st;
-  const uint4 none = [] {
-    uint4 v;
-    T* e = reinterpret_cast<T*>(&v);
-#pragma unroll
-    for (int j = 0; j < E; ++j) e[j] = neg_inf<T>();
-    return v;
-  }();
+  const uint4 none = no_elements<T>();
   for (int i = 0; i < sl.nv; i += kPiece) {
     uint4 v[kUnroll];
 #pragma unroll

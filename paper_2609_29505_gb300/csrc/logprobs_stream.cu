@@ -1,0 +1,495 @@
+// Scoring of many long rows (logprobs.cu has the formulas): the rows stream through the SMs.
+//
+// One CTA per SM stays for the whole call.  A producer warp keeps a ring of 16 KB tiles filled by bulk
+// copies, across the ends of rows; 8 warps take the tiles' statistics and never wait for anything but
+// data; 4 warps finish a row (sums, likeliest tokens, outputs) while the others are at the next one.
+// Where there are too few rows for the SMs, the CTAs of a cluster share each row and the first of
+// them merges their parts.
+//
+// The likeliest tokens without a second pass over the row: the streaming warps leave the maximum of
+// each group of vectors (of one thread, in consecutive tiles; at most 4096 groups).  The k-th largest of
+// the 256 threads' maxima is a threshold that k elements or a few more reach; only the groups whose
+// maximum reaches it are read again (some 64 bytes each, from L2).  For the single likeliest token
+// the tile of each thread's first maximum is enough.
+//
+// Every wait is bounded.  After one has expired (recorded in the status word) each role leaves its loop;
+// the teams that share a hardware barrier leave together.
+#include "logprobs.cuh"
+
+namespace sgd {
+namespace rows {
+namespace {
+
+constexpr int kStreamWarps = 8, kStreamThreads = 32 * kStreamWarps;  // = kThreads: a tile is kPiece vectors
+constexpr int kFinishWarps = 4, kFinishThreads = 32 * kFinishWarps;
+constexpr int kAll = kStreamThreads + kFinishThreads + 32;
+constexpr int kSlots = 10;
+constexpr int kTileBytes = kPiece * 16;
+constexpr int kGroupTiles = 16;  // groups of one thread
+constexpr int kMaxGroups = 1024; // groups read again
+constexpr int kStreamCluster = 8;
+static_assert(kStreamThreads == kThreads, "a tile is a vector of every thread, kUnroll times");
+
+using Finishers = Team<kFinishThreads, 1>;
+
+struct Shared {
+  uint64_t full[kSlots], empty[kSlots];
+  uint64_t part_full[2], part_free[2];    // a row's statistics in this CTA
+  uint64_t row_full[2], row_free[2];      // its parts from all CTAs, in the first one
+  int abort_flag;
+  int slot_row[kSlots];                   // row of a tile; -1: no more
+  int part_row[2];
+  float4 part[2][kStreamWarps];
+  uint32_t max_key[2][kStreamThreads];
+  int max_tile[2][kStreamThreads];
+  float4 slot[2][kStreamCluster];
+  float result[2];
+  int first_tile, best;
+  int n_groups;
+};
+struct Many {
+  TopShared top;
+  int groups[kMaxGroups];
+  uint32_t group_key[2][kGroupTiles * kStreamThreads];
+};
+
+__device__ __forceinline__ bool wait_cluster(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* status, int code) {
+  uint64_t t0 = 0;
+  for (uint32_t i = 1;; ++i) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity)
+        : "memory");
+    if (__all_sync(0xffffffffu, ok)) return true;
+    if (i % kPollsPerTimer == 0) {
+      int stop = *abort_flag;
+      if (!stop && wait_expired(t0)) {
+        *abort_flag = stop = 1;
+        if (status) atomicCAS(status, 0, code);
+      }
+      if (__any_sync(0xffffffffu, stop)) return false;
+    }
+  }
+}
+
+// Rows first, first + step, ... of those that are asked for, in order (a whole warp calls it).
+struct Rows {
+  const ScoreArgs& p;
+  int64_t target, step;
+  int64_t base = 0, before = 0;  // rows and asked-for rows ahead of the window
+  uint32_t window[4] = {0, 0, 0, 0};
+  int in_window = 0;
+  bool fresh = true;
+
+  __device__ Rows(const ScoreArgs& q, int first, int n) : p(q), target(first), step(n) {}
+  __device__ void look() {  // the 128 rows from base on
+    int id[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int64_t r = base + 32 * j + lane_id();
+      id[j] = r < p.rows ? p.row_ids[r] : 0;
+    }
+    in_window = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int64_t r = base + 32 * j + lane_id();
+      window[j] = __ballot_sync(0xffffffffu, r < p.rows && id[j] == p.row_id);
+      in_window += __popc(window[j]);
+    }
+  }
+  __device__ int next() {
+    const int64_t want = target;
+    target += step;
+    if (!p.row_ids) return want < p.rows ? static_cast<int>(want) : -1;
+    if (fresh) look();
+    fresh = false;
+    while (want >= before + in_window) {
+      before += in_window;
+      base += 128;
+      if (base >= p.rows) {
+        in_window = 0;
+        return -1;
+      }
+      look();
+    }
+    int n = static_cast<int>(want - before);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int c = __popc(window[j]);
+      if (n < c) {
+        uint32_t m = window[j];
+        for (; n > 0; --n) m &= m - 1;
+        return static_cast<int>(base) + 32 * j + __ffs(m) - 1;
+      }
+      n -= c;
+    }
+    return -1;
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ int tiles_of(const Slice<T>& sl) { return max(1, (sl.nv + kPiece - 1) / kPiece); }
+
+struct Ring {
+  int slot = 0;
+  uint32_t phase = 0;
+  __device__ void next() {
+    if (++slot == kSlots) {
+      slot = 0;
+      phase ^= 1;
+    }
+  }
+};
+
+template <typename T, int TOP, bool ENT>
+__global__ void __launch_bounds__(kAll, 1) logprobs_stream_kernel(const ScoreArgs p) {
+  extern __shared__ __align__(128) uint4 buf[];
+  __shared__ Shared sh;
+  Many& many = *reinterpret_cast<Many*>(buf + kSlots * kPiece);  // (kTopMany)
+  uint64_t* lists = reinterpret_cast<uint64_t*>(buf + kSlots * kPiece + sizeof(Many) / 16);  // [2][n_ctas][top_k]
+  const int rank = cluster_rank(), n_ctas = cluster_ctas();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  volatile int* abort_flag = &sh.abort_flag;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kSlots; ++i) {
+      mbar_init(&sh.full[i], 1);
+      mbar_init(&sh.empty[i], kStreamWarps);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sh.part_full[i], kStreamWarps);
+      mbar_init(&sh.part_free[i], 1);
+      mbar_init(&sh.row_full[i], n_ctas);
+      mbar_init(&sh.row_free[i], 1);
+    }
+    sh.abort_flag = 0;
+    fence_mbar_init();
+    fence_proxy_async_smem();
+  }
+  __syncthreads();
+  cluster_sync();
+  const T* logits = static_cast<const T*>(p.logits);
+  const float c = p.scale * kLog2e;
+
+  if (warp == kStreamWarps + kFinishWarps) {
+    // ----- producer
+    Rows rows(p, blockIdx.x / n_ctas, gridDim.x / n_ctas);
+    Ring ring;
+    bool ok = true;
+    int issued = 0;
+    while (ok) {
+      const int r = rows.next();
+      const Slice<T> sl(logits + (r < 0 ? 0 : r) * p.ld, p.vocab, rank, n_ctas);
+      const char* src = reinterpret_cast<const char*>(sl.row + sl.first_element(0));
+      const int lo = sl.nv > 0 && !sl.whole(0) ? 1 : 0;
+      const int hi = sl.nv > 0 && !sl.whole(sl.nv - 1) ? sl.nv - 1 : sl.nv;
+      const int tiles = r < 0 ? 1 : tiles_of(sl);
+      for (int t = 0; t < tiles && ok; ++t, ring.next()) {
+        if (lane == 0) {
+          ok = mbar_wait(&sh.empty[ring.slot], ring.phase ^ 1u, abort_flag, p.status, 63);
+          if (ok) {
+            sh.slot_row[ring.slot] = r;
+            const int a = max(t * kPiece, lo), b = min((t + 1) * kPiece, hi);
+            if (r >= 0 && b > a) {
+              mbar_arrive_expect_tx(&sh.full[ring.slot], (b - a) * 16u);
+              bulk_load(buf + ring.slot * kPiece + (a - t * kPiece), src + static_cast<int64_t>(a) * 16, (b - a) * 16u,
+                        &sh.full[ring.slot]);
+            } else {
+              mbar_arrive(&sh.full[ring.slot]);
+            }
+          }
+        }
+        ok = __shfl_sync(0xffffffffu, ok, 0);
+        issued += ok;
+      }
+      if (r < 0) break;
+    }
+    if (!ok && lane == 0) {  // no copy may land after the CTA has left
+      for (int i = 0; i < kSlots && i < issued; ++i) {
+        const int n = issued - 1 - i;
+        mbar_drain(&sh.full[n % kSlots], (n / kSlots) & 1);
+      }
+    }
+  } else if (warp < kStreamWarps) {
+    // ----- statistics
+    Ring ring;
+    const uint4 none = no_elements<T>();
+    for (int it = 0;; ++it) {
+      const int b = it & 1;
+      if (!mbar_wait_warp(smem_u32(&sh.full[ring.slot]), ring.phase, abort_flag, p.status, 64)) break;
+      const int r = sh.slot_row[ring.slot];
+      if (!mbar_wait_warp(smem_u32(&sh.part_free[b]), ((it >> 1) & 1) ^ 1u, abort_flag, p.status, 65)) break;
+      if (r < 0) {
+        if (threadIdx.x == 0) sh.part_row[b] = -1;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.part_full[b]);
+        break;
+      }
+      const Slice<T> sl(logits + r * p.ld, p.vocab, rank, n_ctas);
+      const int tiles = tiles_of(sl), per_group = (tiles + kGroupTiles - 1) / kGroupTiles;
+      Stat st;
+      int at = 0;
+      float group = -kInf;
+      int in_group = 0, g = 0;
+      bool ok = true;
+      for (int t = 0; t < tiles; ++t) {
+        if (t > 0 && !(ok = mbar_wait_warp(smem_u32(&sh.full[ring.slot]), ring.phase, abort_flag, p.status, 64))) break;
+        uint4 v[kUnroll];
+        const uint4* tile = buf + ring.slot * kPiece + threadIdx.x;
+        if (t > 0 && t < tiles - 1) {
+#pragma unroll
+          for (int u = 0; u < kUnroll; ++u) v[u] = tile[u * kStreamThreads];
+        } else {  // the slice's ends
+#pragma unroll
+          for (int u = 0; u < kUnroll; ++u) {
+            const int k = t * kPiece + u * kStreamThreads + threadIdx.x;
+            v[u] = k >= sl.nv ? none : (sl.whole(k) ? tile[u * kStreamThreads] : sl.gather(k));
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.empty[ring.slot]);
+        ring.next();
+        const float before = st.m, m = stat_add<T, kUnroll, ENT>(st, v, c);
+        if (TOP == kTopOne && m > before) at = t;
+        if (TOP == kTopMany) {
+          group = fmaxf(group, m);
+          if (++in_group == per_group || t == tiles - 1) {
+            many.group_key[b][g * kStreamThreads + threadIdx.x] = order_key(group);
+            ++g;
+            in_group = 0;
+            group = -kInf;
+          }
+        }
+      }
+      if (!ok) break;
+      if (TOP != kTopNone) sh.max_key[b][threadIdx.x] = order_key(st.m);
+      if (TOP == kTopOne) sh.max_tile[b][threadIdx.x] = at;
+      const float m = key_value(__reduce_max_sync(0xffffffffu, order_key(st.m)));
+      float s = st.s, u = st.t;
+      rebase(st.m, c, reference(m, c), s, u);
+      s = warp_sum(s);
+      if (ENT) u = warp_sum(u);
+      if (lane == 0) sh.part[b][warp] = make_float4(m, s, u, 0.f);
+      if (threadIdx.x == 0) sh.part_row[b] = r;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.part_full[b]);
+    }
+  } else {
+    // ----- the rest of a row
+    const Finishers team{static_cast<int>(threadIdx.x) - kStreamThreads};
+    const int tid = team.tid;
+    for (int it = 0;; ++it) {
+      const int b = it & 1;
+      const uint32_t phase = (it >> 1) & 1;
+      bool ok = mbar_wait_warp(smem_u32(&sh.part_full[b]), phase, abort_flag, p.status, 66);
+      const int r = ok ? sh.part_row[b] : -1;
+      if (tid == 0) {
+        sh.best = sh.first_tile = 0x7FFFFFFF;
+        sh.n_groups = 0;
+      }
+      if (team.count(!ok) || r < 0) break;
+      const T* row = logits + r * p.ld;
+      const Slice<T> sl(row, p.vocab, rank, n_ctas);
+      Given<T> given;
+      if (rank == 0) given.fetch(p, row, r, tid);
+      auto fetch = [&](int i) { return sl.fetch(i); };
+      float m = -kInf;
+#pragma unroll
+      for (int w = 0; w < kStreamWarps; ++w) m = fmaxf(m, sh.part[b][w].x);
+      if (TOP == kTopOne) {
+        const uint32_t key = order_key(m), k0 = sh.max_key[b][tid], k1 = sh.max_key[b][tid + kFinishThreads];
+        const int t0 = sh.max_tile[b][tid], t1 = sh.max_tile[b][tid + kFinishThreads];
+        const int first = __reduce_min_sync(0xffffffffu, min(k0 == key ? t0 : 0x7FFFFFFF, k1 == key ? t1 : 0x7FFFFFFF));
+        if ((tid & 31) == 0) atomicMin(&sh.first_tile, first);
+        team.sync();
+        const int tile = sh.first_tile;
+        if (m == -kInf) {
+          if (tid == 0 && sl.nv > 0) sh.best = max(sl.first_element(0), 0);
+        } else {
+          int found = 0x7FFFFFFF;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if ((h ? k1 : k0) != key || (h ? t1 : t0) != tile) continue;
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+              const int i = tile * kPiece + u * kStreamThreads + h * kFinishThreads + tid;
+              if (i >= sl.nv) continue;
+              float f[Elem<T>::kPer];
+              unpack(sl.fetch(i), f, static_cast<const T*>(nullptr));
+#pragma unroll
+              for (int j = 0; j < Elem<T>::kPer; ++j)
+                if (f[j] == m) found = min(found, sl.first_element(i) + j);
+            }
+          }
+          if (found != 0x7FFFFFFF) atomicMin(&sh.best, found);
+        }
+        team.sync();
+      }
+      if (TOP == kTopMany) {
+        const int tiles = tiles_of(sl), per_group = (tiles + kGroupTiles - 1) / kGroupTiles;
+        const int n_keys = (tiles + per_group - 1) / per_group * kStreamThreads;
+        const uint32_t keys[2] = {sh.max_key[b][tid], sh.max_key[b][tid + kFinishThreads]};
+        uint32_t above;
+        const uint32_t lo = threshold(team, keys, p.top_k, many.top, above);
+        for (int i = 4 * tid; i < n_keys; i += 4 * kFinishThreads) {
+          const uint4 k = *reinterpret_cast<const uint4*>(&many.group_key[b][i]);
+          const uint32_t q[4] = {k.x, k.y, k.z, k.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (q[j] >= lo) {
+              const int n = atomicAdd(&sh.n_groups, 1);
+              if (n < kMaxGroups) many.groups[n] = i + j;
+            }
+        }
+        team.sync();
+        const int n = sh.n_groups, per = per_group * kUnroll;  // vectors of a group
+        if (n <= kMaxGroups) {
+          const float bar = key_value(lo);
+          for (int j = tid; j < n * per; j += kFinishThreads) {
+            const int q = j / per, w = j - q * per, grp = many.groups[q];
+            const int tile = grp / kStreamThreads * per_group + w / kUnroll;
+            const int i = tile * kPiece + (w % kUnroll) * kStreamThreads + grp % kStreamThreads;
+            if (i >= sl.nv) continue;
+            const uint4 v = sl.fetch(i);
+            if (lo > kKeyNegInf && !(vec_max<1>(&v, static_cast<const T*>(nullptr)) >= bar)) continue;
+            append(sl, v, sl.first_element(i), lo, many.top);
+          }
+        }
+        team.sync();
+        if (n > kMaxGroups || many.top.n > kCap) candidates_of_many(team, sl, fetch, lo, above, p.top_k, many.top);
+      }
+      // to the first CTA, once it is done with the row before the last
+      if (n_ctas > 1) {
+        ok = wait_cluster(&sh.row_free[b], phase ^ 1u, abort_flag, p.status, 67);
+        if (team.count(!ok)) break;
+      }
+      if (TOP == kTopMany) {
+        const uint32_t to = map_to_rank(smem_u32(lists + (b * n_ctas + rank) * p.top_k), 0);
+        rank_candidates(team, many.top, p.top_k, [&](int place, uint64_t x) { st_cluster(to + 8 * place, x); });
+      }
+      if (tid < 32) {
+        float s = 0.f, t = 0.f;
+        if (tid < kStreamWarps) {
+          s = sh.part[b][tid].y;
+          t = sh.part[b][tid].z;
+          rebase(sh.part[b][tid].x, c, reference(m, c), s, t);
+        }
+        s = warp_sum(s);
+        if (ENT) t = warp_sum(t);
+        if (tid == 0)
+          st_cluster(map_to_rank(smem_u32(&sh.slot[b][rank]), 0), make_float4(m, s, t, __int_as_float(TOP == kTopOne ? sh.best : 0)));
+      }
+      team.sync();
+      if (tid == 0) {
+        mbar_arrive(&sh.part_free[b]);
+        if (n_ctas > 1) mbar_arrive_cluster(map_to_rank(smem_u32(&sh.row_full[b]), 0));
+      }
+      if (rank == 0) {
+        if (n_ctas > 1) {
+          ok = wait_cluster(&sh.row_full[b], phase, abort_flag, p.status, 68);
+          if (team.count(!ok)) break;
+        }
+        finish<T, TOP, ENT>(team, p, r, row, given, sh.slot[b], lists + b * n_ctas * p.top_k, n_ctas, sh.result);
+        team.sync();
+        if (n_ctas > 1 && tid < n_ctas) mbar_arrive_cluster(map_to_rank(smem_u32(&sh.row_free[b]), tid));
+      }
+    }
+  }
+  __syncwarp();
+  cluster_sync();  // no CTA leaves while another may still write to it
+}
+
+size_t smem_bytes(const ScoreArgs& p, int cluster) {
+  return kSlots * kTileBytes + (p.top_k > 1 ? sizeof(Many) + 2 * sizeof(uint64_t) * cluster * p.top_k : 0);
+}
+static_assert(sizeof(Many) % 16 == 0, "the lists follow it");
+
+// Clusters of `c` CTAs that run at once, asked for once per kernel, device and size.
+template <auto kKernel>
+cudaError_t resident(int c, size_t smem, int* n) {
+  static std::atomic<int> known[64][4];
+  int dev = 0, k = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  while ((1 << k) < c) ++k;
+  if (dev < 64 && known[dev][k].load() > 0) {
+    *n = known[dev][k].load();
+    return cudaSuccess;
+  }
+  e = cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(num_sms() / c * c));
+  cfg.blockDim = dim3(kAll);
+  cfg.dynamicSmemBytes = smem;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = c;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  e = cudaOccupancyMaxActiveClusters(n, kKernel, &cfg);
+  if (e != cudaSuccess) return e;
+  if (dev < 64) known[dev][k].store(*n);
+  return cudaSuccess;
+}
+
+template <auto kKernel>
+cudaError_t launch_stream(const ScoreArgs& p, cudaStream_t s) {
+  // the cluster size that leaves the SMs idle least: rounds over the rows, each a share of a row long
+  constexpr int kMaxLists = 2 * static_cast<int>(sizeof(uint64_t)) * kStreamCluster * kMaxTop;
+  const size_t most = kSlots * kTileBytes + (p.top_k > 1 ? sizeof(Many) + kMaxLists : 0);
+  int best = 0, clusters = 0;
+  double cost = 0;
+  for (int c = 1; c <= kStreamCluster; c *= 2) {
+    int n = 0;
+    const cudaError_t e = resident<kKernel>(c, most, &n);
+    if (e != cudaSuccess) return e;
+    if (n < 1) continue;
+    const double t = static_cast<double>((p.rows + n - 1) / n) / c;
+    if (!best || t < 0.98 * cost) {
+      best = c;
+      cost = t;
+      clusters = n;
+    }
+  }
+  if (!best) return cudaErrorInvalidConfiguration;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(clusters < p.rows ? clusters : p.rows) * best);
+  cfg.blockDim = dim3(kAll);
+  cfg.dynamicSmemBytes = smem_bytes(p, best);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = best;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kKernel, p);
+}
+
+template <typename T, int TOP>
+cudaError_t stream_ent(const ScoreArgs& p, cudaStream_t s) {
+  return p.entropy ? launch_stream<&logprobs_stream_kernel<T, TOP, true>>(p, s)
+                   : launch_stream<&logprobs_stream_kernel<T, TOP, false>>(p, s);
+}
+
+}  // namespace
+
+bool stream_pays(int rows, int64_t row_bytes) { return row_bytes >= 32 * 1024 && rows * row_bytes >= (32 << 20); }
+
+template <typename T>
+cudaError_t score_stream(const ScoreArgs& p, cudaStream_t s) {
+  if (p.top_k == 0) return stream_ent<T, kTopNone>(p, s);
+  if (p.top_k == 1) return stream_ent<T, kTopOne>(p, s);
+  return stream_ent<T, kTopMany>(p, s);
+}
+template cudaError_t score_stream<f16>(const ScoreArgs&, cudaStream_t);
+template cudaError_t score_stream<bf16>(const ScoreArgs&, cudaStream_t);
+template cudaError_t score_stream<float>(const ScoreArgs&, cudaStream_t);
+
+}  // namespace rows
+}  // namespace sgd

@@ -112,6 +112,21 @@ struct Slice {
     const int e = first_element(i);
     return e >= 0 && e + Elem<T>::kPer <= vocab;
   }
+  // local vector i from global memory
+  __device__ uint4 fetch(int i) const {
+    const T* at = row + first_element(i);
+    if (whole(i)) return *reinterpret_cast<const uint4*>(at);
+    return gather(i);
+  }
+  // one that is not whole: -inf where there is no element
+  __device__ uint4 gather(int i) const {
+    const int e = first_element(i);
+    uint4 v;
+    T* f = reinterpret_cast<T*>(&v);
+#pragma unroll
+    for (int j = 0; j < Elem<T>::kPer; ++j) f[j] = e + j >= 0 && e + j < vocab ? row[e + j] : neg_inf<T>();
+    return v;
+  }
   // local vector that holds element e, or -1
   __device__ int vector_of(int e) const {
     const int i = (e + shift) / Elem<T>::kPer - v0;
@@ -161,12 +176,12 @@ struct Stat {
   float m = -kInf, R = 0.f, s = 0.f, t = 0.f;
 };
 
-// Takes N vectors in.  The maximum moves at most once per call: no rescaling per element.
+// Takes N vectors in, whose largest value is returned.  The maximum moves at most once per call: no
+// rescaling per element.
 template <typename T, int N, bool ENT>
-__device__ __forceinline__ bool stat_add(Stat& st, const uint4* v, float c) {
+__device__ __forceinline__ float stat_add(Stat& st, const uint4* v, float c) {
   const float m = vec_max<N>(v, static_cast<const T*>(nullptr));
-  const bool up = m > st.m;
-  if (up) {
+  if (m > st.m) {
     const float R = __fmul_rn(m, c);
     if (st.m != -kInf) {
       const float d = st.R - R, f = ex2_approx(d);
@@ -193,10 +208,20 @@ __device__ __forceinline__ bool stat_add(Stat& st, const uint4* v, float c) {
   }
   st.s = sum_f32x2(s2);
   if (ENT) st.t = sum_f32x2(t2);
-  return up;
+  return m;
 }
 
 __device__ __forceinline__ float reference(float m, float c) { return m == -kInf ? 0.f : __fmul_rn(m, c); }
+
+// A vector without an element: of a slice's end.
+template <typename T>
+__device__ __forceinline__ uint4 no_elements() {
+  uint4 v;
+  T* e = reinterpret_cast<T*>(&v);
+#pragma unroll
+  for (int j = 0; j < Elem<T>::kPer; ++j) e[j] = neg_inf<T>();
+  return v;
+}
 
 // s and t of a part with maximum m (reference fl(m c)) at the reference R of a maximum >= m.
 __device__ __forceinline__ void rebase(float m, float c, float R, float& s, float& t) {
@@ -225,6 +250,11 @@ __device__ __forceinline__ void st_cluster(uint32_t addr, uint64_t v) {
 }
 __device__ __forceinline__ void st_cluster(uint32_t addr, float v) {
   asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
+}
+__device__ __forceinline__ uint32_t cluster_ctas() {
+  uint32_t n;
+  asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(n));
+  return n;
 }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }

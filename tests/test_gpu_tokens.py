@@ -250,6 +250,65 @@ def test_offsets_past_32_bits(B):
     _check_distill(loss, z, z0, ids, logq, 1.0, True, None)
 
 
+# many long rows (32 MiB and more of them): they stream, and the CTAs of a cluster share a row where that
+# fills the SMs better (152: one each; 153, 301: one round more)
+@pytest.mark.parametrize("rows,vocab,dtype,pad,offset", [
+    (152, 126464, "f16", 0, 0), (153, 126464, "f16", 0, 0), (301, 126464, "f16", 0, 0), (700, 32003, "bf16", 0, 1),
+    (541, 32003, "f16", 13, 0), (211, 50021, "f32", 0, 3), (1100, 16387, "f16", 5, 2), (70, 300007, "bf16", 1, 0),
+    (12, 3 << 19, "f16", 0, 0), (14, 700001, "f32", 2, 1)])
+@pytest.mark.parametrize("k", [0, 1, 9, 64])
+def test_logprobs_of_many_rows(B, rows, vocab, dtype, pad, offset, k):
+    assert rows * vocab * torch.finfo(DT[dtype]).bits // 8 >= 32 << 20
+    z = torch.empty(rows, vocab + pad, dtype=DT[dtype], device="cuda").normal_(0, 2, generator=torch.Generator("cuda").manual_seed(rows))
+    buf = torch.full((offset + rows * (vocab + pad),), 3e4, dtype=DT[dtype], device="cuda")
+    v = buf[offset:].view(rows, vocab + pad)
+    v[:, :vocab] = z[:, :vocab]
+    z = v[:, :vocab]
+    z[rows // 2, vocab // 3:] = -INF
+    got, tokens = _score(B, z, k=k, n=2)
+    some = sorted({0, 1, rows // 2, rows - 1, *range(3, rows, max(1, rows // 5))})
+    _check_score({n: x[some] for n, x in got.items()}, tokens[some], z[some], k)
+    # every row, against the kernel for few rows: the same list, and statistics within the tolerance of both
+    for a in range(0, rows, 8):
+        few, _ = _score(B, z[a:a + 8], k=k, tokens=torch.from_numpy(tokens[a:a + 8]))
+        for n in few:
+            if n == "top_ids":
+                assert np.array_equal(few[n], got[n][a:a + 8])
+            else:
+                _near(got[n][a:a + 8], few[n], 2 * (SUM * (1 + 2 * np.abs(np.where(np.isfinite(few[n]), few[n], 0))) + 64 * U))
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("k", [1, 3, 64])
+def test_hard_rows_among_many(B, k, dtype):
+    hard = torch.from_numpy(_rows_that_are_hard(126464)).to(DT[dtype])
+    n = len(hard)
+    z = hard.repeat(13, 1).cuda()
+    assert z.numel() * z.element_size() >= 32 << 20
+    got, tokens = _score(B, z, k=k, tokens=torch.arange(2 * n).view(n, 2).int().repeat(13, 1))
+    _check_score({m: x[:n] for m, x in got.items()}, tokens[:n], hard, k)
+    for x in got.values():
+        x = x.reshape(13, n, -1)
+        assert np.array_equal(x, np.broadcast_to(x[:1], x.shape), equal_nan=True)
+
+
+@pytest.mark.parametrize("share", [0.0, 0.004, 0.5, 1.0])
+@pytest.mark.parametrize("k", [1, 6])
+def test_rows_that_are_not_asked_for_stay_among_many(B, k, share):
+    rows, vocab = 2500, 20001
+    g = torch.Generator("cuda").manual_seed(4)
+    z = torch.empty(rows, vocab, dtype=torch.float16, device="cuda").normal_(0, 2, generator=g)
+    on = torch.rand(rows, device="cuda", generator=g) < share
+    ids = torch.where(on, 5, 4).int()
+    want, tokens = _score(B, z, k=k)
+    z[~on] = math.nan
+    got, _ = _score(B, z, k=k, row_ids=ids, row_id=5)
+    on = on.cpu().numpy()
+    for n, v in got.items():
+        assert (v[~on] == (-7 if v.dtype == np.int32 else 77.0)).all()
+        assert np.array_equal(v[on], want[n][on])
+
+
 # ---------------------------------------------------------------------------
 # distillation
 # ---------------------------------------------------------------------------
