@@ -77,6 +77,30 @@ __device__ __forceinline__ float vec_max(const uint4* v, const f16*) { return ve
 template <int N>
 __device__ __forceinline__ float vec_max(const uint4* v, const bf16*) { return vec_max_packed<N, __nv_bfloat162>(v); }
 
+// Whether one of n vectors' values is -inf.
+template <int N>
+__device__ __forceinline__ bool holds_neg_inf(const uint4* v, const float*) {
+  float m = __uint_as_float(v[0].x);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    m = min3(m, __uint_as_float(v[i].x), __uint_as_float(v[i].y));
+    m = min3(m, __uint_as_float(v[i].z), __uint_as_float(v[i].w));
+  }
+  return m == -kInf;
+}
+template <int N, typename P>
+__device__ __forceinline__ bool holds_neg_inf_packed(const uint4* v) {
+  const P* p = reinterpret_cast<const P*>(v);
+  P m = p[0];
+#pragma unroll
+  for (int i = 1; i < 4 * N; ++i) m = __hmin2(m, p[i]);
+  return fminf(to_f(m.x), to_f(m.y)) == -kInf;
+}
+template <int N>
+__device__ __forceinline__ bool holds_neg_inf(const uint4* v, const f16*) { return holds_neg_inf_packed<N, __half2>(v); }
+template <int N>
+__device__ __forceinline__ bool holds_neg_inf(const uint4* v, const bf16*) { return holds_neg_inf_packed<N, __nv_bfloat162>(v); }
+
 // Order of fp32 values as unsigned integers: -0 and +0 are equal, NaN stands with -inf.
 __device__ __forceinline__ uint32_t order_key(float x) {
   const uint32_t b = __float_as_uint(x + 0.0f);
@@ -176,6 +200,27 @@ struct Stat {
   float m = -kInf, R = 0.f, s = 0.f, t = 0.f;
 };
 
+template <typename T, int N, bool ENT, bool CUT>
+__device__ __forceinline__ void add_terms(Stat& st, const uint4* v, float c) {
+  const uint64_t c2 = pack_f32x2(c, c), r2 = pack_f32x2(-st.R, -st.R);
+  uint64_t s2 = pack_f32x2(st.s, 0.f), t2 = pack_f32x2(st.t, 0.f);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    float f[Elem<T>::kPer];
+    unpack(v[i], f, static_cast<const T*>(nullptr));
+#pragma unroll
+    for (int j = 0; j < Elem<T>::kPer; j += 2) {
+      uint64_t y = fma_f32x2(pack_f32x2(f[j], f[j + 1]), c2, r2);
+      const uint64_t e = pack_f32x2(ex2_approx(lo_f32x2(y)), ex2_approx(hi_f32x2(y)));
+      s2 = add_f32x2(s2, e);
+      if (CUT) y = pack_f32x2(fmaxf(lo_f32x2(y), -1000.f), fmaxf(hi_f32x2(y), -1000.f));
+      if (ENT) t2 = fma_f32x2(y, e, t2);
+    }
+  }
+  st.s = sum_f32x2(s2);
+  if (ENT) st.t = sum_f32x2(t2);
+}
+
 // Takes N vectors in, whose largest value is returned.  The maximum moves at most once per call: no
 // rescaling per element.
 template <typename T, int N, bool ENT>
@@ -191,23 +236,9 @@ __device__ __forceinline__ float stat_add(Stat& st, const uint4* v, float c) {
     st.m = m;
     st.R = R;
   }
-  const uint64_t c2 = pack_f32x2(c, c), r2 = pack_f32x2(-st.R, -st.R);
-  uint64_t s2 = pack_f32x2(st.s, 0.f), t2 = pack_f32x2(st.t, 0.f);
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    float f[Elem<T>::kPer];
-    unpack(v[i], f, static_cast<const T*>(nullptr));
-#pragma unroll
-    for (int j = 0; j < Elem<T>::kPer; j += 2) {
-      const uint64_t y = fma_f32x2(pack_f32x2(f[j], f[j + 1]), c2, r2);
-      const uint64_t e = pack_f32x2(ex2_approx(lo_f32x2(y)), ex2_approx(hi_f32x2(y)));
-      s2 = add_f32x2(s2, e);
-      // -inf has the term 0, not -inf times 0
-      if (ENT) t2 = fma_f32x2(pack_f32x2(fmaxf(lo_f32x2(y), -1000.f), fmaxf(hi_f32x2(y), -1000.f)), e, t2);
-    }
-  }
-  st.s = sum_f32x2(s2);
-  if (ENT) st.t = sum_f32x2(t2);
+  // -inf has the term 0 in t, not -inf times 0: its exponent is cut, where there is one
+  if (ENT && holds_neg_inf<N>(v, static_cast<const T*>(nullptr))) add_terms<T, N, true, true>(st, v, c);
+  else add_terms<T, N, ENT, false>(st, v, c);
   return m;
 }
 
