@@ -1,0 +1,228 @@
+// What the two distillation kernels share: parameters, the list, a row's scalars and the stores of a gradient.
+#pragma once
+
+#include <type_traits>
+
+#include "vocab_rows.cuh"
+
+namespace sgd {
+namespace rows {
+
+constexpr int kMaxList = kMaxTop;
+static_assert(kMaxList == 64, "two warps hold the list");
+
+struct DistillArgs {
+  const void* logits;
+  int64_t ld;
+  int rows, vocab;
+  float scale;
+  const int32_t* ids;
+  const float* logq;
+  int k;
+  const float* weight;
+  int bucket;
+  float* loss;
+  void* grad;
+  int64_t ld_grad;
+  int* status;
+};
+
+struct NoGrad {};
+
+template <typename G>
+struct Out;
+template <>
+struct Out<float> {
+  __device__ static float one(float x) { return x; }
+};
+template <>
+struct Out<f16> {  // rounded as they are: a gradient out of fp16's range is inf, as a loss scaler expects
+  __device__ static f16 one(float x) { return __float2half_rn(x); }
+};
+template <>
+struct Out<bf16> {
+  __device__ static bf16 one(float x) { return __float2bfloat16_rn(x); }
+};
+
+// N values to an address aligned to N sizeof(G) (at most 16) bytes
+template <int N>
+__device__ __forceinline__ void store_vec(float* to, const float* f) {
+#pragma unroll
+  for (int i = 0; i < N; i += 4) reinterpret_cast<float4*>(to)[i / 4] = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
+}
+template <int N>
+__device__ __forceinline__ void store_words(void* to, const uint32_t* w) {
+  if constexpr (N == 8) *static_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
+  else *static_cast<uint2*>(to) = make_uint2(w[0], w[1]);
+}
+template <int N>
+__device__ __forceinline__ void store_vec(bf16* to, const float* f) {
+  uint32_t w[N / 2];
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) w[i] = pack_bf16x2(f[2 * i], f[2 * i + 1]);
+  store_words<N>(to, w);
+}
+template <int N>
+__device__ __forceinline__ void store_vec(f16* to, const float* f) {
+  uint32_t w[N / 2];
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) {
+    const __half2 h = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
+    w[i] = *reinterpret_cast<const uint32_t*>(&h);
+  }
+  store_words<N>(to, w);
+}
+
+// The slice's part of a gradient row: value(i, f) gives vector i of the logits' slice; stored whole where
+// the gradient's address allows it.
+template <typename T, typename G, typename F>
+__device__ __forceinline__ void write_grad(const Slice<T>& sl, G* grow, int tid, int threads, const F& value) {
+  constexpr int E = Elem<T>::kPer;
+  constexpr uintptr_t kAlign = E * sizeof(G) < 16 ? E * sizeof(G) : 16;
+  if (sl.nv == 0) return;
+  G* g0 = grow + sl.first_element(0);
+  const bool aligned = (reinterpret_cast<uintptr_t>(g0) & (kAlign - 1)) == 0;
+  const int lo = aligned && sl.whole(0) ? 0 : 1, hi = aligned && sl.whole(sl.nv - 1) ? sl.nv : sl.nv - 1;
+  if (aligned) {
+#pragma unroll 4
+    for (int i = lo + tid; i < hi; i += threads) {
+      float f[E];
+      value(i, f);
+      store_vec<E>(g0 + static_cast<int64_t>(i) * E, f);
+    }
+    if (lo == 0 && hi == sl.nv) return;
+  }
+  // element by element: the row's ends, or all of it
+  for (int i = tid; i < sl.nv; i += threads) {
+    if (aligned && i >= lo && i < hi) continue;
+    float f[E];
+    value(i, f);
+    const int e = sl.first_element(i);
+#pragma unroll
+    for (int j = 0; j < E; ++j)
+      if (e + j >= 0 && e + j < sl.vocab) grow[e + j] = Out<G>::one(f[j]);
+  }
+}
+
+// A row's sums: maximum, and sum of 2^(c x - R) over the tail and over the list.
+struct RowSums {
+  float all, tail, in;
+};
+
+// From the CTAs' parts {maximum, tail, list} (a whole warp; every lane gets them).
+__device__ __forceinline__ RowSums row_sums(const float4* slot, int n_ctas, float c) {
+  const int lane = lane_id();
+  float4 v = make_float4(-kInf, 0.f, 0.f, 0.f);
+  if (lane < n_ctas) v = slot[lane];
+  RowSums r;
+  r.all = key_value(__reduce_max_sync(0xffffffffu, order_key(v.x)));
+  const float R = reference(r.all, c);
+  float unused = 0.f;
+  rebase(v.x, c, R, v.y, unused);
+  rebase(v.x, c, R, v.z, unused);
+  r.tail = warp_sum(v.y);
+  r.in = warp_sum(v.z);
+  return r;
+}
+
+// Sums of two floats, hi + lo, for a row's scalars.  (fp64 instructions take some 15 cycles a warp here: a
+// division of them costs more than a row's exponentials do.)
+struct Float2 {
+  float hi, lo;
+};
+__device__ __forceinline__ Float2 two_sum(float a, float b) {  // a + b exactly
+  const float s = __fadd_rn(a, b), t = __fsub_rn(s, a);
+  return Float2{s, __fadd_rn(__fsub_rn(a, __fsub_rn(s, t)), __fsub_rn(b, t))};
+}
+__device__ __forceinline__ Float2 operator+(Float2 a, Float2 b) {
+  const Float2 s = two_sum(a.hi, b.hi);
+  return Float2{s.hi, s.lo + (a.lo + b.lo)};
+}
+__device__ __forceinline__ Float2 operator-(Float2 a) { return Float2{-a.hi, -a.lo}; }
+__device__ __forceinline__ Float2 two_prod(float a, float b) {  // a b exactly
+  const float p = __fmul_rn(a, b);
+  return Float2{p, fmaf(a, b, -p)};
+}
+// ln x of a normal x > 0: logf of the significand, whose rounding is that of a number below 0.7, and the
+// exponent times ln 2 in two parts (the first one short: e times it is exact).
+__device__ __forceinline__ Float2 ln2parts(float x) {
+  int e = 0;
+  const float f = frexpf(x, &e), n = static_cast<float>(e);
+  return Float2{n * 0.693145751953125f, n * 1.42860677e-6f} + Float2{logf(f), 0.f};
+}
+
+// What a row's list adds up to: Q in two parts, and q_T.
+struct ListSums {
+  float Q, Q_lo, q_tail;
+};
+__device__ __forceinline__ ListSums list_sums(double Q, bool bucket) {
+  const float hi = static_cast<float>(Q), lo = static_cast<float>(Q - hi);
+  return ListSums{hi, lo, bucket ? fmaxf(0.f, (1.f - hi) - lo) : 0.f};
+}
+
+// The scalars of a row's gradient: p_j = inv_s 2^(c x_j - R); outside the list the gradient is
+// mul 2^(c x_j - ref), inside it p_j f_in - q q_in.
+struct RowScale {
+  float R, inv_s, f_in, q_in;
+  float ref, mul;
+  float s;
+  bool empty, has_tail;
+};
+
+__device__ __forceinline__ RowScale row_scale(const RowSums& r, const ListSums& l, float w, float scale, bool bucket, float c) {
+  RowScale o;
+  o.R = reference(r.all, c);
+  o.s = r.tail + r.in;
+  o.empty = r.all == -kInf && o.s == 0.f;  // every logit -inf: p = 0
+  o.inv_s = o.empty ? 0.f : 1.f / o.s;
+  o.has_tail = bucket && r.tail > 0.f;
+  o.f_in = w * scale;
+  o.q_in = bucket ? o.f_in : o.f_in / l.Q;
+  // w scale p_j (1 - q_T / p_T) = F 2^(c x_j - R), F = w scale (1 / s - q_T / tail).  F's exponent k goes into
+  // the reference, so that a small tail's large factor overflows nowhere; what rounding the
+  // reference takes goes into the factor.
+  const float g = o.inv_s - (o.has_tail ? l.q_tail / r.tail : 0.f);  // (finite: tail >= 2^-126)
+  int k = 0, k2 = 0;
+  float f = o.f_in * g;
+  if (isfinite(o.f_in) && isfinite(g)) f = frexpf(g, &k) * frexpf(o.f_in, &k2);
+  const Float2 ref = two_sum(o.R, -static_cast<float>(k + k2));
+  o.ref = ref.hi;
+  o.mul = f * ex2_approx(-ref.lo);
+  return o;
+}
+
+// One entry's term of the loss, q (ln q - ln p), and the loss from their sum.  Where the two models agree these are
+// differences of larger numbers: ln q - ln p is taken in two parts, and the terms are added up in fp64.
+__device__ __forceinline__ float loss_term(const RowScale& o, const RowSums& r, float q, float lq, float z, float scale, float c) {
+  if (q == 0.f) return 0.f;
+  if (o.empty || z == -kInf) return q * kInf;
+  const float delta = r.all == -kInf ? 0.f : fmaf(r.all, c, -o.R);
+  const Float2 ln_s = ln2parts(o.s) + Float2{-delta * kLn2, 0.f};
+  const Float2 d = two_sum(z, -r.all), x = two_prod(d.hi, scale);
+  const Float2 diff = Float2{lq, 0.f} + -Float2{x.hi, fmaf(d.lo, scale, x.lo)} + ln_s;
+  return q * (diff.hi + diff.lo);
+}
+__device__ __forceinline__ float row_loss(const RowScale& o, const RowSums& r, double terms, const ListSums& l, float w, bool bucket) {
+  const float hi = static_cast<float>(terms);
+  if (!isfinite(hi)) return w * hi;
+  if (!bucket) {  // terms / Q - ln Q
+    const float q1 = hi / l.Q, rest = fmaf(-q1, l.Q, hi) + static_cast<float>(terms - hi) - q1 * l.Q_lo;
+    const Float2 L = Float2{q1, rest / l.Q} + -ln2parts(l.Q) + Float2{-l.Q_lo / l.Q, 0.f};
+    return w * (L.hi + L.lo);
+  }
+  float tail = 0.f;
+  if (o.has_tail && l.q_tail > 0.f) {
+    const float P = r.in / o.s;
+    const float ln_pt = P < 0.5f ? log1pf(-P) : logf(r.tail / o.s);
+    const float ln_qt = l.Q < 0.5f ? log1pf(-l.Q) : logf(l.q_tail);
+    tail = l.q_tail * (ln_qt - ln_pt);
+  }
+  return w * static_cast<float>(terms + tail);
+}
+
+template <typename T>
+cudaError_t distill_stream(const DistillArgs& p, int grad_dtype, cudaStream_t s);  // distill_stream.cu
+bool distill_stream_pays(int rows, int64_t row_bytes);
+
+}  // namespace rows
+}  // namespace sgd

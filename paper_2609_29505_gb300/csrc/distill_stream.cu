@@ -1,0 +1,435 @@
+// Distillation of many long rows (distill.cu has the formulas): the rows stream through clusters that stay
+// for the whole call.
+//
+// A CTA holds slices of several rows in shared memory, a buffer each.  8 warps work on them in turn: the
+// sums of one row, then the gradient of an earlier one, whose sums have crossed the cluster meanwhile.
+// Each buffer has a warp of its own that sees a row through, one step after another: it starts the bulk
+// copies, takes the list's tokens out of the slice (they become -inf), adds up the sums, exchanges them
+// with the cluster's other CTAs, gives the gradient its scalars, prepares the next row's list while the
+// gradient is written, starts the next copies, and then writes the list's own gradients and (in the first
+// CTA) the loss.  These steps are chains of
+// latency (a few us a row); as many of them as there are buffers run at once, and the 8 warps wait for
+// none of them but through the barriers of the buffers.
+//
+// What a CTA sends to the others alternates between two places per buffer: the second row after a row is
+// sent when all CTAs have sent the one between, after they have read the first.
+//
+// The loss alone keeps a buffer only until the sums are taken: the next row's copies start before they are
+// exchanged.  Rows of weight 0 are written only; they are dealt out to the clusters apart from the others.
+//
+// Every wait is bounded.  After one has expired (recorded in the status word) each warp leaves its loop.
+#include "distill.cuh"
+#include "persistent.cuh"
+
+namespace sgd {
+namespace rows {
+namespace {
+
+constexpr int kWorkWarps = 8, kWork = 32 * kWorkWarps;
+constexpr int kMinBuffers = 3, kMaxBuffers = 6;
+constexpr int kAllThreads = kWork + 32 * kMaxBuffers;
+constexpr int kDeep = 4;
+constexpr int kBufferBytes = 200 * 1024;
+constexpr int kMaxStreamCluster = 8;
+constexpr int kHalves = kMaxList / 32;  // list entries of a lane
+
+struct Buffer {
+  uint64_t full;       // the slice has arrived
+  uint64_t ready;      // and the list's tokens are out of it
+  uint64_t part_full;  // the working warps' sums are there
+  uint64_t sums_full[2];  // and those of all CTAs
+  uint64_t scaled;     // the gradient's scalars are there
+  uint64_t done;       // the gradient is written
+  int row;             // -1: no more
+  int live;            // 0: loss and gradient are 0
+  float ref, mul;      // of the gradient (RowScale)
+  float2 part[kWorkWarps];
+  float4 slot[2][kMaxStreamCluster];
+  float list_z[2][kMaxList];  // first CTA: the list's logits
+  __align__(16) int ids[32];
+};
+
+// Buffers of `vectors` vectors (a multiple of kWork) each; the gradient of a row is written `lag` rows after its
+// sums were taken.
+struct Shape {
+  int vectors, buffers, lag;
+};
+
+// A row's list, kHalves entries a lane.
+struct List {
+  int row;
+  bool lives;
+  float w;
+  int id[kHalves];  // -1: none
+  float q[kHalves], lq[kHalves];
+  ListSums sums;
+};
+
+template <typename T, typename G>
+__global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const DistillArgs p, const Shape shape) {
+  constexpr bool kGrad = !std::is_same<G, NoGrad>::value;
+  constexpr int E = Elem<T>::kPer;
+  extern __shared__ __align__(128) uint4 buf[];
+  __shared__ Buffer buffers[kMaxBuffers];
+  __shared__ int abort_shared;
+  __shared__ RowLists rows;
+  const int rank = cluster_rank(), n_ctas = cluster_ctas();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  volatile int* abort_flag = &abort_shared;
+  if (threadIdx.x < shape.buffers) {
+    Buffer& b = buffers[threadIdx.x];
+    mbar_init(&b.full, 1);
+    mbar_init(&b.ready, 1);
+    mbar_init(&b.part_full, kWorkWarps);
+    mbar_init(&b.sums_full[0], n_ctas);
+    mbar_init(&b.sums_full[1], n_ctas);
+    mbar_init(&b.scaled, 1);
+    mbar_init(&b.done, kWorkWarps);
+    fence_mbar_init();
+  }
+  if (threadIdx.x == 0) abort_shared = 0;
+  // behind a slice's vectors its buffer holds -inf: no copy writes there
+  const uint4 none = no_elements<T>();
+  for (int i = threadIdx.x; i < shape.vectors * shape.buffers; i += kAllThreads) buf[i] = none;
+  fence_proxy_async_smem();
+  const int cluster = blockIdx.x / n_ctas, clusters = gridDim.x / n_ctas;
+  const bool listed = p.weight && make_row_lists<kAllThreads>(rows, p.rows, cluster, clusters, [&](int r) { return p.weight[r] != 0.f; });
+  __syncthreads();
+  cluster_sync();
+  const T* logits = static_cast<const T*>(p.logits);
+  const float c = p.scale * kLog2e;
+  auto slice_of = [&](int r) { return Slice<T>(logits + r * p.ld, p.vocab, rank, n_ctas); };
+
+  if (warp < kWorkWarps) {
+    // ----- sums of a row, gradient of an earlier one
+    auto take_sums = [&](int n) {
+      Buffer& b = buffers[n];
+      if (b.live) {
+        const uint4* at = buf + n * shape.vectors + threadIdx.x;
+        int left = (slice_of(b.row).nv + kWork - 1) / kWork;
+        Stat st;
+        for (; left >= kDeep; left -= kDeep, at += kDeep * kWork) {
+          uint4 v[kDeep];
+#pragma unroll
+          for (int u = 0; u < kDeep; ++u) v[u] = at[u * kWork];
+          stat_add<T, kDeep, false>(st, v, c);
+        }
+        for (; left > 0; --left, at += kWork) {
+          const uint4 v = *at;
+          stat_add<T, 1, false>(st, &v, c);
+        }
+        const float m = key_value(__reduce_max_sync(0xffffffffu, order_key(st.m)));
+        float s = st.s, unused = 0.f;
+        rebase(st.m, c, reference(m, c), s, unused);
+        s = warp_sum(s);
+        if (lane == 0) b.part[warp] = make_float2(m, s);
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&b.part_full);
+    };
+    auto put_gradient = [&](int n, uint32_t phase) {  // false: a wait has expired
+      if constexpr (kGrad) {
+        Buffer& b = buffers[n];
+        if (!mbar_wait_warp(smem_u32(&b.scaled), phase, abort_flag, p.status, 71)) return false;
+        const Slice<T> sl = slice_of(b.row);
+        G* grow = static_cast<G*>(p.grad) + b.row * p.ld_grad;
+        if (b.live) {
+          const float ref = b.ref, mul = b.mul;
+          const uint4* slice = buf + n * shape.vectors;
+          const uint64_t c2 = pack_f32x2(c, c), r2 = pack_f32x2(-ref, -ref);
+          write_grad<T, G>(sl, grow, threadIdx.x, kWork, [&](int i, float* f) {
+            unpack(slice[i], f, static_cast<const T*>(nullptr));
+#pragma unroll
+            for (int j = 0; j < E; j += 2) {
+              const uint64_t y = fma_f32x2(pack_f32x2(f[j], f[j + 1]), c2, r2);
+              f[j] = mul * ex2_approx(lo_f32x2(y));
+              f[j + 1] = mul * ex2_approx(hi_f32x2(y));
+            }
+          });
+        } else {
+          write_grad<T, G>(sl, grow, threadIdx.x, kWork, [](int, float* f) {
+#pragma unroll
+            for (int j = 0; j < E; ++j) f[j] = 0.f;
+          });
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&b.done);
+      }
+      return true;
+    };
+    uint32_t over = 0, phase = 0;  // buffers without further rows
+    int n = 0, behind = 0;         // rows whose gradient is still to be written: in the buffers ...
+    int queue = 0;                 // (4 bits each, the oldest lowest: buffer, and its phase above)
+    bool ok = true;
+    while (ok && over != (1u << shape.buffers) - 1u) {
+      if (!(over >> n & 1)) {
+        // (near the end of the rows the other buffers may have none: this one's next row waits for its gradient)
+        if (behind > 0 && (queue & 7) == n) {
+          if (!(ok = put_gradient(n, queue >> 3 & 1))) break;
+          queue >>= 4;
+          --behind;
+        }
+        ok = mbar_wait_warp(smem_u32(&buffers[n].ready), phase, abort_flag, p.status, 70);
+        if (!ok) break;
+        if (buffers[n].row < 0) {
+          over |= 1u << n;
+        } else {
+          take_sums(n);
+          if (kGrad) {
+            queue |= (n | static_cast<int>(phase) << 3) << (4 * behind++);
+            if (behind > shape.lag) {
+              ok = put_gradient(queue & 7, queue >> 3 & 1);
+              queue >>= 4;
+              --behind;
+            }
+          }
+        }
+      }
+      if (++n == shape.buffers) {
+        n = 0;
+        phase ^= 1;
+      }
+    }
+    for (; ok && behind > 0; --behind, queue >>= 4) ok = put_gradient(queue & 7, queue >> 3 & 1);
+  } else if (warp - kWorkWarps < shape.buffers) {
+    // ----- one buffer's rows
+    const int n = warp - kWorkWarps;
+    Buffer& b = buffers[n];
+    uint4* slice = buf + n * shape.vectors;
+    int turn = n;  // of the cluster's rows: those of both kinds alternate while there are any
+    auto next_row = [&]() {
+      const int i = turn;
+      turn += shape.buffers;
+      if (!listed) {
+        const int64_t r = cluster + static_cast<int64_t>(i) * clusters;
+        return r < p.rows ? static_cast<int>(r) : -1;
+      }
+      const int both = min(rows.n_first, rows.n_rest);
+      if (i < 2 * both) return i & 1 ? rows.of_rest[i >> 1] : rows.of_first[i >> 1];
+      if (i - both >= max(rows.n_first, rows.n_rest)) return -1;
+      return rows.n_first > rows.n_rest ? rows.of_first[i - both] : rows.of_rest[i - both];
+    };
+    // the next row's list as it is in memory; used later
+    auto fetch_list = [&]() {
+      List x;
+      x.row = next_row();
+      x.lives = x.row >= 0;
+      x.w = 1.f;
+      if (x.lives && p.weight) x.w = p.weight[x.row];
+#pragma unroll
+      for (int h = 0; h < kHalves; ++h) {
+        const int i = lane + 32 * h;
+        const int64_t at = static_cast<int64_t>(x.row) * p.k + i;
+        x.id[h] = x.lives && i < p.k ? p.ids[at] : -1;
+        x.lq[h] = x.lives && i < p.k ? p.logq[at] : 0.f;
+      }
+      return x;
+    };
+    // an id counts at its first place; what is no token is left out
+    auto sort_out = [&](List& x) {
+#pragma unroll
+      for (int h = 0; h < kHalves; ++h) {
+        if (x.id[h] < 0 || x.id[h] >= p.vocab) x.id[h] = -1;
+        if (lane != __ffs(__match_any_sync(0xffffffffu, x.id[h])) - 1) x.id[h] = -1;
+        if (32 * (h + 1) >= p.k) break;  // (the other halves hold no id)
+        if (h + 1 < kHalves) b.ids[lane] = x.id[h];
+      }
+      if (p.k > 32) {
+        static_assert(kHalves == 2, "the second half is compared with the first");
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 32; j += 4) {
+          const int4 o = *reinterpret_cast<const int4*>(&b.ids[j]);
+          if (x.id[1] == o.x || x.id[1] == o.y || x.id[1] == o.z || x.id[1] == o.w) x.id[1] = -1;
+        }
+        __syncwarp();
+      }
+      double sum = 0.0;
+      bool any = false;
+#pragma unroll
+      for (int h = 0; h < kHalves; ++h) {
+        x.q[h] = x.id[h] >= 0 ? expf(x.lq[h]) : 0.f;
+        sum += x.q[h];
+        any |= x.id[h] >= 0;
+      }
+      const double Q = warp_sum(sum);
+      x.sums = list_sums(Q, p.bucket);
+      x.lives = __any_sync(0xffffffffu, any) && x.w != 0.f && (p.bucket || Q != 0.0);
+    };
+
+    List x = fetch_list(), old;  // of the row to come, and of the one in the buffer
+    sort_out(x);
+    old.row = -1;
+    RowSums sums;
+    RowScale scale;
+    float z[kHalves] = {-kInf, -kInf};
+    int vec[kHalves] = {-1, -1};
+    int place = 0;  // of what the others send
+    uint32_t full_phase = 0, phase = 0, sums_phase = 0;
+    // the old row's sums across the cluster, and its scalars; false: a wait has expired
+    auto exchange = [&]() {
+      const float2 v = lane < kWorkWarps ? b.part[lane] : make_float2(-kInf, 0.f);
+      const float m = key_value(__reduce_max_sync(0xffffffffu, max(order_key(v.x), max(order_key(z[0]), order_key(z[1])))));
+      const float R = reference(m, c);
+      float tail = v.y, unused = 0.f, in = 0.f;
+      rebase(v.x, c, R, tail, unused);
+#pragma unroll
+      for (int h = 0; h < kHalves; ++h) in += vec[h] >= 0 ? ex2_approx(fmaf(z[h], c, -R)) : 0.f;
+      tail = warp_sum(tail);
+      in = warp_sum(in);
+      if (lane < n_ctas) st_cluster(map_to_rank(smem_u32(&b.slot[place][rank]), lane), make_float4(m, tail, in, 0.f));
+      __syncwarp();
+      if (lane < n_ctas) mbar_arrive_cluster(map_to_rank(smem_u32(&b.sums_full[place]), lane));
+      __syncwarp();
+      if (!wait_cluster(&b.sums_full[place], sums_phase, abort_flag, p.status, 74)) return false;
+      sums = row_sums(b.slot[place], n_ctas, c);
+      scale = row_scale(sums, old.sums, old.w, p.scale, p.bucket, c);
+      return true;
+    };
+    for (;; phase ^= 1) {
+      const Slice<T> sl = slice_of(max(x.row, 0));
+      if (lane == 0) {
+        b.row = x.row;
+        b.live = x.lives;
+        if (x.lives) {
+          const char* src = reinterpret_cast<const char*>(sl.row + sl.first_element(0));
+          const int lo = sl.nv > 0 && !sl.whole(0) ? 1 : 0;
+          const int hi = sl.nv > 0 && !sl.whole(sl.nv - 1) ? sl.nv - 1 : sl.nv;
+          const uint32_t bytes = hi > lo ? (hi - lo) * 16u : 0u;
+          mbar_arrive_expect_tx(&b.full, bytes);
+          for (int a = lo; a < hi; a += kPiece)
+            bulk_load(slice + a, src + static_cast<int64_t>(a) * 16, min(kPiece, hi - a) * 16u, &b.full);
+        }
+      }
+      __syncwarp();
+      // what is left of the old row
+      bool ok = true;
+      if (old.row >= 0) {
+        if (old.lives) {
+          if constexpr (kGrad) {
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h)
+              if (vec[h] >= 0)
+                (static_cast<G*>(p.grad) + old.row * p.ld_grad)[old.id[h]] =
+                    Out<G>::one(ex2_approx(fmaf(z[h], c, -scale.R)) * scale.inv_s * scale.f_in - old.q[h] * scale.q_in);
+          } else {
+            ok = exchange();
+          }
+        }
+        if (ok && rank == 0) {
+          double terms = 0.0;
+          if (old.lives) {
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h)
+              terms += loss_term(scale, sums, old.q[h], old.lq[h], b.list_z[place][lane + 32 * h], p.scale, c);
+            terms = warp_sum(terms);
+          }
+          if (lane == 0) p.loss[old.row] = old.lives ? row_loss(scale, sums, terms, old.sums, old.w, p.bucket) : 0.f;
+        }
+        if (old.lives) {
+          place ^= 1;
+          sums_phase ^= place == 0;
+        }
+      }
+      if (ok && x.row < 0) {
+        if (lane == 0) mbar_arrive(&b.ready);
+        break;
+      }
+      old = x;
+      x = fetch_list();
+      if (old.lives) {
+        // the row's ragged ends, and what lies behind the slice (rows that start elsewhere in a vector have a
+        // few vectors more or less in it)
+        const bool ragged = lane < 2 * E && sl.nv > 0 && !(lane >= E && sl.nv == 1) && !sl.whole(lane < E ? 0 : sl.nv - 1);
+        const int e = sl.first_element(lane < E ? 0 : sl.nv - 1) + lane % E;
+        T end = neg_inf<T>();
+        if (ragged && e >= 0 && e < sl.vocab) end = sl.row[e];
+        if (!mbar_wait_warp(smem_u32(&b.full), full_phase, abort_flag, p.status, 72)) {
+          mbar_drain(&b.full, full_phase);  // no copy may land after the CTA has left
+          break;
+        }
+        full_phase ^= 1;
+        if (ragged) reinterpret_cast<T*>(slice + (lane < E ? 0 : sl.nv - 1))[lane % E] = end;
+        if (lane <= kMaxStreamCluster && sl.nv + lane < shape.vectors) slice[sl.nv + lane] = none;
+        __syncwarp();
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h) {
+          z[h] = -kInf;
+          vec[h] = old.id[h] >= 0 ? sl.vector_of(old.id[h]) : -1;
+          if (vec[h] >= 0) {
+            T* at = reinterpret_cast<T*>(slice + vec[h]) + sl.place_of(old.id[h]);
+            z[h] = to_f(*at);
+            *at = neg_inf<T>();
+            st_cluster(map_to_rank(smem_u32(&b.list_z[place][lane + 32 * h]), 0), z[h]);
+          }
+        }
+        fence_proxy_async_smem();
+      }
+      if (!ok) break;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&b.ready);
+      if (!kGrad) sort_out(x);
+      if (!mbar_wait_warp(smem_u32(&b.part_full), phase, abort_flag, p.status, 73)) break;
+      if constexpr (kGrad) {
+        if (old.lives) {
+          if (!exchange()) break;
+          if (lane == 0) {
+            b.ref = scale.ref;
+            b.mul = scale.mul;
+          }
+          __syncwarp();
+        }
+        if (lane == 0) mbar_arrive(&b.scaled);
+        sort_out(x);
+        if (!mbar_wait_warp(smem_u32(&b.done), phase, abort_flag, p.status, 75)) break;
+      }
+    }
+  }
+  __syncwarp();
+  cluster_sync();  // no CTA leaves while another may still write to it
+}
+
+// Vectors of a buffer for rows of these bytes over c CTAs (one more where a row starts inside one).
+int buffer_vectors(int64_t row_bytes, int c) {
+  const int64_t total = (row_bytes + 15) / 16 + 1, per = (total + c - 1) / c;
+  return static_cast<int>((per + kWork - 1) / kWork * kWork);
+}
+
+template <typename T, typename G>
+cudaError_t launch_stream(const DistillArgs& p, cudaStream_t s) {
+  const int64_t bytes = static_cast<int64_t>(p.vocab) * sizeof(T);
+  auto buffers = [&](int c) { return kBufferBytes / (16 * buffer_vectors(bytes, c)); };
+  int least = 1;
+  while (least < kMaxStreamCluster && buffers(least) < kMinBuffers) least *= 2;
+  constexpr auto kKernel = &distill_stream_kernel<T, G>;
+  Clusters l;
+  const cudaError_t e = choose_clusters<kKernel>(p.rows, least, kMaxStreamCluster, kAllThreads, kBufferBytes, &l);
+  if (e != cudaSuccess) return e;
+  Shape shape;
+  shape.vectors = buffer_vectors(bytes, l.size);
+  shape.buffers = buffers(l.size) < kMaxBuffers ? buffers(l.size) : kMaxBuffers;
+  shape.lag = shape.buffers >= 5 ? 2 : 1;
+  return launch_clusters<kKernel>(l, kAllThreads, static_cast<size_t>(shape.buffers) * shape.vectors * 16, s, p, shape);
+}
+static_assert(kBufferBytes + kMaxBuffers * sizeof(Buffer) + sizeof(RowLists) <= 226 * 1024, "a CTA's shared memory");
+
+}  // namespace
+
+bool distill_stream_pays(int rows, int64_t row_bytes) {
+  return row_bytes >= 32 * 1024 && rows * row_bytes >= (32 << 20) &&
+         kBufferBytes / (16 * static_cast<int64_t>(buffer_vectors(row_bytes, kMaxStreamCluster))) >= kMinBuffers;
+}
+
+template <typename T>
+cudaError_t distill_stream(const DistillArgs& p, int grad_dtype, cudaStream_t s) {
+  if (!p.grad) return launch_stream<T, NoGrad>(p, s);
+  if (grad_dtype == SGD_F16) return launch_stream<T, f16>(p, s);
+  if (grad_dtype == SGD_BF16) return launch_stream<T, bf16>(p, s);
+  return launch_stream<T, float>(p, s);
+}
+template cudaError_t distill_stream<f16>(const DistillArgs&, int, cudaStream_t);
+template cudaError_t distill_stream<bf16>(const DistillArgs&, int, cudaStream_t);
+template cudaError_t distill_stream<float>(const DistillArgs&, int, cudaStream_t);
+
+}  // namespace rows
+}  // namespace sgd

@@ -15,6 +15,7 @@
 // Every wait is bounded.  After one has expired (recorded in the status word) each role leaves its loop;
 // the teams that share a hardware barrier leave together.
 #include "logprobs.cuh"
+#include "persistent.cuh"
 
 namespace sgd {
 namespace rows {
@@ -27,7 +28,7 @@ constexpr int kAll = kStreamThreads + 2 * kFinishThreads + 32;
 constexpr int kSlots = 5;
 constexpr int kTileBytes = kTile * 16;
 constexpr int kGroupTiles = 8;   // groups of one thread
-constexpr int kMaxGroups = 512;  // groups read again
+constexpr int kMaxGroups = 256;  // groups read again
 constexpr int kStreamCluster = 8;
 constexpr int kMaxima = kStreamThreads / kFinishThreads;  // streaming threads' maxima per finishing thread
 
@@ -45,89 +46,12 @@ struct Shared {
   float result[2][2];
   int first_tile[2], best[2];
   int n_groups[2];
+  RowLists rows;
 };
 struct Many {
   TopShared top[2];
   int groups[2][kMaxGroups];
   uint32_t group_key[2][kGroupTiles * kStreamThreads];
-};
-
-__device__ __forceinline__ bool wait_cluster(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* status, int code) {
-  uint64_t t0 = 0;
-  for (uint32_t i = 1;; ++i) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(smem_u32(bar)), "r"(parity)
-        : "memory");
-    if (__all_sync(0xffffffffu, ok)) return true;
-    if (i % kPollsPerTimer == 0) {
-      int stop = *abort_flag;
-      if (!stop && wait_expired(t0)) {
-        *abort_flag = stop = 1;
-        if (status) atomicCAS(status, 0, code);
-      }
-      if (__any_sync(0xffffffffu, stop)) return false;
-    }
-  }
-}
-
-// Rows first, first + step, ... of those that are asked for, in order (a whole warp calls it).
-struct Rows {
-  const ScoreArgs& p;
-  int64_t target, step;
-  int64_t base = 0, before = 0;  // rows and asked-for rows ahead of the window
-  uint32_t window[4] = {0, 0, 0, 0};
-  int in_window = 0;
-  bool fresh = true;
-
-  __device__ Rows(const ScoreArgs& q, int first, int n) : p(q), target(first), step(n) {}
-  __device__ void look() {  // the 128 rows from base on
-    int id[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int64_t r = base + 32 * j + lane_id();
-      id[j] = r < p.rows ? p.row_ids[r] : 0;
-    }
-    in_window = 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int64_t r = base + 32 * j + lane_id();
-      window[j] = __ballot_sync(0xffffffffu, r < p.rows && id[j] == p.row_id);
-      in_window += __popc(window[j]);
-    }
-  }
-  __device__ int next() {
-    const int64_t want = target;
-    target += step;
-    if (!p.row_ids) return want < p.rows ? static_cast<int>(want) : -1;
-    if (fresh) look();
-    fresh = false;
-    while (want >= before + in_window) {
-      before += in_window;
-      base += 128;
-      if (base >= p.rows) {
-        in_window = 0;
-        return -1;
-      }
-      look();
-    }
-    int n = static_cast<int>(want - before);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int c = __popc(window[j]);
-      if (n < c) {
-        uint32_t m = window[j];
-        for (; n > 0; --n) m &= m - 1;
-        return static_cast<int>(base) + 32 * j + __ffs(m) - 1;
-      }
-      n -= c;
-    }
-    return -1;
-  }
 };
 
 template <typename T>
@@ -302,6 +226,9 @@ __global__ void __launch_bounds__(kAll, 1) logprobs_stream_kernel(const ScoreArg
     fence_mbar_init();
     fence_proxy_async_smem();
   }
+  const int cluster = blockIdx.x / n_ctas, clusters = gridDim.x / n_ctas;
+  const bool listed = p.row_ids && make_row_lists<kAll>(sh.rows, p.rows, cluster, clusters,
+                                                        [&](int r) { return p.row_ids[r] == p.row_id; });
   __syncthreads();
   cluster_sync();
   const T* logits = static_cast<const T*>(p.logits);
@@ -309,12 +236,27 @@ __global__ void __launch_bounds__(kAll, 1) logprobs_stream_kernel(const ScoreArg
 
   if (warp == kStreamWarps + 2 * kFinishWarps) {
     // ----- producer
-    Rows rows(p, blockIdx.x / n_ctas, gridDim.x / n_ctas);
+    int at = listed ? 0 : cluster;
+    auto next_row = [&]() {
+      if (listed) return at < sh.rows.n_first ? sh.rows.of_first[at++] : -1;
+      if (p.row_ids) {  // 32 of the cluster's rows at a time
+        while (at < p.rows) {
+          const int64_t r = at + static_cast<int64_t>(lane) * clusters;
+          const uint32_t asked = __ballot_sync(0xffffffffu, r < p.rows && p.row_ids[r] == p.row_id);
+          const int64_t to = at + static_cast<int64_t>(asked ? __ffs(asked) - 1 : 32) * clusters;
+          at = static_cast<int>(to < p.rows ? to : p.rows);
+          if (asked) break;
+        }
+      }
+      const int r = at < p.rows ? at : -1;
+      if (r >= 0) at = clusters < p.rows - at ? at + clusters : p.rows;
+      return r;
+    };
     Ring ring;
     bool ok = true;
     int issued = 0;
     while (ok) {
-      const int r = rows.next();
+      const int r = next_row();
       const Slice<T> sl(logits + (r < 0 ? 0 : r) * p.ld, p.vocab, rank, n_ctas);
       const char* src = reinterpret_cast<const char*>(sl.row + sl.first_element(0));
       const int lo = sl.nv > 0 && !sl.whole(0) ? 1 : 0;
@@ -432,67 +374,12 @@ static_assert(sizeof(Many) % 16 == 0, "the lists follow it");
 constexpr size_t kMaxLists = 2 * sizeof(uint64_t) * kStreamCluster * kMaxTop;
 static_assert(kSlots * kTileBytes + sizeof(Many) + kMaxLists + sizeof(Shared) <= 226 * 1024, "a CTA's shared memory");
 
-// Clusters of `c` CTAs that run at once, asked for once per kernel, device and size.
-template <auto kKernel>
-cudaError_t resident(int c, size_t smem, int* n) {
-  static std::atomic<int> known[64][4];
-  int dev = 0, k = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  while ((1 << k) < c) ++k;
-  if (dev < 64 && known[dev][k].load() > 0) {
-    *n = known[dev][k].load();
-    return cudaSuccess;
-  }
-  e = cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
-  if (e != cudaSuccess) return e;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(num_sms() / c * c));
-  cfg.blockDim = dim3(kAll);
-  cfg.dynamicSmemBytes = smem;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = c;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  e = cudaOccupancyMaxActiveClusters(n, kKernel, &cfg);
-  if (e != cudaSuccess) return e;
-  if (dev < 64) known[dev][k].store(*n);
-  return cudaSuccess;
-}
-
 template <auto kKernel>
 cudaError_t launch_stream(const ScoreArgs& p, cudaStream_t s) {
-  // the cluster size that leaves the SMs idle least: rounds over the rows, each a share of a row long
   const size_t most = kSlots * kTileBytes + (p.top_k > 1 ? sizeof(Many) + kMaxLists : 0);
-  int best = 0, clusters = 0;
-  double cost = 0;
-  for (int c = 1; c <= kStreamCluster; c *= 2) {
-    int n = 0;
-    const cudaError_t e = resident<kKernel>(c, most, &n);
-    if (e != cudaSuccess) return e;
-    if (n < 1) continue;
-    const double t = static_cast<double>((p.rows + n - 1) / n) / c;
-    if (!best || t < 0.98 * cost) {
-      best = c;
-      cost = t;
-      clusters = n;
-    }
-  }
-  if (!best) return cudaErrorInvalidConfiguration;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(clusters < p.rows ? clusters : p.rows) * best);
-  cfg.blockDim = dim3(kAll);
-  cfg.dynamicSmemBytes = smem_bytes(p, best);
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = best;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kKernel, p);
+  Clusters l;
+  const cudaError_t e = choose_clusters<kKernel>(p.rows, 1, kStreamCluster, kAll, most, &l);
+  return e != cudaSuccess ? e : launch_clusters<kKernel>(l, kAll, smem_bytes(p, l.size), s, p);
 }
 
 template <typename T, int TOP>

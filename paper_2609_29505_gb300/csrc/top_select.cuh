@@ -11,26 +11,6 @@ namespace rows {
 
 constexpr int kCap = 512;  // candidates that are ranked
 
-// kN threads of a CTA (whole warps) with a hardware barrier of their own.
-template <int kN, int kBar>
-struct Team {
-  static constexpr int kSize = kN, kWarps = kN / 32;
-  int tid;
-  __device__ void sync() const { asm volatile("barrier.cta.sync.aligned %0, %1;" ::"n"(kBar), "n"(kN) : "memory"); }
-  // number of threads whose predicate holds; a barrier as well
-  __device__ int count(bool p) const {
-    int n;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %1, 0;\n\t"
-        "barrier.cta.red.popc.aligned.u32 %0, %2, %3, p;\n\t}"
-        : "=r"(n)
-        : "r"(static_cast<int>(p)), "n"(kBar), "n"(kN)
-        : "memory");
-    return n;
-  }
-};
-
 // value of a candidate above, (reversed) index below: larger is likelier, ties to the lower index
 __device__ __forceinline__ uint64_t candidate(uint32_t key, int index) {
   return static_cast<uint64_t>(key) << 32 | (0xFFFFFFFFu - static_cast<uint32_t>(index));

@@ -122,11 +122,11 @@ struct Slice {
   int v0;     // first vector of this CTA
   int nv;     // its vectors (0: none)
 
-  __device__ Slice(const T* r, int n, int rank, int n_ctas) : row(r), vocab(n) {
+  __device__ Slice(const T* r, int n, int rank, int n_ctas) : row(r), vocab(n) {  // n_ctas: a power of two
     constexpr int E = Elem<T>::kPer;
     shift = static_cast<int>((reinterpret_cast<uintptr_t>(r) & 15u) / sizeof(T));
     total = (shift + vocab + E - 1) / E;
-    const int per = (total + n_ctas - 1) / n_ctas;
+    const int per = (total + n_ctas - 1) >> (31 - __clz(n_ctas));
     v0 = rank * per;
     nv = min(per, total - v0);
     if (nv < 0) nv = 0;
@@ -289,6 +289,26 @@ __device__ __forceinline__ uint32_t cluster_ctas() {
 }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+// kN threads of a CTA (whole warps) with a hardware barrier of their own.
+template <int kN, int kBar>
+struct Team {
+  static constexpr int kSize = kN, kWarps = kN / 32;
+  int tid;
+  __device__ void sync() const { asm volatile("barrier.cta.sync.aligned %0, %1;" ::"n"(kBar), "n"(kN) : "memory"); }
+  // number of threads whose predicate holds; a barrier as well
+  __device__ int count(bool p) const {
+    int n;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %1, 0;\n\t"
+        "barrier.cta.red.popc.aligned.u32 %0, %2, %3, p;\n\t}"
+        : "=r"(n)
+        : "r"(static_cast<int>(p)), "n"(kBar), "n"(kN)
+        : "memory");
+    return n;
+  }
+};
 
 // Grid: a cluster per row.  The cluster size is a power of two: slices of at most kSlice bytes, and
 // smaller ones where there are too few rows to fill the SMs.

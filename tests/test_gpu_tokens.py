@@ -493,6 +493,97 @@ def test_a_small_tail_is_not_lost(B):
     _distill(B, z, ids, logq)
 
 
+def _check_rows(loss, grad, z, ids, logq, bucket, w):
+    """_check_distill at scale 1 in float64 on the device, for rows of which there are many."""
+    rows, vocab = z.shape
+    lp = torch.log_softmax(z.double(), 1)
+    p = lp.exp()
+    here = (ids >= 0) & (ids < vocab)
+    here &= ~torch.tril(ids[:, :, None] == ids[:, None, :], -1).any(2)
+    at = torch.where(here, ids.long(), vocab)
+    lq = logq.double()
+    q = torch.where(here, lq.exp(), 0.0)
+    Q = q.sum(1, keepdim=True)
+    live = (w[:, None] != 0) & here.any(1, keepdim=True)
+    scatter = lambda v: torch.zeros(rows, vocab + 1, dtype=torch.float64, device=z.device).scatter_(1, at, v)[:, :vocab]  # noqa: E731
+    S = scatter(torch.ones_like(q)) > 0
+    lps = torch.gather(lp, 1, at.clamp(max=vocab - 1))
+    if bucket:
+        qt, pt = (1 - Q).clamp(min=0), torch.where(S, 0.0, p).sum(1, keepdim=True)
+    else:
+        q, lq, qt, pt = q / Q, lq - Q.log(), torch.zeros_like(Q), torch.ones_like(Q)
+    terms = torch.where(q > 0, q * (lq - lps), 0.0)
+    L = terms.sum(1, keepdim=True) + torch.where(qt > 0, qt * (qt.log() - pt.log()), 0.0)
+    tol = SUM * (q.sum(1, keepdim=True) + 2 * qt) + 2 * U * terms.abs().sum(1, keepdim=True)
+    tol = tol + torch.where(qt > 0, 4 * U * Q * (qt.log() - pt.log() + 1).abs(), 0.0)
+    w = torch.where(live, w[:, None].double(), 0.0)
+    L = torch.where(live, w * L, 0.0)
+    assert ((loss[:, None].double() - L).abs() <= w.abs() * torch.where(live, tol, 0.0) + U * L.abs()).all()
+    if grad is None:
+        return
+    G = grad.dtype
+    half, least = torch.finfo(G).eps / 2, torch.finfo(G).smallest_normal * torch.finfo(G).eps / 2
+    qs, ratio = scatter(q), qt / pt
+    g = torch.where(live, w * torch.where(S, p - qs, p * (1 - ratio)), 0.0)
+    ep = SUM + (4 + 3 * torch.where(p > 0, lp.abs(), 0.0)) * U
+    tol = p * ep + torch.where(S, qs * (4 * U if bucket else SUM), p * ratio * (2 * SUM + ep))
+    if bucket:
+        tol = tol + torch.where(S, 0.0, p / pt * 2 * U * Q)
+    tol = torch.where(live, w.abs() * tol, 0.0)
+    err = (grad.double() - g).abs()
+    assert (err <= tol + half * (g.abs() + tol) + least).all(), (err / (tol + half * (g.abs() + tol) + least)).max()
+
+
+# many long rows: they stream through clusters of 1 to 8 CTAs
+@pytest.mark.parametrize("rows,vocab,dtype,grad,pad,offset", [
+    (152, 126464, "f16", "bf16", 0, 0), (301, 126464, "f16", "f16", 0, 0), (140, 126464, "f16", "", 0, 0),
+    (700, 32003, "bf16", "bf16", 0, 1), (541, 32003, "f16", "f32", 13, 0), (211, 50021, "f32", "f32", 0, 3),
+    (1100, 16387, "f16", "f16", 5, 2), (1100, 16387, "bf16", "", 1, 0), (70, 266176, "f16", "bf16", 0, 0),
+    (66, 133081, "f32", "bf16", 2, 1), (90, 126464, "f32", "f32", 0, 0)])
+@pytest.mark.parametrize("bucket,k", [(True, 32), (False, 64), (True, 1)])
+def test_distill_of_many_rows(B, rows, vocab, dtype, grad, pad, offset, bucket, k):
+    assert rows * vocab * torch.finfo(DT[dtype]).bits // 8 >= 32 << 20
+    g = torch.Generator("cuda").manual_seed(rows)
+    buf = torch.full((offset + rows * (vocab + pad),), 3e4, dtype=DT[dtype], device="cuda")
+    z = buf[offset:].view(rows, vocab + pad)[:, :vocab]
+    z.copy_(torch.empty(rows, vocab, device="cuda").normal_(0, 2, generator=g))
+    z[rows // 3, vocab // 2:] = -INF
+    top = torch.topk(z.float() + torch.empty(rows, vocab, device="cuda").normal_(0, 1, generator=g), k, dim=1)
+    ids = top.indices.int()
+    logq = top.values - math.log(vocab) - 2.0
+    ids[3, k // 2:] = -1
+    ids[4, :] = -1
+    ids[5, k - 1] = ids[5, 0]
+    w = 0.5 + torch.rand(rows, device="cuda", generator=g)
+    w[torch.rand(rows, device="cuda", generator=g) < 0.3] = 0
+    loss, out = _distill(B, z, ids, logq, bucket=bucket, weight=w, grad=grad, check=False)
+    some = sorted({0, 1, 3, 4, 5, rows // 3, rows - 1, *range(7, rows, max(1, rows // 5))})
+    _check_distill(loss[some], None if out is None else out[some], z[some], ids[some], logq[some], 1.0, bucket, w[some])
+    for a in range(0, rows, 16):
+        b = slice(a, a + 16)
+        _check_rows(loss[b], out[b] if grad else None, z[b], ids[b], logq[b], bucket, w[b])
+    if dtype == grad:  # in the place of the logits
+        l2 = torch.empty_like(loss)
+        B.sgd_kernel_distill(z, ids, logq, l2, grad=z, row_weight=w, tail=B.TAIL_BUCKET if bucket else B.TAIL_RENORM)
+        assert torch.equal(l2, loss) and torch.equal(z, out)
+        assert (buf[:offset] == 3e4).all() and (buf[offset:].view(rows, vocab + pad)[:, vocab:] == 3e4).all()
+
+
+@pytest.mark.parametrize("weights", ["none", "zero", "one left", "none given"])
+def test_weights_of_many_rows(B, weights):
+    rows, vocab = 1200, 20000
+    z = torch.empty(rows, vocab, dtype=torch.float16, device="cuda").normal_(0, 2, generator=torch.Generator("cuda").manual_seed(1))
+    ids, logq = torch.randint(0, vocab, (rows, 3), dtype=torch.int32).cuda(), torch.full((rows, 3), -1.2).cuda()
+    w = None if weights == "none given" else torch.zeros(rows, device="cuda") if weights != "none" else torch.ones(rows, device="cuda")
+    if weights == "one left":
+        w[777] = 2.0
+    loss, g = _distill(B, z, ids, logq, weight=w, grad="bf16", check=False)
+    some = [0, 5, 776, 777, 778, rows - 1]
+    _check_distill(loss[some], g[some], z[some], ids[some], logq[some], 1.0, True, None if w is None else w[some])
+    if weights in ("zero", "one left"):
+        assert int((loss != 0).sum()) == (weights == "one left") and int((g != 0).any(1).sum()) == (weights == "one left")
+
+
 @pytest.mark.parametrize("bucket", [True, False])
 def test_gradient_is_the_difference_of_the_loss(B, bucket):
     """(L(z + h v) - L(z - h v)) / 2 h against <gradient, v>, through the kernel alone: fp32 losses off by
