@@ -15,6 +15,11 @@ using namespace rows;
 
 using Block = Team<kThreads, 0>;
 
+struct InShared {
+  const uint4* buf;
+  __device__ uint4 operator()(int i) const { return buf[i]; }
+};
+
 template <typename T, int TOP, bool ENT>
 __global__ void __launch_bounds__(kThreads, 3) logprobs_kernel(const ScoreArgs p, uint32_t list_offset) {
   extern __shared__ __align__(128) uint4 buf[];
@@ -97,7 +102,6 @@ __global__ void __launch_bounds__(kThreads, 3) logprobs_kernel(const ScoreArgs p
   uint64_t* lists = reinterpret_cast<uint64_t*>(reinterpret_cast<char*>(buf) + list_offset);
   TopShared& top = *reinterpret_cast<TopShared*>(top_raw);
   if (TOP == kTopMany) {
-    auto fetch = [&](int i) { return buf[i]; };
     const uint32_t keys[1] = {order_key(st.m)};
     uint32_t above;
     const uint32_t lo = threshold(team, keys, p.top_k, top, above);
@@ -106,11 +110,11 @@ __global__ void __launch_bounds__(kThreads, 3) logprobs_kernel(const ScoreArgs p
       for (int i = threadIdx.x; i < sl.nv; i += kThreads) {
         const uint4 v = buf[i];
         if (lo > kKeyNegInf && !(vec_max<1>(&v, static_cast<const T*>(nullptr)) >= bar)) continue;
-        append(sl, v, sl.first_element(i), lo, top);
+        append<T>(v, sl.first_element(i), sl.vocab, lo, &top);
       }
     }
     __syncthreads();
-    if (top.n > kCap) candidates_of_many(team, sl, fetch, lo, above, p.top_k, top);
+    if (top.n > kCap) candidates_of_many(team, sl, InShared{buf}, lo, above, p.top_k, top);
   }
   __syncwarp();
   cluster_wait();  // every CTA of the cluster runs: the leader's shared memory may be written

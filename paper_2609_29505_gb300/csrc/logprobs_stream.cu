@@ -1,19 +1,18 @@
 // Scoring of many long rows (logprobs.cu has the formulas): the rows stream through the SMs.
 //
-// One CTA per SM stays for the whole call.  A producer warp keeps a ring of 16 KB tiles filled by bulk
-// copies, across the ends of rows; 8 warps take the tiles' statistics and never wait for anything but
-// data; 4 warps finish a row (sums, likeliest tokens, outputs) while the others are at the next one.
-// Where there are too few rows for the SMs, the CTAs of a cluster share each row and the first of
-// them merges their parts.
+// One CTA per SM stays for the whole call.  A producer warp keeps a ring of 32 KB tiles filled by bulk
+// copies, across the ends of rows; 16 warps take the tiles' statistics and wait for nothing but data; 6
+// warps finish the rows, each a row of its own (sums, likeliest tokens, outputs: a chain of latency of
+// several us, so that as many of them run at once).  Where there are too few rows for the SMs, the CTAs of
+// a cluster share each row and the first of them merges their parts.
 //
-// The likeliest tokens without a second pass over the row: the streaming warps leave the maximum of
-// each group of vectors (of one thread, in consecutive tiles; at most 4096 groups).  The k-th largest of
-// the 256 threads' maxima is a threshold that k elements or a few more reach; only the groups whose
-// maximum reaches it are read again (some 64 bytes each, from L2).  For the single likeliest token
-// the tile of each thread's first maximum is enough.
+// The likeliest tokens without a second pass over the row: the k-th largest of the 512 streaming threads'
+// maxima is a threshold that k elements or a few more reach; of the threads whose maximum reaches it, the
+// maxima of four parts of what they saw tell which part to read again (k / 2048 of the row).  One batch of
+// loads does: a load takes some 3 us here, behind the copies that keep the memory busy.  For the single
+// likeliest token the tile of each thread's first maximum is enough.
 //
-// Every wait is bounded.  After one has expired (recorded in the status word) each role leaves its loop;
-// the teams that share a hardware barrier leave together.
+// Every wait is bounded.  After one has expired (recorded in the status word) each warp leaves its loop.
 #include "logprobs.cuh"
 #include "persistent.cuh"
 
@@ -23,40 +22,46 @@ namespace {
 
 constexpr int kStreamWarps = 16, kStreamThreads = 32 * kStreamWarps;
 constexpr int kDeep = 4, kTile = kStreamThreads * kDeep;  // vectors of a tile: kDeep per thread
-constexpr int kFinishWarps = 4, kFinishThreads = 32 * kFinishWarps;  // of each of two teams, which take turns
-constexpr int kAll = kStreamThreads + 2 * kFinishThreads + 32;
-constexpr int kSlots = 5;
+constexpr int kFinishWarps = 6;
+constexpr int kAll = kStreamThreads + 32 * (kFinishWarps + 1);
 constexpr int kTileBytes = kTile * 16;
-constexpr int kGroupTiles = 8;   // groups of one thread
-constexpr int kMaxGroups = 256;  // groups read again
-constexpr int kStreamCluster = 8;
-constexpr int kMaxima = kStreamThreads / kFinishThreads;  // streaming threads' maxima per finishing thread
+constexpr int kStreamCluster = 4;
+constexpr int kMaxima = kStreamThreads / 32;  // streaming threads' maxima per lane
+constexpr int kParts = 4;       // of what a thread sees of a row: consecutive tiles
+constexpr int kMaxGroups = 256;
+constexpr int slots(int top) { return top == kTopMany ? 4 : 5; }
+
+// A row on its way from the streaming warps to its finishing warp, and across the cluster.
+struct Row {
+  uint64_t part_full, part_free;  // its statistics in this CTA
+  uint64_t row_full, row_free;    // its parts from all CTAs, in the first one
+  int row;                        // -1: no more
+  float result[2];
+  float4 part[kStreamWarps];
+  float4 slot[kStreamCluster];
+  uint32_t max_key[kStreamThreads];
+  uint16_t max_tile[kStreamThreads];  // of the first maximum; the threads that are looked at again
+};
+
+// What a finishing warp needs for lists of more than one.
+struct Many {
+  TopShared top;
+  uint16_t groups[kMaxGroups];                        // parts that are read again: thread and part
+  uint16_t group_key[kParts * kStreamThreads];  // upper halves of the parts' maxima's keys
+};
 
 struct Shared {
-  uint64_t full[kSlots], empty[kSlots];
-  uint64_t part_full[2], part_free[2];    // a row's statistics in this CTA
-  uint64_t row_full[2], row_free[2];      // its parts from all CTAs, in the first one
+  uint64_t full[5], empty[5];
+  int slot_row[5];  // row of a tile; -1: no more
   int abort_flag;
-  int slot_row[kSlots];                   // row of a tile; -1: no more
-  int part_row[2];
-  float4 part[2][kStreamWarps];
-  uint32_t max_key[2][kStreamThreads];
-  int max_tile[2][kStreamThreads];
-  float4 slot[2][kStreamCluster];
-  float result[2][2];
-  int first_tile[2], best[2];
-  int n_groups[2];
-  RowLists rows;
-};
-struct Many {
-  TopShared top[2];
-  int groups[2][kMaxGroups];
-  uint32_t group_key[2][kGroupTiles * kStreamThreads];
+  Row row[kFinishWarps];
+  RowLists lists;
 };
 
 template <typename T>
 __device__ __forceinline__ int tiles_of(const Slice<T>& sl) { return max(1, (sl.nv + kTile - 1) / kTile); }
 
+template <int kSlots>
 struct Ring {
   int slot = 0;
   uint32_t phase = 0;
@@ -68,146 +73,165 @@ struct Ring {
   }
 };
 
-// The rows whose statistics are left in buffer b, one after another: their likeliest tokens in this CTA, and in
-// the cluster's first CTA their outputs.
-template <typename T, int TOP, bool ENT, typename Tm>
-__device__ __forceinline__ void finish_rows(const Tm team, const int b, const ScoreArgs& p, Shared& sh, Many& many,
-                                            uint64_t* lists, const int rank, const int n_ctas) {
+template <typename T>
+struct FromRow {
+  Slice<T> sl;
+  __device__ uint4 operator()(int i) const { return sl.fetch(i); }
+};
+
+// Tiles of a part.
+__device__ __forceinline__ int tiles_of_part(int tiles) { return (tiles + kParts - 1) / kParts; }
+
+// The slice's k likeliest elements are among the candidates left in many.top.
+template <typename T>
+__device__ __forceinline__ void candidates(const WarpTeam& team, const Slice<T>& sl, Row& x, int k, Many& many) {
+  const int lane = team.tid;
+  TopShared& top = many.top;
+  uint32_t keys[kMaxima], above;
+#pragma unroll
+  for (int h = 0; h < kMaxima; ++h) keys[h] = x.max_key[lane + 32 * h];
+  const uint32_t lo = threshold(team, keys, k, top, above);
+  int n = 0;
+#pragma unroll
+  for (int h = 0; h < kMaxima; ++h) {
+    const uint32_t hit = __ballot_sync(0xffffffffu, keys[h] >= lo);
+    if (keys[h] >= lo) x.max_tile[n + __popc(hit & ((1u << lane) - 1u))] = static_cast<uint16_t>(lane + 32 * h);
+    n += __popc(hit);
+  }
+  __syncwarp();
+  int groups = 0;
+  for (int j0 = 0; j0 < n * kParts; j0 += 32) {
+    const int j = j0 + lane;
+    const int g = j < n * kParts ? j % kParts * kStreamThreads + x.max_tile[j / kParts] : -1;
+    const bool is = g >= 0 && many.group_key[max(g, 0)] >= lo >> 16;
+    const uint32_t hit = __ballot_sync(0xffffffffu, is);
+    const int at = groups + __popc(hit & ((1u << lane) - 1u));
+    if (is && at < kMaxGroups) many.groups[at] = static_cast<uint16_t>(g);
+    groups += __popc(hit);
+  }
+  __syncwarp();
+  if (groups <= kMaxGroups) {
+    const float bar = key_value(lo);
+    const uint4 none = no_elements<T>();
+    // 8 lanes take 8 vectors of a part; 10 such loads of a lane are on their way at once
+    constexpr int kAhead = 10;
+    const int vectors = tiles_of_part(tiles_of(sl)) * kDeep, per = (vectors + 7) >> 3;
+    const float per_inv = 1.f / per;
+    auto vector = [&](int c) {  // local vector of chunk c for this lane; -1: none, or not whole
+      if (c >= groups * per) return -1;
+      const int q = static_cast<int>((c + 0.5f) * per_inv);  // c / per: exact, c is far below 2^22
+      const int w = (c - q * per) * 8 + (lane & 7), g = many.groups[q], thread = g % kStreamThreads;
+      const int i = (g / kStreamThreads * vectors + w) * kStreamThreads + thread;
+      return w < vectors && i < sl.nv && sl.whole(i) ? i : -1;
+    };
+#pragma unroll 1
+    for (int c0 = lane >> 3; c0 < groups * per; c0 += 4 * kAhead) {
+      uint4 v[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int i = vector(c0 + 4 * u);
+        v[u] = none;
+        if (i >= 0) v[u] = *reinterpret_cast<const uint4*>(sl.row + sl.first_element(i));
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        if (vec_max<1>(&v[u], static_cast<const T*>(nullptr)) >= bar) {
+          const int i = vector(c0 + 4 * u);  // (-1: the threshold is -inf)
+          if (i >= 0) append<T>(v[u], sl.first_element(i), sl.vocab, lo, &top);
+        }
+    }
+    if (lane < 2 && sl.nv > 0) {  // the slice's ragged ends
+      const int i = lane ? sl.nv - 1 : 0;
+      if (!sl.whole(i) && !(lane && i == 0)) append<T>(sl.gather(i), sl.first_element(i), sl.vocab, lo, &top);
+    }
+  }
+  __syncwarp();
+  if (groups > kMaxGroups || top.n > kCap) candidates_of_many(team, sl, FromRow<T>{sl}, lo, above, k, top);
+}
+
+// The rows of one finishing warp, one after another.
+template <typename T, int TOP, bool ENT>
+__device__ __forceinline__ void finish_rows(const ScoreArgs& p, Row& x, Many& many, uint64_t* lists, volatile int* abort_flag,
+                                            const int rank, const int n_ctas) {
   const T* logits = static_cast<const T*>(p.logits);
   const float c = p.scale * kLog2e;
-  const int tid = team.tid;
-  volatile int* abort_flag = &sh.abort_flag;
-  TopShared& top = many.top[b];
+  const int lane = lane_id();
+  const WarpTeam team{lane};
   for (uint32_t phase = 0;; phase ^= 1) {
-    bool ok = mbar_wait_warp(smem_u32(&sh.part_full[b]), phase, abort_flag, p.status, 66);
-    const int r = ok ? sh.part_row[b] : -1;
-    if (tid == 0) {
-      sh.best[b] = sh.first_tile[b] = 0x7FFFFFFF;
-      sh.n_groups[b] = 0;
-    }
-    if (team.count(!ok) || r < 0) break;
+    if (!mbar_wait_warp(smem_u32(&x.part_full), phase, abort_flag, p.status, 66)) break;
+    const int r = x.row;
+    if (r < 0) break;
     const T* row = logits + r * p.ld;
     const Slice<T> sl(row, p.vocab, rank, n_ctas);
     Given<T> given;
-    if (rank == 0) given.fetch(p, row, r, tid);
-    auto fetch = [&](int i) { return sl.fetch(i); };
-    float m = -kInf;
-#pragma unroll
-    for (int w = 0; w < kStreamWarps; ++w) m = fmaxf(m, sh.part[b][w].x);
+    if (rank == 0) given.fetch(p, row, r, lane);
+    float4 v = make_float4(-kInf, 0.f, 0.f, 0.f);
+    if (lane < kStreamWarps) v = x.part[lane];
+    const float m = key_value(__reduce_max_sync(0xffffffffu, order_key(v.x)));
+    int best = 0x7FFFFFFF;
     if (TOP == kTopOne) {
       const uint32_t key = order_key(m);
-      int mine[kMaxima], first = 0x7FFFFFFF;
+      int mine[kMaxima], tile = 0x7FFFFFFF;
 #pragma unroll
       for (int h = 0; h < kMaxima; ++h) {
-        const int i = tid + h * kFinishThreads;
-        mine[h] = sh.max_key[b][i] == key ? sh.max_tile[b][i] : 0x7FFFFFFF;
-        first = min(first, mine[h]);
+        const int i = lane + 32 * h;
+        mine[h] = x.max_key[i] == key ? x.max_tile[i] : 0x7FFFFFFF;
+        tile = min(tile, mine[h]);
       }
-      first = __reduce_min_sync(0xffffffffu, first);
-      if ((tid & 31) == 0) atomicMin(&sh.first_tile[b], first);
-      team.sync();
-      const int tile = sh.first_tile[b];
+      tile = __reduce_min_sync(0xffffffffu, tile);
       if (m == -kInf) {
-        if (tid == 0 && sl.nv > 0) sh.best[b] = max(sl.first_element(0), 0);
+        if (sl.nv > 0) best = max(sl.first_element(0), 0);
       } else {
-        int found = 0x7FFFFFFF;
 #pragma unroll
         for (int h = 0; h < kMaxima; ++h) {
           if (mine[h] != tile) continue;
-#pragma unroll
           for (int u = 0; u < kDeep; ++u) {
-            const int i = tile * kTile + u * kStreamThreads + h * kFinishThreads + tid;
+            const int i = tile * kTile + u * kStreamThreads + 32 * h + lane;
             if (i >= sl.nv) continue;
             float f[Elem<T>::kPer];
             unpack(sl.fetch(i), f, static_cast<const T*>(nullptr));
 #pragma unroll
             for (int j = 0; j < Elem<T>::kPer; ++j)
-              if (f[j] == m) found = min(found, sl.first_element(i) + j);
+              if (f[j] == m) best = min(best, sl.first_element(i) + j);
           }
         }
-        if (found != 0x7FFFFFFF) atomicMin(&sh.best[b], found);
+        best = __reduce_min_sync(0xffffffffu, best);
       }
-      team.sync();
     }
+    if (TOP == kTopMany) candidates(team, sl, x, p.top_k, many);
+    // to the first CTA, once it is done with this warp's row before
+    if (n_ctas > 1 && !wait_cluster(&x.row_free, phase ^ 1u, abort_flag, p.status, 67)) break;
     if (TOP == kTopMany) {
-      const int tiles = tiles_of(sl), per_group = (tiles + kGroupTiles - 1) / kGroupTiles;
-      const int n_keys = (tiles + per_group - 1) / per_group * kStreamThreads;
-      uint32_t keys[kMaxima];
-#pragma unroll
-      for (int h = 0; h < kMaxima; ++h) keys[h] = sh.max_key[b][tid + h * kFinishThreads];
-      uint32_t above;
-      const uint32_t lo = threshold(team, keys, p.top_k, top, above);
-      for (int i = 4 * tid; i < n_keys; i += 4 * kFinishThreads) {
-        const uint4 k = *reinterpret_cast<const uint4*>(&many.group_key[b][i]);
-        const uint32_t q[4] = {k.x, k.y, k.z, k.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (q[j] >= lo) {
-            const int n = atomicAdd(&sh.n_groups[b], 1);
-            if (n < kMaxGroups) many.groups[b][n] = i + j;
-          }
-      }
-      team.sync();
-      const int n = sh.n_groups[b], per = per_group * kDeep;  // vectors of a group
-      if (n <= kMaxGroups) {
-        const float bar = key_value(lo);
-        for (int j = tid; j < n * per; j += kFinishThreads) {
-          const int q = j / per, w = j - q * per, grp = many.groups[b][q];
-          const int tile = grp / kStreamThreads * per_group + w / kDeep;
-          const int i = tile * kTile + (w % kDeep) * kStreamThreads + grp % kStreamThreads;
-          if (i >= sl.nv) continue;
-          const uint4 v = sl.fetch(i);
-          if (lo > kKeyNegInf && !(vec_max<1>(&v, static_cast<const T*>(nullptr)) >= bar)) continue;
-          append(sl, v, sl.first_element(i), lo, top);
-        }
-      }
-      team.sync();
-      if (n > kMaxGroups || top.n > kCap) candidates_of_many(team, sl, fetch, lo, above, p.top_k, top);
+      const uint32_t to = map_to_rank(smem_u32(lists + rank * p.top_k), 0);
+      rank_candidates(team, many.top, p.top_k, [&](int place, uint64_t y) { st_cluster(to + 8 * place, y); });
     }
-    // to the first CTA, once it is done with the row before the last
-    if (n_ctas > 1) {
-      ok = wait_cluster(&sh.row_free[b], phase ^ 1u, abort_flag, p.status, 67);
-      if (team.count(!ok)) break;
-    }
-    if (TOP == kTopMany) {
-      const uint32_t to = map_to_rank(smem_u32(lists + (b * n_ctas + rank) * p.top_k), 0);
-      rank_candidates(team, top, p.top_k, [&](int place, uint64_t x) { st_cluster(to + 8 * place, x); });
-    }
-    if (tid < 32) {
-      float s = 0.f, t = 0.f;
-      if (tid < kStreamWarps) {
-        s = sh.part[b][tid].y;
-        t = sh.part[b][tid].z;
-        rebase(sh.part[b][tid].x, c, reference(m, c), s, t);
-      }
-      s = warp_sum(s);
-      if (ENT) t = warp_sum(t);
-      if (tid == 0)
-        st_cluster(map_to_rank(smem_u32(&sh.slot[b][rank]), 0), make_float4(m, s, t, __int_as_float(TOP == kTopOne ? sh.best[b] : 0)));
-    }
-    team.sync();
-    if (tid == 0) {
-      mbar_arrive(&sh.part_free[b]);
-      if (n_ctas > 1) mbar_arrive_cluster(map_to_rank(smem_u32(&sh.row_full[b]), 0));
+    rebase(v.x, c, reference(m, c), v.y, v.z);
+    v.y = warp_sum(v.y);
+    if (ENT) v.z = warp_sum(v.z);
+    if (lane == 0) st_cluster(map_to_rank(smem_u32(&x.slot[rank]), 0), make_float4(m, v.y, v.z, __int_as_float(best)));
+    __syncwarp();
+    if (lane == 0) {
+      mbar_arrive(&x.part_free);
+      if (n_ctas > 1) mbar_arrive_cluster(map_to_rank(smem_u32(&x.row_full), 0));
     }
     if (rank == 0) {
-      if (n_ctas > 1) {
-        ok = wait_cluster(&sh.row_full[b], phase, abort_flag, p.status, 68);
-        if (team.count(!ok)) break;
-      }
-      finish<T, TOP, ENT>(team, p, r, row, given, sh.slot[b], lists + b * n_ctas * p.top_k, n_ctas, sh.result[b]);
-      team.sync();
-      if (n_ctas > 1 && tid < n_ctas) mbar_arrive_cluster(map_to_rank(smem_u32(&sh.row_free[b]), tid));
+      __syncwarp();
+      if (n_ctas > 1 && !wait_cluster(&x.row_full, phase, abort_flag, p.status, 68)) break;
+      finish<T, TOP, ENT>(team, p, r, row, given, x.slot, lists, n_ctas, x.result);
+      __syncwarp();
+      if (n_ctas > 1 && lane < n_ctas) mbar_arrive_cluster(map_to_rank(smem_u32(&x.row_free), lane));
     }
+    __syncwarp();
   }
 }
 
 template <typename T, int TOP, bool ENT>
 __global__ void __launch_bounds__(kAll, 1) logprobs_stream_kernel(const ScoreArgs p) {
+  constexpr int kSlots = slots(TOP);
   extern __shared__ __align__(128) uint4 buf[];
   __shared__ Shared sh;
-  Many& many = *reinterpret_cast<Many*>(buf + kSlots * kTile);  // (kTopMany)
-  uint64_t* lists = reinterpret_cast<uint64_t*>(buf + kSlots * kTile + sizeof(Many) / 16);  // [2][n_ctas][top_k]
+  Many* many = reinterpret_cast<Many*>(buf + kSlots * kTile);          // (kTopMany: of each finishing warp)
+  uint64_t* lists = reinterpret_cast<uint64_t*>(many + kFinishWarps);  // [kFinishWarps][n_ctas][top_k]
   const int rank = cluster_rank(), n_ctas = cluster_ctas();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   volatile int* abort_flag = &sh.abort_flag;
@@ -216,29 +240,29 @@ __global__ void __launch_bounds__(kAll, 1) logprobs_stream_kernel(const ScoreArg
       mbar_init(&sh.full[i], 1);
       mbar_init(&sh.empty[i], kStreamWarps);
     }
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(&sh.part_full[i], kStreamWarps);
-      mbar_init(&sh.part_free[i], 1);
-      mbar_init(&sh.row_full[i], n_ctas);
-      mbar_init(&sh.row_free[i], 1);
+    for (int i = 0; i < kFinishWarps; ++i) {
+      mbar_init(&sh.row[i].part_full, kStreamWarps);
+      mbar_init(&sh.row[i].part_free, 1);
+      mbar_init(&sh.row[i].row_full, n_ctas);
+      mbar_init(&sh.row[i].row_free, 1);
     }
     sh.abort_flag = 0;
     fence_mbar_init();
     fence_proxy_async_smem();
   }
   const int cluster = blockIdx.x / n_ctas, clusters = gridDim.x / n_ctas;
-  const bool listed = p.row_ids && make_row_lists<kAll>(sh.rows, p.rows, cluster, clusters,
+  const bool listed = p.row_ids && make_row_lists<kAll>(sh.lists, p.rows, cluster, clusters,
                                                         [&](int r) { return p.row_ids[r] == p.row_id; });
   __syncthreads();
   cluster_sync();
   const T* logits = static_cast<const T*>(p.logits);
   const float c = p.scale * kLog2e;
 
-  if (warp == kStreamWarps + 2 * kFinishWarps) {
+  if (warp == kStreamWarps + kFinishWarps) {
     // ----- producer
     int at = listed ? 0 : cluster;
     auto next_row = [&]() {
-      if (listed) return at < sh.rows.n_first ? sh.rows.of_first[at++] : -1;
+      if (listed) return at < sh.lists.n_first ? sh.lists.of_first[at++] : -1;
       if (p.row_ids) {  // 32 of the cluster's rows at a time
         while (at < p.rows) {
           const int64_t r = at + static_cast<int64_t>(lane) * clusters;
@@ -252,7 +276,7 @@ __global__ void __launch_bounds__(kAll, 1) logprobs_stream_kernel(const ScoreArg
       if (r >= 0) at = clusters < p.rows - at ? at + clusters : p.rows;
       return r;
     };
-    Ring ring;
+    Ring<kSlots> ring;
     bool ok = true;
     int issued = 0;
     while (ok) {
@@ -290,31 +314,33 @@ __global__ void __launch_bounds__(kAll, 1) logprobs_stream_kernel(const ScoreArg
     }
   } else if (warp < kStreamWarps) {
     // ----- statistics
-    Ring ring;
+    Ring<kSlots> ring;
     const uint4 none = no_elements<T>();
-    for (int it = 0;; ++it) {
-      const int b = it & 1;
+    int n = 0;  // finishing warp of the row
+    uint32_t phase = 0;
+    for (bool ok = true;; phase ^= ++n == kFinishWarps, n = n == kFinishWarps ? 0 : n) {
       if (!mbar_wait_warp(smem_u32(&sh.full[ring.slot]), ring.phase, abort_flag, p.status, 64)) break;
       const int r = sh.slot_row[ring.slot];
-      if (!mbar_wait_warp(smem_u32(&sh.part_free[b]), ((it >> 1) & 1) ^ 1u, abort_flag, p.status, 65)) break;
-      if (r < 0) {  // both teams have to know
-        const int o = b ^ 1;
-        if (!mbar_wait_warp(smem_u32(&sh.part_free[o]), (((it + 1) >> 1) & 1) ^ 1u, abort_flag, p.status, 65)) break;
-        if (threadIdx.x == 0) sh.part_row[0] = sh.part_row[1] = -1;
-        __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(&sh.part_full[b]);
-          mbar_arrive(&sh.part_full[o]);
+      if (r < 0) {  // every finishing warp has to know
+        for (int i = 0; i < kFinishWarps; ++i) {
+          Row& x = sh.row[n];
+          if (!mbar_wait_warp(smem_u32(&x.part_free), phase ^ 1u, abort_flag, p.status, 65)) break;
+          if (threadIdx.x == 0) x.row = -1;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&x.part_full);
+          phase ^= ++n == kFinishWarps;
+          if (n == kFinishWarps) n = 0;
         }
         break;
       }
+      Row& x = sh.row[n];
+      if (!mbar_wait_warp(smem_u32(&x.part_free), phase ^ 1u, abort_flag, p.status, 65)) break;
       const Slice<T> sl(logits + r * p.ld, p.vocab, rank, n_ctas);
-      const int tiles = tiles_of(sl), per_group = (tiles + kGroupTiles - 1) / kGroupTiles;
+      const int tiles = tiles_of(sl), per_part = tiles_of_part(tiles);
       Stat st;
-      int at = 0;
-      float group = -kInf;
-      int in_group = 0, g = 0;
-      bool ok = true;
+      int at = 0, in_part = 0;
+      float part = -kInf;
+      uint16_t* part_key = many[n].group_key + threadIdx.x;
       for (int t = 0; t < tiles; ++t) {
         if (t > 0 && !(ok = mbar_wait_warp(smem_u32(&sh.full[ring.slot]), ring.phase, abort_flag, p.status, 64))) break;
         uint4 v[kDeep];
@@ -335,51 +361,53 @@ __global__ void __launch_bounds__(kAll, 1) logprobs_stream_kernel(const ScoreArg
         const float before = st.m, m = stat_add<T, kDeep, ENT>(st, v, c);
         if (TOP == kTopOne && m > before) at = t;
         if (TOP == kTopMany) {
-          group = fmaxf(group, m);
-          if (++in_group == per_group || t == tiles - 1) {
-            many.group_key[b][g * kStreamThreads + threadIdx.x] = order_key(group);
-            ++g;
-            in_group = 0;
-            group = -kInf;
+          part = fmaxf(part, m);
+          if (++in_part == per_part || t == tiles - 1) {
+            *part_key = static_cast<uint16_t>(order_key(part) >> 16);
+            part_key += kStreamThreads;
+            in_part = 0;
+            part = -kInf;
           }
         }
       }
       if (!ok) break;
-      if (TOP != kTopNone) sh.max_key[b][threadIdx.x] = order_key(st.m);
-      if (TOP == kTopOne) sh.max_tile[b][threadIdx.x] = at;
+      if (TOP != kTopNone) x.max_key[threadIdx.x] = order_key(st.m);
+      if (TOP == kTopOne) x.max_tile[threadIdx.x] = static_cast<uint16_t>(at);
       const float m = key_value(__reduce_max_sync(0xffffffffu, order_key(st.m)));
       float s = st.s, u = st.t;
       rebase(st.m, c, reference(m, c), s, u);
       s = warp_sum(s);
       if (ENT) u = warp_sum(u);
-      if (lane == 0) sh.part[b][warp] = make_float4(m, s, u, 0.f);
-      if (threadIdx.x == 0) sh.part_row[b] = r;
+      if (lane == 0) x.part[warp] = make_float4(m, s, u, 0.f);
+      if (threadIdx.x == 0) x.row = r;
       __syncwarp();
-      if (lane == 0) mbar_arrive(&sh.part_full[b]);
+      if (lane == 0) mbar_arrive(&x.part_full);
     }
-  } else if (warp < kStreamWarps + kFinishWarps) {
-    finish_rows<T, TOP, ENT>(Team<kFinishThreads, 1>{static_cast<int>(threadIdx.x) - kStreamThreads}, 0, p, sh, many, lists, rank, n_ctas);
   } else {
-    finish_rows<T, TOP, ENT>(Team<kFinishThreads, 2>{static_cast<int>(threadIdx.x) - kStreamThreads - kFinishThreads}, 1, p, sh, many, lists,
-                             rank, n_ctas);
+    // ----- the rest of a row
+    const int i = warp - kStreamWarps;
+    finish_rows<T, TOP, ENT>(p, sh.row[i], many[i], lists + i * n_ctas * p.top_k, abort_flag, rank, n_ctas);
   }
   __syncwarp();
   cluster_sync();  // no CTA leaves while another may still write to it
 }
 
-size_t smem_bytes(const ScoreArgs& p, int cluster) {
-  return kSlots * kTileBytes + (p.top_k > 1 ? sizeof(Many) + 2 * sizeof(uint64_t) * cluster * p.top_k : 0);
+size_t smem_bytes(int top_k, int cluster) {
+  if (top_k <= 1) return slots(kTopOne) * kTileBytes;
+  return slots(kTopMany) * kTileBytes + kFinishWarps * (sizeof(Many) + sizeof(uint64_t) * cluster * top_k);
 }
-static_assert(sizeof(Many) % 16 == 0, "the lists follow it");
-constexpr size_t kMaxLists = 2 * sizeof(uint64_t) * kStreamCluster * kMaxTop;
-static_assert(kSlots * kTileBytes + sizeof(Many) + kMaxLists + sizeof(Shared) <= 226 * 1024, "a CTA's shared memory");
+static_assert(slots(kTopMany) * kTileBytes + kFinishWarps * (sizeof(Many) + sizeof(uint64_t) * kStreamCluster * kMaxTop) +
+                      sizeof(Shared) <= 226 * 1024 &&
+                  slots(kTopOne) * kTileBytes + sizeof(Shared) <= 226 * 1024,
+              "a CTA's shared memory");
+static_assert((kMaxRowBytes / 16 + 2) / kTile < 65535, "tiles of a row in 16 bits");
 
 template <auto kKernel>
 cudaError_t launch_stream(const ScoreArgs& p, cudaStream_t s) {
-  const size_t most = kSlots * kTileBytes + (p.top_k > 1 ? sizeof(Many) + kMaxLists : 0);
   Clusters l;
-  const cudaError_t e = choose_clusters<kKernel>(p.rows, 1, kStreamCluster, kAll, most, &l);
-  return e != cudaSuccess ? e : launch_clusters<kKernel>(l, kAll, smem_bytes(p, l.size), s, p);
+  const cudaError_t e =
+      choose_clusters<kKernel>(p.rows, 1, kStreamCluster, kAll, smem_bytes(p.top_k > 1 ? kMaxTop : 1, kStreamCluster), &l);
+  return e != cudaSuccess ? e : launch_clusters<kKernel>(l, kAll, smem_bytes(p.top_k, l.size), s, p);
 }
 
 template <typename T, int TOP>

@@ -9,7 +9,7 @@
 namespace sgd {
 namespace rows {
 
-constexpr int kCap = 512;  // candidates that are ranked
+constexpr int kCap = 256;  // candidates that are ranked
 
 // value of a candidate above, (reversed) index below: larger is likelier, ties to the lower index
 __device__ __forceinline__ uint64_t candidate(uint32_t key, int index) {
@@ -28,17 +28,18 @@ struct TopShared {
 };
 
 // Appends the elements of vector `v` (its first element: e) with a key of at least `from` to the list, as
-// many as it holds, and adds their number to sh.n.
+// many as it holds, and adds their number to sh->n.  (Not inlined: it is rare, and the loops around it
+// should stay in the instruction cache.)
 template <typename T>
-__device__ __forceinline__ void append(const Slice<T>& sl, const uint4& v, int e, uint32_t from, TopShared& sh) {
+__device__ __noinline__ void append(uint4 v, int e, int vocab, uint32_t from, TopShared* sh) {
   float f[Elem<T>::kPer];
   unpack(v, f, static_cast<const T*>(nullptr));
 #pragma unroll
   for (int j = 0; j < Elem<T>::kPer; ++j) {
     const uint32_t key = order_key(f[j]);
-    if (key >= from && e + j >= 0 && e + j < sl.vocab) {
-      const int at = atomicAdd(&sh.n, 1);
-      if (at < kCap) sh.list[at] = candidate(key, e + j);
+    if (key >= from && e + j >= 0 && e + j < vocab) {
+      const int at = atomicAdd(&sh->n, 1);
+      if (at < kCap) sh->list[at] = candidate(key, e + j);
     }
   }
 }
@@ -50,7 +51,7 @@ __device__ __forceinline__ void collect(const Tm& team, const Slice<T>& sl, cons
   for (int i = team.tid; i < sl.nv; i += Tm::kSize) {
     const uint4 v = fetch(i);
     if (from > kKeyNegInf && !(vec_max<1>(&v, static_cast<const T*>(nullptr)) >= bar)) continue;
-    append(sl, v, sl.first_element(i), from, sh);
+    append<T>(v, sl.first_element(i), sl.vocab, from, &sh);
   }
   team.sync();
 }
@@ -117,7 +118,7 @@ __device__ void collect_ties(const Tm& team, const Slice<T>& sl, const F& fetch,
 }
 
 // A threshold lo with count(maxima >= lo) >= k, near k where the maxima allow it: bisection over their
-// keys, counting with the barrier.  N keys per thread, at least k in all.  `top`: a key above all.
+// keys, counting over the team.  N keys per thread, at least k in all.  `top`: a key above all.
 template <int N, typename Tm>
 __device__ uint32_t threshold(const Tm& team, const uint32_t (&key)[N], int k, TopShared& sh, uint32_t& top) {
   const int warp = team.tid >> 5, lane = team.tid & 31;
@@ -144,8 +145,14 @@ __device__ uint32_t threshold(const Tm& team, const uint32_t (&key)[N], int k, T
   while (hi - lo > 1) {
     const uint32_t mid = lo + (hi - lo) / 2;
     int n = 0;
+    if constexpr (Tm::kWarps == 1) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) n += team.count(key[i] >= mid);
+      for (int i = 0; i < N; ++i) n += key[i] >= mid;
+      n = __reduce_add_sync(0xffffffffu, n);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) n += team.count(key[i] >= mid);
+    }
     if (n >= k) lo = mid; else hi = mid;
     if (n >= k && n <= k + k / 4) break;
   }
@@ -157,8 +164,8 @@ __device__ uint32_t threshold(const Tm& team, const uint32_t (&key)[N], int k, T
 // k-th largest value itself; then what is above it is taken, and the first of those equal to it.  A
 // row of many equal values is over at once, the others take up to 32 counts.
 template <typename T, typename Tm, typename F>
-__device__ void candidates_of_many(const Tm& team, const Slice<T>& sl, const F& fetch, uint32_t lo, uint32_t top, int k,
-                                   TopShared& sh) {
+__device__ __noinline__ void candidates_of_many(const Tm team, const Slice<T> sl, const F fetch, uint32_t lo, uint32_t top, int k,
+                                                TopShared& sh) {
   team.sync();
   uint32_t hi = top, mid = lo + 1;
   int turn = 0, n = 0;

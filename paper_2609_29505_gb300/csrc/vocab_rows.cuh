@@ -310,6 +310,14 @@ struct Team {
   }
 };
 
+// The same for one warp.
+struct WarpTeam {
+  static constexpr int kSize = 32, kWarps = 1;
+  int tid;
+  __device__ void sync() const { __syncwarp(); }
+  __device__ int count(bool p) const { return __popc(__ballot_sync(0xffffffffu, p)); }
+};
+
 // Grid: a cluster per row.  The cluster size is a power of two: slices of at most kSlice bytes, and
 // smaller ones where there are too few rows to fill the SMs.
 struct Launch {
