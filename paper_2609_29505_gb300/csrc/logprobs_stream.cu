@@ -29,6 +29,7 @@ constexpr int kStreamCluster = 4;
 constexpr int kMaxima = kStreamThreads / 32;  // streaming threads' maxima per lane
 constexpr int kParts = 4;       // of what a thread sees of a row: consecutive tiles
 constexpr int kMaxGroups = 256;
+constexpr int kStaged = 96;
 constexpr int slots(int top) { return top == kTopMany ? 4 : 5; }
 
 // A row on its way from the streaming warps to its finishing warp, and across the cluster.
@@ -46,6 +47,8 @@ struct Row {
 // What a finishing warp needs for lists of more than one.
 struct Many {
   TopShared top;
+  __align__(16) uint4 staged[kStaged];
+  int staged_at[kStaged];
   uint16_t groups[kMaxGroups];                        // parts that are read again: thread and part
   uint16_t group_key[kParts * kStreamThreads];  // upper halves of the parts' maxima's keys
 };
@@ -110,6 +113,7 @@ __device__ __forceinline__ void candidates(const WarpTeam& team, const Slice<T>&
     groups += __popc(hit);
   }
   __syncwarp();
+  bool crowded = false;  // more than there is room for: a row of many equal values, say
   if (groups <= kMaxGroups) {
     const float bar = key_value(lo);
     const uint4 none = no_elements<T>();
@@ -125,7 +129,8 @@ __device__ __forceinline__ void candidates(const WarpTeam& team, const Slice<T>&
       return w < vectors && i < sl.nv && sl.whole(i) ? i : -1;
     };
 #pragma unroll 1
-    for (int c0 = lane >> 3; c0 < groups * per; c0 += 4 * kAhead) {
+    for (int first = 0; first < groups * per; first += 4 * kAhead) {  // (as often in every lane: the warp meets in it)
+      const int c0 = first + (lane >> 3);
       uint4 v[kAhead];
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
@@ -133,12 +138,29 @@ __device__ __forceinline__ void candidates(const WarpTeam& team, const Slice<T>&
         v[u] = none;
         if (i >= 0) v[u] = *reinterpret_cast<const uint4*>(sl.row + sl.first_element(i));
       }
+      // the few that hold something are put side by side, so that a lane has one of them to sort out
+      int staged = 0;
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u)
-        if (vec_max<1>(&v[u], static_cast<const T*>(nullptr)) >= bar) {
-          const int i = vector(c0 + 4 * u);  // (-1: the threshold is -inf)
-          if (i >= 0) append<T>(v[u], sl.first_element(i), sl.vocab, lo, &top);
+      for (int u = 0; u < kAhead; ++u) {
+        const bool is = vec_max<1>(&v[u], static_cast<const T*>(nullptr)) >= bar;
+        const uint32_t hit = __ballot_sync(0xffffffffu, is);
+        if (hit == 0) continue;
+        const int at = staged + __popc(hit & ((1u << lane) - 1u));
+        const int i = is && at < kStaged ? vector(c0 + 4 * u) : -1;
+        if (is && at < kStaged) {
+          many.staged[at] = v[u];
+          many.staged_at[at] = i >= 0 ? sl.first_element(i) : -Elem<T>::kPer;  // (no vector: the threshold is -inf)
         }
+        staged += __popc(hit);
+      }
+      __syncwarp();
+      if (staged > kStaged) {
+        crowded = true;
+        break;
+      }
+#pragma unroll 1
+      for (int i = lane; i < staged; i += 32) append<T>(many.staged[i], many.staged_at[i], sl.vocab, lo, &top);
+      __syncwarp();
     }
     if (lane < 2 && sl.nv > 0) {  // the slice's ragged ends
       const int i = lane ? sl.nv - 1 : 0;
@@ -146,7 +168,7 @@ __device__ __forceinline__ void candidates(const WarpTeam& team, const Slice<T>&
     }
   }
   __syncwarp();
-  if (groups > kMaxGroups || top.n > kCap) candidates_of_many(team, sl, FromRow<T>{sl}, lo, above, k, top);
+  if (crowded || groups > kMaxGroups || top.n > kCap) candidates_of_many(team, sl, FromRow<T>{sl}, lo, above, k, top);
 }
 
 // The rows of one finishing warp, one after another.
@@ -337,6 +359,7 @@ __global__ void __launch_bounds__(kAll, 1) logprobs_stream_kernel(const ScoreArg
       if (!mbar_wait_warp(smem_u32(&x.part_free), phase ^ 1u, abort_flag, p.status, 65)) break;
       const Slice<T> sl(logits + r * p.ld, p.vocab, rank, n_ctas);
       const int tiles = tiles_of(sl), per_part = tiles_of_part(tiles);
+      const int lo = sl.nv > 0 && !sl.whole(0) ? 1 : 0, hi = sl.nv > 0 && !sl.whole(sl.nv - 1) ? sl.nv - 1 : sl.nv;
       Stat st;
       int at = 0, in_part = 0;
       float part = -kInf;
@@ -345,14 +368,16 @@ __global__ void __launch_bounds__(kAll, 1) logprobs_stream_kernel(const ScoreArg
         if (t > 0 && !(ok = mbar_wait_warp(smem_u32(&sh.full[ring.slot]), ring.phase, abort_flag, p.status, 64))) break;
         uint4 v[kDeep];
         const uint4* tile = buf + ring.slot * kTile + threadIdx.x;
-        if (t > 0 && t < tiles - 1) {
+        const int k0 = t * kTile + threadIdx.x;
+        if (t * kTile >= lo && (t + 1) * kTile <= hi) {
 #pragma unroll
           for (int u = 0; u < kDeep; ++u) v[u] = tile[u * kStreamThreads];
-        } else {  // the slice's ends
+        } else {  // the slice's ends: copies bring whole vectors alone
 #pragma unroll
           for (int u = 0; u < kDeep; ++u) {
-            const int k = t * kTile + u * kStreamThreads + threadIdx.x;
-            v[u] = k >= sl.nv ? none : (sl.whole(k) ? tile[u * kStreamThreads] : sl.gather(k));
+            const int k = k0 + u * kStreamThreads;
+            v[u] = k >= lo && k < hi ? tile[u * kStreamThreads] : none;
+            if (k < sl.nv && (k < lo || k >= hi)) v[u] = sl.gather(k);
           }
         }
         __syncwarp();
