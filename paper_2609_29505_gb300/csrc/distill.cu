@@ -26,10 +26,11 @@ namespace {
 
 using namespace rows;
 
-template <typename T, typename G>
-__global__ void __launch_bounds__(kThreads, 3) distill_kernel(const DistillArgs p) {
+template <typename T, typename G, int kThreads>
+__global__ void __launch_bounds__(kThreads, 768 / kThreads) distill_kernel(const DistillArgs p) {
   constexpr bool kGrad = !std::is_same<G, NoGrad>::value;
-  constexpr int E = Elem<T>::kPer;
+  constexpr int E = Elem<T>::kPer, kWarps = kThreads / 32, kStep = kThreads * kUnroll;
+  static_assert(kThreads >= kMaxList, "a thread per entry of the list");
   extern __shared__ __align__(128) uint4 buf[];
   __shared__ uint64_t bars[kMaxPieces];
   __shared__ int abort_flag;
@@ -122,7 +123,7 @@ __global__ void __launch_bounds__(kThreads, 3) distill_kernel(const DistillArgs 
   const float c = p.scale * kLog2e;
   Stat st;
   const uint4 none = no_elements<T>();
-  for (int i = 0; i < sl.nv; i += kPiece) {
+  for (int i = 0; i < sl.nv; i += kStep) {
     uint4 v[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
@@ -185,15 +186,19 @@ __global__ void __launch_bounds__(kThreads, 3) distill_kernel(const DistillArgs 
   if (threadIdx.x == 0) p.loss[r] = row_loss(o, sums, loss_sum[0] + loss_sum[1], ls, w, p.bucket);
 }
 
+template <typename T, int kThreads>
+cudaError_t launch_threads(const DistillArgs& p, int grad_dtype, const Launch& l, cudaStream_t s) {
+  const size_t smem = l.slice_bytes;
+  if (!p.grad) return launch<&distill_kernel<T, NoGrad, kThreads>>(p.rows, l, smem, s, p);
+  if (grad_dtype == SGD_F16) return launch<&distill_kernel<T, f16, kThreads>>(p.rows, l, smem, s, p);
+  if (grad_dtype == SGD_BF16) return launch<&distill_kernel<T, bf16, kThreads>>(p.rows, l, smem, s, p);
+  return launch<&distill_kernel<T, float, kThreads>>(p.rows, l, smem, s, p);
+}
 template <typename T>
 cudaError_t launch_type(const DistillArgs& p, int grad_dtype, cudaStream_t s) {
   if (distill_stream_pays(p.rows, static_cast<int64_t>(p.vocab) * sizeof(T))) return distill_stream<T>(p, grad_dtype, s);
   const Launch l = plan(p.rows, p.vocab, sizeof(T));
-  const size_t smem = l.slice_bytes;
-  if (!p.grad) return launch<&distill_kernel<T, NoGrad>>(p.rows, l, smem, s, p);
-  if (grad_dtype == SGD_F16) return launch<&distill_kernel<T, f16>>(p.rows, l, smem, s, p);
-  if (grad_dtype == SGD_BF16) return launch<&distill_kernel<T, bf16>>(p.rows, l, smem, s, p);
-  return launch<&distill_kernel<T, float>>(p.rows, l, smem, s, p);
+  return l.threads == 64 ? launch_threads<T, 64>(p, grad_dtype, l, s) : launch_threads<T, 256>(p, grad_dtype, l, s);
 }
 
 }  // namespace

@@ -15,7 +15,8 @@
 // sent when all CTAs have sent the one between, after they have read the first.
 //
 // The loss alone keeps a buffer only until the sums are taken: the next row's copies start before they are
-// exchanged.  Rows of weight 0 are written only; they are dealt out to the clusters apart from the others.
+// exchanged.  Rows of weight 0 are dealt out to the clusters apart from the others, and two warps of their
+// own write their zeros: in a buffer's turn they would keep it from loading.
 //
 // Every wait is bounded.  After one has expired (recorded in the status word) each warp leaves its loop.
 #include "distill.cuh"
@@ -27,7 +28,8 @@ namespace {
 
 constexpr int kWorkWarps = 8, kWork = 32 * kWorkWarps;
 constexpr int kMinBuffers = 3, kMaxBuffers = 6;
-constexpr int kAllThreads = kWork + 32 * kMaxBuffers;
+constexpr int kZeroWarps = 2, kZero = 32 * kZeroWarps;
+constexpr int kAllThreads = kWork + 32 * kMaxBuffers + kZero;
 constexpr int kDeep = 4;
 constexpr int kBufferBytes = 200 * 1024;
 constexpr int kMaxStreamCluster = 8;
@@ -58,7 +60,8 @@ struct Shape {
 // A row's list, kHalves entries a lane.
 struct List {
   int row;
-  bool lives;
+  bool copied;  // it has a weight
+  bool lives;   // and its list a token
   float w;
   int id[kHalves];  // -1: none
   float q[kHalves], lq[kHalves];
@@ -191,37 +194,45 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
       }
     }
     for (; ok && behind > 0; --behind, queue >>= 4) ok = put_gradient(queue & 7, queue >> 3 & 1);
+  } else if (warp >= kWorkWarps + kMaxBuffers) {
+    // ----- rows of weight 0
+    const int tid = threadIdx.x - (kAllThreads - kZero);
+    for (int i = 0; listed && i < rows.n_rest; ++i) {
+      const int r = rows.of_rest[i];
+      if constexpr (kGrad)
+        write_grad<T, G>(slice_of(r), static_cast<G*>(p.grad) + r * p.ld_grad, tid, kZero, [](int, float* f) {
+#pragma unroll
+          for (int j = 0; j < E; ++j) f[j] = 0.f;
+        });
+      if (rank == 0 && tid == 0) p.loss[r] = 0.f;
+    }
   } else if (warp - kWorkWarps < shape.buffers) {
     // ----- one buffer's rows
     const int n = warp - kWorkWarps;
     Buffer& b = buffers[n];
     uint4* slice = buf + n * shape.vectors;
-    int turn = n;  // of the cluster's rows: those of both kinds alternate while there are any
+    int turn = n;  // of the cluster's rows
     auto next_row = [&]() {
       const int i = turn;
       turn += shape.buffers;
-      if (!listed) {
-        const int64_t r = cluster + static_cast<int64_t>(i) * clusters;
-        return r < p.rows ? static_cast<int>(r) : -1;
-      }
-      const int both = min(rows.n_first, rows.n_rest);
-      if (i < 2 * both) return i & 1 ? rows.of_rest[i >> 1] : rows.of_first[i >> 1];
-      if (i - both >= max(rows.n_first, rows.n_rest)) return -1;
-      return rows.n_first > rows.n_rest ? rows.of_first[i - both] : rows.of_rest[i - both];
+      if (listed) return i < rows.n_first ? rows.of_first[i] : -1;
+      const int64_t r = cluster + static_cast<int64_t>(i) * clusters;
+      return r < p.rows ? static_cast<int>(r) : -1;
     };
     // the next row's list as it is in memory; used later
     auto fetch_list = [&]() {
       List x;
       x.row = next_row();
-      x.lives = x.row >= 0;
       x.w = 1.f;
-      if (x.lives && p.weight) x.w = p.weight[x.row];
+      if (x.row >= 0 && p.weight) x.w = p.weight[x.row];
+      x.copied = x.row >= 0 && x.w != 0.f;
+      x.lives = false;
 #pragma unroll
       for (int h = 0; h < kHalves; ++h) {
         const int i = lane + 32 * h;
         const int64_t at = static_cast<int64_t>(x.row) * p.k + i;
-        x.id[h] = x.lives && i < p.k ? p.ids[at] : -1;
-        x.lq[h] = x.lives && i < p.k ? p.logq[at] : 0.f;
+        x.id[h] = x.copied && i < p.k ? p.ids[at] : -1;
+        x.lq[h] = x.copied && i < p.k ? p.logq[at] : 0.f;
       }
       return x;
     };
@@ -254,11 +265,10 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
       }
       const double Q = warp_sum(sum);
       x.sums = list_sums(Q, p.bucket);
-      x.lives = __any_sync(0xffffffffu, any) && x.w != 0.f && (p.bucket || Q != 0.0);
+      x.lives = __any_sync(0xffffffffu, any) && x.copied && (p.bucket || Q != 0.0);
     };
 
     List x = fetch_list(), old;  // of the row to come, and of the one in the buffer
-    sort_out(x);
     old.row = -1;
     RowSums sums;
     RowScale scale;
@@ -277,6 +287,11 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
       for (int h = 0; h < kHalves; ++h) in += vec[h] >= 0 ? ex2_approx(fmaf(z[h], c, -R)) : 0.f;
       tail = warp_sum(tail);
       in = warp_sum(in);
+      if (n_ctas == 1) {
+        sums = RowSums{m, tail, in};
+        scale = row_scale(sums, old.sums, old.w, p.scale, p.bucket, c);
+        return true;
+      }
       if (lane < n_ctas) st_cluster(map_to_rank(smem_u32(&b.slot[place][rank]), lane), make_float4(m, tail, in, 0.f));
       __syncwarp();
       if (lane < n_ctas) mbar_arrive_cluster(map_to_rank(smem_u32(&b.sums_full[place]), lane));
@@ -290,8 +305,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
       const Slice<T> sl = slice_of(max(x.row, 0));
       if (lane == 0) {
         b.row = x.row;
-        b.live = x.lives;
-        if (x.lives) {
+        if (x.copied) {
           const char* src = reinterpret_cast<const char*>(sl.row + sl.first_element(0));
           const int lo = sl.nv > 0 && !sl.whole(0) ? 1 : 0;
           const int hi = sl.nv > 0 && !sl.whole(sl.nv - 1) ? sl.nv - 1 : sl.nv;
@@ -302,9 +316,10 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
         }
       }
       __syncwarp();
-      // what is left of the old row
       bool ok = true;
-      if (old.row >= 0) {
+      if (old.row < 0) {
+        sort_out(x);  // (of the first row: its copies are under way; the others' lists are ready before)
+      } else {  // what is left of the old row
         if (old.lives) {
           if constexpr (kGrad) {
 #pragma unroll
@@ -337,7 +352,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
       }
       old = x;
       x = fetch_list();
-      if (old.lives) {
+      if (old.copied) {
         // the row's ragged ends, and what lies behind the slice (rows that start elsewhere in a vector have a
         // few vectors more or less in it)
         const bool ragged = lane < 2 * E && sl.nv > 0 && !(lane >= E && sl.nv == 1) && !sl.whole(lane < E ? 0 : sl.nv - 1);
@@ -366,6 +381,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
         fence_proxy_async_smem();
       }
       if (!ok) break;
+      if (lane == 0) b.live = old.lives;
       __syncwarp();
       if (lane == 0) mbar_arrive(&b.ready);
       if (!kGrad) sort_out(x);
@@ -416,7 +432,7 @@ static_assert(kBufferBytes + kMaxBuffers * sizeof(Buffer) + sizeof(RowLists) <= 
 }  // namespace
 
 bool distill_stream_pays(int rows, int64_t row_bytes) {
-  return row_bytes >= 32 * 1024 && rows * row_bytes >= (32 << 20) &&
+  return row_bytes >= 16 * 1024 && rows * row_bytes >= (48 << 20) &&
          kBufferBytes / (16 * static_cast<int64_t>(buffer_vectors(row_bytes, kMaxStreamCluster))) >= kMinBuffers;
 }
 

@@ -13,15 +13,15 @@ namespace {
 
 using namespace rows;
 
-using Block = Team<kThreads, 0>;
-
 struct InShared {
   const uint4* buf;
   __device__ uint4 operator()(int i) const { return buf[i]; }
 };
 
-template <typename T, int TOP, bool ENT>
-__global__ void __launch_bounds__(kThreads, 3) logprobs_kernel(const ScoreArgs p, uint32_t list_offset) {
+template <typename T, int TOP, bool ENT, int kThreads>
+__global__ void __launch_bounds__(kThreads, 768 / kThreads) logprobs_kernel(const ScoreArgs p, uint32_t list_offset) {
+  constexpr int kWarps = kThreads / 32, kStep = kThreads * kUnroll;
+  static_assert(kPiece % kStep == 0, "a thread's vectors lie in one piece");
   extern __shared__ __align__(128) uint4 buf[];
   __shared__ uint64_t bars[kMaxPieces];
   __shared__ int abort_flag;
@@ -30,7 +30,7 @@ __global__ void __launch_bounds__(kThreads, 3) logprobs_kernel(const ScoreArgs p
   __shared__ float result[2];
   __shared__ int best;
   __shared__ __align__(16) unsigned char top_raw[TOP == kTopMany ? sizeof(TopShared) : 16];
-  const Block team{static_cast<int>(threadIdx.x)};
+  const Team<kThreads, 0> team{static_cast<int>(threadIdx.x)};
   const int rank = cluster_rank(), n_ctas = cluster_ctas();
   const int64_t r = blockIdx.x / n_ctas;
   if (p.row_ids && p.row_ids[r] != p.row_id) return;  // the whole cluster
@@ -53,14 +53,14 @@ __global__ void __launch_bounds__(kThreads, 3) logprobs_kernel(const ScoreArgs p
 
   const float c = p.scale * kLog2e;
   Stat st;
-  int at = 0;  // piece in which the maximum was met first
+  int at = 0;  // step in which the maximum was met first
   const uint4 none = no_elements<T>();
-  for (int i = 0; i * kPiece < sl.nv; ++i) {
-    wait_piece(bars, i, &abort_flag, p.status, 61);
+  for (int i = 0; i * kStep < sl.nv; ++i) {
+    if (i * kStep % kPiece == 0) wait_piece(bars, i * kStep / kPiece, &abort_flag, p.status, 61);
     uint4 v[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      const int k = i * kPiece + u * kThreads + threadIdx.x;
+      const int k = i * kStep + u * kThreads + threadIdx.x;
       v[u] = k < sl.nv ? buf[k] : none;
     }
     const float before = st.m;
@@ -86,7 +86,7 @@ __global__ void __launch_bounds__(kThreads, 3) logprobs_kernel(const ScoreArgs p
       int found = 0x7FFFFFFF;
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
-        const int k = at * kPiece + u * kThreads + threadIdx.x;
+        const int k = at * kStep + u * kThreads + threadIdx.x;
         if (k < sl.nv && found == 0x7FFFFFFF) {
           float f[Elem<T>::kPer];
           unpack(buf[k], f, static_cast<const T*>(nullptr));
@@ -142,8 +142,11 @@ __global__ void __launch_bounds__(kThreads, 3) logprobs_kernel(const ScoreArgs p
 template <typename T, int TOP>
 cudaError_t launch_ent(const ScoreArgs& p, const Launch& l, size_t smem, cudaStream_t s) {
   const uint32_t lists = l.slice_bytes;
-  return p.entropy ? launch<&logprobs_kernel<T, TOP, true>>(p.rows, l, smem, s, p, lists)
-                   : launch<&logprobs_kernel<T, TOP, false>>(p.rows, l, smem, s, p, lists);
+  if (l.threads == 64)
+    return p.entropy ? launch<&logprobs_kernel<T, TOP, true, 64>>(p.rows, l, smem, s, p, lists)
+                     : launch<&logprobs_kernel<T, TOP, false, 64>>(p.rows, l, smem, s, p, lists);
+  return p.entropy ? launch<&logprobs_kernel<T, TOP, true, 256>>(p.rows, l, smem, s, p, lists)
+                   : launch<&logprobs_kernel<T, TOP, false, 256>>(p.rows, l, smem, s, p, lists);
 }
 template <typename T>
 cudaError_t launch_type(const ScoreArgs& p, cudaStream_t s) {

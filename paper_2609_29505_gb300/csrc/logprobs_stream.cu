@@ -443,7 +443,10 @@ cudaError_t stream_ent(const ScoreArgs& p, cudaStream_t s) {
 
 }  // namespace
 
-bool stream_pays(int rows, int64_t row_bytes) { return row_bytes >= 32 * 1024 && rows * row_bytes >= (32 << 20); }
+bool stream_pays(int rows, int64_t row_bytes) {
+  const double share = (256 << 10) / static_cast<double>(row_bytes);
+  return row_bytes >= 96 * 1024 && rows * row_bytes >= (24 << 20) * share * share;
+}
 
 template <typename T>
 cudaError_t score_stream(const ScoreArgs& p, cudaStream_t s) {

@@ -138,7 +138,7 @@ cudaError_t choose_clusters(int rows, int least, int most, int threads, size_t s
     if (e != cudaSuccess) return e;
     if (n < 1) continue;
     const double t = static_cast<double>((rows + n - 1) / n) / c;
-    if (!out->size || t < 0.98 * cost) {
+    if (!out->size || t < 0.95 * cost) {
       cost = t;
       *out = Clusters{c, n < rows ? n : rows};
     }

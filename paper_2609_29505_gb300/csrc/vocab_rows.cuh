@@ -16,11 +16,9 @@
 namespace sgd {
 namespace rows {
 
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
-constexpr int kUnroll = 4;                       // vectors a thread takes at a time
-constexpr int kPiece = kThreads * kUnroll;       // vectors of one bulk copy (16 KB), with a barrier of its own
-constexpr int kMaxPieces = 13;                   // of a slice: 208 KB
+constexpr int kUnroll = 4;      // vectors a thread takes at a time
+constexpr int kPiece = 1024;    // vectors of one bulk copy (16 KB), with a barrier of its own
+constexpr int kMaxPieces = 13;  // of a slice: 208 KB
 constexpr int kMaxCluster = 16;
 constexpr float kInf = __builtin_huge_valf(), kNan = __builtin_nanf("");
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -323,8 +321,12 @@ struct WarpTeam {
 struct Launch {
   int cluster;
   int slice_bytes;
+  int threads;
 };
 constexpr int kSlice = 64 * 1024;
+// Vectors of a slice that 64 threads take instead of 256: what a row costs beside its elements (barriers,
+// reductions) is then a quarter.
+constexpr int kShortSlice = 512;
 constexpr int kMaxDynamic = (227 - 16) * 1024;  // beside at most 16 KB of static shared memory
 
 inline Launch plan(int rows, int64_t vocab, int elem) {
@@ -333,7 +335,8 @@ inline Launch plan(int rows, int64_t vocab, int elem) {
   while (c < kMaxCluster && (bytes + c - 1) / c > kSlice) c *= 2;
   while (c < kMaxCluster && static_cast<int64_t>(rows) * c < num_sms() && bytes / c > 8192) c *= 2;
   const int64_t total = (bytes + 15) / 16 + 1;  // (one more vector where the row starts inside one)
-  return Launch{c, static_cast<int>((total + c - 1) / c) * 16};
+  const int vectors = static_cast<int>((total + c - 1) / c);
+  return Launch{c, vectors * 16, vectors <= kShortSlice ? 64 : 256};
 }
 
 template <auto kKernel, typename... Args>
@@ -352,7 +355,7 @@ cudaError_t launch(int rows, const Launch& l, size_t smem, cudaStream_t stream, 
   }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(rows) * l.cluster);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(l.threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
