@@ -60,7 +60,7 @@ EXPORTED = [
 ]
 EXEC_JAGGED_GRAPH, EXEC_EAGER, EXEC_PADDED_GRAPH = 0, 1, 2
 POLICY_STATIC, POLICY_DRIFT = 0, 1
-DTYPE_NAMES = {"torch.float16": 0, "torch.bfloat16": 1, "torch.float32": 2}  # sgd_dtype
+DTYPES = {"float16": 0, "bfloat16": 1, "float32": 2}  # sgd_dtype, by torch's names
 TAIL_RENORM, TAIL_BUCKET = 0, 1
 TAIL = {"renorm": TAIL_RENORM, "bucket": TAIL_BUCKET}
 
@@ -296,23 +296,23 @@ def sgd_sampler_update(z, eps, alpha, beta, stream=None):
 # sees only pointers: shapes, types and devices (TypeError / ValueError), before anything is launched.
 
 def _tensor(t, name, dtype, shape, device):
-    """`t` (or None): a dense tensor of this type, shape and device."""
+    """Address of `t` (or None): a dense tensor of this type, shape and device."""
     if t is None:
         return None
+    if t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous():
+        return t.data_ptr()
     if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
     if t.shape != shape:
         raise ValueError(f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, not on {device}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    return t.data_ptr()
+    raise ValueError(f"{name} must be contiguous")
 
 
 def _rows(t, name):
     """(type, row stride) of a [rows, vocab] tensor on a CUDA device with dense rows."""
-    kind = DTYPE_NAMES.get(str(t.dtype))
+    kind = _dtypes().get(t.dtype)
     if kind is None:
         raise TypeError(f"{name} must be float16, bfloat16 or float32, not {t.dtype}")
     if t.dim() != 2 or not t.is_cuda:
@@ -324,13 +324,31 @@ def _rows(t, name):
     return kind, ld if rows > 1 else max(ld, vocab)
 
 
-def _call_on(device, name, stream, *args):
-    """The library launches on the current device: that of the tensors, for the time of the call."""
+_dtype_codes = None
+
+
+def _dtypes():
+    global _dtype_codes
+    if _dtype_codes is None:
+        import torch
+        _dtype_codes = {getattr(torch, n): c for n, c in DTYPES.items()}
+    return _dtype_codes
+
+
+def _call_on(device, fn, name, stream, *args):
+    """The library launches on the current device: that of the tensors, for the time of the call.  The
+    current stream comes as its handle where torch has a call for that: making the stream's object takes
+    longer than launching a small kernel."""
     import torch
+    if stream is None:
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        stream = torch.cuda.current_stream(device) if raw is None else raw(device.index)
     if torch.cuda.current_device() == device.index:
-        return check(getattr(lib(), name)(*args, _stream(stream)), name)
-    with torch.cuda.device(device):
-        return check(getattr(lib(), name)(*args, _stream(stream)), name)
+        rc = fn(*args, _stream(stream))
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, _stream(stream))
+    return rc if rc == SGD_OK else check(rc, name)
 
 
 def sgd_kernel_logprobs(logits, tokens=None, token_logprobs=None, entropy=None, top_ids=None, top_logprobs=None,
@@ -345,18 +363,18 @@ def sgd_kernel_logprobs(logits, tokens=None, token_logprobs=None, entropy=None, 
     device, i32, f32 = logits.device, torch.int32, torch.float32
     if (tokens is None) != (token_logprobs is None):
         raise ValueError("tokens and token_logprobs go together")
-    n = 0
+    n = k = 0
     if tokens is not None:
         if tokens.dim() != 2:
             raise ValueError("tokens must have the shape [rows, n]")
         n = tokens.shape[1]
     top = top_ids if top_ids is not None else top_logprobs
-    k = 0
     if top is not None:
         if top.dim() != 2:
             raise ValueError("top_ids and top_logprobs must have the shape [rows, k]")
         k = top.shape[1]
-    return _call_on(device, "sgd_kernel_logprobs", stream, logits.data_ptr(), kind, ld, rows, vocab, scale,
+    return _call_on(device, lib().sgd_kernel_logprobs, "sgd_kernel_logprobs", stream,
+                    logits.data_ptr(), kind, ld, rows, vocab, scale,
                     _tensor(row_ids, "row_ids", i32, (rows,), device), row_id,
                     _tensor(tokens, "tokens", i32, (rows, n), device), n,
                     _tensor(token_logprobs, "token_logprobs", f32, (rows, n), device),
@@ -373,7 +391,7 @@ def sgd_kernel_distill(logits, teacher_ids, teacher_logprobs, loss, grad=None, r
     import torch
     kind, ld = _rows(logits, "logits")
     rows, vocab = logits.shape
-    device = logits.device
+    device, f32 = logits.device, torch.float32
     if teacher_ids.dim() != 2:
         raise ValueError("teacher_ids must have the shape [rows, k]")
     k = teacher_ids.shape[1]
@@ -382,16 +400,17 @@ def sgd_kernel_distill(logits, teacher_ids, teacher_logprobs, loss, grad=None, r
         gkind, ldg = _rows(grad, "grad")
         if grad.shape != logits.shape or grad.device != device:
             raise ValueError("grad must have the shape and the device of logits")
-    return _call_on(device, "sgd_kernel_distill", stream, logits.data_ptr(), kind, ld, rows, vocab, scale,
+    return _call_on(device, lib().sgd_kernel_distill, "sgd_kernel_distill", stream,
+                    logits.data_ptr(), kind, ld, rows, vocab, scale,
                     _tensor(teacher_ids, "teacher_ids", torch.int32, (rows, k), device),
-                    _tensor(teacher_logprobs, "teacher_logprobs", torch.float32, (rows, k), device), k,
-                    _tensor(row_weight, "row_weight", torch.float32, (rows,), device), tail,
-                    _tensor(loss, "loss", torch.float32, (rows,), device),
+                    _tensor(teacher_logprobs, "teacher_logprobs", f32, (rows, k), device), k,
+                    _tensor(row_weight, "row_weight", f32, (rows,), device), tail,
+                    _tensor(loss, "loss", f32, (rows,), device),
                     None if grad is None else grad.data_ptr(), gkind, ldg)
 
 
 def _column(t, name, dtype, shape, device):
-    """(pointer, stride) of a [batch, n_tokens] tensor whose positions are evenly spaced (a column of a
+    """(address, stride) of a [batch, n_tokens] tensor whose positions are evenly spaced (a column of a
     [batch, n_tokens, k] one, say)."""
     if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
@@ -417,8 +436,9 @@ def sgd_sampler_reveal(ids, cand, score, n_reveal, ids_out, mask_id, lowest=Fals
     batch, n = shape
     pc, sc = _column(cand, "cand", i32, shape, device)
     ps, ss = _column(score, "score", torch.float32, shape, device)
-    return _call_on(device, "sgd_sampler_reveal", stream, _tensor(ids, "ids", i32, shape, device), pc, sc, ps, ss,
-                    int(lowest), _tensor(n_reveal, "n_reveal", i32, (batch,), device),
+    return _call_on(device, lib().sgd_sampler_reveal, "sgd_sampler_reveal", stream,
+                    _tensor(ids, "ids", i32, shape, device), pc, sc, ps, ss, int(lowest),
+                    _tensor(n_reveal, "n_reveal", i32, (batch,), device),
                     _tensor(window, "window", i32, (batch, 2), device),
                     _tensor(ids_out, "ids_out", i32, shape, device),
                     _tensor(n_left, "n_left", i32, (batch,), device), batch, n, mask_id)

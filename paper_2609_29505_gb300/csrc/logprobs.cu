@@ -29,6 +29,8 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) logprobs_kernel(cons
   __shared__ float4 slot[kMaxCluster];
   __shared__ float result[2];
   __shared__ int best;
+  __shared__ int n_reaching;
+  __shared__ uint16_t reaching[TOP == kTopMany ? kThreads : 1];
   __shared__ __align__(16) unsigned char top_raw[TOP == kTopMany ? sizeof(TopShared) : 16];
   const Team<kThreads, 0> team{static_cast<int>(threadIdx.x)};
   const int rank = cluster_rank(), n_ctas = cluster_ctas();
@@ -43,11 +45,12 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) logprobs_kernel(cons
     fence_proxy_async_smem();
     abort_flag = 0;
     best = 0x7FFFFFFF;
+    n_reaching = 0;
     start_copies(sl, buf, bars);
   }
   fill_ends(sl, buf);
   Given<T> given;
-  if (rank == 0) given.fetch(p, row, r, threadIdx.x);
+  if (rank == 0) given.fetch_token(p, r, threadIdx.x);
   __syncthreads();
   cluster_arrive();
 
@@ -66,6 +69,8 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) logprobs_kernel(cons
     const float before = st.m;
     if (stat_add<T, kUnroll, ENT>(st, v, c) > before) at = i;
   }
+
+  if (rank == 0) given.fetch_logit(p, row);
 
   // the CTA's statistics
   float m = key_value(__reduce_max_sync(0xffffffffu, order_key(st.m)));
@@ -105,13 +110,19 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) logprobs_kernel(cons
     const uint32_t keys[1] = {order_key(st.m)};
     uint32_t above;
     const uint32_t lo = threshold(team, keys, p.top_k, top, above);
+    // what the threads hold whose maximum reaches the threshold, looked at by all threads
+    if (keys[0] >= lo) reaching[atomicAdd(&n_reaching, 1)] = static_cast<uint16_t>(threadIdx.x);
+    __syncthreads();
     const float bar = key_value(lo);
-    if (keys[0] >= lo) {  // the threads alone that hold one
-      for (int i = threadIdx.x; i < sl.nv; i += kThreads) {
-        const uint4 v = buf[i];
-        if (lo > kKeyNegInf && !(vec_max<1>(&v, static_cast<const T*>(nullptr)) >= bar)) continue;
-        append<T>(v, sl.first_element(i), sl.vocab, lo, &top);
-      }
+    const int steps = (sl.nv + kThreads - 1) / kThreads, all = n_reaching * steps;
+    const float steps_inv = 1.f / steps;
+    for (int j = threadIdx.x; j < all; j += kThreads) {
+      const int q = static_cast<int>((j + 0.5f) * steps_inv);  // j / steps: exact, j is far below 2^22
+      const int i = (j - q * steps) * kThreads + reaching[q];
+      if (i >= sl.nv) continue;
+      const uint4 v = buf[i];
+      if (lo > kKeyNegInf && !(vec_max<1>(&v, static_cast<const T*>(nullptr)) >= bar)) continue;
+      append<T>(v, sl.first_element(i), sl.vocab, lo, &top);
     }
     __syncthreads();
     if (top.n > kCap) candidates_of_many(team, sl, InShared{buf}, lo, above, p.top_k, top);

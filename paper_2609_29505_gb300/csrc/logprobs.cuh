@@ -25,15 +25,17 @@ struct ScoreArgs {
 
 enum { kTopNone = 0, kTopOne = 1, kTopMany = 2 };
 
-// A row's given tokens, one per thread of the team (more in finish()): fetched ahead of the statistics.
+// A row's given tokens, one per thread of the team (more in finish()): the token is fetched ahead of the row, its
+// logit while the row's statistics are reduced (a thread waits at the first use of what it loads).
 template <typename T>
 struct Given {
   int token = -1;
   float z = 0.f;
-  __device__ __forceinline__ void fetch(const ScoreArgs& p, const T* row, int64_t r, int tid) {
-    if (tid >= p.n_tokens) return;
-    token = p.tokens[r * p.n_tokens + tid];
-    z = token >= 0 && token < p.vocab ? to_f(row[token]) : kNan;
+  __device__ __forceinline__ void fetch_token(const ScoreArgs& p, int64_t r, int tid) {
+    if (tid < p.n_tokens) token = p.tokens[r * p.n_tokens + tid];
+  }
+  __device__ __forceinline__ void fetch_logit(const ScoreArgs& p, const T* row) {
+    if (token >= 0) z = token < p.vocab ? to_f(row[token]) : kNan;
   }
 };
 

@@ -186,7 +186,7 @@ __device__ __forceinline__ void finish_rows(const ScoreArgs& p, Row& x, Many& ma
     const T* row = logits + r * p.ld;
     const Slice<T> sl(row, p.vocab, rank, n_ctas);
     Given<T> given;
-    if (rank == 0) given.fetch(p, row, r, lane);
+    if (rank == 0) given.fetch_token(p, r, lane);
     float4 v = make_float4(-kInf, 0.f, 0.f, 0.f);
     if (lane < kStreamWarps) v = x.part[lane];
     const float m = key_value(__reduce_max_sync(0xffffffffu, order_key(v.x)));
@@ -220,6 +220,7 @@ __device__ __forceinline__ void finish_rows(const ScoreArgs& p, Row& x, Many& ma
         best = __reduce_min_sync(0xffffffffu, best);
       }
     }
+    if (rank == 0) given.fetch_logit(p, row);
     if (TOP == kTopMany) candidates(team, sl, x, p.top_k, many);
     // to the first CTA, once it is done with this warp's row before
     if (n_ctas > 1 && !wait_cluster(&x.row_free, phase ^ 1u, abort_flag, p.status, 67)) break;

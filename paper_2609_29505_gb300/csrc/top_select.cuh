@@ -202,6 +202,17 @@ __device__ __forceinline__ void rank_candidates(const Tm& team, const TopShared&
 // The k largest of n_lists sorted lists of k (0: no entry).
 template <typename Tm, typename P>
 __device__ __forceinline__ void merge_lists(const Tm& team, const uint64_t* lists, int n_lists, int k, const P& put) {
+  const int all = n_lists * k;
+  if (all <= 256) {  // counted: loads that do not wait for one another
+    for (int i = team.tid; i < all; i += Tm::kSize) {
+      const uint64_t x = lists[i];
+      int place = 0;
+#pragma unroll 8
+      for (int j = 0; j < all; ++j) place += lists[j] > x;
+      if (x != 0 && place < k) put(place, x);
+    }
+    return;
+  }
   for (int i = team.tid; i < n_lists * k; i += Tm::kSize) {
     const uint64_t x = lists[i];
     if (x == 0) continue;

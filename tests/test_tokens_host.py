@@ -163,6 +163,6 @@ def test_type_codes_follow_the_header():
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     src = open(os.path.join(root, "include", "sgd_kernels.h")).read()
     want = {n: int(v) for n, v in re.findall(r"\b(SGD_(?:F16|BF16|F32|TAIL_RENORM|TAIL_BUCKET)) = (\d)", src)}
-    assert want == {"SGD_F16": binding.DTYPE_NAMES["torch.float16"], "SGD_BF16": binding.DTYPE_NAMES["torch.bfloat16"],
-                    "SGD_F32": binding.DTYPE_NAMES["torch.float32"], "SGD_TAIL_RENORM": binding.TAIL_RENORM,
+    assert want == {"SGD_F16": binding.DTYPES["float16"], "SGD_BF16": binding.DTYPES["bfloat16"],
+                    "SGD_F32": binding.DTYPES["float32"], "SGD_TAIL_RENORM": binding.TAIL_RENORM,
                     "SGD_TAIL_BUCKET": binding.TAIL_BUCKET}
