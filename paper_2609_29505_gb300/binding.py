@@ -507,6 +507,23 @@ class Denoiser:
         return check(lib().sgd_step(self.handle, _ptr(state), _ptr(out), float(t),
                                     C.byref(cond), step, _stream(stream)), "sgd_step")
 
+    def step_tokens(self, ids, ids_out, logits, t: float, step: int, cand, score, n_reveal, mask_id: int,
+                    by: str = "confidence", scale: float = 1.0, window=None, n_left=None, stream=None):
+        """One step of a masked-token trajectory (argmax remasking), queued on one stream: the denoiser on ids
+        int32 [B, N] into logits fp16 [B, N, V], the best token of every masked position into cand int32 [B, N]
+        with its log-probability (by "confidence") or its row's entropy (by "entropy") in score float32
+        [B, N], and the n_reveal best of them revealed in ids_out (which may be ids).  What cand and
+        score hold at other positions stays."""
+        if by not in ("confidence", "entropy"):
+            raise ValueError("by must be confidence or entropy")
+        self.step(ids, logits, t, step, stream=stream)
+        rows = logits.view(-1, logits.shape[-1])
+        out = dict(top_logprobs=score.view(-1, 1)) if by == "confidence" else dict(entropy=score.view(-1))
+        sgd_kernel_logprobs(rows, top_ids=cand.view(-1, 1), scale=scale, row_ids=ids.view(-1), row_id=mask_id,
+                            stream=stream, **out)
+        return sgd_sampler_reveal(ids, cand, score, n_reveal, ids_out, mask_id, lowest=by == "entropy", window=window,
+                                  n_left=n_left, stream=stream)
+
     def step_host(self, state_host, out_host, t: float, step: int, class_ids_host=None,
                   ctx_host=None, stream=None):
         """Host (preferably pinned) torch tensors in and out; synchronous."""

@@ -11,6 +11,10 @@ command that the committed ncu summaries under profiles/ were captured from.
     python -m paper_2609_29505_gb300.kernel_bench frozen --rows 4096 --d 4096 --caches 8
     python -m paper_2609_29505_gb300.kernel_bench norm --rows 4096 --d 4096
     python -m paper_2609_29505_gb300.kernel_bench trajectory --config dit --budget 0.5 --reps 2
+    python -m paper_2609_29505_gb300.kernel_bench trajectory --config llada --T 16 --remask entropy
+    python -m paper_2609_29505_gb300.kernel_bench logprobs --rows 4096 --vocab 126464 --top 32
+    python -m paper_2609_29505_gb300.kernel_bench distill --rows 4096 --vocab 126464 --top 32 --grad bf16
+    python -m paper_2609_29505_gb300.kernel_bench reveal --batch 16 --tokens 4096
 """
 from __future__ import annotations
 
@@ -149,6 +153,70 @@ def case_norm(a):
     return dict(case="norm", rows=a.rows, d=a.d, ms=ms, gbs=6.0 * a.rows * a.d / ms / 1e6)
 
 
+DTYPES = {"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def _logits(a):
+    g = torch.Generator(device="cuda").manual_seed(0)
+    z = torch.empty(a.rows, a.vocab, device="cuda", dtype=DTYPES[a.dtype])
+    for r in range(0, a.rows, 256):
+        z[r:r + 256] = 2.0 * torch.randn(min(256, a.rows - r), a.vocab, device="cuda", generator=g)
+    return z
+
+
+def case_logprobs(a):
+    z = _logits(a)
+    out = {}
+    if a.top:
+        out = dict(top_ids=torch.empty(a.rows, a.top, device="cuda", dtype=torch.int32),
+                   top_logprobs=torch.empty(a.rows, a.top, device="cuda"))
+    if a.entropy or not a.top:
+        out["entropy"] = torch.empty(a.rows, device="cuda")
+    ms = _time(lambda: binding.sgd_kernel_logprobs(z, **out), a.iters, a.warmup)
+    return dict(case="logprobs", rows=a.rows, vocab=a.vocab, dtype=a.dtype, top=a.top, entropy="entropy" in out, ms=ms,
+                gbs=z.numel() * z.element_size() / ms / 1e6)
+
+
+def case_distill(a):
+    z = _logits(a)
+    k = a.top or 1
+    ids = torch.empty(a.rows, k, device="cuda", dtype=torch.int32)
+    lq = torch.empty(a.rows, k, device="cuda")
+    binding.sgd_kernel_logprobs(z, top_ids=ids, top_logprobs=lq)  # the model's own lists
+    loss = torch.empty(a.rows, device="cuda")
+    grad = torch.empty(a.rows, a.vocab, device="cuda", dtype=DTYPES[a.grad]) if a.grad else None
+    ms = _time(lambda: binding.sgd_kernel_distill(z, ids, lq, loss, grad=grad), a.iters, a.warmup)
+    bytes_ = z.numel() * z.element_size() + (grad.numel() * grad.element_size() if a.grad else 0)
+    return dict(case="distill", rows=a.rows, vocab=a.vocab, dtype=a.dtype, top=k, grad=a.grad, ms=ms, gbs=bytes_ / ms / 1e6)
+
+
+def case_reveal(a):
+    ids = torch.zeros(a.batch, a.tokens, device="cuda", dtype=torch.int32)
+    out, score = torch.empty_like(ids), torch.rand(a.batch, a.tokens, device="cuda")
+    n = torch.full((a.batch,), max(1, a.tokens // 16), device="cuda", dtype=torch.int32)
+    ms = _time(lambda: binding.sgd_sampler_reveal(ids, ids, score, n, out, 0), a.iters, a.warmup)
+    return dict(case="reveal", batch=a.batch, tokens=a.tokens, ms=ms)
+
+
+def _remask(a, cfg, model, logits):
+    """A trajectory whose ids follow the model's own logits: each step reveals an even share of what is masked."""
+    from . import synth
+    T, mask = a.T or cfg.T, synth.mask_id(cfg)
+    shape = (cfg.batch, cfg.n_tokens)
+    ids = torch.full(shape, mask, device="cuda", dtype=torch.int32)
+    cand, score = torch.empty_like(ids), torch.empty(shape, device="cuda")
+    left = torch.empty(cfg.batch, device="cuda", dtype=torch.int32)
+    n = [torch.full((cfg.batch,), (s * cfg.n_tokens) // T - ((s - 1) * cfg.n_tokens) // T, device="cuda", dtype=torch.int32)
+         for s in range(1, T + 1)]
+
+    def run():
+        ids.fill_(mask)
+        for s in range(1, T + 1):
+            model.step_tokens(ids, ids, logits, synth.timestep(cfg, s, T), s, cand, score, n[s - 1], mask, by=a.remask,
+                              n_left=left)
+    return run, left
+
+
 def case_trajectory(a):
     """Whole trajectories of a synthetic model through sgd_step (its CUDA graphs), timed with
     CUDA events: the launch sequence the step programs run, for launch lists and captures of
@@ -173,13 +241,20 @@ def case_trajectory(a):
         out = torch.empty(cfg.batch, cfg.n_out_tokens, cfg.out_channels, device="cuda")
     cls = None if inp.class_ids is None else inp.class_ids.cuda()
     ctx = None if inp.ctx is None else inp.ctx.cuda()
+    run, left = None, None
+    if a.remask:
+        if cfg.head != "logits":
+            raise SystemExit("--remask needs a token model")
+        run, left = _remask(a, cfg, model, out)
     times = []
     for _ in range(a.reps):
         model.reset()
         torch.cuda.synchronize()
         e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
         e0.record()
-        for s in range(1, T + 1):
+        if run:
+            run()
+        for s in range(1, 0 if run else T + 1):
             model.step(xs[s - 1], out, synth.timestep(cfg, s, T), s, class_ids=cls, ctx=ctx)
         e1.record()
         torch.cuda.synchronize()
@@ -187,13 +262,17 @@ def case_trajectory(a):
     model.check_device()
     model.close()
     ms = min(times) / T
-    return dict(case="trajectory", config=a.config, T=T, budget=a.budget, reps=a.reps, ms=ms,
-                steps_per_s=1e3 / ms)
+    res = dict(case="trajectory", config=a.config, T=T, budget=a.budget, reps=a.reps, ms=ms,
+               steps_per_s=1e3 / ms)
+    if run:
+        res.update(remask=a.remask, still_masked=int(left.sum()))
+    return res
 
 
 def main():
     ap = argparse.ArgumentParser()
-    ap.add_argument("case", choices=["gemm", "attention", "frozen", "norm", "trajectory"])
+    ap.add_argument("case", choices=["gemm", "attention", "frozen", "norm", "trajectory", "logprobs", "distill",
+                                     "reveal"])
     ap.add_argument("--config", default="dit", help="trajectory: synthetic model config")
     ap.add_argument("--T", type=int, default=0, help="trajectory: horizon (0: the config's)")
     ap.add_argument("--budget", type=float, default=0.5, help="trajectory: layer-step budget")
@@ -225,6 +304,13 @@ def main():
     ap.add_argument("--rows", type=int, default=4096)
     ap.add_argument("--d", type=int, default=4096)
     ap.add_argument("--caches", type=int, default=8)
+    ap.add_argument("--vocab", type=int, default=126464)
+    ap.add_argument("--dtype", default="f16", choices=list(DTYPES), help="logprobs, distill: type of the logits")
+    ap.add_argument("--top", type=int, default=1, help="logprobs: likeliest tokens; distill: length of the lists")
+    ap.add_argument("--entropy", action="store_true", help="logprobs: the entropy too")
+    ap.add_argument("--grad", default="", choices=["", *DTYPES], help="distill: type of the gradient (none: the loss alone)")
+    ap.add_argument("--remask", default="", choices=["", "confidence", "entropy"],
+                    help="trajectory of a token model: positions revealed by the model's own logits")
     ap.add_argument("--iters", type=int, default=20)
     ap.add_argument("--warmup", type=int, default=3)
     ap.add_argument("--graph", action="store_true",
@@ -235,7 +321,8 @@ def main():
     build.build()
     binding.lib()
     res = {"gemm": case_gemm, "attention": case_attention, "frozen": case_frozen,
-           "norm": case_norm, "trajectory": case_trajectory}[a.case](a)
+           "norm": case_norm, "trajectory": case_trajectory, "logprobs": case_logprobs, "distill": case_distill,
+           "reveal": case_reveal}[a.case](a)
     res["graph"] = a.graph
     res["status"] = binding.sgd_kernel_status()
     print(json.dumps(res))

@@ -250,15 +250,14 @@ def test_offsets_past_32_bits(B):
     _check_distill(loss, z, z0, ids, logq, 1.0, True, None)
 
 
-# many long rows (32 MiB and more of them): they stream, and the CTAs of a cluster share a row where that
-# fills the SMs better (152: one each; 153, 301: one round more)
+# many long rows: they stream, and the CTAs of a cluster share a row where that fills the SMs better (152: one
+# each; 153, 301: one round more); the last two are too short for that
 @pytest.mark.parametrize("rows,vocab,dtype,pad,offset", [
-    (152, 126464, "f16", 0, 0), (153, 126464, "f16", 0, 0), (301, 126464, "f16", 0, 0), (700, 32003, "bf16", 0, 1),
-    (541, 32003, "f16", 13, 0), (211, 50021, "f32", 0, 3), (1100, 16387, "f16", 5, 2), (70, 300007, "bf16", 1, 0),
-    (12, 3 << 19, "f16", 0, 0), (14, 700001, "f32", 2, 1)])
+    (152, 126464, "f16", 0, 0), (153, 126464, "f16", 0, 0), (301, 126464, "f16", 0, 0), (1100, 60001, "bf16", 0, 1),
+    (400, 100003, "f16", 13, 0), (230, 50021, "f32", 0, 3), (300, 126461, "f16", 5, 2), (70, 300007, "bf16", 1, 0),
+    (12, 3 << 19, "f16", 0, 0), (14, 700001, "f32", 2, 1), (1100, 16387, "f16", 5, 2), (700, 32003, "bf16", 0, 1)])
 @pytest.mark.parametrize("k", [0, 1, 9, 64])
 def test_logprobs_of_many_rows(B, rows, vocab, dtype, pad, offset, k):
-    assert rows * vocab * torch.finfo(DT[dtype]).bits // 8 >= 32 << 20
     z = torch.empty(rows, vocab + pad, dtype=DT[dtype], device="cuda").normal_(0, 2, generator=torch.Generator("cuda").manual_seed(rows))
     buf = torch.full((offset + rows * (vocab + pad),), 3e4, dtype=DT[dtype], device="cuda")
     v = buf[offset:].view(rows, vocab + pad)
@@ -295,7 +294,7 @@ def test_hard_rows_among_many(B, k, dtype):
 @pytest.mark.parametrize("share", [0.0, 0.004, 0.5, 1.0])
 @pytest.mark.parametrize("k", [1, 6])
 def test_rows_that_are_not_asked_for_stay_among_many(B, k, share):
-    rows, vocab = 2500, 20001
+    rows, vocab = 900, 70001
     g = torch.Generator("cuda").manual_seed(4)
     z = torch.empty(rows, vocab, dtype=torch.float16, device="cuda").normal_(0, 2, generator=g)
     on = torch.rand(rows, device="cuda", generator=g) < share
@@ -534,15 +533,15 @@ def _check_rows(loss, grad, z, ids, logq, bucket, w):
     assert (err <= tol + half * (g.abs() + tol) + least).all(), (err / (tol + half * (g.abs() + tol) + least)).max()
 
 
-# many long rows: they stream through clusters of 1 to 8 CTAs
+# many long rows (48 MiB and more of them): they stream through clusters of 1 to 8 CTAs
 @pytest.mark.parametrize("rows,vocab,dtype,grad,pad,offset", [
-    (152, 126464, "f16", "bf16", 0, 0), (301, 126464, "f16", "f16", 0, 0), (140, 126464, "f16", "", 0, 0),
-    (700, 32003, "bf16", "bf16", 0, 1), (541, 32003, "f16", "f32", 13, 0), (211, 50021, "f32", "f32", 0, 3),
-    (1100, 16387, "f16", "f16", 5, 2), (1100, 16387, "bf16", "", 1, 0), (70, 266176, "f16", "bf16", 0, 0),
-    (66, 133081, "f32", "bf16", 2, 1), (90, 126464, "f32", "f32", 0, 0)])
+    (200, 126464, "f16", "bf16", 0, 0), (301, 126464, "f16", "f16", 0, 0), (210, 126464, "f16", "", 0, 0),
+    (800, 32003, "bf16", "bf16", 0, 1), (801, 32003, "f16", "f32", 13, 0), (260, 50021, "f32", "f32", 0, 3),
+    (1600, 16387, "f16", "f16", 5, 2), (1600, 16387, "bf16", "", 1, 0), (100, 266176, "f16", "bf16", 0, 0),
+    (98, 133081, "f32", "bf16", 2, 1), (102, 126464, "f32", "f32", 0, 0), (5000, 8209, "f16", "bf16", 0, 0)])
 @pytest.mark.parametrize("bucket,k", [(True, 32), (False, 64), (True, 1)])
 def test_distill_of_many_rows(B, rows, vocab, dtype, grad, pad, offset, bucket, k):
-    assert rows * vocab * torch.finfo(DT[dtype]).bits // 8 >= 32 << 20
+    assert rows * vocab * torch.finfo(DT[dtype]).bits // 8 >= 48 << 20
     g = torch.Generator("cuda").manual_seed(rows)
     buf = torch.full((offset + rows * (vocab + pad),), 3e4, dtype=DT[dtype], device="cuda")
     z = buf[offset:].view(rows, vocab + pad)[:, :vocab]
@@ -571,7 +570,7 @@ def test_distill_of_many_rows(B, rows, vocab, dtype, grad, pad, offset, bucket, 
 
 @pytest.mark.parametrize("weights", ["none", "zero", "one left", "none given"])
 def test_weights_of_many_rows(B, weights):
-    rows, vocab = 1200, 20000
+    rows, vocab = 1400, 20000
     z = torch.empty(rows, vocab, dtype=torch.float16, device="cuda").normal_(0, 2, generator=torch.Generator("cuda").manual_seed(1))
     ids, logq = torch.randint(0, vocab, (rows, 3), dtype=torch.int32).cuda(), torch.full((rows, 3), -1.2).cuda()
     w = None if weights == "none given" else torch.zeros(rows, device="cuda") if weights != "none" else torch.ones(rows, device="cuda")
