@@ -13,9 +13,8 @@
 // that p_T is a sum of its own: 1 - sum_S p would leave nothing of a small tail.  In the gradient's
 // pass -inf gives S the gradient 0, and its k entries are written after it.
 //
-// The loss is a difference of larger terms where the two models agree: ln q - ln p is taken in two parts, the
-// terms are summed in fp64, 1 - Q is taken of the fp64 sum of the rounded q_i (their rounding then
-// cancels to first order), and ln p_T is ln(1 - P) by log1p.
+// 1 - Q is taken of the fp64 sum of the rounded q_i (their rounding then cancels from the loss to first
+// order); what else is done for a loss that is a difference of larger terms stands at row_loss().
 //
 // The kernel here is for few or short rows: a cluster takes one row, a slice per CTA, and leaves;
 // many long rows stream through distill_stream.cu.
@@ -40,7 +39,6 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) distill_kernel(const
   __shared__ float4 warp_stat[kWarps];
   __shared__ float4 slot[kMaxCluster];
   __shared__ float list_z[kMaxList];  // leader: the list's logits
-  __shared__ double loss_sum[2];
   const int rank = cluster_rank();
   const uint32_t n_ctas = cluster_ctas();
   const int64_t r = blockIdx.x / n_ctas;
@@ -178,12 +176,19 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) distill_kernel(const
   }
   if (rank != 0) return;
 
+  __shared__ float list_q[kMaxList], list_lq[kMaxList];
   if (threadIdx.x < kMaxList) {
-    const double term = warp_sum(static_cast<double>(loss_term(o, sums, q, lq, list_z[threadIdx.x], p.scale, c)));
-    if (lane == 0) loss_sum[warp] = term;
+    list_q[threadIdx.x] = q;
+    list_lq[threadIdx.x] = lq;
+    if (id < 0) list_z[threadIdx.x] = -kInf;  // no entry
   }
   __syncthreads();
-  if (threadIdx.x == 0) p.loss[r] = row_loss(o, sums, loss_sum[0] + loss_sum[1], ls, w, p.bucket);
+  if (warp == 0) {
+    const float qs[2] = {list_q[lane], list_q[lane + 32]}, lqs[2] = {list_lq[lane], list_lq[lane + 32]};
+    const float zs[2] = {list_z[lane], list_z[lane + 32]};
+    const float loss = row_loss(o, sums, ls, w, p.bucket, p.scale, c, qs, lqs, zs);
+    if (lane == 0) p.loss[r] = loss;
+  }
 }
 
 template <typename T, int kThreads>

@@ -143,12 +143,18 @@ __device__ __forceinline__ Float2 two_prod(float a, float b) {  // a b exactly
   const float p = __fmul_rn(a, b);
   return Float2{p, fmaf(a, b, -p)};
 }
-// ln x of a normal x > 0: logf of the significand, whose rounding is that of a number below 0.7, and the
-// exponent times ln 2 in two parts (the first one short: e times it is exact).
+// ln(j / 16), j = 8 .. 16, in two parts.
+__device__ const float kLnHigh[9] = {-0.693147182f, -0.575364172f, -0.470003635f, -0.374693453f, -0.287682086f,
+                                     -0.207639366f, -0.133531392f, -0.0645385236f, 0.f};
+__device__ const float kLnLow[9] = {1.90465421e-09f, 2.75550871e-08f, 5.44550272e-09f,  3.87050969e-09f, 1.37775436e-08f,
+                                    1.61007641e-09f, -1.00388664e-09f, 2.41723086e-09f, 0.f};
+// ln x of a normal x > 0, to some 4e-9: the exponent times ln 2 in two parts (the first one short: e times it is
+// exact), the logarithm of the nearest j / 16 to the significand, and log1pf of what is left (at most 1 / 16).
 __device__ __forceinline__ Float2 ln2parts(float x) {
   int e = 0;
-  const float f = frexpf(x, &e), n = static_cast<float>(e);
-  return Float2{n * 0.693145751953125f, n * 1.42860677e-6f} + Float2{logf(f), 0.f};
+  const float f = 16.f * frexpf(x, &e), j = rintf(f), n = static_cast<float>(e);
+  const int i = min(max(static_cast<int>(j) - 8, 0), 8);  // (x may be no number)
+  return Float2{n * 0.693145751953125f, n * 1.42860677e-6f} + Float2{kLnHigh[i], kLnLow[i]} + Float2{log1pf((f - j) / j), 0.f};
 }
 
 // What a row's list adds up to: Q in two parts, and q_T.
@@ -191,18 +197,46 @@ __device__ __forceinline__ RowScale row_scale(const RowSums& r, const ListSums& 
   return o;
 }
 
-// One entry's term of the loss, q (ln q - ln p), and the loss from their sum.  Where the two models agree these are
-// differences of larger numbers: ln q - ln p is taken in two parts, and the terms are added up in fp64.
-__device__ __forceinline__ float loss_term(const RowScale& o, const RowSums& r, float q, float lq, float z, float scale, float c) {
-  if (q == 0.f) return 0.f;
-  if (o.empty || z == -kInf) return q * kInf;
+// The loss (a whole warp; every lane gets it), from entries lane, lane + 32, ... of the list.  Where the two
+// models agree it is a difference of terms some ten to a thousand times its size, so that these are kept apart:
+//   - the list's sum is taken anew, with expf of exponents that are not rounded, and added up in fp64 (an error of
+//     1e-7 in it moved losses by 2e-6; one of the tail's sum cancels);
+//   - ln q - ln p is a sum of pairs of floats, and the terms are added up in fp64;
+//   - ln q_T - ln p_T is ln(1 + (in - Q s) / tail).
+template <int N>
+__device__ __forceinline__ float row_loss(const RowScale& o, const RowSums& r, const ListSums& l, float w, bool bucket, float scale,
+                                          float c, const float (&q)[N], const float (&lq)[N], const float (&z)[N]) {
+  // in units of e^(scale m), m the row's maximum: the sums hold 2^delta of it, delta = c m - R
   const float delta = r.all == -kInf ? 0.f : fmaf(r.all, c, -o.R);
-  const Float2 ln_s = ln2parts(o.s) + Float2{-delta * kLn2, 0.f};
-  const Float2 d = two_sum(z, -r.all), x = two_prod(d.hi, scale);
-  const Float2 diff = Float2{lq, 0.f} + -Float2{x.hi, fmaf(d.lo, scale, x.lo)} + ln_s;
-  return q * (diff.hi + diff.lo);
-}
-__device__ __forceinline__ float row_loss(const RowScale& o, const RowSums& r, double terms, const ListSums& l, float w, bool bucket) {
+  Float2 x[N];  // scale (z - m)
+  double sum = 0.0;
+#pragma unroll
+  for (int h = 0; h < N; ++h) {
+    const Float2 d = two_sum(z[h], -r.all), p = two_prod(d.hi, scale);
+    x[h] = Float2{p.hi, fmaf(d.lo, scale, p.lo)};
+    if (q[h] == 0.f || z[h] == -kInf) continue;  // no entry, or no weight (left to `in`), or no probability
+    const float e = expf(x[h].hi);
+    sum += static_cast<double>(fmaf(e, x[h].lo, e));
+  }
+  sum = warp_sum(sum);
+  // what has no weight in the list belongs to its sum too; then the sum is taken as it is
+  bool all_weighted = true;
+#pragma unroll
+  for (int h = 0; h < N; ++h) all_weighted &= !(q[h] == 0.f && z[h] > -kInf);
+  const float tail = r.tail * ex2_approx(-delta);
+  const float in0 = r.in * ex2_approx(-delta);
+  const bool anew = __all_sync(0xffffffffu, all_weighted) && r.all > -kInf;
+  const float in = anew ? static_cast<float>(sum) : in0, in_lo = anew ? static_cast<float>(sum - in) : 0.f;
+  const Float2 s = Float2{tail, 0.f} + Float2{in, in_lo};
+  const Float2 ln_s = ln2parts(s.hi) + Float2{s.lo / s.hi, 0.f};
+  double terms = 0.0;
+#pragma unroll
+  for (int h = 0; h < N; ++h) {
+    if (q[h] == 0.f) continue;  // (a NaN is no 0)
+    const Float2 diff = Float2{lq[h], 0.f} + -x[h] + ln_s;
+    terms += o.empty || z[h] == -kInf ? q[h] * kInf : q[h] * (diff.hi + diff.lo);
+  }
+  terms = warp_sum(terms);
   const float hi = static_cast<float>(terms);
   if (!isfinite(hi)) return w * hi;
   if (!bucket) {  // terms / Q - ln Q
@@ -210,14 +244,13 @@ __device__ __forceinline__ float row_loss(const RowScale& o, const RowSums& r, d
     const Float2 L = Float2{q1, rest / l.Q} + -ln2parts(l.Q) + Float2{-l.Q_lo / l.Q, 0.f};
     return w * (L.hi + L.lo);
   }
-  float tail = 0.f;
+  float of_tail = 0.f;
   if (o.has_tail && l.q_tail > 0.f) {
-    const float P = r.in / o.s;
-    const float ln_pt = P < 0.5f ? log1pf(-P) : logf(r.tail / o.s);
-    const float ln_qt = l.Q < 0.5f ? log1pf(-l.Q) : logf(l.q_tail);
-    tail = l.q_tail * (ln_qt - ln_pt);
+    const Float2 qs = two_prod(l.Q, s.hi);
+    const float off = (((in - qs.hi) - qs.lo) + in_lo - l.Q_lo * s.hi - l.Q * s.lo) / tail;
+    of_tail = l.q_tail * (off > -0.5f ? log1pf(off) : logf(l.q_tail) - logf(tail / s.hi));
   }
-  return w * static_cast<float>(terms + tail);
+  return w * static_cast<float>(terms + of_tail);
 }
 
 template <typename T>

@@ -6,8 +6,8 @@
 // Each buffer has a warp of its own that sees a row through, one step after another: it starts the bulk
 // copies, takes the list's tokens out of the slice (they become -inf), adds up the sums, exchanges them
 // with the cluster's other CTAs, gives the gradient its scalars, prepares the next row's list while the
-// gradient is written, starts the next copies, and then writes the list's own gradients and (in the first
-// CTA) the loss.  These steps are chains of
+// gradient is written, starts the next copies, and then writes the list's own gradients and (in the CTA of
+// the cluster whose turn it is) the loss.  These steps are chains of
 // latency (a few us a row); as many of them as there are buffers run at once, and the 8 warps wait for
 // none of them but through the barriers of the buffers.
 //
@@ -47,7 +47,7 @@ struct Buffer {
   float ref, mul;      // of the gradient (RowScale)
   float2 part[kWorkWarps];
   float4 slot[2][kMaxStreamCluster];
-  float list_z[2][kMaxList];  // first CTA: the list's logits
+  float list_z[2][kMaxList];  // the list's logits, in the CTA that puts down the loss
   __align__(16) int ids[32];
 };
 
@@ -275,6 +275,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
     float z[kHalves] = {-kInf, -kInf};
     int vec[kHalves] = {-1, -1};
     int place = 0;  // of what the others send
+    int owner = 0;  // the CTA that puts down the loss of the buffer's row: each in turn
     uint32_t full_phase = 0, phase = 0, sums_phase = 0;
     // the old row's sums across the cluster, and its scalars; false: a wait has expired
     auto exchange = [&]() {
@@ -331,16 +332,17 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
             ok = exchange();
           }
         }
-        if (ok && rank == 0) {
-          double terms = 0.0;
+        if (ok && rank == owner) {
+          float loss = 0.f;
           if (old.lives) {
+            float zs[kHalves];
 #pragma unroll
-            for (int h = 0; h < kHalves; ++h)
-              terms += loss_term(scale, sums, old.q[h], old.lq[h], b.list_z[place][lane + 32 * h], p.scale, c);
-            terms = warp_sum(terms);
+            for (int h = 0; h < kHalves; ++h) zs[h] = old.id[h] >= 0 ? b.list_z[place][lane + 32 * h] : -kInf;
+            loss = row_loss(scale, sums, old.sums, old.w, p.bucket, p.scale, c, old.q, old.lq, zs);
           }
-          if (lane == 0) p.loss[old.row] = old.lives ? row_loss(scale, sums, terms, old.sums, old.w, p.bucket) : 0.f;
+          if (lane == 0) p.loss[old.row] = loss;
         }
+        owner = owner + 1 == n_ctas ? 0 : owner + 1;
         if (old.lives) {
           place ^= 1;
           sums_phase ^= place == 0;
@@ -375,7 +377,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
             T* at = reinterpret_cast<T*>(slice + vec[h]) + sl.place_of(old.id[h]);
             z[h] = to_f(*at);
             *at = neg_inf<T>();
-            st_cluster(map_to_rank(smem_u32(&b.list_z[place][lane + 32 * h]), 0), z[h]);
+            st_cluster(map_to_rank(smem_u32(&b.list_z[place][lane + 32 * h]), owner), z[h]);
           }
         }
         fence_proxy_async_smem();
