@@ -6,17 +6,17 @@
 // Each buffer has a warp of its own that sees a row through, one step after another: it starts the bulk
 // copies, takes the list's tokens out of the slice (they become -inf), adds up the sums, exchanges them
 // with the cluster's other CTAs, gives the gradient its scalars, prepares the next row's list while the
-// gradient is written, starts the next copies, and then writes the list's own gradients and (in the CTA of
-// the cluster whose turn it is) the loss.  These steps are chains of
-// latency (a few us a row); as many of them as there are buffers run at once, and the 8 warps wait for
-// none of them but through the barriers of the buffers.
+// gradient is written, starts the next copies, writes the list's own gradients and hands the row (in the CTA
+// of the cluster whose turn it is) to the warp that does the losses.  These steps are chains of latency (a
+// few us a row); as many of them as there are buffers run at once, and the 8 warps wait for none of them
+// but through the barriers of the buffers.
 //
 // What a CTA sends to the others alternates between two places per buffer: the second row after a row is
 // sent when all CTAs have sent the one between, after they have read the first.
 //
 // The loss alone keeps a buffer only until the sums are taken: the next row's copies start before they are
-// exchanged.  Rows of weight 0 are dealt out to the clusters apart from the others, and two warps of their
-// own write their zeros: in a buffer's turn they would keep it from loading.
+// exchanged.  Rows of weight 0 are dealt out to the clusters apart from the others, and a warp of its own
+// writes their zeros: in a buffer's turn they would keep it from loading.
 //
 // Every wait is bounded.  After one has expired (recorded in the status word) each warp leaves its loop.
 #include "distill.cuh"
@@ -28,8 +28,7 @@ namespace {
 
 constexpr int kWorkWarps = 8, kWork = 32 * kWorkWarps;
 constexpr int kMinBuffers = 3, kMaxBuffers = 6;
-constexpr int kZeroWarps = 2, kZero = 32 * kZeroWarps;
-constexpr int kAllThreads = kWork + 32 * kMaxBuffers + kZero;
+constexpr int kAllThreads = kWork + 32 * kMaxBuffers + 64;  // and a warp for losses, one for zeros
 constexpr int kDeep = 4;
 constexpr int kBufferBytes = 200 * 1024;
 constexpr int kMaxStreamCluster = 8;
@@ -48,6 +47,7 @@ struct Buffer {
   float2 part[kWorkWarps];
   float4 slot[2][kMaxStreamCluster];
   float list_z[2][kMaxList];  // the list's logits, in the CTA that puts down the loss
+  uint64_t loss_full, loss_free;
   __align__(16) int ids[32];
 };
 
@@ -68,12 +68,24 @@ struct List {
   ListSums sums;
 };
 
+// What a row's loss is made of, on its way to the warp that does it.
+struct LossRow {
+  int row;  // -1: no more
+  bool lives;
+  float w;
+  ListSums list;
+  RowSums sums;
+  RowScale scale;
+  float q[kMaxList], lq[kMaxList], z[kMaxList];
+};
+
 template <typename T, typename G>
 __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const DistillArgs p, const Shape shape) {
   constexpr bool kGrad = !std::is_same<G, NoGrad>::value;
   constexpr int E = Elem<T>::kPer;
   extern __shared__ __align__(128) uint4 buf[];
   __shared__ Buffer buffers[kMaxBuffers];
+  __shared__ LossRow losses[kMaxBuffers];
   __shared__ int abort_shared;
   __shared__ RowLists rows;
   const int rank = cluster_rank(), n_ctas = cluster_ctas();
@@ -88,6 +100,8 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
     mbar_init(&b.sums_full[1], n_ctas);
     mbar_init(&b.scaled, 1);
     mbar_init(&b.done, kWorkWarps);
+    mbar_init(&b.loss_full, 1);
+    mbar_init(&b.loss_free, 1);
     fence_mbar_init();
   }
   if (threadIdx.x == 0) abort_shared = 0;
@@ -194,17 +208,45 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
       }
     }
     for (; ok && behind > 0; --behind, queue >>= 4) ok = put_gradient(queue & 7, queue >> 3 & 1);
-  } else if (warp >= kWorkWarps + kMaxBuffers) {
+  } else if (warp == kWorkWarps + kMaxBuffers) {
+    // ----- losses: of the buffers in turn, as the working warps go through them
+    uint32_t over = 0, phases = 0;
+    for (int n = 0; over != (1u << shape.buffers) - 1u; n = n + 1 == shape.buffers ? 0 : n + 1) {
+      if (over >> n & 1) continue;
+      Buffer& b = buffers[n];
+      if (!mbar_wait_warp(smem_u32(&b.loss_full), phases >> n & 1, abort_flag, p.status, 77)) break;
+      phases ^= 1u << n;
+      const LossRow& x = losses[n];
+      const int row = x.row;
+      if (row < 0) {
+        over |= 1u << n;
+        continue;
+      }
+      float loss = 0.f;
+      if (x.lives) {
+        float q[kHalves], lq[kHalves], z[kHalves];
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h) {
+          q[h] = x.q[lane + 32 * h];
+          lq[h] = x.lq[lane + 32 * h];
+          z[h] = x.z[lane + 32 * h];
+        }
+        loss = row_loss(x.scale, x.sums, x.list, x.w, p.bucket, p.scale, c, q, lq, z);
+      }
+      if (lane == 0) p.loss[row] = loss;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&b.loss_free);
+    }
+  } else if (warp == kWorkWarps + kMaxBuffers + 1) {
     // ----- rows of weight 0
-    const int tid = threadIdx.x - (kAllThreads - kZero);
     for (int i = 0; listed && i < rows.n_rest; ++i) {
       const int r = rows.of_rest[i];
       if constexpr (kGrad)
-        write_grad<T, G>(slice_of(r), static_cast<G*>(p.grad) + r * p.ld_grad, tid, kZero, [](int, float* f) {
+        write_grad<T, G>(slice_of(r), static_cast<G*>(p.grad) + r * p.ld_grad, lane, 32, [](int, float* f) {
 #pragma unroll
           for (int j = 0; j < E; ++j) f[j] = 0.f;
         });
-      if (rank == 0 && tid == 0) p.loss[r] = 0.f;
+      if (rank == 0 && lane == 0) p.loss[r] = 0.f;
     }
   } else if (warp - kWorkWarps < shape.buffers) {
     // ----- one buffer's rows
@@ -302,6 +344,31 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
       scale = row_scale(sums, old.sums, old.w, p.scale, p.bucket, c);
       return true;
     };
+    // the old row to the warp that does the losses, once that is done with this buffer's last one
+    uint32_t loss_phase = 0;
+    auto send_loss = [&](int row) {
+      if (!mbar_wait_warp(smem_u32(&b.loss_free), loss_phase ^ 1u, abort_flag, p.status, 76)) return false;
+      loss_phase ^= 1;
+      LossRow& l = losses[n];
+#pragma unroll
+      for (int h = 0; h < kHalves; ++h) {
+        const int i = lane + 32 * h;
+        l.q[i] = old.q[h];
+        l.lq[i] = old.lq[h];
+        l.z[i] = row >= 0 && old.lives && old.id[h] >= 0 ? b.list_z[place][i] : -kInf;
+      }
+      if (lane == 0) {
+        l.row = row;
+        l.lives = old.lives;
+        l.w = old.w;
+        l.list = old.sums;
+        l.sums = sums;
+        l.scale = scale;
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&b.loss_full);
+      return true;
+    };
     for (;; phase ^= 1) {
       const Slice<T> sl = slice_of(max(x.row, 0));
       if (lane == 0) {
@@ -332,16 +399,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
             ok = exchange();
           }
         }
-        if (ok && rank == owner) {
-          float loss = 0.f;
-          if (old.lives) {
-            float zs[kHalves];
-#pragma unroll
-            for (int h = 0; h < kHalves; ++h) zs[h] = old.id[h] >= 0 ? b.list_z[place][lane + 32 * h] : -kInf;
-            loss = row_loss(scale, sums, old.sums, old.w, p.bucket, p.scale, c, old.q, old.lq, zs);
-          }
-          if (lane == 0) p.loss[old.row] = loss;
-        }
+        if (ok && rank == owner) ok = send_loss(old.row);
         owner = owner + 1 == n_ctas ? 0 : owner + 1;
         if (old.lives) {
           place ^= 1;
@@ -350,6 +408,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
       }
       if (ok && x.row < 0) {
         if (lane == 0) mbar_arrive(&b.ready);
+        send_loss(-1);
         break;
       }
       old = x;
@@ -429,7 +488,7 @@ cudaError_t launch_stream(const DistillArgs& p, cudaStream_t s) {
   shape.lag = shape.buffers >= 5 ? 2 : 1;
   return launch_clusters<kKernel>(l, kAllThreads, static_cast<size_t>(shape.buffers) * shape.vectors * 16, s, p, shape);
 }
-static_assert(kBufferBytes + kMaxBuffers * sizeof(Buffer) + sizeof(RowLists) <= 226 * 1024, "a CTA's shared memory");
+static_assert(kBufferBytes + kMaxBuffers * (sizeof(Buffer) + sizeof(LossRow)) + sizeof(RowLists) <= 226 * 1024, "a CTA's shared memory");
 
 }  // namespace
 
