@@ -222,7 +222,8 @@ typedef enum { SGD_F16 = 0, SGD_BF16 = 1, SGD_F32 = 2 } sgd_dtype;
  * -inf masks a token: its ln p is -inf.  A row of -inf alone has ln p = -inf, entropy 0 and the
  * top tokens 0, 1, ...; a row that holds NaN or +inf has NaN for every ln p and for the entropy,
  * and NaN ranks with -inf.
- * 0 <= top_k <= 64 and <= vocab; vocab * element size <= 3 MiB (else SGD_ERR_SHAPE).  No workspace:
+ * 0 <= top_k <= 64 and <= vocab (else SGD_ERR_ARG); vocab * element size <= 3 MiB (else SGD_ERR_SHAPE).
+ * No output may overlap an input or another output.  No workspace:
  * calls on several streams and replays of captured ones may overlap.  Results are the same on
  * every run.
  */
@@ -254,7 +255,8 @@ typedef enum {
  * NaN in a row, or +inf, makes its loss and gradient NaN.
  * grad of type grad_dtype, rows ld_grad elements apart, each value rounded once from fp32 (out of
  * fp16's range: inf).  grad may be logits itself (same type and ld); it must not overlap it
- * otherwise (SGD_ERR_ARG).  1 <= top_k <= 64; vocab * element size of logits <= 3 MiB (else SGD_ERR_SHAPE).
+ * otherwise (SGD_ERR_ARG), and nothing else may overlap.  1 <= top_k <= 64 (else SGD_ERR_ARG); vocab * element
+ * size of logits <= 3 MiB (else SGD_ERR_SHAPE).
  * No workspace: calls on several streams and replays of captured ones may overlap.  Results are
  * the same on every run.
  */

@@ -419,7 +419,7 @@ def _column(t, name, dtype, shape, device):
     a, b = t.stride()
     if shape[1] <= 1:
         b = a
-    if shape[0] > 1 and a != b * shape[1]:
+    if t.numel() > 1 and (b < 1 or shape[0] > 1 and a != b * shape[1]):
         raise ValueError(f"the positions of {name} must be evenly spaced")
     return t.data_ptr(), max(b, 1)
 

@@ -108,12 +108,12 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) logprobs_kernel(cons
   TopShared& top = *reinterpret_cast<TopShared*>(top_raw);
   if (TOP == kTopMany) {
     const uint32_t keys[1] = {order_key(st.m)};
-    uint32_t above;
-    const uint32_t lo = threshold(team, keys, p.top_k, top, above);
+    const Threshold th = threshold(team, keys, p.top_k, top);
+    const uint32_t from = th.from();
     // what the threads hold whose maximum reaches the threshold, looked at by all threads
-    if (keys[0] >= lo) reaching[atomicAdd(&n_reaching, 1)] = static_cast<uint16_t>(threadIdx.x);
+    if (keys[0] >= from) reaching[atomicAdd(&n_reaching, 1)] = static_cast<uint16_t>(threadIdx.x);
     __syncthreads();
-    const float bar = key_value(lo);
+    const float bar = key_value(from);
     const int steps = (sl.nv + kThreads - 1) / kThreads, all = n_reaching * steps;
     const float steps_inv = 1.f / steps;
     for (int j = threadIdx.x; j < all; j += kThreads) {
@@ -121,11 +121,14 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) logprobs_kernel(cons
       const int i = (j - q * steps) * kThreads + reaching[q];
       if (i >= sl.nv) continue;
       const uint4 v = buf[i];
-      if (lo > kKeyNegInf && !(vec_max<1>(&v, static_cast<const T*>(nullptr)) >= bar)) continue;
-      append<T>(v, sl.first_element(i), sl.vocab, lo, &top);
+      if (from > kKeyNegInf && !(vec_max<1>(&v, static_cast<const T*>(nullptr)) >= bar)) continue;
+      append<T>(v, sl.first_element(i), sl.vocab, from, &top);
     }
     __syncthreads();
-    if (top.n > kCap) candidates_of_many(team, sl, InShared{buf}, lo, above, p.top_k, top);
+    const int found = top.n;
+    __syncthreads();
+    if (found > kCap) candidates_of_many(team, sl, InShared{buf}, th.lo, th.top, p.top_k, top);
+    else if (th.tied && found < p.top_k) collect_ties(team, sl, InShared{buf}, th.lo, p.top_k - found, top);
   }
   __syncwarp();
   cluster_wait();  // every CTA of the cluster runs: the leader's shared memory may be written

@@ -90,10 +90,11 @@ template <typename T>
 __device__ __forceinline__ void candidates(const WarpTeam& team, const Slice<T>& sl, Row& x, int k, Many& many) {
   const int lane = team.tid;
   TopShared& top = many.top;
-  uint32_t keys[kMaxima], above;
+  uint32_t keys[kMaxima];
 #pragma unroll
   for (int h = 0; h < kMaxima; ++h) keys[h] = x.max_key[lane + 32 * h];
-  const uint32_t lo = threshold(team, keys, k, top, above);
+  const Threshold th = threshold(team, keys, k, top);
+  const uint32_t lo = th.from();
   int n = 0;
 #pragma unroll
   for (int h = 0; h < kMaxima; ++h) {
@@ -168,7 +169,10 @@ __device__ __forceinline__ void candidates(const WarpTeam& team, const Slice<T>&
     }
   }
   __syncwarp();
-  if (crowded || groups > kMaxGroups || top.n > kCap) candidates_of_many(team, sl, FromRow<T>{sl}, lo, above, k, top);
+  const int found = top.n;
+  __syncwarp();
+  if (crowded || groups > kMaxGroups || found > kCap) candidates_of_many(team, sl, FromRow<T>{sl}, th.lo, th.top, k, top);
+  else if (th.tied && found < k) collect_ties(team, sl, FromRow<T>{sl}, th.lo, k - found, top);
 }
 
 // The rows of one finishing warp, one after another.

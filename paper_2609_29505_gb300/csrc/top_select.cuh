@@ -117,10 +117,18 @@ __device__ void collect_ties(const Tm& team, const Slice<T>& sl, const F& fetch,
   team.sync();
 }
 
-// A threshold lo with count(maxima >= lo) >= k, near k where the maxima allow it: bisection over their
-// keys, counting over the team.  N keys per thread, at least k in all.  `top`: a key above all.
+// A threshold on the maxima: count(maxima >= lo) >= k, and near k unless many are equal to lo (`tied`); then
+// fewer than k are above it.  `top`: a key above all.
+struct Threshold {
+  uint32_t lo, top;
+  bool tied;
+  // what is looked for among all elements: those above lo alone where it is tied, as the equal ones are many
+  __device__ uint32_t from() const { return tied ? lo + 1 : lo; }
+};
+
+// By bisection over the keys, counting over the team.  N keys per thread, at least k in all.
 template <int N, typename Tm>
-__device__ uint32_t threshold(const Tm& team, const uint32_t (&key)[N], int k, TopShared& sh, uint32_t& top) {
+__device__ Threshold threshold(const Tm& team, const uint32_t (&key)[N], int k, TopShared& sh) {
   const int warp = team.tid >> 5, lane = team.tid & 31;
   uint32_t lo = key[0], hi = key[0];
 #pragma unroll
@@ -141,7 +149,8 @@ __device__ uint32_t threshold(const Tm& team, const uint32_t (&key)[N], int k, T
     lo = min(lo, sh.warp_lo[w]);
     hi = max(hi, sh.warp_hi[w]);
   }
-  top = hi = hi + 1;  // the largest key is that of +inf
+  const uint32_t top = hi = hi + 1;  // the largest key is that of +inf
+  bool tied = true;
   while (hi - lo > 1) {
     const uint32_t mid = lo + (hi - lo) / 2;
     int n = 0;
@@ -154,15 +163,18 @@ __device__ uint32_t threshold(const Tm& team, const uint32_t (&key)[N], int k, T
       for (int i = 0; i < N; ++i) n += team.count(key[i] >= mid);
     }
     if (n >= k) lo = mid; else hi = mid;
-    if (n >= k && n <= k + k / 4) break;
+    if (n >= k && n <= k + k / 4) {
+      tied = false;
+      break;
+    }
   }
-  return lo;
+  return Threshold{lo, top, tied};
 }
 
-// Where more than kCap elements reach lo (rows that are nearly constant, or sorted so that few threads
-// hold the largest values): the threshold is bisected over all elements until few reach it, or it is the
-// k-th largest value itself; then what is above it is taken, and the first of those equal to it.  A
-// row of many equal values is over at once, the others take up to 32 counts.
+// Where the elements that were looked for do not fit into the list (rows sorted so that few threads hold the
+// largest values, say): the threshold is bisected over all elements until few reach it, or it is the
+// k-th largest value itself; then what is above it is taken, and the first of those equal to it.
+// Up to 32 counts.
 template <typename T, typename Tm, typename F>
 __device__ __noinline__ void candidates_of_many(const Tm team, const Slice<T> sl, const F fetch, uint32_t lo, uint32_t top, int k,
                                                 TopShared& sh) {

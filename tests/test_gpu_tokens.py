@@ -159,6 +159,12 @@ def _rows_that_are_hard(vocab):
     z[-1], z[0] = 60000.0, 59968.0  # far above the rest
     rows.append(z)
     rows.append(np.where(np.arange(vocab) % 2 == 0, 65504.0, -65504.0))
+    z = np.full(vocab, 2.0)
+    z[rng.permutation(vocab)[:min(vocab, 30)]] = 5.0 + np.arange(min(vocab, 30)) // 3  # a few above many equal ones
+    rows.append(z)
+    z = np.full(vocab, -INF)
+    z[rng.permutation(vocab)[:min(vocab, 30)]] = rng.standard_normal(min(vocab, 30))  # a few tokens allowed
+    rows.append(z)
     return np.stack(rows)
 
 
@@ -233,6 +239,46 @@ def test_the_largest_rows(B, dtype, vocab):
     z = _logits(2, vocab, dtype, 14)
     got, tokens = _score(B, z, k=9)
     _check_score(got, tokens, z, 9)
+    ids, logq = _lists(z, 9, 14)
+    _distill(B, z, ids, logq)
+
+
+@pytest.mark.parametrize("rows,vocab", [(70000, 49200), (70000, 8200)])
+def test_more_rows_than_a_cluster_lists(B, rows, vocab):
+    """Above 448 rows of a cluster, rows that are asked for or have a weight are not listed beforehand.  A block of
+    rows again and again: the same outputs."""
+    n = 500
+    block = torch.empty(n, vocab, dtype=torch.float16, device="cuda").normal_(0, 2, generator=torch.Generator("cuda").manual_seed(3))
+    z = block.repeat(rows // n, 1)
+    g = torch.Generator("cuda").manual_seed(4)
+    on = torch.rand(rows, device="cuda", generator=g) < 0.5
+    on[1234:1234 + 7000] = False
+    tokens = torch.arange(n, device="cuda").int()[:, None].repeat(rows // n, 1)
+    few, _ = _score(B, block, k=3, tokens=tokens[:n])
+    got, _ = _score(B, z, k=3, tokens=tokens, row_ids=on.int(), row_id=1)
+    on_ = on.cpu().numpy()
+    for name, v in got.items():
+        want = np.tile(few[name].reshape(n, -1), (rows // n, 1))[on_]
+        v = v.reshape(rows, -1)
+        assert (v[~on_] == (-7 if v.dtype == np.int32 else 77.0)).all()
+        if v.dtype == np.int32:
+            assert np.array_equal(v[on_], want)
+        else:  # (another kernel: both are off by less than SUM and the roundings)
+            _near(v[on_], want, 2 * (SUM * (1 + 2 * np.abs(want)) + 64 * U))
+    if vocab > 10000:
+        return
+    ids, logq = _lists(block, 4, 5)
+    ids, logq = ids.repeat(rows // n, 1), logq.repeat(rows // n, 1)
+    w = on.float() * 0.5
+    loss, grad = _distill(B, z, ids, logq, weight=w, grad="bf16", check=False)
+    assert (loss[~on] == 0).all() and not grad[~on].any()
+    some = torch.nonzero(on)[:, 0][::1777]
+    _check_rows(loss[some], grad[some], z[some], ids[some], logq[some], True, w[some])
+    first = {}
+    for r in torch.nonzero(on)[:, 0][:4000].tolist():  # rows of one kind agree bit for bit
+        if r % n in first:
+            assert torch.equal(grad[r], grad[first[r % n]]) and loss[r] == loss[first[r % n]]
+        first.setdefault(r % n, r)
 
 
 def test_offsets_past_32_bits(B):

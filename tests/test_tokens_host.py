@@ -153,8 +153,9 @@ def test_binding_refuses_what_the_pointers_cannot_show():
         binding._tensor(z, "x", torch.float32, (2, 8), torch.device("cuda:0"))
     assert binding._column(torch.zeros(2, 8, 3)[:, :, 1], "x", torch.float32, (2, 8), cpu)[1] == 3
     assert binding._column(torch.zeros(2, 1, 3)[:, :, 1], "x", torch.float32, (2, 1), cpu)[1] == 3
-    with pytest.raises(ValueError, match="evenly"):
-        binding._column(torch.zeros(2, 9)[:, :8], "x", torch.float32, (2, 8), cpu)
+    for bad in (torch.zeros(2, 9)[:, :8], torch.zeros(2, 1).expand(2, 8), torch.zeros(1, 1).expand(2, 8)):
+        with pytest.raises(ValueError, match="evenly"):
+            binding._column(bad, "x", torch.float32, (2, 8), cpu)
 
 
 def test_type_codes_follow_the_header():
