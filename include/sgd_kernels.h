@@ -15,6 +15,10 @@
  *     residual stream                        -> sgd_kernel_frozen_run (one pass over h
  *     for a run of consecutive frozen units).
  *
+ * Beside them stand operators on what a token model's step writes, its logits, for programs that turn them
+ * into tokens or compare two evaluations: sgd_kernel_logprobs and sgd_kernel_distill (and sgd.h's
+ * sgd_sampler_reveal).
+ *
  * All pointers are device pointers; all calls are asynchronous on `stream`
  * (a cudaStream_t) and return an sgd_status (sgd.h).  Arguments are validated on
  * the host (SGD_ERR_ARG / SGD_ERR_SHAPE); nothing is launched on a validation error.

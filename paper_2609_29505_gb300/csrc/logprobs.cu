@@ -6,6 +6,11 @@
 //
 // The kernel here is for few or short rows: a cluster takes one row, a slice per CTA, and leaves
 // (vocab_rows.cuh); many long rows stream through logprobs_stream.cu.
+//
+// Measured (GB300): 1 x 126464 fp16, the 4 likeliest tokens, entropy and one given token, on a cluster of 16:
+// 5.5 us, latency (the copy, four reductions, the cluster's barrier); 1003 x 32003 bf16, the 8 likeliest,
+// entropy, 4 given tokens: 29.5 us = 2.2 TB/s: three CTAs of 64 KB an SM, each without a copy on its way for
+// half of its time.
 #include "logprobs.cuh"
 
 namespace sgd {

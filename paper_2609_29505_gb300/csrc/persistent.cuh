@@ -128,7 +128,8 @@ cudaError_t resident_clusters(int c, int threads, size_t smem, int* n) {
 }
 
 // The cluster size in [least, most] that leaves the SMs idle least over these rows: rounds, each a share of a
-// row long.
+// row long; a larger cluster has to save 5%, as it exchanges more (2048 rows of 32000 bf16 with gradients, 13.5
+// rounds of pairs: 60 us, 14 of single CTAs: 47 us).
 template <auto kKernel>
 cudaError_t choose_clusters(int rows, int least, int most, int threads, size_t smem, Clusters* out) {
   double cost = 0;

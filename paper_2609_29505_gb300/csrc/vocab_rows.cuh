@@ -317,7 +317,8 @@ struct WarpTeam {
 };
 
 // Grid: a cluster per row.  The cluster size is a power of two: slices of at most kSlice bytes, and
-// smaller ones where there are too few rows to fill the SMs.
+// smaller ones where there are too few rows to fill the SMs.  (Slices of 64 KB, 32 KB and 128 KB: 414, 503 and
+// 546 us for 4096 x 126464 fp16 with lists of 32, before such rows streamed.)
 struct Launch {
   int cluster;
   int slice_bytes;
@@ -325,7 +326,8 @@ struct Launch {
 };
 constexpr int kSlice = 64 * 1024;
 // Vectors of a slice that 64 threads take instead of 256: what a row costs beside its elements (barriers,
-// reductions) is then a quarter.
+// reductions) is then a quarter.  131072 x 2000 fp16, 64 threads against 256: 436 / 827 us scored, 632 / 1377 us
+// for a loss, 747 / 1821 us with a gradient; 65536 x 4000: 247 / 430, 333 / 696, 424 / 937 us.
 constexpr int kShortSlice = 512;
 constexpr int kMaxDynamic = (227 - 16) * 1024;  // beside at most 16 KB of static shared memory
 
