@@ -143,10 +143,10 @@ __device__ __forceinline__ Float2 two_prod(float a, float b) {  // a b exactly
   const float p = __fmul_rn(a, b);
   return Float2{p, fmaf(a, b, -p)};
 }
-// ln(j / 16), j = 8 .. 16, in two parts.
-__device__ const float kLnHigh[9] = {-0.693147182f, -0.575364172f, -0.470003635f, -0.374693453f, -0.287682086f,
+// ln(j / 16), j = 8 .. 16, in two parts (constant memory: a load from global memory takes microseconds here).
+__constant__ float kLnHigh[9] = {-0.693147182f, -0.575364172f, -0.470003635f, -0.374693453f, -0.287682086f,
                                      -0.207639366f, -0.133531392f, -0.0645385236f, 0.f};
-__device__ const float kLnLow[9] = {1.90465421e-09f, 2.75550871e-08f, 5.44550272e-09f,  3.87050969e-09f, 1.37775436e-08f,
+__constant__ float kLnLow[9] = {1.90465421e-09f, 2.75550871e-08f, 5.44550272e-09f,  3.87050969e-09f, 1.37775436e-08f,
                                     1.61007641e-09f, -1.00388664e-09f, 2.41723086e-09f, 0.f};
 // ln x of a normal x > 0, to some 4e-9: the exponent times ln 2 in two parts (the first one short: e times it is
 // exact), the logarithm of the nearest j / 16 to the significand, and log1pf of what is left (at most 1 / 16).

@@ -7,7 +7,7 @@
 // copies, takes the list's tokens out of the slice (they become -inf), adds up the sums, exchanges them
 // with the cluster's other CTAs, gives the gradient its scalars, prepares the next row's list while the
 // gradient is written, starts the next copies, writes the list's own gradients and hands the row (in the CTA
-// of the cluster whose turn it is) to the warp that does the losses.  These steps are chains of latency (a
+// of the cluster whose turn it is) to one of the warps that do the losses.  These steps are chains of latency (a
 // few us a row); as many of them as there are buffers run at once, and the 8 warps wait for none of them
 // but through the barriers of the buffers.
 //
@@ -19,12 +19,12 @@
 // writes their zeros: in a buffer's turn they would keep it from loading.
 //
 // Measured (GB300, replayed from a graph over rotating inputs), lists of 32, 126464 fp16 logits a row: 4096 rows
-// with a bf16 gradient 339 us = 6.1 TB/s (a copy moves 6.8): the 8 warps are busy for 5.1 of the 5.9 thousand
+// with a bf16 gradient 342 us = 6.1 TB/s (a copy moves 6.8): the 8 warps are busy for 5.1 of the 5.9 thousand
 // clocks of a row (sums 2.6, gradient 2.5), the rest is waiting for copies.  The loss alone, 1024 rows: 63 us
 // = 4.1 TB/s: a buffer's chain (copy, list, sums, exchange) over three buffers.  Three slices of 64 KB are what
 // an SM holds; clusters of 8 with slices of half the size leave 32 SMs idle (15 of them fit: 495 us).
-// 12 working warps: 349 us; the next vectors fetched ahead of the sums: 356 us; slices copied and given free
-// in four pieces: 367 us.
+// Tried at 338 us: 12 working warps 349 us, the next vectors fetched ahead of the sums 356 us, slices copied
+// and given free in four pieces 367 us.  The gradient a row later than the next row's sums: no difference.
 //
 // Every wait is bounded.  After one has expired (recorded in the status word) each warp leaves its loop.
 #include "distill.cuh"
@@ -35,8 +35,9 @@ namespace rows {
 namespace {
 
 constexpr int kWorkWarps = 8, kWork = 32 * kWorkWarps;
-constexpr int kMinBuffers = 3, kMaxBuffers = 6;
-constexpr int kAllThreads = kWork + 32 * kMaxBuffers + 64;  // and a warp for losses, one for zeros
+constexpr int kMinBuffers = 3, kMaxBuffers = 5;
+constexpr int kLossWarps = 4;
+constexpr int kAllThreads = kWork + 32 * (kMaxBuffers + kLossWarps + 1);  // the last warp: zeros
 constexpr int kDeep = 4;
 constexpr int kBufferBytes = 200 * 1024;
 constexpr int kMaxStreamCluster = 8;
@@ -59,10 +60,9 @@ struct Buffer {
   __align__(16) int ids[32];
 };
 
-// Buffers of `vectors` vectors (a multiple of kWork) each; the gradient of a row is written `lag` rows after its
-// sums were taken.
+// Buffers of `vectors` vectors (a multiple of kWork) each.
 struct Shape {
-  int vectors, buffers, lag;
+  int vectors, buffers;
 };
 
 // A row's list, kHalves entries a lane.
@@ -182,31 +182,28 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
       }
       return true;
     };
-    uint32_t over = 0, phase = 0;  // buffers without further rows
-    int n = 0, behind = 0;         // rows whose gradient is still to be written: in the buffers ...
-    int queue = 0;                 // (4 bits each, the oldest lowest: buffer, and its phase above)
+    uint32_t over = 0, phase = 0;      // buffers without further rows
+    int n = 0, late = -1;              // the buffer of the row whose gradient is still to be written
+    uint32_t late_phase = 0;
     bool ok = true;
+    auto catch_up = [&]() {
+      if (late >= 0) ok = put_gradient(late, late_phase);
+      late = -1;
+    };
     while (ok && over != (1u << shape.buffers) - 1u) {
       if (!(over >> n & 1)) {
         // (near the end of the rows the other buffers may have none: this one's next row waits for its gradient)
-        if (behind > 0 && (queue & 7) == n) {
-          if (!(ok = put_gradient(n, queue >> 3 & 1))) break;
-          queue >>= 4;
-          --behind;
-        }
-        ok = mbar_wait_warp(smem_u32(&buffers[n].ready), phase, abort_flag, p.status, 70);
+        if (late == n) catch_up();
+        ok = ok && mbar_wait_warp(smem_u32(&buffers[n].ready), phase, abort_flag, p.status, 70);
         if (!ok) break;
         if (buffers[n].row < 0) {
           over |= 1u << n;
         } else {
           take_sums(n);
           if (kGrad) {
-            queue |= (n | static_cast<int>(phase) << 3) << (4 * behind++);
-            if (behind > shape.lag) {
-              ok = put_gradient(queue & 7, queue >> 3 & 1);
-              queue >>= 4;
-              --behind;
-            }
+            catch_up();
+            late = n;
+            late_phase = phase;
           }
         }
       }
@@ -215,11 +212,13 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
         phase ^= 1;
       }
     }
-    for (; ok && behind > 0; --behind, queue >>= 4) ok = put_gradient(queue & 7, queue >> 3 & 1);
-  } else if (warp == kWorkWarps + kMaxBuffers) {
-    // ----- losses: of the buffers in turn, as the working warps go through them
-    uint32_t over = 0, phases = 0;
-    for (int n = 0; over != (1u << shape.buffers) - 1u; n = n + 1 == shape.buffers ? 0 : n + 1) {
+    if (ok) catch_up();
+  } else if (warp >= kWorkWarps + kMaxBuffers && warp < kWorkWarps + kMaxBuffers + kLossWarps) {
+    // ----- losses: a buffer's (the first and the last buffer's by turns), as the working warps go through them
+    const int first = warp - kWorkWarps - kMaxBuffers;
+    uint32_t all = 0, over = 0, phases = 0;
+    for (int n = first; n < shape.buffers; n += kLossWarps) all |= 1u << n;
+    for (int n = first; over != all; n = n + kLossWarps < shape.buffers ? n + kLossWarps : first) {
       if (over >> n & 1) continue;
       Buffer& b = buffers[n];
       if (!mbar_wait_warp(smem_u32(&b.loss_full), phases >> n & 1, abort_flag, p.status, 77)) break;
@@ -245,7 +244,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
       __syncwarp();
       if (lane == 0) mbar_arrive(&b.loss_free);
     }
-  } else if (warp == kWorkWarps + kMaxBuffers + 1) {
+  } else if (warp == kWorkWarps + kMaxBuffers + kLossWarps) {
     // ----- rows of weight 0
     for (int i = 0; listed && i < rows.n_rest; ++i) {
       const int r = rows.of_rest[i];
@@ -493,17 +492,17 @@ cudaError_t launch_stream(const DistillArgs& p, cudaStream_t s) {
   Shape shape;
   shape.vectors = buffer_vectors(bytes, l.size);
   shape.buffers = buffers(l.size) < kMaxBuffers ? buffers(l.size) : kMaxBuffers;
-  shape.lag = shape.buffers >= 5 ? 2 : 1;
   return launch_clusters<kKernel>(l, kAllThreads, static_cast<size_t>(shape.buffers) * shape.vectors * 16, s, p, shape);
 }
 static_assert(kBufferBytes + kMaxBuffers * (sizeof(Buffer) + sizeof(LossRow)) + sizeof(RowLists) <= 226 * 1024, "a CTA's shared memory");
 
 }  // namespace
 
-// Streaming against a cluster per row, us, the loss / with a bf16 gradient, fp16 logits: rows of 253 KB: 128 MB 33 /
-// 54 against 42 / 65, 64 MB 22 / 33 against 25 / 37, 32 MB 16 / 22 against 16 / 20; of 64 KB: 128 MB 35 / 62 against 44 /
-// 64; of 16 KB: 512 MB 161 / 351 against 354 / 518, 64 MB 27 / 53 against 46 / 67, 32 MB 25 / 48 against 27 / 35; of 8 KB:
-// 128 MB 81 / 173 against 87 / 110.
+// Streaming against a cluster per row, us, the loss / with a bf16 gradient, fp16 logits: rows of 253 KB: 128 MB 34 /
+// 54 against 42 / 65, 64 MB 22 / 34 against 25 / 37, 32 MB 17 / 21 against 16 / 20; of 64 KB: 512 MB 91 / 169 against 148 /
+// 215, 64 MB 21 / 34 against 26 / 37; of 32 KB: 512 MB 110 / 283 against 191 / 311, 64 MB 23 / 44 against 29 / 45; of 16
+// KB: 512 MB 174 / 508 against 354 / 518, 64 MB 30 / 69 against 46 / 67, 32 MB 29 / 39 against 27 / 35; of 8 KB: 128 MB 81 /
+// 173 against 87 / 110.  (Without the loss the gradient of 32 KB rows takes 194 us: its code beside the other warps'.)
 bool distill_stream_pays(int rows, int64_t row_bytes) {
   return row_bytes >= 16 * 1024 && rows * row_bytes >= (48 << 20) &&
          kBufferBytes / (16 * static_cast<int64_t>(buffer_vectors(row_bytes, kMaxStreamCluster))) >= kMinBuffers;
