@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
     }
     if (ok) catch_up();
   } else if (warp >= kWorkWarps + kMaxBuffers && warp < kWorkWarps + kMaxBuffers + kLossWarps) {
-    // ----- losses: a buffer's (the first and the last buffer's by turns), as the working warps go through them
+    // ----- losses: of the buffers first, first + kLossWarps, ... in turn, as the working warps go through them
     const int first = warp - kWorkWarps - kMaxBuffers;
     uint32_t all = 0, over = 0, phases = 0;
     for (int n = first; n < shape.buffers; n += kLossWarps) all |= 1u << n;
@@ -498,13 +498,17 @@ static_assert(kBufferBytes + kMaxBuffers * (sizeof(Buffer) + sizeof(LossRow)) + 
 
 }  // namespace
 
-// Streaming against a cluster per row, us, the loss / with a bf16 gradient, fp16 logits: rows of 253 KB: 128 MB 34 /
-// 54 against 42 / 65, 64 MB 22 / 34 against 25 / 37, 32 MB 17 / 21 against 16 / 20; of 64 KB: 512 MB 91 / 169 against 148 /
-// 215, 64 MB 21 / 34 against 26 / 37; of 32 KB: 512 MB 110 / 283 against 191 / 311, 64 MB 23 / 44 against 29 / 45; of 16
-// KB: 512 MB 174 / 508 against 354 / 518, 64 MB 30 / 69 against 46 / 67, 32 MB 29 / 39 against 27 / 35; of 8 KB: 128 MB 81 /
-// 173 against 87 / 110.  (Without the loss the gradient of 32 KB rows takes 194 us: its code beside the other warps'.)
+// Streaming against a cluster per row, us, the loss / with a bf16 gradient, fp16 logits:
+//   row       32 MB                 64 MB                  128 MB                   512 MB
+//   253 KB    17 / 22, 17 / 21      23 / 34, 26 / 38       35 / 56, 43 / 65         108 / 174, 147 / 220
+//   64 KB     17 / 27, 18 / 22      21 / 34, 27 / 38       31 / 55, 46 / 67         89 / 169, 156 / 230
+//   32 KB     16 / 25, 17 / 26      23 / 44, 30 / 47       35 / 78, 54 / 85         110 / 283, 196 / 323
+//   16 KB     19 / 37, 29 / 39      30 / 69, 50 / 75       50 / 133, 96 / 144       174 / 509, 367 / 566
+//   8.4 KB    27 / 61, 44 / 63      46 / 117, 83 / 124     84 / 228, 167 / 243      310 / 891, 648 / 954
+// Rows that 64 threads take (kShortSlice) stay with them: 65536 x 4000 333 / 424 us.  (Without the loss the gradient
+// of 32 KB rows, 512 MB, takes 194 us: the loss warps' code beside the other warps'.)
 bool distill_stream_pays(int rows, int64_t row_bytes) {
-  return row_bytes >= 16 * 1024 && rows * row_bytes >= (48 << 20) &&
+  return row_bytes > 16 * kShortSlice && rows * row_bytes >= (48 << 20) &&
          kBufferBytes / (16 * static_cast<int64_t>(buffer_vectors(row_bytes, kMaxStreamCluster))) >= kMinBuffers;
 }
 
