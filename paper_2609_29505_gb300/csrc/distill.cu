@@ -201,8 +201,10 @@ cudaError_t launch_threads(const DistillArgs& p, int grad_dtype, const Launch& l
 }
 template <typename T>
 cudaError_t launch_type(const DistillArgs& p, int grad_dtype, cudaStream_t s) {
-  if (distill_stream_pays(p.rows, static_cast<int64_t>(p.vocab) * sizeof(T))) return distill_stream<T>(p, grad_dtype, s);
-  const Launch l = plan(p.rows, p.vocab, sizeof(T));
+  const int64_t row_bytes = static_cast<int64_t>(p.vocab) * sizeof(T);
+  if (distill_stream_pays(p.rows, row_bytes, p.grad)) return distill_stream<T>(p, grad_dtype, s);
+  Launch l = plan(p.rows, p.vocab, sizeof(T));
+  if (p.grad && row_bytes <= kShortGradRow && p.rows * row_bytes >= kManyBytes) l.threads = 64;
   return l.threads == 64 ? launch_threads<T, 64>(p, grad_dtype, l, s) : launch_threads<T, 256>(p, grad_dtype, l, s);
 }
 

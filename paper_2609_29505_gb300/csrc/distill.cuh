@@ -255,7 +255,9 @@ __device__ __forceinline__ float row_loss(const RowScale& o, const RowSums& r, c
 
 template <typename T>
 cudaError_t distill_stream(const DistillArgs& p, int grad_dtype, cudaStream_t s);  // distill_stream.cu
-bool distill_stream_pays(int rows, int64_t row_bytes);
+constexpr int64_t kManyBytes = 48 << 20;     // of all rows
+constexpr int64_t kShortGradRow = 32 * 1024;  // bytes of a row, with a gradient
+bool distill_stream_pays(int rows, int64_t row_bytes, bool grad);
 
 }  // namespace rows
 }  // namespace sgd

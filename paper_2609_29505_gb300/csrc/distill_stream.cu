@@ -505,10 +505,12 @@ static_assert(kBufferBytes + kMaxBuffers * (sizeof(Buffer) + sizeof(LossRow)) + 
 //   32 KB     16 / 25, 17 / 26      23 / 44, 30 / 47       35 / 78, 54 / 85         110 / 283, 196 / 323
 //   16 KB     19 / 37, 29 / 39      30 / 69, 50 / 75       50 / 133, 96 / 144       174 / 509, 367 / 566
 //   8.4 KB    27 / 61, 44 / 63      46 / 117, 83 / 124     84 / 228, 167 / 243      310 / 891, 648 / 954
-// Rows that 64 threads take (kShortSlice) stay with them: 65536 x 4000 333 / 424 us.  (Without the loss the gradient
-// of 32 KB rows, 512 MB, takes 194 us: the loss warps' code beside the other warps'.)
-bool distill_stream_pays(int rows, int64_t row_bytes) {
-  return row_bytes > 16 * kShortSlice && rows * row_bytes >= (48 << 20) &&
+// with 256 threads a row.  With 64 threads, 64 and 512 MB: 32 KB 28 / 40, 155 / 227; 16 KB 32 / 43, 206 / 275; 8.4 KB
+// 49 / 61, 352 / 442.  So gradients of rows of up to 32 KB take 64 threads a row (the loss warps' code beside the
+// working warps' is what holds the stream back: 283 us are 194 without it), losses alone stream from 8 KB on; below
+// that 64 threads win both (65536 x 4000: 333 / 424 us).
+bool distill_stream_pays(int rows, int64_t row_bytes, bool grad) {
+  return row_bytes > (grad ? kShortGradRow : 16 * kShortSlice) && rows * row_bytes >= kManyBytes &&
          kBufferBytes / (16 * static_cast<int64_t>(buffer_vectors(row_bytes, kMaxStreamCluster))) >= kMinBuffers;
 }
 

@@ -585,7 +585,8 @@ def _check_rows(loss, grad, z, ids, logq, bucket, w):
     (800, 32003, "bf16", "bf16", 0, 1), (801, 32003, "f16", "f32", 13, 0), (260, 50021, "f32", "f32", 0, 3),
     (1600, 16387, "f16", "f16", 5, 2), (1600, 16387, "bf16", "", 1, 0), (100, 266176, "f16", "bf16", 0, 0),
     (98, 133081, "f32", "bf16", 2, 1), (102, 126464, "f32", "f32", 0, 0), (5000, 8209, "f16", "bf16", 0, 0),
-    (6100, 4177, "f16", "bf16", 3, 0), (3000, 4409, "f32", "", 0, 1)])
+    (6100, 4177, "f16", "bf16", 3, 0), (6100, 4177, "f16", "", 3, 0), (3000, 4409, "f32", "", 0, 1), (1600, 8190, "f32", "f32", 0, 1),
+    (1700, 16384, "bf16", "bf16", 0, 0)])
 @pytest.mark.parametrize("bucket,k", [(True, 32), (False, 64), (True, 1)])
 def test_distill_of_many_rows(B, rows, vocab, dtype, grad, pad, offset, bucket, k):
     assert rows * vocab * torch.finfo(DT[dtype]).bits // 8 >= 48 << 20
