@@ -438,7 +438,9 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
 #pragma unroll
         for (int h = 0; h < kHalves; ++h) {
           z[h] = -kInf;
-          vec[h] = old.id[h] >= 0 ? sl.vector_of(old.id[h]) : -1;
+          // (of a row that lives alone: the others' sums cross the cluster for no other, so that nothing would order
+          // a write to list_z for it against the writes for later rows)
+          vec[h] = old.lives && old.id[h] >= 0 ? sl.vector_of(old.id[h]) : -1;
           if (vec[h] >= 0) {
             T* at = reinterpret_cast<T*>(slice + vec[h]) + sl.place_of(old.id[h]);
             z[h] = to_f(*at);
