@@ -206,6 +206,7 @@ __device__ __forceinline__ RowScale row_scale(const RowSums& r, const ListSums& 
 template <int N>
 __device__ __forceinline__ float row_loss(const RowScale& o, const RowSums& r, const ListSums& l, float w, bool bucket, float scale,
                                           float c, const float (&q)[N], const float (&lq)[N], const float (&z)[N]) {
+  if (o.s != o.s) return kNan;  // (NaN or +inf in the row, wherever it stands, also where the list has no weight)
   // in units of e^(scale m), m the row's maximum: the sums hold 2^delta of it, delta = c m - R
   const float delta = r.all == -kInf ? 0.f : fmaf(r.all, c, -o.R);
   Float2 x[N];  // scale (z - m)

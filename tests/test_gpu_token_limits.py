@@ -62,3 +62,27 @@ def test_lists_without_weight_between_others(B, rows, vocab, dtype, grad):
         B.sgd_kernel_distill(z, ids, logq, again, tail=B.TAIL_RENORM)
         assert torch.equal(again, loss) or g is not None
         assert ((again[live].double() - want).abs() <= tol + U * want.abs()).all()
+
+
+@pytest.mark.parametrize("rows,vocab,dtype", [(12, 700, "f16"), (12, 9001, "f32"), (420, 126464, "f16")])
+@pytest.mark.parametrize("bucket", [True, False])
+@pytest.mark.parametrize("bad", [math.nan, INF])
+def test_what_is_no_number_shows_wherever_it_stands(B, rows, vocab, dtype, bucket, bad):
+    """NaN or +inf at a token that the list gives no weight, at one that it does, outside the list beside a masked token
+    that has weight, and alone in a row of -inf."""
+    z = _normal(rows, vocab, dtype, 3)
+    ids = torch.arange(4, dtype=torch.int32, device="cuda").repeat(rows, 1) * 5
+    logq = torch.tensor([-1.0, -2.0, -INF, -3.0], device="cuda").repeat(rows, 1)
+    z[0, 10], z[1, 5] = bad, bad
+    z[2, 0], z[2, vocab - 1] = -INF, bad
+    z[3, :] = -INF
+    z[3, 7] = bad
+    z[4, :], ids[4, 1:] = -INF, -1
+    z[4, 10] = bad
+    z[5, 10] = -INF  # a number, as it has no weight
+    for grad in ("", "f32"):
+        loss = torch.empty(rows, device="cuda")
+        g = torch.empty(rows, vocab, dtype=DT[grad], device="cuda") if grad else None
+        B.sgd_kernel_distill(z, ids, logq, loss, grad=g, tail=B.TAIL_BUCKET if bucket else B.TAIL_RENORM)
+        assert torch.isnan(loss[:5]).all() and torch.isfinite(loss[5:]).all()
+        assert g is None or torch.isnan(g[:5]).all() and torch.isfinite(g[5:]).all()
