@@ -223,7 +223,8 @@ typedef enum { SGD_F16 = 0, SGD_BF16 = 1, SGD_F32 = 2 } sgd_dtype;
  * logits [rows, vocab] of type dtype, rows ld elements apart, aligned to their elements alone.
  * scale > 0 (1 / temperature).  row_ids int32 [rows]: where given, only rows with row_ids[r] == row_id
  * (positions that are still masked, say) are read, and what the others' outputs held stays.
- * -inf masks a token: its ln p is -inf.  A row of -inf alone has ln p = -inf, entropy 0 and the
+ * -inf masks a token: its ln p is -inf.  Finite logits may be of any magnitude (masks of the type's lowest value, of
+ * -1e10), at any scale: what fp32 does not hold of their ln p is -inf.  A row of -inf alone has ln p = -inf, entropy 0 and the
  * top tokens 0, 1, ...; a row that holds NaN or +inf has NaN for every ln p and for the entropy,
  * and NaN ranks with -inf.
  * 0 <= top_k <= 64 and <= vocab (else SGD_ERR_ARG); vocab * element size <= 3 MiB (else SGD_ERR_SHAPE).

@@ -36,7 +36,7 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) distill_kernel(const
   __shared__ int ids[kMaxList];
   __shared__ double q_sum[2];
   __shared__ int q_any[2];
-  __shared__ float4 warp_stat[kWarps];
+  __shared__ float4 parts[kWarps];
   __shared__ float4 slot[kMaxCluster];
   __shared__ float list_z[kMaxList];  // leader: the list's logits
   const int rank = cluster_rank();
@@ -128,27 +128,26 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) distill_kernel(const
       const int k = i + u * kThreads + threadIdx.x;
       v[u] = k < sl.nv ? buf[k] : none;
     }
-    stat_add<T, kUnroll, false>(st, v, c);
+    stat_add<T, kUnroll, false>(st, v, c, 0.f);
   }
   // the CTA's sums, of the tail and of its part of S
-  float m = key_value(__reduce_max_sync(0xffffffffu, max(order_key(st.m), order_key(z))));
+  const float3 tail = warp_stat<T, false>(st, c, threadIdx.x, kThreads, sl.nv, InShared{buf});
+  float m = key_value(__reduce_max_sync(0xffffffffu, max(order_key(tail.x), order_key(z))));
   {
     const float R = reference(m, c);
-    float s = st.s, unused = 0.f;
-    rebase(st.m, c, R, s, unused);
-    float in = vec >= 0 ? ex2_approx(fmaf(z, c, -R)) : 0.f;
-    s = warp_sum(s);
-    in = warp_sum(in);
-    if (lane == 0) warp_stat[warp] = make_float4(m, s, in, 0.f);
+    float s = tail.y, unused = 0.f;
+    rebase(tail.x, c, m, R, s, unused);
+    const float in = warp_sum(vec >= 0 ? ex2_approx(exponent(z, m, R, c)) : 0.f);
+    if (lane == 0) parts[warp] = make_float4(m, s, in, 0.f);
   }
   __syncthreads();
   if (warp == 0) {
-    float4 v = lane < kWarps ? warp_stat[lane] : make_float4(-kInf, 0.f, 0.f, 0.f);
+    float4 v = lane < kWarps ? parts[lane] : make_float4(-kInf, 0.f, 0.f, 0.f);
     m = key_value(__reduce_max_sync(0xffffffffu, order_key(v.x)));
     const float R = reference(m, c);
     float unused = 0.f;
-    rebase(v.x, c, R, v.y, unused);
-    rebase(v.x, c, R, v.z, unused);
+    rebase(v.x, c, m, R, v.y, unused);
+    rebase(v.x, c, m, R, v.z, unused);
     v.y = warp_sum(v.y);
     v.z = warp_sum(v.z);
     if (lane < n_ctas) st_cluster(map_to_rank(smem_u32(&slot[rank]), lane), make_float4(m, v.y, v.z, 0.f));
@@ -161,18 +160,9 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) distill_kernel(const
   const RowScale o = row_scale(sums, ls, w, p.scale, p.bucket, c);
   if constexpr (kGrad) {
     G* grow = static_cast<G*>(p.grad) + r * p.ld_grad;
-    const uint64_t c2 = pack_f32x2(c, c), r2 = pack_f32x2(-o.ref, -o.ref);
-    write_grad<T, G>(sl, grow, threadIdx.x, kThreads, [&](int i, float* f) {
-      unpack(buf[i], f, static_cast<const T*>(nullptr));
-#pragma unroll
-      for (int j = 0; j < E; j += 2) {
-        const uint64_t y = fma_f32x2(pack_f32x2(f[j], f[j + 1]), c2, r2);
-        f[j] = o.mul * ex2_approx(lo_f32x2(y));
-        f[j + 1] = o.mul * ex2_approx(hi_f32x2(y));
-      }
-    });
+    write_tail_grad<T, G>(sl, buf, grow, threadIdx.x, kThreads, Outside{o.ref, o.mul, sums.all, is_far(o.R)}, c);
     __syncthreads();
-    if (vec >= 0) grow[id] = Out<G>::one(ex2_approx(fmaf(z, c, -o.R)) * o.inv_s * o.f_in - q * o.q_in);
+    if (vec >= 0) grow[id] = Out<G>::one(ex2_approx(exponent(z, sums.all, o.R, c)) * o.inv_s * o.f_in - q * o.q_in);
   }
   if (rank != 0) return;
 

@@ -104,7 +104,44 @@ __device__ __forceinline__ void write_grad(const Slice<T>& sl, G* grow, int tid,
   }
 }
 
-// A row's sums: maximum, and sum of 2^(c x - R) over the tail and over the list.
+// The gradient outside the list: mul 2^(c x - ref), or mul 2^((x - m) c - ref) where the reference is far.
+struct Outside {
+  float ref, mul, m;
+  bool far;
+};
+
+template <typename T, typename G>
+__device__ __noinline__ void write_far_grad(const Slice<T> sl, const uint4* slice, G* grow, int tid, int threads, const Outside o, float c) {
+  for (int i = tid; i < sl.nv; i += threads) {
+    float f[Elem<T>::kPer];
+    unpack(slice[i], f, static_cast<const T*>(nullptr));
+    const int e = sl.first_element(i);
+#pragma unroll
+    for (int j = 0; j < Elem<T>::kPer; ++j)
+      if (e + j >= 0 && e + j < sl.vocab) grow[e + j] = Out<G>::one(o.mul * ex2_approx(fmaf(f[j] - o.m, c, -o.ref)));
+  }
+}
+template <typename T, typename G>
+__device__ __forceinline__ void write_tail_grad(const Slice<T>& sl, const uint4* slice, G* grow, int tid, int threads, const Outside o,
+                                                float c) {
+  if (o.far) {
+    write_far_grad<T, G>(sl, slice, grow, tid, threads, o, c);
+    return;
+  }
+  const uint64_t c2 = pack_f32x2(c, c), r2 = pack_f32x2(-o.ref, -o.ref);
+  const float mul = o.mul;
+  write_grad<T, G>(sl, grow, tid, threads, [&](int i, float* f) {
+    unpack(slice[i], f, static_cast<const T*>(nullptr));
+#pragma unroll
+    for (int j = 0; j < Elem<T>::kPer; j += 2) {
+      const uint64_t y = fma_f32x2(pack_f32x2(f[j], f[j + 1]), c2, r2);
+      f[j] = mul * ex2_approx(lo_f32x2(y));
+      f[j + 1] = mul * ex2_approx(hi_f32x2(y));
+    }
+  });
+}
+
+// A row's sums: maximum, and sum of its terms over the tail and over the list.
 struct RowSums {
   float all, tail, in;
 };
@@ -118,8 +155,8 @@ __device__ __forceinline__ RowSums row_sums(const float4* slot, int n_ctas, floa
   r.all = key_value(__reduce_max_sync(0xffffffffu, order_key(v.x)));
   const float R = reference(r.all, c);
   float unused = 0.f;
-  rebase(v.x, c, R, v.y, unused);
-  rebase(v.x, c, R, v.z, unused);
+  rebase(v.x, c, r.all, R, v.y, unused);
+  rebase(v.x, c, r.all, R, v.z, unused);
   r.tail = warp_sum(v.y);
   r.in = warp_sum(v.z);
   return r;
@@ -166,11 +203,11 @@ __device__ __forceinline__ ListSums list_sums(double Q, bool bucket) {
   return ListSums{hi, lo, bucket ? fmaxf(0.f, (1.f - hi) - lo) : 0.f};
 }
 
-// The scalars of a row's gradient: p_j = inv_s 2^(c x_j - R); outside the list the gradient is
-// mul 2^(c x_j - ref), inside it p_j f_in - q q_in.
+// The scalars of a row's gradient: p_j = inv_s 2^y, y its exponent against (m, R); inside the list the gradient is
+// p_j f_in - q q_in.  (m is the row's maximum.)
 struct RowScale {
   float R, inv_s, f_in, q_in;
-  float ref, mul;
+  float ref, mul;  // of the gradient outside
   float s;
   bool empty, has_tail;
 };
@@ -184,14 +221,15 @@ __device__ __forceinline__ RowScale row_scale(const RowSums& r, const ListSums& 
   o.has_tail = bucket && r.tail > 0.f;
   o.f_in = w * scale;
   o.q_in = bucket ? o.f_in : o.f_in / l.Q;
-  // w scale p_j (1 - q_T / p_T) = F 2^(c x_j - R), F = w scale (1 / s - q_T / tail).  F's exponent k goes into
+  // w scale p_j (1 - q_T / p_T) = F 2^y, F = w scale (1 / s - q_T / tail).  F's exponent k goes into
   // the reference, so that a small tail's large factor overflows nowhere; what rounding the
   // reference takes goes into the factor.
   const float g = o.inv_s - (o.has_tail ? l.q_tail / r.tail : 0.f);  // (finite: tail >= 2^-126)
   int k = 0, k2 = 0;
   float f = o.f_in * g;
   if (isfinite(o.f_in) && isfinite(g)) f = frexpf(g, &k) * frexpf(o.f_in, &k2);
-  const Float2 ref = two_sum(o.R, -static_cast<float>(k + k2));
+  const bool far = is_far(o.R);
+  const Float2 ref = two_sum(far ? 0.f : o.R, -static_cast<float>(k + k2));
   o.ref = ref.hi;
   o.mul = f * ex2_approx(-ref.lo);
   return o;
@@ -208,13 +246,14 @@ __device__ __forceinline__ float row_loss(const RowScale& o, const RowSums& r, c
                                           float c, const float (&q)[N], const float (&lq)[N], const float (&z)[N]) {
   if (o.s != o.s) return kNan;  // (NaN or +inf in the row, wherever it stands, also where the list has no weight)
   // in units of e^(scale m), m the row's maximum: the sums hold 2^delta of it, delta = c m - R
-  const float delta = r.all == -kInf ? 0.f : fmaf(r.all, c, -o.R);
+  const float delta = delta_of(r.all, c, o.R);
   Float2 x[N];  // scale (z - m)
   double sum = 0.0;
 #pragma unroll
   for (int h = 0; h < N; ++h) {
     const Float2 d = two_sum(z[h], -r.all), p = two_prod(d.hi, scale);
     x[h] = Float2{p.hi, fmaf(d.lo, scale, p.lo)};
+    if (!isfinite(p.hi)) x[h] = Float2{z[h] * scale - r.all * scale, 0.f};  // (the difference was out of range)
     if (q[h] == 0.f || z[h] == -kInf) continue;  // no entry, or no weight (left to `in`), or no probability
     const float e = expf(x[h].hi);
     sum += static_cast<double>(fmaf(e, x[h].lo, e));
@@ -235,7 +274,7 @@ __device__ __forceinline__ float row_loss(const RowScale& o, const RowSums& r, c
   for (int h = 0; h < N; ++h) {
     if (q[h] == 0.f) continue;  // (a NaN is no 0)
     const Float2 diff = Float2{lq[h], 0.f} + -x[h] + ln_s;
-    terms += o.empty || z[h] == -kInf ? q[h] * kInf : q[h] * (diff.hi + diff.lo);
+    terms += o.empty || x[h].hi == -kInf ? q[h] * kInf : q[h] * (diff.hi + diff.lo);
   }
   terms = warp_sum(terms);
   const float hi = static_cast<float>(terms);

@@ -52,7 +52,7 @@ struct Buffer {
   uint64_t done;       // the gradient is written
   int row;             // -1: no more
   int live;            // 0: loss and gradient are 0
-  float ref, mul;      // of the gradient (RowScale)
+  Outside out;         // of the gradient
   float2 part[kWorkWarps];
   float4 slot[2][kMaxStreamCluster];
   float list_z[2][kMaxList];  // the list's logits, in the CTA that puts down the loss
@@ -131,23 +131,21 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
       Buffer& b = buffers[n];
       if (b.live) {
         const uint4* at = buf + n * shape.vectors + threadIdx.x;
-        int left = (slice_of(b.row).nv + kWork - 1) / kWork;
+        const int nv = slice_of(b.row).nv;
+        int left = (nv + kWork - 1) / kWork;
         Stat st;
         for (; left >= kDeep; left -= kDeep, at += kDeep * kWork) {
           uint4 v[kDeep];
 #pragma unroll
           for (int u = 0; u < kDeep; ++u) v[u] = at[u * kWork];
-          stat_add<T, kDeep, false>(st, v, c);
+          stat_add<T, kDeep, false>(st, v, c, 0.f);
         }
         for (; left > 0; --left, at += kWork) {
           const uint4 v = *at;
-          stat_add<T, 1, false>(st, &v, c);
+          stat_add<T, 1, false>(st, &v, c, 0.f);
         }
-        const float m = key_value(__reduce_max_sync(0xffffffffu, order_key(st.m)));
-        float s = st.s, unused = 0.f;
-        rebase(st.m, c, reference(m, c), s, unused);
-        s = warp_sum(s);
-        if (lane == 0) b.part[warp] = make_float2(m, s);
+        const float3 w_stat = warp_stat<T, false>(st, c, threadIdx.x, kWork, nv, InShared{buf + n * shape.vectors});
+        if (lane == 0) b.part[warp] = make_float2(w_stat.x, w_stat.y);
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&b.part_full);
@@ -159,18 +157,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
         const Slice<T> sl = slice_of(b.row);
         G* grow = static_cast<G*>(p.grad) + b.row * p.ld_grad;
         if (b.live) {
-          const float ref = b.ref, mul = b.mul;
-          const uint4* slice = buf + n * shape.vectors;
-          const uint64_t c2 = pack_f32x2(c, c), r2 = pack_f32x2(-ref, -ref);
-          write_grad<T, G>(sl, grow, threadIdx.x, kWork, [&](int i, float* f) {
-            unpack(slice[i], f, static_cast<const T*>(nullptr));
-#pragma unroll
-            for (int j = 0; j < E; j += 2) {
-              const uint64_t y = fma_f32x2(pack_f32x2(f[j], f[j + 1]), c2, r2);
-              f[j] = mul * ex2_approx(lo_f32x2(y));
-              f[j + 1] = mul * ex2_approx(hi_f32x2(y));
-            }
-          });
+          write_tail_grad<T, G>(sl, buf + n * shape.vectors, grow, threadIdx.x, kWork, b.out, c);
         } else {
           write_grad<T, G>(sl, grow, threadIdx.x, kWork, [](int, float* f) {
 #pragma unroll
@@ -332,9 +319,9 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
       const float m = key_value(__reduce_max_sync(0xffffffffu, max(order_key(v.x), max(order_key(z[0]), order_key(z[1])))));
       const float R = reference(m, c);
       float tail = v.y, unused = 0.f, in = 0.f;
-      rebase(v.x, c, R, tail, unused);
+      rebase(v.x, c, m, R, tail, unused);
 #pragma unroll
-      for (int h = 0; h < kHalves; ++h) in += vec[h] >= 0 ? ex2_approx(fmaf(z[h], c, -R)) : 0.f;
+      for (int h = 0; h < kHalves; ++h) in += vec[h] >= 0 ? ex2_approx(exponent(z[h], m, R, c)) : 0.f;
       tail = warp_sum(tail);
       in = warp_sum(in);
       if (n_ctas == 1) {
@@ -401,7 +388,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
             for (int h = 0; h < kHalves; ++h)
               if (vec[h] >= 0)
                 (static_cast<G*>(p.grad) + old.row * p.ld_grad)[old.id[h]] =
-                    Out<G>::one(ex2_approx(fmaf(z[h], c, -scale.R)) * scale.inv_s * scale.f_in - old.q[h] * scale.q_in);
+                    Out<G>::one(ex2_approx(exponent(z[h], sums.all, scale.R, c)) * scale.inv_s * scale.f_in - old.q[h] * scale.q_in);
           } else {
             ok = exchange();
           }
@@ -459,10 +446,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
       if constexpr (kGrad) {
         if (old.lives) {
           if (!exchange()) break;
-          if (lane == 0) {
-            b.ref = scale.ref;
-            b.mul = scale.mul;
-          }
+          if (lane == 0) b.out = Outside{scale.ref, scale.mul, sums.all, is_far(scale.R)};
           __syncwarp();
         }
         if (lane == 0) mbar_arrive(&b.scaled);

@@ -18,11 +18,6 @@ namespace {
 
 using namespace rows;
 
-struct InShared {
-  const uint4* buf;
-  __device__ uint4 operator()(int i) const { return buf[i]; }
-};
-
 template <typename T, int TOP, bool ENT, int kThreads>
 __global__ void __launch_bounds__(kThreads, 768 / kThreads) logprobs_kernel(const ScoreArgs p, uint32_t list_offset) {
   constexpr int kWarps = kThreads / 32, kStep = kThreads * kUnroll;
@@ -30,7 +25,7 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) logprobs_kernel(cons
   extern __shared__ __align__(128) uint4 buf[];
   __shared__ uint64_t bars[kMaxPieces];
   __shared__ int abort_flag;
-  __shared__ float4 warp_stat[kWarps];
+  __shared__ float4 parts[kWarps];
   __shared__ float4 slot[kMaxCluster];
   __shared__ float result[2];
   __shared__ int best;
@@ -60,6 +55,7 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) logprobs_kernel(cons
   cluster_arrive();
 
   const float c = p.scale * kLog2e;
+  const float lowest = lowest_value(c);
   Stat st;
   int at = 0;  // step in which the maximum was met first
   const uint4 none = no_elements<T>();
@@ -72,23 +68,18 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) logprobs_kernel(cons
       v[u] = k < sl.nv ? buf[k] : none;
     }
     const float before = st.m;
-    if (stat_add<T, kUnroll, ENT>(st, v, c) > before) at = i;
+    if (stat_add<T, kUnroll, ENT>(st, v, c, lowest) > before) at = i;
   }
 
   if (rank == 0) given.fetch_logit(p, row);
 
   // the CTA's statistics
-  float m = key_value(__reduce_max_sync(0xffffffffu, order_key(st.m)));
-  {
-    float s = st.s, t = st.t;
-    rebase(st.m, c, reference(m, c), s, t);
-    s = warp_sum(s);
-    if (ENT) t = warp_sum(t);
-    if (lane == 0) warp_stat[warp] = make_float4(m, s, t, 0.f);
-  }
+  const float3 w_stat = warp_stat<T, ENT>(st, c, threadIdx.x, kThreads, sl.nv, InShared{buf});
+  if (lane == 0) parts[warp] = make_float4(w_stat.x, w_stat.y, w_stat.z, 0.f);
   __syncthreads();
+  float m = w_stat.x;
 #pragma unroll
-  for (int w = 0; w < kWarps; ++w) m = fmaxf(m, warp_stat[w].x);
+  for (int w = 0; w < kWarps; ++w) m = fmaxf(m, parts[w].x);
   if (TOP == kTopOne) {
     if (m == -kInf) {
       if (threadIdx.x == 0 && sl.nv > 0) best = max(sl.first_element(0), 0);
@@ -144,9 +135,9 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) logprobs_kernel(cons
   if (warp == 0) {
     float s = 0.f, t = 0.f;
     if (lane < kWarps) {
-      s = warp_stat[lane].y;
-      t = warp_stat[lane].z;
-      rebase(warp_stat[lane].x, c, reference(m, c), s, t);
+      s = parts[lane].y;
+      t = parts[lane].z;
+      rebase(parts[lane].x, c, m, reference(m, c), s, t);
     }
     s = warp_sum(s);
     if (ENT) t = warp_sum(t);

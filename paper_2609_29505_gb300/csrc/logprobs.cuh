@@ -51,14 +51,14 @@ __device__ __forceinline__ void finish(const Tm& team, const ScoreArgs& p, int64
     const float all = key_value(__reduce_max_sync(0xffffffffu, order_key(v.x)));
     const float R = reference(all, c);
     float s = v.y, t = v.z;
-    rebase(v.x, c, R, s, t);
+    rebase(v.x, c, all, R, s, t);
     s = warp_sum(s);
     if (ENT) t = warp_sum(t);
     // of the CTAs that have the maximum the first has it at the lowest index
     const int index = __reduce_min_sync(0xffffffffu, team.tid < n_ctas && v.x == all ? __float_as_int(v.w) : 0x7FFFFFFF);
     if (team.tid == 0) {
       const bool empty = all == -kInf && s == 0.f;  // (NaN: s is NaN)
-      const float delta = all == -kInf ? 0.f : fmaf(all, c, -R);
+      const float delta = delta_of(all, c, R);
       const float ln_s = empty ? 0.f : logf(s) - delta * kLn2;
       result[0] = empty ? kInf : all;  // an empty row: every difference to it is -inf
       result[1] = ln_s;
@@ -73,7 +73,11 @@ __device__ __forceinline__ void finish(const Tm& team, const ScoreArgs& p, int64
   if (TOP != kTopMany && p.n_tokens == 0) return;
   team.sync();
   const float all = result[0], ln_s = result[1];
-  auto logprob = [&](float z) { return (z - all) * p.scale - ln_s; };
+  auto logprob = [&](float z) {
+    float d = (z - all) * p.scale;
+    if (d == -kInf && z > -kInf) d = z * p.scale - all * p.scale;  // (their difference may be out of range where this is not)
+    return d - ln_s;
+  };
   if (team.tid < p.n_tokens)
     p.token_logprobs[r * p.n_tokens + team.tid] = given.token < 0 ? 0.f : logprob(given.z);
   for (int i = team.tid + Tm::kSize; i < p.n_tokens; i += Tm::kSize) {

@@ -238,7 +238,7 @@ __device__ __forceinline__ void finish_rows(const ScoreArgs& p, Row& x, Many& ma
       const uint32_t to = map_to_rank(smem_u32(lists + rank * p.top_k), 0);
       rank_candidates(team, many.top, p.top_k, [&](int place, uint64_t y) { st_cluster(to + 8 * place, y); });
     }
-    rebase(v.x, c, reference(m, c), v.y, v.z);
+    rebase(v.x, c, m, reference(m, c), v.y, v.z);
     v.y = warp_sum(v.y);
     if (ENT) v.z = warp_sum(v.z);
     if (lane == 0) st_cluster(map_to_rank(smem_u32(&x.slot[rank]), 0), make_float4(m, v.y, v.z, __int_as_float(best)));
@@ -290,6 +290,7 @@ __global__ void __launch_bounds__(kAll, 1) logprobs_stream_kernel(const ScoreArg
   cluster_sync();
   const T* logits = static_cast<const T*>(p.logits);
   const float c = p.scale * kLog2e;
+  const float lowest = lowest_value(c);
 
   if (warp == kStreamWarps + kFinishWarps) {
     // ----- producer
@@ -394,7 +395,7 @@ __global__ void __launch_bounds__(kAll, 1) logprobs_stream_kernel(const ScoreArg
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh.empty[ring.slot]);
         ring.next();
-        const float before = st.m, m = stat_add<T, kDeep, ENT>(st, v, c);
+        const float before = st.m, m = stat_add<T, kDeep, ENT>(st, v, c, lowest);
         if (TOP == kTopOne && m > before) at = t;
         if (TOP == kTopMany) {
           part = fmaxf(part, m);
@@ -409,12 +410,8 @@ __global__ void __launch_bounds__(kAll, 1) logprobs_stream_kernel(const ScoreArg
       if (!ok) break;
       if (TOP != kTopNone) x.max_key[threadIdx.x] = order_key(st.m);
       if (TOP == kTopOne) x.max_tile[threadIdx.x] = static_cast<uint16_t>(at);
-      const float m = key_value(__reduce_max_sync(0xffffffffu, order_key(st.m)));
-      float s = st.s, u = st.t;
-      rebase(st.m, c, reference(m, c), s, u);
-      s = warp_sum(s);
-      if (ENT) u = warp_sum(u);
-      if (lane == 0) x.part[warp] = make_float4(m, s, u, 0.f);
+      const float3 w_stat = warp_stat<T, ENT>(st, c, threadIdx.x, kStreamThreads, sl.nv, FromRow<T>{sl});
+      if (lane == 0) x.part[warp] = make_float4(w_stat.x, w_stat.y, w_stat.z, 0.f);
       if (threadIdx.x == 0) x.row = r;
       __syncwarp();
       if (lane == 0) mbar_arrive(&x.part_full);

@@ -75,29 +75,29 @@ __device__ __forceinline__ float vec_max(const uint4* v, const f16*) { return ve
 template <int N>
 __device__ __forceinline__ float vec_max(const uint4* v, const bf16*) { return vec_max_packed<N, __nv_bfloat162>(v); }
 
-// Whether one of n vectors' values is -inf.
+// Smallest value of n vectors; a NaN is passed over.
 template <int N>
-__device__ __forceinline__ bool holds_neg_inf(const uint4* v, const float*) {
+__device__ __forceinline__ float vec_min(const uint4* v, const float*) {
   float m = __uint_as_float(v[0].x);
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     m = min3(m, __uint_as_float(v[i].x), __uint_as_float(v[i].y));
     m = min3(m, __uint_as_float(v[i].z), __uint_as_float(v[i].w));
   }
-  return m == -kInf;
+  return m;
 }
 template <int N, typename P>
-__device__ __forceinline__ bool holds_neg_inf_packed(const uint4* v) {
+__device__ __forceinline__ float vec_min_packed(const uint4* v) {
   const P* p = reinterpret_cast<const P*>(v);
   P m = p[0];
 #pragma unroll
   for (int i = 1; i < 4 * N; ++i) m = __hmin2(m, p[i]);
-  return fminf(to_f(m.x), to_f(m.y)) == -kInf;
+  return fminf(to_f(m.x), to_f(m.y));
 }
 template <int N>
-__device__ __forceinline__ bool holds_neg_inf(const uint4* v, const f16*) { return holds_neg_inf_packed<N, __half2>(v); }
+__device__ __forceinline__ float vec_min(const uint4* v, const f16*) { return vec_min_packed<N, __half2>(v); }
 template <int N>
-__device__ __forceinline__ bool holds_neg_inf(const uint4* v, const bf16*) { return holds_neg_inf_packed<N, __nv_bfloat162>(v); }
+__device__ __forceinline__ float vec_min(const uint4* v, const bf16*) { return vec_min_packed<N, __nv_bfloat162>(v); }
 
 // Order of fp32 values as unsigned integers: -0 and +0 are equal, NaN stands with -inf.
 __device__ __forceinline__ uint32_t order_key(float x) {
@@ -190,10 +190,37 @@ __device__ __forceinline__ void wait_piece(uint64_t* bars, int p, volatile int* 
   if (!mbar_wait_warp(smem_u32(&bars[p]), 0, abort_flag, status, code)) mbar_drain(&bars[p], 0);
 }
 
-// Running softmax statistics of one thread, in base 2: with c = scale log2(e) and a reference
-// R = fl(m c), s = sum 2^(x c - R) and, where ENT, t = sum (x c - R) 2^(x c - R).  One rounding per
-// exponent (an fma); that of R itself is taken back at the end, through
-// delta = m c - R = fma(m, c, -R), so that ln sum e^(scale (x - m)) = ln s - delta ln 2.
+// Exponents are taken in base 2 against a reference, with c = scale log2(e) and the largest value m:
+//   x c - R, R = fl(m c): one rounding (an fma).  R's own rounding is taken back at the end, through
+//   delta = m c - R = fma(m, c, -R), so that ln sum e^(scale (x - m)) = ln s - delta ln 2.
+//   (x - m) c where |m c| is above kFar, as R's rounding would then be an exponent of its own (half a unit of R
+//   passes 128 at 2^32, and R overflows for a mask of the type's lowest value).  The reference is m c
+//   itself, delta = 0.
+constexpr float kFar = 1048576.f;  // 2^20: delta is below 2^-4
+// Exponents below this are cut: 2^x is 0 there, and a sum's factor stays finite.
+constexpr float kCut = -1000.f;
+
+__device__ __forceinline__ float reference(float m, float c) { return m == -kInf ? 0.f : __fmul_rn(m, c); }
+__device__ __forceinline__ bool is_far(float R) { return fabsf(R) > kFar; }
+__device__ __forceinline__ float delta_of(float m, float c, float R) {
+  return m == -kInf || is_far(R) ? 0.f : fmaf(m, c, -R);
+}
+
+// Exponent of x against the reference (m, R).
+__device__ __forceinline__ float exponent(float x, float m, float R, float c) {
+  return is_far(R) ? __fmul_rn(x - m, c) : fmaf(x, c, -R);
+}
+// From the reference (m1, R1) to that of M >= m1: what is added to exponents.
+__device__ __forceinline__ float shift(float m1, float R1, float M, float R, float c) {
+  float d = R1 - R;
+  if (is_far(R1) || is_far(R)) d = fmaf(m1 - M, c, delta_of(M, c, R) - delta_of(m1, c, R1));
+  return fmaxf(d, kCut);  // (a NaN, of infinities, too)
+}
+
+// Running softmax statistics of one thread: s = sum 2^y and, where ENT, t = sum y 2^y over y = x c - R.  R is at least
+// -kFar here: where the thread's values lie below, their terms are as small as they come out beside what other
+// threads of the warp have, or the warp's maximum is far itself.  Then, and where a value is far above, warp_stat()
+// takes the sums anew.
 struct Stat {
   float m = -kInf, R = 0.f, s = 0.f, t = 0.f;
 };
@@ -211,7 +238,7 @@ __device__ __forceinline__ void add_terms(Stat& st, const uint4* v, float c) {
       uint64_t y = fma_f32x2(pack_f32x2(f[j], f[j + 1]), c2, r2);
       const uint64_t e = pack_f32x2(ex2_approx(lo_f32x2(y)), ex2_approx(hi_f32x2(y)));
       s2 = add_f32x2(s2, e);
-      if (CUT) y = pack_f32x2(fmaxf(lo_f32x2(y), -1000.f), fmaxf(hi_f32x2(y), -1000.f));
+      if (CUT) y = pack_f32x2(fmaxf(lo_f32x2(y), kCut), fmaxf(hi_f32x2(y), kCut));
       if (ENT) t2 = fma_f32x2(y, e, t2);
     }
   }
@@ -219,13 +246,16 @@ __device__ __forceinline__ void add_terms(Stat& st, const uint4* v, float c) {
   if (ENT) st.t = sum_f32x2(t2);
 }
 
+// Values up to this one have an exponent that may overflow: x c is above -2^127 where x is above it.
+__device__ __forceinline__ float lowest_value(float c) { return fmaxf(-1.5e38f / c, -3.4028234e38f); }
+
 // Takes N vectors in, whose largest value is returned.  The maximum moves at most once per call: no
 // rescaling per element.
 template <typename T, int N, bool ENT>
-__device__ __forceinline__ float stat_add(Stat& st, const uint4* v, float c) {
+__device__ __forceinline__ float stat_add(Stat& st, const uint4* v, float c, float lowest) {
   const float m = vec_max<N>(v, static_cast<const T*>(nullptr));
   if (m > st.m) {
-    const float R = __fmul_rn(m, c);
+    const float R = fmaxf(__fmul_rn(m, c), -kFar);
     if (st.m != -kInf) {
       const float d = st.R - R, f = ex2_approx(d);
       if (ENT) st.t = f * (st.t + d * st.s);
@@ -234,13 +264,12 @@ __device__ __forceinline__ float stat_add(Stat& st, const uint4* v, float c) {
     st.m = m;
     st.R = R;
   }
-  // -inf has the term 0 in t, not -inf times 0: its exponent is cut, where there is one
-  if (ENT && holds_neg_inf<N>(v, static_cast<const T*>(nullptr))) add_terms<T, N, true, true>(st, v, c);
+  // a masked token (-inf, or a value whose exponent overflows) has the term 0 in t, not -inf times 0: its exponent
+  // is cut, where there is one
+  if (ENT && vec_min<N>(v, static_cast<const T*>(nullptr)) <= lowest) add_terms<T, N, true, true>(st, v, c);
   else add_terms<T, N, ENT, false>(st, v, c);
   return m;
 }
-
-__device__ __forceinline__ float reference(float m, float c) { return m == -kInf ? 0.f : __fmul_rn(m, c); }
 
 // A vector without an element: of a slice's end.
 template <typename T>
@@ -252,13 +281,6 @@ __device__ __forceinline__ uint4 no_elements() {
   return v;
 }
 
-// s and t of a part with maximum m (reference fl(m c)) at the reference R of a maximum >= m.
-__device__ __forceinline__ void rebase(float m, float c, float R, float& s, float& t) {
-  const float d = __fmul_rn(m, c) - R, f = m == -kInf ? 0.f : ex2_approx(d);
-  t = m == -kInf ? 0.f : f * (t + d * s);
-  s *= f;
-}
-
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -268,6 +290,54 @@ __device__ __forceinline__ double warp_sum(double v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
+}
+
+// s and t of a part with maximum m at the reference (M, R) of a maximum M >= m.
+__device__ __forceinline__ void rebase(float m, float c, float M, float R, float& s, float& t) {
+  const float d = shift(m, reference(m, c), M, R, c), f = m == -kInf ? 0.f : ex2_approx(d);
+  t = m == -kInf ? 0.f : f * (t + d * s);
+  s *= f;
+}
+
+// Vector i of a slice in shared memory.
+struct InShared {
+  const uint4* buf;
+  __device__ uint4 operator()(int i) const { return buf[i]; }
+};
+
+// A warp's statistics {maximum, s, t} from its threads'.  Where its maximum is far the sums are taken anew over the
+// threads' vectors, which fetch(i) gives for i = tid, tid + threads, ... below nv.
+template <typename T, bool ENT, typename F>
+__device__ __noinline__ float2 far_sums(float m, float c, int tid, int threads, int nv, F fetch) {
+  float s = 0.f, t = 0.f;
+#pragma unroll 1
+  for (int i = tid; i < nv; i += threads) {
+    float x[Elem<T>::kPer];
+    unpack(fetch(i), x, static_cast<const T*>(nullptr));
+#pragma unroll
+    for (int j = 0; j < Elem<T>::kPer; ++j) {
+      const float y = __fmul_rn(x[j] - m, c), e = ex2_approx(y);
+      s += e;
+      if (ENT) t = fmaf(fmaxf(y, kCut), e, t);
+    }
+  }
+  return make_float2(s, t);
+}
+template <typename T, bool ENT, typename F>
+__device__ __forceinline__ float3 warp_stat(const Stat& st, float c, int tid, int threads, int nv, const F& fetch) {
+  const float m = key_value(__reduce_max_sync(0xffffffffu, order_key(st.m)));
+  const float R = reference(m, c);
+  float s = 0.f, t = 0.f;
+  if (!is_far(R)) {
+    const float d = st.R - R, f = st.m == -kInf ? 0.f : ex2_approx(d);
+    t = st.m == -kInf ? 0.f : f * (st.t + d * st.s);
+    s = st.s * f;
+  } else {
+    const float2 a = far_sums<T, ENT>(m, c, tid, threads, nv, fetch);
+    s = a.x;
+    t = a.y;
+  }
+  return make_float3(m, warp_sum(s), ENT ? warp_sum(t) : 0.f);
 }
 
 __device__ __forceinline__ void st_cluster(uint32_t addr, float4 v) {
