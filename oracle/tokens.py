@@ -57,7 +57,7 @@ def distill_row(logits, ids, logq, scale=1.0, bucket=True, weight=1.0):
     def term(a, la, lb):  # a (ln a - ln b), 0 where a = 0
         return 0.0 if a == 0 else a * (la - lb)
 
-    with np.errstate(invalid="ignore"):
+    with np.errstate(invalid="ignore", over="ignore"):
         if not bucket:
             lq, q = lq - np.log(Q), q / Q
             loss = sum(term(a, la, lp[i]) for a, la, i in zip(q, lq, S))
@@ -67,11 +67,16 @@ def distill_row(logits, ids, logq, scale=1.0, bucket=True, weight=1.0):
             qt = max(0.0, 1.0 - Q)
             out = np.ones(vocab, bool)
             out[S] = False
-            pt = p[out].sum()
             loss = sum(term(a, la, lp[i]) for a, la, i in zip(q, lq, S))
-            if qt > 0 and pt > 0:
-                loss += qt * (np.log(qt) - np.log(pt))
-            grad = p * (1.0 - (qt / pt if pt > 0 else 0.0))
+            grad = p.copy()
+            # the tail by itself: p_T may be below what float64 holds
+            x = z * scale
+            most = x[out].max(initial=-np.inf)
+            if qt > 0 and most != -np.inf:
+                e = np.where(out, np.exp(x - most), 0.0)
+                lpt = (most - x.max()) + np.log(e.sum()) - np.log(np.exp(x - x.max()).sum())
+                loss += qt * (np.log(qt) - lpt)
+                grad -= qt * e / e.sum()
             grad[S] = p[S] - q
     return weight * loss, weight * scale * grad
 

@@ -132,25 +132,22 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) distill_kernel(const
   }
   // the CTA's sums, of the tail and of its part of S
   const float3 tail = warp_stat<T, false>(st, c, threadIdx.x, kThreads, sl.nv, InShared{buf});
-  float m = key_value(__reduce_max_sync(0xffffffffu, max(order_key(tail.x), order_key(z))));
   {
-    const float R = reference(m, c);
-    float s = tail.y, unused = 0.f;
-    rebase(tail.x, c, m, R, s, unused);
-    const float in = warp_sum(vec >= 0 ? ex2_approx(exponent(z, m, R, c)) : 0.f);
-    if (lane == 0) parts[warp] = make_float4(m, s, in, 0.f);
+    const float m = key_value(__reduce_max_sync(0xffffffffu, order_key(z)));
+    const float in = warp_sum(vec >= 0 ? ex2_approx(exponent(z, m, reference(m, c), c)) : 0.f);
+    if (lane == 0) parts[warp] = make_float4(tail.x, tail.y, m, in);
   }
   __syncthreads();
   if (warp == 0) {
-    float4 v = lane < kWarps ? parts[lane] : make_float4(-kInf, 0.f, 0.f, 0.f);
-    m = key_value(__reduce_max_sync(0xffffffffu, order_key(v.x)));
-    const float R = reference(m, c);
+    float4 v = lane < kWarps ? parts[lane] : make_float4(-kInf, 0.f, -kInf, 0.f);
+    const float m = key_value(__reduce_max_sync(0xffffffffu, order_key(v.x)));
+    const float m_list = key_value(__reduce_max_sync(0xffffffffu, order_key(v.z)));
     float unused = 0.f;
-    rebase(v.x, c, m, R, v.y, unused);
-    rebase(v.x, c, m, R, v.z, unused);
+    rebase(v.x, c, m, reference(m, c), v.y, unused);
+    rebase(v.z, c, m_list, reference(m_list, c), v.w, unused);
     v.y = warp_sum(v.y);
-    v.z = warp_sum(v.z);
-    if (lane < n_ctas) st_cluster(map_to_rank(smem_u32(&slot[rank]), lane), make_float4(m, v.y, v.z, 0.f));
+    v.w = warp_sum(v.w);
+    if (lane < n_ctas) st_cluster(map_to_rank(smem_u32(&slot[rank]), lane), make_float4(m, v.y, m_list, v.w));
   }
   __syncwarp();
   cluster_sync();
@@ -160,7 +157,7 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) distill_kernel(const
   const RowScale o = row_scale(sums, ls, w, p.scale, p.bucket, c);
   if constexpr (kGrad) {
     G* grow = static_cast<G*>(p.grad) + r * p.ld_grad;
-    write_tail_grad<T, G>(sl, buf, grow, threadIdx.x, kThreads, Outside{o.ref, o.mul, sums.all, is_far(o.R)}, c);
+    write_tail_grad<T, G>(sl, buf, grow, threadIdx.x, kThreads, outside(o, sums, c), c);
     __syncthreads();
     if (vec >= 0) grow[id] = Out<G>::one(ex2_approx(exponent(z, sums.all, o.R, c)) * o.inv_s * o.f_in - q * o.q_in);
   }

@@ -141,25 +141,30 @@ __device__ __forceinline__ void write_tail_grad(const Slice<T>& sl, const uint4*
   });
 }
 
-// A row's sums: maximum, and sum of its terms over the tail and over the list.
+// A row's sums: its maximum, the tail's with the sum of the tail's terms against that (in units of the row's maximum a tail
+// that is far below would be 0), and the sum of the list's terms against the row's maximum.
 struct RowSums {
-  float all, tail, in;
+  float all, tail_max, tail, in;
 };
+// `in` against the list's own maximum.
+__device__ __forceinline__ RowSums join_sums(float tail_max, float tail, float list_max, float in, float c) {
+  const float all = fmaxf(tail_max, list_max);
+  float unused = 0.f;
+  rebase(list_max, c, all, reference(all, c), in, unused);
+  return RowSums{all, tail_max, tail, in};
+}
 
-// From the CTAs' parts {maximum, tail, list} (a whole warp; every lane gets them).
+// From the CTAs' parts {the tail's maximum and sum, the list's} (a whole warp; every lane gets them).
 __device__ __forceinline__ RowSums row_sums(const float4* slot, int n_ctas, float c) {
   const int lane = lane_id();
-  float4 v = make_float4(-kInf, 0.f, 0.f, 0.f);
+  float4 v = make_float4(-kInf, 0.f, -kInf, 0.f);
   if (lane < n_ctas) v = slot[lane];
-  RowSums r;
-  r.all = key_value(__reduce_max_sync(0xffffffffu, order_key(v.x)));
-  const float R = reference(r.all, c);
+  const float tail_max = key_value(__reduce_max_sync(0xffffffffu, order_key(v.x)));
+  const float list_max = key_value(__reduce_max_sync(0xffffffffu, order_key(v.z)));
   float unused = 0.f;
-  rebase(v.x, c, r.all, R, v.y, unused);
-  rebase(v.x, c, r.all, R, v.z, unused);
-  r.tail = warp_sum(v.y);
-  r.in = warp_sum(v.z);
-  return r;
+  rebase(v.x, c, tail_max, reference(tail_max, c), v.y, unused);
+  rebase(v.z, c, list_max, reference(list_max, c), v.w, unused);
+  return join_sums(tail_max, warp_sum(v.y), list_max, warp_sum(v.w), c);
 }
 
 // Sums of two floats, hi + lo, for a row's scalars.  (fp64 instructions take some 15 cycles a warp here: a
@@ -208,31 +213,40 @@ __device__ __forceinline__ ListSums list_sums(double Q, bool bucket) {
 struct RowScale {
   float R, inv_s, f_in, q_in;
   float ref, mul;  // of the gradient outside
-  float s;
-  bool empty, has_tail;
+  float tail, s;   // the tail's sum, and that of all, against the row's maximum
+  bool empty;
+  bool pulls;      // the list leaves the tail a probability, and there is one
 };
 
 __device__ __forceinline__ RowScale row_scale(const RowSums& r, const ListSums& l, float w, float scale, bool bucket, float c) {
   RowScale o;
   o.R = reference(r.all, c);
-  o.s = r.tail + r.in;
+  const float R_tail = reference(r.tail_max, c);
+  const float to_all = r.tail_max == -kInf ? 0.f : ex2_approx(shift(r.tail_max, R_tail, r.all, o.R, c));
+  o.tail = r.tail * to_all;
+  o.s = o.tail + r.in;
   o.empty = r.all == -kInf && o.s == 0.f;  // every logit -inf: p = 0
   o.inv_s = o.empty ? 0.f : 1.f / o.s;
-  o.has_tail = bucket && r.tail > 0.f;
+  o.pulls = bucket && r.tail > 0.f && l.q_tail > 0.f;
   o.f_in = w * scale;
   o.q_in = bucket ? o.f_in : o.f_in / l.Q;
-  // w scale p_j (1 - q_T / p_T) = F 2^y, F = w scale (1 / s - q_T / tail).  F's exponent k goes into
-  // the reference, so that a small tail's large factor overflows nowhere; what rounding the
-  // reference takes goes into the factor.
-  const float g = o.inv_s - (o.has_tail ? l.q_tail / r.tail : 0.f);  // (finite: tail >= 2^-126)
+  // w scale p_j (1 - q_T / p_T) = F 2^y, F = w scale (2^d / s - q_T / tail) with y and tail against the tail's maximum, d from
+  // there to the row's.  F's exponent k goes into the reference; what rounding the reference takes goes into the
+  // factor.
+  const float g = o.pulls ? o.inv_s * to_all - l.q_tail / r.tail : o.inv_s;
   int k = 0, k2 = 0;
   float f = o.f_in * g;
   if (isfinite(o.f_in) && isfinite(g)) f = frexpf(g, &k) * frexpf(o.f_in, &k2);
-  const bool far = is_far(o.R);
-  const Float2 ref = two_sum(far ? 0.f : o.R, -static_cast<float>(k + k2));
+  const float R = o.pulls ? R_tail : o.R;
+  const Float2 ref = two_sum(is_far(R) ? 0.f : R, -static_cast<float>(k + k2));
   o.ref = ref.hi;
   o.mul = f * ex2_approx(-ref.lo);
   return o;
+}
+
+__device__ __forceinline__ Outside outside(const RowScale& o, const RowSums& r, float c) {
+  const float m = o.pulls ? r.tail_max : r.all;
+  return Outside{o.ref, o.mul, m, is_far(reference(m, c))};
 }
 
 // The loss (a whole warp; every lane gets it), from entries lane, lane + 32, ... of the list.  Where the two
@@ -240,7 +254,7 @@ __device__ __forceinline__ RowScale row_scale(const RowSums& r, const ListSums& 
 //   - the list's sum is taken anew, with expf of exponents that are not rounded, and added up in fp64 (an error of
 //     1e-7 in it moved losses by 2e-6; one of the tail's sum cancels);
 //   - ln q - ln p is a sum of pairs of floats, and the terms are added up in fp64;
-//   - ln q_T - ln p_T is ln(1 + (in - Q s) / tail).
+//   - ln q_T - ln p_T is ln(1 + (in - Q s) / tail), unless the tail is far below.
 template <int N>
 __device__ __forceinline__ float row_loss(const RowScale& o, const RowSums& r, const ListSums& l, float w, bool bucket, float scale,
                                           float c, const float (&q)[N], const float (&lq)[N], const float (&z)[N]) {
@@ -263,7 +277,7 @@ __device__ __forceinline__ float row_loss(const RowScale& o, const RowSums& r, c
   bool all_weighted = true;
 #pragma unroll
   for (int h = 0; h < N; ++h) all_weighted &= !(q[h] == 0.f && z[h] > -kInf);
-  const float tail = r.tail * ex2_approx(-delta);
+  const float tail = o.tail * ex2_approx(-delta);
   const float in0 = r.in * ex2_approx(-delta);
   const bool anew = __all_sync(0xffffffffu, all_weighted) && r.all > -kInf;
   const float in = anew ? static_cast<float>(sum) : in0, in_lo = anew ? static_cast<float>(sum - in) : 0.f;
@@ -285,7 +299,12 @@ __device__ __forceinline__ float row_loss(const RowScale& o, const RowSums& r, c
     return w * (L.hi + L.lo);
   }
   float of_tail = 0.f;
-  if (o.has_tail && l.q_tail > 0.f) {
+  if (o.pulls && tail < 1e-18f * s.hi) {
+    const float delta_tail = delta_of(r.tail_max, c, reference(r.tail_max, c));
+    float below = (r.tail_max - r.all) * scale;
+    if (below == -kInf) below = r.tail_max * scale - r.all * scale;
+    of_tail = l.q_tail * (logf(l.q_tail) - (logf(r.tail) - delta_tail * kLn2) + (ln_s.hi + ln_s.lo) - below);
+  } else if (o.pulls) {
     const Float2 qs = two_prod(l.Q, s.hi);
     const float off = (((in - qs.hi) - qs.lo) + in_lo - l.Q_lo * s.hi - l.Q * s.lo) / tail;
     of_tail = l.q_tail * (off > -0.5f ? log1pf(off) : logf(l.q_tail) - logf(tail / s.hi));

@@ -53,6 +53,8 @@ struct Buffer {
   int row;             // -1: no more
   int live;            // 0: loss and gradient are 0
   Outside out;         // of the gradient
+  RowSums sums;        // of the row, and its scalars (here and not in registers: a spilled one is read back behind the copies)
+  RowScale scale;
   float2 part[kWorkWarps];
   float4 slot[2][kMaxStreamCluster];
   float list_z[2][kMaxList];  // the list's logits, in the CTA that puts down the loss
@@ -306,8 +308,6 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
 
     List x = fetch_list(), old;  // of the row to come, and of the one in the buffer
     old.row = -1;
-    RowSums sums;
-    RowScale scale;
     float z[kHalves] = {-kInf, -kInf};
     int vec[kHalves] = {-1, -1};
     int place = 0;  // of what the others send
@@ -316,26 +316,33 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
     // the old row's sums across the cluster, and its scalars; false: a wait has expired
     auto exchange = [&]() {
       const float2 v = lane < kWorkWarps ? b.part[lane] : make_float2(-kInf, 0.f);
-      const float m = key_value(__reduce_max_sync(0xffffffffu, max(order_key(v.x), max(order_key(z[0]), order_key(z[1])))));
-      const float R = reference(m, c);
+      const float m = key_value(__reduce_max_sync(0xffffffffu, order_key(v.x)));
+      const float m_list = key_value(__reduce_max_sync(0xffffffffu, max(order_key(z[0]), order_key(z[1]))));
+      const float R_list = reference(m_list, c);
       float tail = v.y, unused = 0.f, in = 0.f;
-      rebase(v.x, c, m, R, tail, unused);
+      rebase(v.x, c, m, reference(m, c), tail, unused);
 #pragma unroll
-      for (int h = 0; h < kHalves; ++h) in += vec[h] >= 0 ? ex2_approx(exponent(z[h], m, R, c)) : 0.f;
+      for (int h = 0; h < kHalves; ++h) in += vec[h] >= 0 ? ex2_approx(exponent(z[h], m_list, R_list, c)) : 0.f;
       tail = warp_sum(tail);
       in = warp_sum(in);
+      RowSums sums;
       if (n_ctas == 1) {
-        sums = RowSums{m, tail, in};
-        scale = row_scale(sums, old.sums, old.w, p.scale, p.bucket, c);
-        return true;
+        sums = join_sums(m, tail, m_list, in, c);
+      } else {
+        if (lane < n_ctas) st_cluster(map_to_rank(smem_u32(&b.slot[place][rank]), lane), make_float4(m, tail, m_list, in));
+        __syncwarp();
+        if (lane < n_ctas) mbar_arrive_cluster(map_to_rank(smem_u32(&b.sums_full[place]), lane));
+        __syncwarp();
+        if (!wait_cluster(&b.sums_full[place], sums_phase, abort_flag, p.status, 74)) return false;
+        sums = row_sums(b.slot[place], n_ctas, c);
       }
-      if (lane < n_ctas) st_cluster(map_to_rank(smem_u32(&b.slot[place][rank]), lane), make_float4(m, tail, in, 0.f));
+      const RowScale scale = row_scale(sums, old.sums, old.w, p.scale, p.bucket, c);
+      if (lane == 0) {
+        b.sums = sums;
+        b.scale = scale;
+        if (kGrad) b.out = outside(scale, sums, c);
+      }
       __syncwarp();
-      if (lane < n_ctas) mbar_arrive_cluster(map_to_rank(smem_u32(&b.sums_full[place]), lane));
-      __syncwarp();
-      if (!wait_cluster(&b.sums_full[place], sums_phase, abort_flag, p.status, 74)) return false;
-      sums = row_sums(b.slot[place], n_ctas, c);
-      scale = row_scale(sums, old.sums, old.w, p.scale, p.bucket, c);
       return true;
     };
     // the old row to the warp that does the losses, once that is done with this buffer's last one
@@ -356,8 +363,8 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
         l.lives = old.lives;
         l.w = old.w;
         l.list = old.sums;
-        l.sums = sums;
-        l.scale = scale;
+        l.sums = b.sums;
+        l.scale = b.scale;
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&b.loss_full);
@@ -384,11 +391,12 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
       } else {  // what is left of the old row
         if (old.lives) {
           if constexpr (kGrad) {
+            const RowScale& scale = b.scale;
 #pragma unroll
             for (int h = 0; h < kHalves; ++h)
               if (vec[h] >= 0)
                 (static_cast<G*>(p.grad) + old.row * p.ld_grad)[old.id[h]] =
-                    Out<G>::one(ex2_approx(exponent(z[h], sums.all, scale.R, c)) * scale.inv_s * scale.f_in - old.q[h] * scale.q_in);
+                    Out<G>::one(ex2_approx(exponent(z[h], b.sums.all, scale.R, c)) * scale.inv_s * scale.f_in - old.q[h] * scale.q_in);
           } else {
             ok = exchange();
           }
@@ -444,11 +452,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
       if (!kGrad) sort_out(x);
       if (!mbar_wait_warp(smem_u32(&b.part_full), phase, abort_flag, p.status, 73)) break;
       if constexpr (kGrad) {
-        if (old.lives) {
-          if (!exchange()) break;
-          if (lane == 0) b.out = Outside{scale.ref, scale.mul, sums.all, is_far(scale.R)};
-          __syncwarp();
-        }
+        if (old.lives && !exchange()) break;
         if (lane == 0) mbar_arrive(&b.scaled);
         sort_out(x);
         if (!mbar_wait_warp(smem_u32(&b.done), phase, abort_flag, p.status, 75)) break;

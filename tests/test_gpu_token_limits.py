@@ -86,3 +86,59 @@ def test_what_is_no_number_shows_wherever_it_stands(B, rows, vocab, dtype, bucke
         B.sgd_kernel_distill(z, ids, logq, loss, grad=g, tail=B.TAIL_BUCKET if bucket else B.TAIL_RENORM)
         assert torch.isnan(loss[:5]).all() and torch.isfinite(loss[5:]).all()
         assert g is None or torch.isnan(g[:5]).all() and torch.isfinite(g[5:]).all()
+
+
+def _check_tails(loss, grad, z, ids, logq, rows):
+    """Rows of lists with distinct tokens and a bucket, as derived in test_gpu_tokens.py, with the tail's share of its
+    tokens in the place of p / p_T.  ln p_T is off by SUM and, as a sum of its parts, by 4 U of their size."""
+    loss, ids, logq = loss.double().cpu().numpy(), ids.cpu().numpy(), logq.double().cpu().numpy()
+    for r in rows:
+        x = z[r].double().cpu().numpy()
+        L, g = ot.distill_row(x, ids[r], logq[r])
+        lp = ot.log_softmax(x[None])[0]
+        p, q = np.exp(lp), np.exp(logq[r])
+        out = np.ones(len(p), bool)
+        out[ids[r]] = False
+        of_tail = np.exp(np.where(out, x - x[out].max(), -np.inf))
+        lpt = x[out].max() - x.max() + np.log(of_tail.sum()) - np.log(np.exp(x - x.max()).sum())
+        Q = q.sum()
+        qt = max(0.0, 1 - Q)
+        assert qt > 0
+        tol = SUM * (Q + 2 * qt) + 4 * U * ((q * np.abs(logq[r] - lp[ids[r]])).sum() + qt * abs(np.log(qt) - lpt))
+        tol += 4 * U * Q * abs(np.log(qt) - lpt + 1)
+        assert abs(loss[r] - L) <= tol + U * abs(L), (r, loss[r], L)
+        if grad is not None:
+            half, least = torch.finfo(grad.dtype).eps / 2, torch.finfo(grad.dtype).smallest_normal * torch.finfo(grad.dtype).eps / 2
+            ep = np.where(p > 0, SUM + (4 + 3 * np.abs(lp)) * U, 0.0)
+            share = of_tail / of_tail.sum()  # off by the exponent's distance from the tail's maximum
+            es = 2 * SUM + (4 + 3 * np.abs(np.log(np.where(share > 0, share, 1.0)))) * U
+            qs = np.zeros(len(p))
+            qs[ids[r]] = q
+            tol = p * ep + np.where(out, share * (qt * es + 2 * U * Q), qs * 4 * U) + 2.0 ** -126  # (ex2 is 0 below)
+            err = np.abs(grad[r].double().cpu().numpy() - g)
+            assert (err <= tol + half * (np.abs(g) + tol) + least).all(), (r, (err / tol).max())
+
+
+@pytest.mark.parametrize("gap", [30.0, 80.0, 90.0, 120.0, 1000.0, 60000.0, 1e10, 3e38])
+@pytest.mark.parametrize("rows,vocab,dtype,grad", [(6, 70, "f32", "f32"), (6, 4001, "f32", "f32"), (6, 4001, "f16", "bf16"), (3, 126464, "bf16", "f32"),
+                                                   (420, 126464, "f16", "f32"), (210, 126464, "f32", "bf16"), (420, 126464, "bf16", "")])
+def test_a_tail_far_below_the_list(B, rows, vocab, dtype, grad, gap):
+    """A student that is certain of the listed tokens alone, while the teacher leaves the others a tenth, a half or a
+    thousandth."""
+    if gap > torch.finfo(DT[dtype]).max / 2:
+        pytest.skip("out of the type's range")
+    k = 4
+    z = _normal(rows, vocab, dtype, 5)
+    rng = np.random.default_rng(6)
+    ids = torch.from_numpy(np.stack([rng.permutation(vocab)[:k] for _ in range(rows)]).astype(np.int32)).cuda()
+    top = gap + 2.0 * torch.from_numpy(rng.random((rows, k))).cuda()
+    z.scatter_(1, ids.long(), top.to(z))
+    part = torch.tensor([0.9, 0.5, 0.999], device="cuda").repeat((rows + 2) // 3)[:rows, None]
+    logq = torch.log(part * torch.softmax(torch.from_numpy(rng.standard_normal((rows, k))).float().cuda(), 1))
+    loss = torch.empty(rows, device="cuda")
+    g = torch.empty(rows, vocab, dtype=DT[grad], device="cuda") if grad else None
+    B.sgd_kernel_distill(z, ids, logq, loss, grad=g)
+    assert B.sgd_kernel_status() == 0
+    _check_tails(loss, g, z, ids, logq, sorted({0, 1, 2, *range(3, rows, max(1, rows // 9))}))
+    if g is not None:  # (off by what each of the tail's tokens and of the list's is)
+        assert (g.double().sum(1).abs() <= 1e-2 if grad == "bf16" else g.double().sum(1).abs() <= 1e-4).all()
