@@ -249,7 +249,9 @@ typedef enum {
  * p = softmax(scale * logits[r, :]), the list's tokens S and q_i = exp(teacher_logprobs_i), Q = sum q_i:
  *   SGD_TAIL_RENORM: L = sum_S (q_i / Q) (ln (q_i / Q) - ln p_i);
  *   SGD_TAIL_BUCKET: L = sum_S q_i (ln q_i - ln p_i) + q_T (ln q_T - ln p_T), q_T = max(0, 1 - Q),
- *                    p_T = sum of p outside S; the second term is left out where q_T or p_T is 0;
+ *                    p_T = sum of p outside S; the second term is left out where q_T or p_T is 0.  Lists are meant
+ *                    to have Q <= 1; where it is more, grad is that of Q = 1 (scale w_r (p - q) in S, scale w_r p
+ *                    outside) and not L's derivative;
  *   loss fp32 [rows] = w_r L;  grad [rows, vocab] = w_r dL / dlogits (NULL: the loss alone).
  * top_k = 1 with teacher_logprobs 0 and SGD_TAIL_RENORM is the cross entropy of the listed token.
  * logits [rows, vocab] of type dtype, rows ld elements apart; teacher_ids int32 and teacher_logprobs

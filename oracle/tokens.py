@@ -77,7 +77,9 @@ def distill_row(logits, ids, logq, scale=1.0, bucket=True, weight=1.0):
                 lpt = (most - x.max()) + np.log(e.sum()) - np.log(np.exp(x - x.max()).sum())
                 loss += qt * (np.log(qt) - lpt)
                 grad -= qt * e / e.sum()
-            grad[S] = p[S] - q
+            # (Q + the q_T that counts: 1, but for a tail that is masked altogether.  Above 1 the list is no distribution; the
+            # gradient is defined as that of Q = 1)
+            grad[S] = (Q if qt > 0 and most == -np.inf else 1.0) * p[S] - q
     return weight * loss, weight * scale * grad
 
 

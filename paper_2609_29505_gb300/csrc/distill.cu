@@ -5,7 +5,9 @@
 //           dL/dz_j = scale (p_j - q^_j);
 //   bucket: q_T = 1 - Q, p_T = sum_{j not in S} p_j,
 //           L = sum q_i (ln q_i - ln p_i) + q_T (ln q_T - ln p_T),
-//           dL/dz_j = scale (p_j - q_j) in S,  scale p_j (1 - q_T / p_T) outside.
+//           dL/dz_j = scale (p_j - q_j) in S,  scale p_j (1 - q_T / p_T) outside;
+//           with p_T = 0 the second term of L is left out: scale (Q p_j - q_j) in S.
+//           (Q > 1, no distribution: q_T = 0, and the gradient is as for Q = 1.)
 // The row is held in shared memory (vocab_rows.cuh), so that it is read once for both the loss and the
 // gradient: 2 passes over it on chip, sizeof(logit) + sizeof(gradient) bytes per token in HBM.
 //

@@ -228,15 +228,17 @@ __device__ __forceinline__ RowScale row_scale(const RowSums& r, const ListSums& 
   o.empty = r.all == -kInf && o.s == 0.f;  // every logit -inf: p = 0
   o.inv_s = o.empty ? 0.f : 1.f / o.s;
   o.pulls = bucket && r.tail > 0.f && l.q_tail > 0.f;
-  o.f_in = w * scale;
-  o.q_in = bucket ? o.f_in : o.f_in / l.Q;
+  const float ws = w * scale;
+  o.q_in = bucket ? ws : ws / l.Q;
+  // p's factor is the weight of all terms: 1, or Q where a tail that is masked altogether leaves the second term out
+  o.f_in = bucket && l.q_tail > 0.f && r.tail == 0.f ? ws * l.Q : ws;
   // w scale p_j (1 - q_T / p_T) = F 2^y, F = w scale (2^d / s - q_T / tail) with y and tail against the tail's maximum, d from
   // there to the row's.  F's exponent k goes into the reference; what rounding the reference takes goes into the
   // factor.
   const float g = o.pulls ? o.inv_s * to_all - l.q_tail / r.tail : o.inv_s;
   int k = 0, k2 = 0;
-  float f = o.f_in * g;
-  if (isfinite(o.f_in) && isfinite(g)) f = frexpf(g, &k) * frexpf(o.f_in, &k2);
+  float f = ws * g;
+  if (isfinite(ws) && isfinite(g)) f = frexpf(g, &k) * frexpf(ws, &k2);
   const float R = o.pulls ? R_tail : o.R;
   const Float2 ref = two_sum(is_far(R) ? 0.f : R, -static_cast<float>(k + k2));
   o.ref = ref.hi;

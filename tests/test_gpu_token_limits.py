@@ -142,3 +142,39 @@ def test_a_tail_far_below_the_list(B, rows, vocab, dtype, grad, gap):
     _check_tails(loss, g, z, ids, logq, sorted({0, 1, 2, *range(3, rows, max(1, rows // 9))}))
     if g is not None:  # (off by what each of the tail's tokens and of the list's is)
         assert (g.double().sum(1).abs() <= 1e-2 if grad == "bf16" else g.double().sum(1).abs() <= 1e-4).all()
+
+
+@pytest.mark.parametrize("rows,vocab,dtype,grad", [(8, 60, "f32", "f32"), (8, 5003, "f16", "bf16"), (420, 126464, "f16", "f32"), (210, 126464, "f32", "f32")])
+def test_a_tail_that_is_masked_altogether(B, rows, vocab, dtype, grad):
+    """Every token outside the list at -inf, the list's mass below 1: against the formula's derivative, which sums to 0
+    (p is off by SUM and its exponent's bound, q by 4 U), and against differences of the kernel's own losses, off by
+    3 SUM each: h = 0.05 leaves 3 SUM / 0.05 + 0.05^2 < 4e-3 in a direction of length 1."""
+    k = 6
+    rng = np.random.default_rng(8)
+    ids = torch.from_numpy(np.stack([rng.permutation(vocab)[:k] for _ in range(rows)]).astype(np.int32)).cuda()
+    z = torch.full((rows, vocab), -INF, dtype=DT[dtype], device="cuda")
+    z.scatter_(1, ids.long(), torch.from_numpy(2 * rng.standard_normal((rows, k))).to(z))
+    logq = torch.from_numpy(np.log(rng.dirichlet(np.ones(k), rows) * rng.uniform(0.2, 0.95, (rows, 1)) + 1e-3)).float().cuda()
+    loss, g = torch.empty(rows, device="cuda"), torch.empty(rows, vocab, dtype=DT[grad], device="cuda")
+    B.sgd_kernel_distill(z, ids, logq, loss, grad=g)
+    for r in sorted({0, 1, 2, rows - 1, *range(3, rows, max(1, rows // 9))}):
+        at, lq = ids[r].cpu().numpy(), logq[r].double().cpu().numpy()
+        L, want = ot.distill_row(z[r].double().cpu().numpy(), at, lq)
+        lp = ot.log_softmax(z[r].double().cpu().numpy()[None])[0][at]
+        assert abs(want.sum()) < 1e-14
+        q = np.exp(lq)
+        assert abs(loss[r].item() - L) <= SUM * q.sum() + 4 * U * (q * np.abs(lq - lp)).sum() + U * abs(L)
+        got = g[r].double().cpu().numpy()
+        tol = np.exp(lp) * (SUM + (4 + 3 * np.abs(lp)) * U) + 4 * U * q
+        assert (np.abs(got[at] - want[at]) <= tol + torch.finfo(DT[grad]).eps / 2 * (np.abs(want[at]) + tol)).all()
+        got[at] = 0
+        assert not got.any()
+    if dtype == "f32":
+        v = torch.randn(rows, k, device="cuda", generator=torch.Generator("cuda").manual_seed(1))
+        v /= v.norm(dim=1, keepdim=True)
+        d = []
+        for h in (0.05, -0.05):
+            loss2 = torch.empty(rows, device="cuda")
+            B.sgd_kernel_distill(z.scatter_add(1, ids.long(), h * v), ids, logq, loss2)
+            d.append(loss2)
+        assert ((d[0] - d[1]) / 0.1 - (torch.gather(g, 1, ids.long()) * v).sum(1)).abs().max() < 4e-3

@@ -20,3 +20,29 @@ def test_a_tail_far_below_the_list(gap):
     np.testing.assert_allclose(grad[:2], 1 / s - 0.45, rtol=1e-12)
     np.testing.assert_allclose(grad[2:], math.exp(-gap) / s - 0.1 / 6, rtol=1e-12)
     assert abs(grad.sum()) < 1e-15
+
+
+def _difference(z, ids, lq, j, **kw):
+    h = np.zeros(len(z))
+    h[j] = 1e-5
+    return (ot.distill_row(z + h, ids, lq, **kw)[0] - ot.distill_row(z - h, ids, lq, **kw)[0]) / 2e-5
+
+
+@pytest.mark.parametrize("scale", [1.0, 0.7])
+def test_gradient_where_the_tail_is_masked_altogether(scale):
+    """The second term is left out, and what is left has the weight Q."""
+    z = np.array([0.3, -math.inf, 1.2, -math.inf, -0.5, -math.inf])
+    ids, lq = [4, 0, 2], np.log([0.2, 0.3, 0.1])
+    loss, grad = ot.distill_row(z, ids, lq, scale=scale, weight=1.3)
+    for j in (0, 2, 4):
+        assert abs(_difference(z, ids, lq, j, scale=scale, weight=1.3) - grad[j]) < 1e-8
+    assert abs(grad.sum()) < 1e-15 and (grad[[1, 3, 5]] == 0).all() and abs(grad[2]) > 0.1
+
+
+def test_gradient_of_a_list_that_is_no_distribution():
+    z = np.random.default_rng(3).standard_normal(9)
+    lp = ot.log_softmax(z[None])[0]
+    _, grad = ot.distill_row(z, [2, 5], np.log([0.9, 0.5]))
+    want = np.exp(lp)
+    want[[2, 5]] -= [0.9, 0.5]
+    np.testing.assert_allclose(grad, want, rtol=1e-14)
