@@ -247,7 +247,8 @@ typedef enum {
  * Divergence of rows of logits from a teacher's likeliest tokens, with its gradient (the full
  * model's lists from sgd_kernel_logprobs against a scheduled model's logits, say).  With
  * p = softmax(scale * logits[r, :]), the list's tokens S and q_i = exp(teacher_logprobs_i), Q = sum q_i:
- *   SGD_TAIL_RENORM: L = sum_S (q_i / Q) (ln (q_i / Q) - ln p_i);
+ *   SGD_TAIL_RENORM: L = sum_S (q_i / Q) (ln (q_i / Q) - ln p_i); only differences of teacher_logprobs count, which
+ *                    may be any scores;
  *   SGD_TAIL_BUCKET: L = sum_S q_i (ln q_i - ln p_i) + q_T (ln q_T - ln p_T), q_T = max(0, 1 - Q),
  *                    p_T = sum of p outside S; the second term is left out where q_T or p_T is 0.  Lists are meant
  *                    to have Q <= 1; where it is more, grad is that of Q = 1 (scale w_r (p - q) in S, scale w_r p
@@ -257,7 +258,7 @@ typedef enum {
  * logits [rows, vocab] of type dtype, rows ld elements apart; teacher_ids int32 and teacher_logprobs
  * fp32 [rows, top_k].  An id outside [0, vocab) pads the list; of ids that are equal the first counts.
  * row_weight fp32 [rows] (NULL: 1): the logits of rows of weight 0 are not read, their loss and
- * gradient are 0; so are those of a row whose list has no token (SGD_TAIL_RENORM: or Q = 0).
+ * gradient are 0; so are those of a row whose list has no token (SGD_TAIL_RENORM: or none that is above -inf).
  * -inf masks a token (p = 0): the loss is +inf where the list gives it weight, the gradient finite.
  * NaN in a row, or +inf, makes its loss and gradient NaN.
  * grad of type grad_dtype, rows ld_grad elements apart, each value rounded once from fp32 (out of

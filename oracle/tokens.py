@@ -47,10 +47,12 @@ def distill_row(logits, ids, logq, scale=1.0, bucket=True, weight=1.0):
             seen[int(i)] = float(lq)
     S = np.array(list(seen), np.int64)
     lq = np.array([seen[i] for i in seen], np.float64)
+    if weight == 0 or S.size == 0 or (not bucket and lq.max() == -np.inf):
+        return 0.0, grad
+    if not bucket:
+        lq = lq - lq.max()  # (only the differences count)
     q = np.exp(lq)
     Q = q.sum()
-    if weight == 0 or S.size == 0 or (not bucket and Q == 0):
-        return 0.0, grad
     lp = log_softmax(z[None], scale)[0]
     p = np.exp(lp)
 

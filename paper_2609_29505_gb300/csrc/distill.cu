@@ -37,6 +37,7 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) distill_kernel(const
   __shared__ int abort_flag;
   __shared__ int ids[kMaxList];
   __shared__ double q_sum[2];
+  __shared__ float q_max[2];
   __shared__ int q_any[2];
   __shared__ float4 parts[kWarps];
   __shared__ float4 slot[kMaxCluster];
@@ -93,13 +94,25 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) distill_kernel(const
     __syncwarp();
     const double sum = warp_sum(static_cast<double>(q));
     const int any = __any_sync(0xffffffffu, id >= 0);
+    const float top = key_value(__reduce_max_sync(0xffffffffu, order_key(id >= 0 ? lq : -kInf)));
     if (lane == 0) {
       q_sum[warp] = sum;
+      q_max[warp] = top;
       q_any[warp] = any;
     }
   }
   __syncthreads();
   cluster_arrive();
+  const float q_top = fmaxf(q_max[0], q_max[1]);
+  if (!p.bucket && out_of_scale(q_top)) {  // (in every thread of the cluster)
+    if (threadIdx.x < kMaxList) {
+      lq -= q_top;
+      q = id >= 0 ? expf(lq) : 0.f;
+      const double sum = warp_sum(static_cast<double>(q));
+      if (lane == 0) q_sum[warp] = sum;
+    }
+    __syncthreads();
+  }
   const double Q = q_sum[0] + q_sum[1];
   const bool pulls = (q_any[0] | q_any[1]) && (p.bucket || Q != 0.0);
 
@@ -140,7 +153,7 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) distill_kernel(const
     if (lane == 0) parts[warp] = make_float4(tail.x, tail.y, m, in);
   }
   __syncthreads();
-  if (warp == 0) {
+  if (n_ctas > 1 && warp == 0) {
     float4 v = lane < kWarps ? parts[lane] : make_float4(-kInf, 0.f, -kInf, 0.f);
     const float m = key_value(__reduce_max_sync(0xffffffffu, order_key(v.x)));
     const float m_list = key_value(__reduce_max_sync(0xffffffffu, order_key(v.z)));
@@ -152,9 +165,9 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) distill_kernel(const
     if (lane < n_ctas) st_cluster(map_to_rank(smem_u32(&slot[rank]), lane), make_float4(m, v.y, m_list, v.w));
   }
   __syncwarp();
-  cluster_sync();
+  if (n_ctas > 1) cluster_sync();
 
-  const RowSums sums = row_sums(slot, n_ctas, c);
+  const RowSums sums = n_ctas > 1 ? row_sums(slot, n_ctas, c) : row_sums(parts, kWarps, c);
   const ListSums ls = list_sums(Q, p.bucket);
   const RowScale o = row_scale(sums, ls, w, p.scale, p.bucket, c);
   if constexpr (kGrad) {

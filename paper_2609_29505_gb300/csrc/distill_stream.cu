@@ -53,7 +53,7 @@ struct Buffer {
   int row;             // -1: no more
   int live;            // 0: loss and gradient are 0
   Outside out;         // of the gradient
-  RowSums sums;        // of the row, and its scalars (here and not in registers: a spilled one is read back behind the copies)
+  RowSums sums;        // of the row, and its gradient's scalars (as registers they spill: read back behind the copies)
   RowScale scale;
   float2 part[kWorkWarps];
   float4 slot[2][kMaxStreamCluster];
@@ -85,7 +85,6 @@ struct LossRow {
   float w;
   ListSums list;
   RowSums sums;
-  RowScale scale;
   float q[kMaxList], lq[kMaxList], z[kMaxList];
 };
 
@@ -227,7 +226,9 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
           lq[h] = x.lq[lane + 32 * h];
           z[h] = x.z[lane + 32 * h];
         }
-        loss = row_loss(x.scale, x.sums, x.list, x.w, p.bucket, p.scale, c, q, lq, z);
+        const RowSums sums = x.sums;
+        const ListSums list = x.list;
+        loss = row_loss(row_scale(sums, list, x.w, p.scale, p.bucket, c), sums, list, x.w, p.bucket, p.scale, c, q, lq, z);
       }
       if (lane == 0) p.loss[row] = loss;
       __syncwarp();
@@ -293,15 +294,24 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
         }
         __syncwarp();
       }
+      uint32_t key = kKeyNegInf;
+#pragma unroll
+      for (int h = 0; h < kHalves; ++h) key = max(key, x.id[h] >= 0 ? order_key(x.lq[h]) : kKeyNegInf);
+      const float top = key_value(__reduce_max_sync(0xffffffffu, key));
+      if (!p.bucket && out_of_scale(top)) {
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h) x.lq[h] -= top;
+      }
       double sum = 0.0;
-      bool any = false;
 #pragma unroll
       for (int h = 0; h < kHalves; ++h) {
         x.q[h] = x.id[h] >= 0 ? expf(x.lq[h]) : 0.f;
         sum += x.q[h];
-        any |= x.id[h] >= 0;
       }
       const double Q = warp_sum(sum);
+      bool any = false;
+#pragma unroll
+      for (int h = 0; h < kHalves; ++h) any |= x.id[h] >= 0;
       x.sums = list_sums(Q, p.bucket);
       x.lives = __any_sync(0xffffffffu, any) && x.copied && (p.bucket || Q != 0.0);
     };
@@ -336,11 +346,13 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
         if (!wait_cluster(&b.sums_full[place], sums_phase, abort_flag, p.status, 74)) return false;
         sums = row_sums(b.slot[place], n_ctas, c);
       }
-      const RowScale scale = row_scale(sums, old.sums, old.w, p.scale, p.bucket, c);
-      if (lane == 0) {
-        b.sums = sums;
-        b.scale = scale;
-        if (kGrad) b.out = outside(scale, sums, c);
+      if (lane == 0) b.sums = sums;
+      if constexpr (kGrad) {
+        const RowScale scale = row_scale(sums, old.sums, old.w, p.scale, p.bucket, c);
+        if (lane == 0) {
+          b.scale = scale;
+          b.out = outside(scale, sums, c);
+        }
       }
       __syncwarp();
       return true;
@@ -364,7 +376,6 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
         l.w = old.w;
         l.list = old.sums;
         l.sums = b.sums;
-        l.scale = b.scale;
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&b.loss_full);
@@ -401,7 +412,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
             ok = exchange();
           }
         }
-        if (ok && rank == owner) ok = send_loss(old.row);
+        if (!kGrad && ok && rank == owner) ok = send_loss(old.row);
         owner = owner + 1 == n_ctas ? 0 : owner + 1;
         if (old.lives) {
           place ^= 1;
@@ -454,6 +465,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) distill_stream_kernel(const Di
       if constexpr (kGrad) {
         if (old.lives && !exchange()) break;
         if (lane == 0) mbar_arrive(&b.scaled);
+        if (rank == owner && !send_loss(old.row)) break;  // (while the gradient is written)
         sort_out(x);
         if (!mbar_wait_warp(smem_u32(&b.done), phase, abort_flag, p.status, 75)) break;
       }

@@ -178,3 +178,36 @@ def test_a_tail_that_is_masked_altogether(B, rows, vocab, dtype, grad):
             B.sgd_kernel_distill(z.scatter_add(1, ids.long(), h * v), ids, logq, loss2)
             d.append(loss2)
         assert ((d[0] - d[1]) / 0.1 - (torch.gather(g, 1, ids.long()) * v).sum(1)).abs().max() < 4e-3
+
+
+@pytest.mark.parametrize("rows,vocab,dtype,grad", [(9, 60, "f32", "f32"), (9, 5003, "f16", "f32"), (420, 126464, "f16", "f32"), (420, 126464, "bf16", "")])
+@pytest.mark.parametrize("k", [1, 5, 40])
+def test_renormalised_lists_of_any_scale(B, rows, vocab, dtype, grad, k):
+    """Scores that are shifted by up to 1000, so that their exponentials are out of fp32's range, or are spread over
+    more than it.  q / Q is off by 4 U and by its exponent's rounding, U of |score| and of |score - largest|."""
+    z = _normal(rows, vocab, dtype, 9)
+    rng = np.random.default_rng(10)
+    ids = torch.from_numpy(np.stack([rng.permutation(vocab)[:k] for _ in range(rows)]).astype(np.int32)).cuda()
+    by = np.array([-1000.0, -104.0, -95.0, -88.0, -60.0, 0.0, 60.0, 89.0, 1000.0])
+    spread = np.where(rng.random((rows, 1)) < 0.3, 100.0, 2.0)
+    logq = torch.from_numpy(by[np.arange(rows) % 9][:, None] - spread * rng.random((rows, k))).float().cuda()
+    loss = torch.empty(rows, device="cuda")
+    g = torch.empty(rows, vocab, dtype=DT[grad], device="cuda") if grad else None
+    B.sgd_kernel_distill(z, ids, logq, loss, grad=g, tail=B.TAIL_RENORM)
+    assert B.sgd_kernel_status() == 0
+    for r in sorted({*range(min(rows, 27)), rows - 1, *range(27, rows, max(1, rows // 9))}):
+        at, lq = ids[r].cpu().numpy(), logq[r].double().cpu().numpy()
+        x = z[r].double().cpu().numpy()
+        L, want = ot.distill_row(x, at, lq, bucket=False)
+        lp = ot.log_softmax(x[None])[0]
+        lh = lq - lq.max()
+        lh = lh - np.log(np.exp(lh).sum())
+        q = np.exp(lh)
+        eq = (8 + 2 * np.abs(lh) + np.abs(lh).max()) * U  # (expf, its rounded exponent, the sum, the quotient)
+        terms = np.where(q > 0, np.abs(lh - lp[at]), 0.0)
+        tol = 2 * SUM + (q * (eq * (terms + 1) + 4 * U * (terms + np.abs(lh)))).sum()
+        assert abs(loss[r].item() - L) <= tol + U * abs(L), (r, loss[r].item(), L)
+        if g is not None:
+            tol = np.exp(lp) * (SUM + (4 + 3 * np.abs(lp)) * U)
+            tol[at] += q * eq + 2.0 ** -126  # (an entry below 2^-126 of the largest may be 0)
+            assert (np.abs(g[r].double().cpu().numpy() - want) <= tol + U * np.abs(want) + 2.0 ** -149).all(), r

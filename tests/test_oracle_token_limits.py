@@ -46,3 +46,15 @@ def test_gradient_of_a_list_that_is_no_distribution():
     want = np.exp(lp)
     want[[2, 5]] -= [0.9, 0.5]
     np.testing.assert_allclose(grad, want, rtol=1e-14)
+
+
+@pytest.mark.parametrize("by", [-700.0, -100.0, 100.0, 1e5])
+def test_only_differences_of_a_renormalised_list_count(by):
+    z = np.random.default_rng(4).standard_normal(9)
+    lq = np.array([-0.5, -1.25, -3.0])
+    a = ot.distill_row(z, [2, 5, 7], lq, bucket=False)
+    b = ot.distill_row(z, [2, 5, 7], lq + by, bucket=False)
+    np.testing.assert_allclose(a[0], b[0], rtol=1e-9)
+    np.testing.assert_allclose(a[1], b[1], rtol=1e-9)
+    loss, grad = ot.distill_row(z, [2, 5], [-math.inf] * 2, bucket=False)
+    assert loss == 0 and not grad.any()
