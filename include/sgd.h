@@ -378,7 +378,7 @@ SGD_API int sgd_sampler_update(float* z_dev, const float* eps_dev, float alpha, 
  * n_reveal int32 [batch] on the device: below 0 is 0, more than there are takes all.  window int32
  * [batch, 2] (first and end position, cut to [0, n_tokens]; NULL: the whole sample).  n_left int32
  * [batch] (may be NULL): positions of ids_out that were masked and were not chosen.
- * n_tokens <= 49152 (else SGD_ERR_SHAPE).
+ * n_tokens <= 49152 (else SGD_ERR_SHAPE).  Pointers to nothing (batch or n_tokens 0) may be NULL.
  */
 SGD_API int sgd_sampler_reveal(const int32_t* ids_dev, const int32_t* cand_dev, int64_t cand_stride,
                        const float* score_dev, int64_t score_stride, int lowest, const int32_t* n_reveal_dev,

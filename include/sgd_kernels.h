@@ -219,7 +219,8 @@ typedef enum { SGD_F16 = 0, SGD_BF16 = 1, SGD_F32 = 2 } sgd_dtype;
  *   entropy fp32 [rows] = - sum p ln p (0 ln 0 = 0);
  *   top_ids int32 [rows, top_k], top_logprobs fp32 [rows, top_k]: the tokens of the largest logits, in
  *     descending order, equal logits (-0 and +0 are equal) in the order of the token.
- * Any of the outputs may be NULL (tokens with n_tokens = 0), but not all.
+ * Any of the outputs may be NULL (tokens with n_tokens = 0), but not all.  With rows = 0 nothing is done, and every
+ * pointer may be NULL (so in sgd_kernel_distill).
  * logits [rows, vocab] of type dtype, rows ld elements apart, aligned to their elements alone.
  * scale > 0 (1 / temperature).  row_ids int32 [rows]: where given, only rows with row_ids[r] == row_id
  * (positions that are still masked, say) are read, and what the others' outputs held stays.

@@ -1714,7 +1714,10 @@ int sgd_sampler_update(float* z, const float* eps, float alpha, float beta, int6
 int sgd_sampler_reveal(const int32_t* ids, const int32_t* cand, int64_t cand_stride, const float* score,
                        int64_t score_stride, int lowest, const int32_t* n_reveal, const int32_t* window,
                        int32_t* ids_out, int32_t* n_left, int batch, int n_tokens, int mask_id, void* stream) {
-  if (!ids || !cand || !score || !n_reveal || !ids_out) return fail(SGD_ERR_ARG, "reveal: null argument");
+  // (an empty tensor may have no address)
+  const bool any = batch != 0 && n_tokens != 0;
+  if ((any && (!ids || !cand || !score || !ids_out)) || (batch != 0 && !n_reveal))
+    return fail(SGD_ERR_ARG, "reveal: null argument");
   if (batch < 0 || n_tokens < 0 || cand_stride < 1 || score_stride < 1)
     return fail(SGD_ERR_ARG, "reveal: negative size, or a stride below 1");
   if (!al4(ids) || !al4(cand) || !al4(score) || !al4(n_reveal) || !al4(window) || !al4(ids_out) || !al4(n_left))
@@ -1960,7 +1963,7 @@ int elem_size(int dtype) { return dtype == SGD_F32 ? 4 : 2; }
 // What the two operators on rows of logits ask of them.
 int check_rows(const char* name, const void* logits, int dtype, int64_t ld, int rows, int vocab, float scale) {
   const std::string n = std::string(name) + ": ";
-  if (!logits) return fail(SGD_ERR_ARG, n + "null logits");
+  if (!logits && rows != 0) return fail(SGD_ERR_ARG, n + "null logits");  // (an empty tensor may have no address)
   if (dtype < SGD_F16 || dtype > SGD_F32) return fail(SGD_ERR_ARG, n + "unknown element type");
   if (rows < 0 || vocab < 1 || ld < vocab) return fail(SGD_ERR_ARG, n + "rows >= 0, vocab >= 1 and ld >= vocab are needed");
   if (!(scale > 0.f) || !std::isfinite(scale)) return fail(SGD_ERR_ARG, n + "scale must be positive and finite");
@@ -1979,13 +1982,14 @@ int sgd_kernel_logprobs(const void* logits, int dtype, int64_t ld, int rows, int
                         void* stream) {
   const int rc = check_rows("logprobs", logits, dtype, ld, rows, vocab, scale);
   if (rc) return rc;
-  if (n_tokens < 0 || (n_tokens > 0) != (tokens && token_logprobs))
+  const bool any = rows != 0;
+  if (n_tokens < 0 || (any && (n_tokens > 0) != (tokens && token_logprobs)))
     return fail(SGD_ERR_ARG, "logprobs: n_tokens, tokens and token_logprobs go together");
   if (top_k < 0 || top_k > kMaxTop || top_k > vocab)
     return fail(SGD_ERR_ARG, "logprobs: top_k must be in 0..64 and at most vocab");
-  if ((top_k > 0) != (top_ids || top_logprobs))
+  if (any && (top_k > 0) != (top_ids || top_logprobs))
     return fail(SGD_ERR_ARG, "logprobs: top_k goes with top_ids or top_logprobs");
-  if (!n_tokens && !entropy && !top_k) return fail(SGD_ERR_ARG, "logprobs: no output asked for");
+  if (any && !n_tokens && !entropy && !top_k) return fail(SGD_ERR_ARG, "logprobs: no output asked for");
   if (!al4(row_ids) || !al4(tokens) || !al4(token_logprobs) || !al4(entropy) || !al4(top_ids) || !al4(top_logprobs))
     return fail(SGD_ERR_ARG, "logprobs: pointers must be 4-byte aligned");
   if (rows == 0) return SGD_OK;
@@ -2001,7 +2005,7 @@ int sgd_kernel_distill(const void* logits, int dtype, int64_t ld, int rows, int 
                        int64_t ld_grad, void* stream) {
   const int rc = check_rows("distill", logits, dtype, ld, rows, vocab, scale);
   if (rc) return rc;
-  if (!teacher_ids || !teacher_logprobs || !loss) return fail(SGD_ERR_ARG, "distill: null argument");
+  if (rows != 0 && (!teacher_ids || !teacher_logprobs || !loss)) return fail(SGD_ERR_ARG, "distill: null argument");
   if (top_k < 1 || top_k > kMaxTop) return fail(SGD_ERR_ARG, "distill: top_k must be in 1..64");
   if (tail != SGD_TAIL_RENORM && tail != SGD_TAIL_BUCKET) return fail(SGD_ERR_ARG, "distill: unknown kind of tail");
   if (!al4(teacher_ids) || !al4(teacher_logprobs) || !al4(row_weight) || !al4(loss))

@@ -211,3 +211,31 @@ def test_renormalised_lists_of_any_scale(B, rows, vocab, dtype, grad, k):
             tol = np.exp(lp) * (SUM + (4 + 3 * np.abs(lp)) * U)
             tol[at] += q * eq + 2.0 ** -126  # (an entry below 2^-126 of the largest may be 0)
             assert (np.abs(g[r].double().cpu().numpy() - want) <= tol + U * np.abs(want) + 2.0 ** -149).all(), r
+
+
+@pytest.mark.parametrize("rows,vocab", [(0, 64), (0, 126464)])
+def test_empty_tensors(B, rows, vocab):
+    z = torch.empty(rows, vocab, dtype=torch.float16, device="cuda")
+    ids, lq = torch.empty(rows, 4, dtype=torch.int32, device="cuda"), torch.empty(rows, 4, device="cuda")
+    one = torch.empty(rows, device="cuda")
+    B.sgd_kernel_logprobs(z, tokens=ids, token_logprobs=lq, entropy=one, top_ids=ids, top_logprobs=lq)
+    B.sgd_kernel_logprobs(z, entropy=one, row_ids=torch.empty(rows, dtype=torch.int32, device="cuda"))
+    B.sgd_kernel_distill(z, ids, lq, one, grad=torch.empty_like(z), row_weight=one)
+
+
+@pytest.mark.parametrize("batch,n", [(0, 5), (3, 0), (0, 0)])
+def test_reveal_of_empty_tensors(B, batch, n):
+    ids, n_reveal = torch.empty(batch, n, dtype=torch.int32, device="cuda"), torch.ones(batch, dtype=torch.int32, device="cuda")
+    left = torch.full((batch,), 9, dtype=torch.int32, device="cuda")
+    window = torch.zeros(batch, 2, dtype=torch.int32, device="cuda")
+    B.sgd_sampler_reveal(ids, ids, torch.empty(batch, n, device="cuda"), n_reveal, ids, 0)
+    B.sgd_sampler_reveal(ids, ids, torch.empty(batch, n, device="cuda"), n_reveal, ids, 0, window=window, n_left=left)
+    assert (left == 0).all()
+
+
+def test_tokens_of_no_number_beside_another_output(B):
+    z = _normal(3, 100, "f16", 1)
+    e, none = torch.empty(3, device="cuda"), torch.empty(3, 0, device="cuda")
+    B.sgd_kernel_logprobs(z, tokens=none.int(), token_logprobs=none, entropy=e, top_ids=none.int(), top_logprobs=none)
+    want = torch.distributions.Categorical(logits=z.double()).entropy()
+    assert ((e.double() - want).abs() < 4 * SUM * (1 + want)).all()
