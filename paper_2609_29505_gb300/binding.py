@@ -508,15 +508,16 @@ class Denoiser:
                                     C.byref(cond), step, _stream(stream)), "sgd_step")
 
     def step_tokens(self, ids, ids_out, logits, t: float, step: int, cand, score, n_reveal, mask_id: int,
-                    by: str = "confidence", scale: float = 1.0, window=None, n_left=None, stream=None):
+                    by: str = "confidence", scale: float = 1.0, window=None, n_left=None, stream=None, class_ids=None,
+                    ctx=None):
         """One step of a masked-token trajectory (argmax remasking), queued on one stream: the denoiser on ids
-        int32 [B, N] into logits fp16 [B, N, V], the best token of every masked position into cand int32 [B, N]
-        with its log-probability (by "confidence") or its row's entropy (by "entropy") in score float32
-        [B, N], and the n_reveal best of them revealed in ids_out (which may be ids).  What cand and
-        score hold at other positions stays."""
+        int32 [B, N] (with class_ids int32 [B] and ctx bf16 [B, L, d_ctx] as step takes them) into logits fp16 [B, N, V],
+        the best token of every masked position into cand int32 [B, N] with its log-probability (by "confidence") or its
+        row's entropy (by "entropy") in score float32 [B, N], and the n_reveal best of them revealed in ids_out
+        (which may be ids).  What cand and score hold at other positions stays."""
         if by not in ("confidence", "entropy"):
             raise ValueError("by must be confidence or entropy")
-        self.step(ids, logits, t, step, stream=stream)
+        self.step(ids, logits, t, step, class_ids=class_ids, ctx=ctx, stream=stream)
         rows = logits.view(-1, logits.shape[-1])
         out = dict(top_logprobs=score.view(-1, 1)) if by == "confidence" else dict(entropy=score.view(-1))
         sgd_kernel_logprobs(rows, top_ids=cand.view(-1, 1), scale=scale, row_ids=ids.view(-1), row_id=mask_id,
