@@ -63,6 +63,7 @@ POLICY_STATIC, POLICY_DRIFT = 0, 1
 DTYPES = {"float16": 0, "bfloat16": 1, "float32": 2}  # sgd_dtype, by torch's names
 TAIL_RENORM, TAIL_BUCKET = 0, 1
 TAIL = {"renorm": TAIL_RENORM, "bucket": TAIL_BUCKET}
+MAX_ROW_BYTES, REVEAL_MAX_TOKENS = 3 << 20, 49152  # of a row of logits; of a sample that is revealed
 
 
 class sgd_model_desc(C.Structure):
@@ -514,9 +515,34 @@ class Denoiser:
         int32 [B, N] (with class_ids int32 [B] and ctx bf16 [B, L, d_ctx] as step takes them) into logits fp16 [B, N, V],
         the best token of every masked position into cand int32 [B, N] with its log-probability (by "confidence") or its
         row's entropy (by "entropy") in score float32 [B, N], and the n_reveal best of them revealed in ids_out
-        (which may be ids).  What cand and score hold at other positions stays."""
+        (which may be ids).  What cand and score hold at other positions stays.  The arguments are checked before the step is
+        launched (TypeError / ValueError)."""
+        import torch
         if by not in ("confidence", "entropy"):
             raise ValueError("by must be confidence or entropy")
+        c = self.cfg
+        if c.stem != "embed" or c.head != "logits":
+            raise ValueError("step_tokens needs a token model (an embed stem and a logits head)")
+        if c.d_out * 2 > MAX_ROW_BYTES or c.n_tokens > REVEAL_MAX_TOKENS:
+            raise ValueError("the vocabulary or the sample is beyond what the operators on logits take")
+        if not 0.0 < C.c_float(scale).value < float("inf"):
+            raise ValueError("scale must be positive and finite")
+        if not -2 ** 31 <= mask_id < 2 ** 31:
+            raise ValueError("mask_id must be a 32-bit integer")
+        device, i32, f32 = ids.device, torch.int32, torch.float32
+        shape = (c.batch, c.n_tokens)
+        for x, name, dtype, of in ((ids, "ids", i32, shape), (ids_out, "ids_out", i32, shape), (cand, "cand", i32, shape),
+                                   (score, "score", f32, shape), (logits, "logits", torch.float16, (*shape, c.d_out)),
+                                   (n_reveal, "n_reveal", i32, (c.batch,))):
+            if x is None:
+                raise TypeError(f"{name} is needed")
+            _tensor(x, name, dtype, of, device)
+        _tensor(window, "window", i32, (c.batch, 2), device)
+        _tensor(n_left, "n_left", i32, (c.batch,), device)
+        _tensor(class_ids, "class_ids", i32, (c.batch,), device)
+        _tensor(ctx, "ctx", torch.bfloat16, (c.batch, c.ctx_len, c.d_ctx), device)
+        if not ids.is_cuda:
+            raise ValueError("ids must be on a CUDA device")
         self.step(ids, logits, t, step, class_ids=class_ids, ctx=ctx, stream=stream)
         rows = logits.view(-1, logits.shape[-1])
         out = dict(top_logprobs=score.view(-1, 1)) if by == "confidence" else dict(entropy=score.view(-1))
