@@ -429,7 +429,8 @@ def sgd_sampler_reveal(ids, cand, score, n_reveal, ids_out, mask_id, lowest=Fals
                        stream=None):
     """The masked positions of ids int32 [batch, n_tokens] with the best scores (n_reveal int32 [batch] of them;
     window int32 [batch, 2]: between these positions) take their candidates in ids_out (which may
-    be ids); n_left int32 [batch]: masked positions that remain."""
+    be ids); n_left int32 [batch]: masked positions that were not chosen (a candidate that is mask_id itself leaves its
+    position masked, and chosen)."""
     import torch
     if ids.dim() != 2 or not ids.is_cuda:
         raise ValueError("ids must be a 2-d tensor on a CUDA device")
@@ -515,7 +516,8 @@ class Denoiser:
         int32 [B, N] (with class_ids int32 [B] and ctx bf16 [B, L, d_ctx] as step takes them) into logits fp16 [B, N, V],
         the best token of every masked position into cand int32 [B, N] with its log-probability (by "confidence") or its
         row's entropy (by "entropy") in score float32 [B, N], and the n_reveal best of them revealed in ids_out
-        (which may be ids).  What cand and score hold at other positions stays.  The arguments are checked before the step is
+        (which may be ids).  What cand and score hold at other positions stays.  A position whose best token is
+        mask_id itself counts as revealed in n_left, and stays masked.  The arguments are checked before the step is
         launched (TypeError / ValueError)."""
         import torch
         if by not in ("confidence", "entropy"):

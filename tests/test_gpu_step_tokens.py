@@ -46,3 +46,17 @@ def test_a_model_with_cross_attention(by):
     assert int((runs[0][0] != mask).sum()) >= 2 * 3 * 50  # (a best token may be the mask)
     model.check_device()
     model.close()
+
+
+def test_a_candidate_that_is_the_mask():
+    """It is taken, leaves its position masked, and counts as chosen."""
+    if not torch.cuda.is_available():
+        pytest.skip("needs a CUDA device")
+    from paper_2609_29505_gb300 import binding, build
+    build.build()
+    ids = torch.full((1, 6), 7, dtype=torch.int32, device="cuda")
+    cand = torch.tensor([[7, 1, 2, 7, 3, 4]], dtype=torch.int32, device="cuda")
+    score = torch.tensor([[5.0, 4.0, 3.0, 2.0, 1.0, 0.0]], device="cuda")
+    out, left = torch.empty_like(ids), torch.empty(1, dtype=torch.int32, device="cuda")
+    binding.sgd_sampler_reveal(ids, cand, score, torch.tensor([4], dtype=torch.int32, device="cuda"), out, 7, n_left=left)
+    assert out.tolist() == [[7, 1, 2, 7, 7, 7]] and left.tolist() == [2]
