@@ -239,3 +239,19 @@ def test_tokens_of_no_number_beside_another_output(B):
     B.sgd_kernel_logprobs(z, tokens=none.int(), token_logprobs=none, entropy=e, top_ids=none.int(), top_logprobs=none)
     want = torch.distributions.Categorical(logits=z.double()).entropy()
     assert ((e.double() - want).abs() < 4 * SUM * (1 + want)).all()
+
+
+@pytest.mark.parametrize("rows,vocab", [(700, 49152), (600, 49151), (500, 70001), (400, 90001), (330, 100003)])
+@pytest.mark.parametrize("k", [2, 64])
+def test_lists_of_slices_of_few_tiles(B, rows, vocab, k):
+    """3, 5, 6 and 7 tiles a row, after a call that leaves the largest values in every place of shared memory."""
+    high = torch.full((320, 126464), 60000.0, dtype=torch.float16, device="cuda")
+    ids, lp = torch.empty(320, 64, dtype=torch.int32, device="cuda"), torch.empty(320, 64, device="cuda")
+    z = _normal(rows, vocab, "f16", 11)
+    top, want = torch.empty(rows, k, dtype=torch.int32, device="cuda"), torch.empty(rows, k, device="cuda")
+    for _ in range(3):
+        B.sgd_kernel_logprobs(high, top_ids=ids, top_logprobs=lp)
+        B.sgd_kernel_logprobs(z, top_ids=top, top_logprobs=want)
+        order = torch.sort(z.float(), dim=1, descending=True, stable=True).indices[:, :k]
+        assert torch.equal(top.long(), order)
+    assert torch.equal(ids.long(), torch.arange(64, device="cuda").expand(320, 64))
