@@ -458,9 +458,14 @@ cudaError_t stream_ent(const ScoreArgs& p, cudaStream_t s) {
 // rows of 253 KB: 64 MB 18.8 / 20.3 against 22.5 / 30.6, 32 MB 13.1 / 14.8 against 14.2 / 20.6, 16 MB 11.2 / 13.8
 // against 8.7 / 12.1; of 128 KB: 128 MB 30.2 / 34.4 against 38.1 / 51.0, 64 MB 23.2 / 27.6 against 22.3 / 31.2, 32
 // MB 18.7 / 24.4 against 14.2 / 20.1; of 64 KB: 512 MB 131 / 176 against 125 / 150.
+// Longer rows do not make the stream's start shorter (clusters of at most 4 CTAs, where a row of its own takes up to 16), so
+// that it takes as many bytes: 494 KB 64 rows 12.5 / 15.1 against 13.7 / 16.1, 48 rows 11.6 / 14.1 against 9.4 / 10.8, 16
+// rows 9.5 / 12.2 against 6.0 / 8.7; 1 MB 32 rows 12.3 / 15.1 against 13.9 / 17.4, 24 rows 11.5 / 14.0 against 12.2 / 15.4, 8 rows
+// 10.6 / 12.9 against 6.4 / 8.5; 1.9 MB 16 rows 18.2 / 19.1 against 22.4 / 26.8, 12 rows 18.0 / 18.9 against 15.8 / 19.3,
+// 1 row 16.9 / 17.7 against 7.2 / 9.4; 3 MB 12 rows 17.0 / 19.7 against 17.7 / 20.4, 4 rows 16.5 / 19.1 against 9.1 / 11.0.
 bool stream_pays(int rows, int64_t row_bytes) {
-  const double share = (256 << 10) / static_cast<double>(row_bytes);
-  return row_bytes >= 96 * 1024 && rows * row_bytes >= (24 << 20) * share * share;
+  const double share = (256 << 10) / static_cast<double>(row_bytes), least = share > 1.08 ? 24 * share * share : 28;  // MB
+  return row_bytes >= 96 * 1024 && rows * row_bytes >= least * (1 << 20);
 }
 
 template <typename T>
