@@ -222,7 +222,7 @@ typedef enum { SGD_F16 = 0, SGD_BF16 = 1, SGD_F32 = 2 } sgd_dtype;
  * Any of the outputs may be NULL (tokens with n_tokens = 0), but not all.  With rows = 0 nothing is done, and every
  * pointer may be NULL (so in sgd_kernel_distill).
  * logits [rows, vocab] of type dtype, rows ld elements apart, aligned to their elements alone.
- * scale > 0 (1 / temperature).  row_ids int32 [rows]: where given, only rows with row_ids[r] == row_id
+ * 0 < scale <= 2e38 (1 / temperature).  row_ids int32 [rows]: where given, only rows with row_ids[r] == row_id
  * (positions that are still masked, say) are read, and what the others' outputs held stays.
  * -inf masks a token: its ln p is -inf.  Finite logits may be of any magnitude (masks of the type's lowest value, of
  * -1e10), at any scale: what fp32 does not hold of their ln p is -inf.  A row of -inf alone has ln p = -inf, entropy 0 and the

@@ -64,6 +64,7 @@ DTYPES = {"float16": 0, "bfloat16": 1, "float32": 2}  # sgd_dtype, by torch's na
 TAIL_RENORM, TAIL_BUCKET = 0, 1
 TAIL = {"renorm": TAIL_RENORM, "bucket": TAIL_BUCKET}
 MAX_ROW_BYTES, REVEAL_MAX_TOKENS = 3 << 20, 49152  # of a row of logits; of a sample that is revealed
+MAX_SCALE = 2e38
 
 
 class sgd_model_desc(C.Structure):
@@ -527,8 +528,8 @@ class Denoiser:
             raise ValueError("step_tokens needs a token model (an embed stem and a logits head)")
         if c.d_out * 2 > MAX_ROW_BYTES or c.n_tokens > REVEAL_MAX_TOKENS:
             raise ValueError("the vocabulary or the sample is beyond what the operators on logits take")
-        if not 0.0 < C.c_float(scale).value < float("inf"):
-            raise ValueError("scale must be positive and finite")
+        if not 0.0 < C.c_float(scale).value <= C.c_float(MAX_SCALE).value:
+            raise ValueError("scale must be positive and at most 2e38")
         if not -2 ** 31 <= mask_id < 2 ** 31:
             raise ValueError("mask_id must be a 32-bit integer")
         device, i32, f32 = ids.device, torch.int32, torch.float32

@@ -1966,7 +1966,7 @@ int check_rows(const char* name, const void* logits, int dtype, int64_t ld, int 
   if (!logits && rows != 0) return fail(SGD_ERR_ARG, n + "null logits");  // (an empty tensor may have no address)
   if (dtype < SGD_F16 || dtype > SGD_F32) return fail(SGD_ERR_ARG, n + "unknown element type");
   if (rows < 0 || vocab < 1 || ld < vocab) return fail(SGD_ERR_ARG, n + "rows >= 0, vocab >= 1 and ld >= vocab are needed");
-  if (!(scale > 0.f) || !std::isfinite(scale)) return fail(SGD_ERR_ARG, n + "scale must be positive and finite");
+  if (!(scale > 0.f) || scale > kMaxScale) return fail(SGD_ERR_ARG, n + "scale must be positive and at most 2e38");
   if (reinterpret_cast<uintptr_t>(logits) % elem_size(dtype)) return fail(SGD_ERR_ARG, n + "misaligned logits");
   if (static_cast<int64_t>(vocab) * elem_size(dtype) > kMaxRowBytes)
     return fail(SGD_ERR_SHAPE, n + "a row of more than 3 MiB");

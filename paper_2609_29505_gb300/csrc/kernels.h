@@ -309,6 +309,7 @@ cudaError_t sampler_launch(float* z, const float* eps, float alpha, float beta, 
 constexpr int64_t kMaxRowBytes = 3ll << 20;
 constexpr int kMaxRows = 0x7FFFFFFF / 16;
 constexpr int kMaxTop = 64;
+constexpr float kMaxScale = 2e38f;  // times log2(e): in fp32's range
 
 // Rows of logits (sgd_kernel_logprobs).  dtype: sgd_dtype.
 struct LogprobsParams {
