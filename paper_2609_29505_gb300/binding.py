@@ -312,6 +312,13 @@ def _tensor(t, name, dtype, shape, device):
     raise ValueError(f"{name} must be contiguous")
 
 
+def _id(value, name):
+    """A token id as the library has it: ctypes would cut one of more than 32 bits down to another."""
+    if not -2 ** 31 <= value < 2 ** 31:
+        raise ValueError(f"{name} must be a 32-bit integer")
+    return value
+
+
 def _rows(t, name):
     """(type, row stride) of a [rows, vocab] tensor on a CUDA device with dense rows."""
     kind = _dtypes().get(t.dtype)
@@ -377,7 +384,7 @@ def sgd_kernel_logprobs(logits, tokens=None, token_logprobs=None, entropy=None, 
         k = top.shape[1]
     return _call_on(device, lib().sgd_kernel_logprobs, "sgd_kernel_logprobs", stream,
                     logits.data_ptr(), kind, ld, rows, vocab, scale,
-                    _tensor(row_ids, "row_ids", i32, (rows,), device), row_id,
+                    _tensor(row_ids, "row_ids", i32, (rows,), device), _id(row_id, "row_id"),
                     _tensor(tokens, "tokens", i32, (rows, n), device), n,
                     _tensor(token_logprobs, "token_logprobs", f32, (rows, n), device),
                     _tensor(entropy, "entropy", f32, (rows,), device), k,
@@ -444,7 +451,7 @@ def sgd_sampler_reveal(ids, cand, score, n_reveal, ids_out, mask_id, lowest=Fals
                     _tensor(n_reveal, "n_reveal", i32, (batch,), device),
                     _tensor(window, "window", i32, (batch, 2), device),
                     _tensor(ids_out, "ids_out", i32, shape, device),
-                    _tensor(n_left, "n_left", i32, (batch,), device), batch, n, mask_id)
+                    _tensor(n_left, "n_left", i32, (batch,), device), batch, n, _id(mask_id, "mask_id"))
 
 
 def make_desc(cfg, flags: int = 0) -> sgd_model_desc:
@@ -530,8 +537,7 @@ class Denoiser:
             raise ValueError("the vocabulary or the sample is beyond what the operators on logits take")
         if not 0.0 < C.c_float(scale).value <= C.c_float(MAX_SCALE).value:
             raise ValueError("scale must be positive and at most 2e38")
-        if not -2 ** 31 <= mask_id < 2 ** 31:
-            raise ValueError("mask_id must be a 32-bit integer")
+        _id(mask_id, "mask_id")
         device, i32, f32 = ids.device, torch.int32, torch.float32
         shape = (c.batch, c.n_tokens)
         for x, name, dtype, of in ((ids, "ids", i32, shape), (ids_out, "ids_out", i32, shape), (cand, "cand", i32, shape),

@@ -255,3 +255,14 @@ def test_lists_of_slices_of_few_tiles(B, rows, vocab, k):
         order = torch.sort(z.float(), dim=1, descending=True, stable=True).indices[:, :k]
         assert torch.equal(top.long(), order)
     assert torch.equal(ids.long(), torch.arange(64, device="cuda").expand(320, 64))
+
+
+def test_ids_of_more_than_32_bits_are_refused(B):
+    """2^32 would be cut down to token 0."""
+    z, e = _normal(2, 100, "f16", 1), torch.empty(2, device="cuda")
+    ids = torch.zeros(2, dtype=torch.int32, device="cuda")
+    for bad in (2 ** 32, 2 ** 31, -2 ** 31 - 1):
+        with pytest.raises(ValueError, match="row_id"):
+            B.sgd_kernel_logprobs(z, entropy=e, row_ids=ids, row_id=bad)
+        with pytest.raises(ValueError, match="mask_id"):
+            B.sgd_sampler_reveal(ids[None], ids[None], e[None], ids[:1], ids[None].clone(), bad)
