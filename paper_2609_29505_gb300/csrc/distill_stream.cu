@@ -6,8 +6,8 @@
 // Each buffer has a warp of its own that sees a row through, one step after another: it starts the bulk
 // copies, takes the list's tokens out of the slice (they become -inf), adds up the sums, exchanges them
 // with the cluster's other CTAs, gives the gradient its scalars, prepares the next row's list while the
-// gradient is written, starts the next copies, writes the list's own gradients and hands the row (in the CTA
-// of the cluster whose turn it is) to one of the warps that do the losses.  These steps are chains of latency (a
+// gradient is written, starts the next copies and writes the list's own gradients.  Once the scalars are there the row
+// goes (in the CTA of the cluster whose turn it is) to one of the warps that do the losses.  These steps are chains of latency (a
 // few us a row); as many of them as there are buffers run at once, and the 8 warps wait for none of them
 // but through the barriers of the buffers.
 //
@@ -19,7 +19,7 @@
 // writes their zeros: in a buffer's turn they would keep it from loading.
 //
 // Measured (GB300, replayed from a graph over rotating inputs), lists of 32, 126464 fp16 logits a row: 4096 rows
-// with a bf16 gradient 342 us = 6.1 TB/s (a copy moves 6.8): the 8 warps are busy for 5.1 of the 5.9 thousand
+// with a bf16 gradient 341 us = 6.1 TB/s (a copy moves 6.8): the 8 warps are busy for 5.1 of the 5.9 thousand
 // clocks of a row (sums 2.6, gradient 2.5), the rest is waiting for copies.  The loss alone, 1024 rows: 63 us
 // = 4.1 TB/s: a buffer's chain (copy, list, sums, exchange) over three buffers.  Three slices of 64 KB are what
 // an SM holds; clusters of 8 with slices of half the size leave 32 SMs idle (15 of them fit: 495 us).
@@ -502,15 +502,16 @@ static_assert(kBufferBytes + kMaxBuffers * (sizeof(Buffer) + sizeof(LossRow)) + 
 
 // Streaming against a cluster per row, us, the loss / with a bf16 gradient, fp16 logits:
 //   row       32 MB                 64 MB                  128 MB                   512 MB
-//   253 KB    17 / 22, 17 / 21      23 / 34, 26 / 38       35 / 56, 43 / 65         108 / 174, 147 / 220
-//   64 KB     17 / 27, 18 / 22      21 / 34, 27 / 38       31 / 55, 46 / 67         89 / 169, 156 / 230
-//   32 KB     16 / 25, 17 / 26      23 / 44, 30 / 47       35 / 78, 54 / 85         110 / 283, 196 / 323
-//   16 KB     19 / 37, 29 / 39      30 / 69, 50 / 75       50 / 133, 96 / 144       174 / 509, 367 / 566
-//   8.4 KB    27 / 61, 44 / 63      46 / 117, 83 / 124     84 / 228, 167 / 243      310 / 891, 648 / 954
-// with 256 threads a row.  With 64 threads, 64 and 512 MB: 32 KB 28 / 40, 155 / 227; 16 KB 32 / 43, 206 / 275; 8.4 KB
-// 49 / 61, 352 / 442.  So gradients of rows of up to 32 KB take 64 threads a row (the loss warps' code beside the
-// working warps' is what holds the stream back: 283 us are 194 without it), losses alone stream from 8 KB on; below
-// that 64 threads win both (65536 x 4000: 333 / 424 us).
+//   253 KB    17 / 21, 18 / 22      23 / 33, 27 / 39       35 / 54, 46 / 68         107 / 175, 160 / 231
+//   64 KB     17 / 26, 18 / 22      21 / 33, 28 / 38       31 / 54, 48 / 67         90 / 172, 168 / 232
+//   32 KB     16 / 25, 18 / 21      23 / 45, 32 / 42       36 / 82, 57 / 76         113 / 296, 208 / 284
+//   16 KB     18 / 38, 29 / 32      29 / 72, 50 / 60       48 / 138, 100 / 116      166 / 532, 377 / 435
+//   8.4 KB    28 / 67, 48 / 54      48 / 130, 90 / 104     89 / 254, 180 / 201      329 / 994, 704 / 783
+// with 256 threads a row.  With 64 threads, 64 and 512 MB: 253 KB 30 / 47, 179 / 278; 64 KB 31 / 47, 180 / 275; 32 KB 28 / 41,
+// 161 / 231; 16 KB 30 / 41, 198 / 259; 8.4 KB 49 / 60, 351 / 423.  So gradients of rows of up to 32 KB take 64 threads a row
+// (of the stream's time there a third is the loss warps' code beside the working warps' in the instruction cache), losses
+// alone stream from 8 KB on; below that 64 threads win the gradients and cost the losses little (4 KB, 512 MB: 675 / 765
+// against 608 / 1791).
 bool distill_stream_pays(int rows, int64_t row_bytes, bool grad) {
   return row_bytes > (grad ? kShortGradRow : 16 * kShortSlice) && rows * row_bytes >= kManyBytes &&
          kBufferBytes / (16 * static_cast<int64_t>(buffer_vectors(row_bytes, kMaxStreamCluster))) >= kMinBuffers;

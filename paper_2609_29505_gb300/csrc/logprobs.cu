@@ -8,8 +8,8 @@
 // (vocab_rows.cuh); many long rows stream through logprobs_stream.cu.
 //
 // Measured (GB300): 1 x 126464 fp16, the 4 likeliest tokens, entropy and one given token, on a cluster of 16:
-// 5.5 us, latency (the copy, four reductions, the cluster's barrier); 1003 x 32003 bf16, the 8 likeliest,
-// entropy, 4 given tokens: 29.5 us = 2.2 TB/s: three CTAs of 64 KB an SM, each without a copy on its way for
+// 5.8 us, latency (the copy, four reductions, the cluster's barrier); 1003 x 32003 bf16, the 8 likeliest,
+// entropy, 4 given tokens: 30 us = 2.1 TB/s: three CTAs of 64 KB an SM, each without a copy on its way for
 // half of its time.
 #include "logprobs.cuh"
 

@@ -12,8 +12,8 @@
 // loads does: a load takes some 3 us here, behind the copies that keep the memory busy.  For the single
 // likeliest token the tile of each thread's first maximum is enough.
 //
-// Measured (GB300, replayed from a graph over rotating inputs): 4096 x 126464 fp16, the 32 likeliest: 168 us =
-// 6.2 TB/s (a copy moves 6.8), bound by HBM; 2048 of 4096 rows, the likeliest one and the entropy: 90 us = 5.8
+// Measured (GB300, replayed from a graph over rotating inputs): 4096 x 126464 fp16, the 32 likeliest: 169 us =
+// 6.1 TB/s (a copy moves 6.8), bound by HBM; 2048 of 4096 rows, the likeliest one and the entropy: 92 us = 5.7
 // TB/s: a tile's 200 instructions a thread (conversion, fma, exponential, two sums, maximum, minimum) and its
 // copy take about as long.  8 streaming warps instead of 16: 127 us; two teams of 4 finishing warps instead of
 // single ones: 191 and 98 us (a team's barriers); 6 warps or 4: 174 and 193 us for the lists.

@@ -396,8 +396,8 @@ struct Launch {
 };
 constexpr int kSlice = 64 * 1024;
 // Vectors of a slice that 64 threads take instead of 256: what a row costs beside its elements (barriers,
-// reductions) is then a quarter.  131072 x 2000 fp16, 64 threads against 256: 436 / 827 us scored, 632 / 1377 us
-// for a loss, 747 / 1821 us with a gradient; 65536 x 4000: 247 / 430, 333 / 696, 424 / 937 us.
+// reductions) is then a quarter.  512 MB of 2000 fp16 logits a row, 64 threads against 256: 440 / 827 us scored, 675 / 1464
+// us for a loss, 765 / 1599 us with a gradient; of 4000 to 4200: 250 / 430, 351 / 704, 423 / 783 us.
 constexpr int kShortSlice = 512;
 constexpr int kMaxDynamic = (227 - 16) * 1024;  // beside at most 16 KB of static shared memory
 
