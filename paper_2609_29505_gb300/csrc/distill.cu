@@ -39,9 +39,8 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) distill_kernel(const
   __shared__ double q_sum[2];
   __shared__ float q_max[2];
   __shared__ int q_any[2];
-  __shared__ float4 parts[kWarps];
-  __shared__ float4 slot[kMaxCluster];
-  __shared__ float list_z[kMaxList];  // leader: the list's logits
+  __shared__ float2 parts[kWarps], slot[kMaxCluster];  // {maximum, sum} of the tail, of warps and CTAs
+  __shared__ float list_z[kMaxList];                   // the list's logits, in every CTA
   const int rank = cluster_rank();
   const uint32_t n_ctas = cluster_ctas();
   const int64_t r = blockIdx.x / n_ctas;
@@ -90,6 +89,7 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) distill_kernel(const
           id = -1;
           break;
         }
+    if (id < 0) list_z[threadIdx.x] = -kInf;  // no entry
     q = id >= 0 ? expf(lq) : 0.f;
     __syncwarp();
     const double sum = warp_sum(static_cast<double>(q));
@@ -129,7 +129,7 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) distill_kernel(const
     T* e = reinterpret_cast<T*>(buf + vec) + sl.place_of(id);
     z = to_f(*e);
     *e = neg_inf<T>();
-    st_cluster(map_to_rank(smem_u32(&list_z[threadIdx.x]), 0), z);
+    for (uint32_t i = 0; i < n_ctas; ++i) st_cluster(map_to_rank(smem_u32(&list_z[threadIdx.x]), i), z);
   }
   __syncthreads();
 
@@ -145,29 +145,25 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) distill_kernel(const
     }
     stat_add<T, kUnroll, false>(st, v, c, 0.f);
   }
-  // the CTA's sums, of the tail and of its part of S
-  const float3 tail = warp_stat<T, false>(st, c, threadIdx.x, kThreads, sl.nv, InShared{buf});
-  {
-    const float m = key_value(__reduce_max_sync(0xffffffffu, order_key(z)));
-    const float in = warp_sum(vec >= 0 ? ex2_approx(exponent(z, m, reference(m, c), c)) : 0.f);
-    if (lane == 0) parts[warp] = make_float4(tail.x, tail.y, m, in);
-  }
+  // the tail's sums, over the CTA and the cluster
+  const float3 of_warp = warp_stat<T, false>(st, c, threadIdx.x, kThreads, sl.nv, InShared{buf});
+  if (lane == 0) parts[warp] = make_float2(of_warp.x, of_warp.y);
   __syncthreads();
-  if (n_ctas > 1 && warp == 0) {
-    float4 v = lane < kWarps ? parts[lane] : make_float4(-kInf, 0.f, -kInf, 0.f);
-    const float m = key_value(__reduce_max_sync(0xffffffffu, order_key(v.x)));
-    const float m_list = key_value(__reduce_max_sync(0xffffffffu, order_key(v.z)));
-    float unused = 0.f;
-    rebase(v.x, c, m, reference(m, c), v.y, unused);
-    rebase(v.z, c, m_list, reference(m_list, c), v.w, unused);
-    v.y = warp_sum(v.y);
-    v.w = warp_sum(v.w);
-    if (lane < n_ctas) st_cluster(map_to_rank(smem_u32(&slot[rank]), lane), make_float4(m, v.y, m_list, v.w));
+  const float2 none_here = make_float2(-kInf, 0.f);
+  float2 v = none_here;
+  if (n_ctas > 1) {
+    if (warp == 0) {
+      v = join_parts(lane < kWarps ? parts[lane] : none_here, c);
+      if (lane < n_ctas) st_cluster(map_to_rank(smem_u32(&slot[rank]), lane), v);
+    }
+    __syncwarp();
+    cluster_sync();
+    if (lane < n_ctas) v = slot[lane];
+    else v = none_here;
+  } else if (lane < kWarps) {
+    v = parts[lane];
   }
-  __syncwarp();
-  if (n_ctas > 1) cluster_sync();
-
-  const RowSums sums = n_ctas > 1 ? row_sums(slot, n_ctas, c) : row_sums(parts, kWarps, c);
+  const RowSums sums = sums_with_list(v, list_z[lane], list_z[lane + 32], c);
   const ListSums ls = list_sums(Q, p.bucket);
   const RowScale o = row_scale(sums, ls, w, p.scale, p.bucket, c);
   if constexpr (kGrad) {
@@ -182,7 +178,6 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) distill_kernel(const
   if (threadIdx.x < kMaxList) {
     list_q[threadIdx.x] = q;
     list_lq[threadIdx.x] = lq;
-    if (id < 0) list_z[threadIdx.x] = -kInf;  // no entry
   }
   __syncthreads();
   if (warp == 0) {

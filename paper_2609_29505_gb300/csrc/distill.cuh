@@ -156,6 +156,22 @@ __device__ __forceinline__ RowSums join_sums(float tail_max, float tail, float l
   return RowSums{all, tail_max, tail, in};
 }
 
+// A warp's {maximum, sum} of the tail as one.
+__device__ __forceinline__ float2 join_parts(float2 v, float c) {
+  const float m = key_value(__reduce_max_sync(0xffffffffu, order_key(v.x)));
+  float unused = 0.f;
+  rebase(v.x, c, m, reference(m, c), v.y, unused);
+  return make_float2(m, warp_sum(v.y));
+}
+// From the parts of the tail {maximum, sum} and the list's logits, two a lane (a whole warp; every lane gets them).
+__device__ __forceinline__ RowSums sums_with_list(float2 v, float z0, float z1, float c) {
+  const float list_max = key_value(__reduce_max_sync(0xffffffffu, max(order_key(z0), order_key(z1))));
+  const float2 tail = join_parts(v, c);
+  const float all = fmaxf(tail.x, list_max), R = reference(all, c);
+  const float in = warp_sum(ex2_approx(exponent(z0, all, R, c)) + ex2_approx(exponent(z1, all, R, c)));
+  return RowSums{all, tail.x, tail.y, in};
+}
+
 // From the CTAs' parts {the tail's maximum and sum, the list's} (a whole warp; every lane gets them).
 __device__ __forceinline__ RowSums row_sums(const float4* slot, int n_ctas, float c) {
   const int lane = lane_id();

@@ -112,10 +112,9 @@ __device__ __forceinline__ void candidates(const WarpTeam& team, const Slice<T>&
   int groups = 0;
   // (a slice of few tiles has fewer parts: no one has written the others' maxima)
   const int tiles = tiles_of(sl), per_part = tiles_of_part(tiles), parts = (tiles + per_part - 1) / per_part;
-  const float parts_inv = 1.f / parts;
-  for (int j0 = 0; j0 < n * parts; j0 += 32) {
-    const int j = j0 + lane, t = static_cast<int>((j + 0.5f) * parts_inv);  // j / parts: exact, j is far below 2^22
-    const int g = j < n * parts ? (j - t * parts) * kStreamThreads + x.max_tile[t] : -1;
+  for (int j0 = 0; j0 < n * kParts; j0 += 32) {
+    const int j = j0 + lane;
+    const int g = j < n * kParts && j % kParts < parts ? j % kParts * kStreamThreads + x.max_tile[j / kParts] : -1;
     const bool is = g >= 0 && many.group_key[max(g, 0)] >= lo >> 16;
     const uint32_t hit = __ballot_sync(0xffffffffu, is);
     const int at = groups + __popc(hit & ((1u << lane) - 1u));
