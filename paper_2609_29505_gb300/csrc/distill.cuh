@@ -291,7 +291,7 @@ __device__ __forceinline__ float row_loss(const RowScale& o, const RowSums& r, c
   for (int h = 0; h < N; ++h) {
     const Float2 d = two_sum(z[h], -r.all), p = two_prod(d.hi, scale);
     x[h] = Float2{p.hi, fmaf(d.lo, scale, p.lo)};
-    if (!isfinite(p.hi)) x[h] = Float2{z[h] * scale - r.all * scale, 0.f};  // (the difference was out of range)
+    if (!isfinite(p.hi)) x[h] = Float2{-kInf, 0.f};  // (out of fp32's range, or z is -inf)
     if (q[h] == 0.f || z[h] == -kInf) continue;  // no entry, or no weight (left to `in`), or no probability
     const float e = expf(x[h].hi);
     sum += static_cast<double>(fmaf(e, x[h].lo, e));
@@ -312,7 +312,8 @@ __device__ __forceinline__ float row_loss(const RowScale& o, const RowSums& r, c
   for (int h = 0; h < N; ++h) {
     if (q[h] == 0.f) continue;  // (a NaN is no 0)
     const Float2 diff = Float2{lq[h], 0.f} + -x[h] + ln_s;
-    terms += o.empty || x[h].hi == -kInf ? q[h] * kInf : q[h] * (diff.hi + diff.lo);
+    if (x[h].hi > -kInf) terms += q[h] * (diff.hi + diff.lo);
+    else terms += o.empty || z[h] == -kInf ? q[h] * kInf : -q[h] * scale * (static_cast<double>(z[h]) - r.all);
   }
   terms = warp_sum(terms);
   const float hi = static_cast<float>(terms);
@@ -322,11 +323,10 @@ __device__ __forceinline__ float row_loss(const RowScale& o, const RowSums& r, c
     const Float2 L = Float2{q1, rest / l.Q} + -ln2parts(l.Q) + Float2{-l.Q_lo / l.Q, 0.f};
     return w * (L.hi + L.lo);
   }
-  float of_tail = 0.f;
+  double of_tail = 0.0;
   if (o.pulls && tail < 1e-18f * s.hi) {
     const float delta_tail = delta_of(r.tail_max, c, reference(r.tail_max, c));
-    float below = (r.tail_max - r.all) * scale;
-    if (below == -kInf) below = r.tail_max * scale - r.all * scale;
+    const double below = scale * (static_cast<double>(r.tail_max) - r.all);  // (may be out of fp32's range)
     of_tail = l.q_tail * (logf(l.q_tail) - (logf(r.tail) - delta_tail * kLn2) + (ln_s.hi + ln_s.lo) - below);
   } else if (o.pulls) {
     const Float2 qs = two_prod(l.Q, s.hi);

@@ -74,9 +74,8 @@ __device__ __forceinline__ void finish(const Tm& team, const ScoreArgs& p, int64
   team.sync();
   const float all = result[0], ln_s = result[1];
   auto logprob = [&](float z) {
-    float d = (z - all) * p.scale;
-    if (d == -kInf && z > -kInf) d = z * p.scale - all * p.scale;  // (their difference may be out of range where this is not)
-    return d - ln_s;
+    const float d = z - all;  // (where it is out of range it may not be so scaled)
+    return (d == -kInf && z > -kInf ? z * p.scale - all * p.scale : d * p.scale) - ln_s;
   };
   if (team.tid < p.n_tokens)
     p.token_logprobs[r * p.n_tokens + team.tid] = given.token < 0 ? 0.f : logprob(given.z);

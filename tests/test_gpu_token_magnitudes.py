@@ -181,3 +181,29 @@ def test_distillation_at_a_large_scale(B, dtype):
     loss, g = torch.empty(len(z), device="cuda"), torch.empty(z.shape, device="cuda")
     B.sgd_kernel_distill(z, ids, logq, loss, grad=g, tail=B.TAIL_RENORM, scale=1e8)
     _check_distill(loss, g, z, ids, logq, 1e8, False)
+
+
+@pytest.mark.parametrize("scale", [10.0, 0.25, 1.0])
+def test_rows_whose_scaled_logits_are_out_of_range(B, scale):
+    """Largest logits of -1e38 and 3e38: scaled ones, their differences or both are out of fp32's range; what is below that
+    has -inf for ln p, and a listed one an infinite loss."""
+    vocab = 300
+    rng = np.random.default_rng(8)
+    z = np.full((4, vocab), -3.2e38)
+    z[0, ::3] = -1e38
+    z[1, ::3] = 3e38
+    z[2, :] = -3e38 + 1e37 * rng.random(vocab)
+    z[3, ::3], z[3, 1::3] = -1e38, -1e38 * (1 + 2.0 ** -20)
+    z = torch.from_numpy(z).float().cuda()
+    got, tokens = _score(B, z, k=5, n=3, scale=scale, tokens=torch.tensor([[0, 1, 2]] * 4, dtype=torch.int32))
+    _check(got, tokens, z, 5, scale)
+    ids = torch.tensor([[0, 1]] * 4, dtype=torch.int32, device="cuda")
+    logq = torch.log(torch.tensor([[0.5, 0.25]] * 4, device="cuda"))
+    for tail in (B.TAIL_BUCKET, B.TAIL_RENORM):
+        loss, g = torch.empty(4, device="cuda"), torch.empty(z.shape, device="cuda")
+        B.sgd_kernel_distill(z, ids, logq, loss, grad=g, tail=tail, scale=scale)
+        for r in range(4):
+            L, want = ot.distill_row(_np(z[r]), [0, 1], _np(logq[r]), scale, tail == B.TAIL_BUCKET)
+            L = np.inf if L > 3.4028235e38 else L
+            assert loss[r].item() == L or abs(loss[r].item() - L) <= 16 * U * L, (r, loss[r].item(), L)
+            assert np.abs(_np(g[r]) - want).max() <= scale * 8 * SUM
