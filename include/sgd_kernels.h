@@ -16,8 +16,9 @@
  *     for a run of consecutive frozen units).
  *
  * Beside them stand operators on what a token model's step writes, its logits, for programs that turn them
- * into tokens or compare two evaluations: sgd_kernel_logprobs and sgd_kernel_distill (and sgd.h's
- * sgd_sampler_reveal).
+ * into tokens or compare two evaluations: sgd_kernel_logprobs, sgd_kernel_sample and sgd_kernel_distill (and sgd.h's
+ * sgd_sampler_reveal); and, for programs that train a token model's ends on that gradient, its embedding with the table's
+ * gradient and the norms' backward pass.
  *
  * All pointers are device pointers; all calls are asynchronous on `stream`
  * (a cudaStream_t) and return an sgd_status (sgd.h).  Arguments are validated on
@@ -273,6 +274,83 @@ SGD_API int sgd_kernel_distill(const void* logits, int dtype, int64_t ld, int ro
                                const int32_t* teacher_ids, const float* teacher_logprobs, int top_k,
                                const float* row_weight, int tail, float* loss, void* grad, int grad_dtype,
                                int64_t ld_grad, void* stream);
+
+/* Tokens of a block of the vocabulary (sgd_kernel_sample). */
+#define SGD_SAMPLE_BLOCK 512
+
+/*
+ * A token drawn from each row of logits.  With x = scale * logits[r, :], w = exp(x - max x) and the tokens in the order
+ * (logit descending, token ascending; -0 and +0 are equal), the tokens that may be drawn are
+ *   K1: of the first top_k of the order (0, or vocab and more: of all) those with w >= min_p (0: all);
+ *   K: the shortest prefix of K1, in the order, whose mass (sum of w) is at least top_p times K1's (1: all of K1).
+ * Two numbers u0, u1 in [0, 1) a row (uniforms fp32 [rows, 2]; what lies outside is taken as 0 or 1, NaN as 0) choose
+ *   b, the first block of SGD_SAMPLE_BLOCK neighbouring tokens whose cumulative mass (of K's tokens, blocks ascending) is above
+ *     u0 mass(K), and the first token of K in b whose cumulative mass inside b (tokens ascending) is above u1 mass(b);
+ *     the last one of positive mass where rounding leaves none.
+ * With independent uniform numbers that is a draw from w over K, with the resolution of both.  Masses are compared as
+ * 64-bit arithmetic has them (to 2^-30 relative; tokens below 2^-44 of the maximum have none).
+ *   ids int32 [rows] = the token;  logprobs fp32 [rows] (NULL: not wanted) = its ln p, p = softmax(x) over all tokens.
+ * scale = 1 / temperature, 0 < scale <= 2e38.  top_k >= 0, 0 < top_p <= 1, 0 <= min_p <= 1 (else SGD_ERR_ARG).
+ * row_ids, row_id, the rows of logits and their limits as in sgd_kernel_logprobs.  -inf masks a token.  A row without a
+ * distribution takes the first token of the order: one of -inf alone token 0 with ln p = -inf, one that holds NaN
+ * (which ranks with -inf) or +inf its ln p = NaN.
+ * No output may overlap an input or the other output.  No workspace: calls on several streams and replays of captured
+ * ones may overlap.  Results are the same on every run.
+ */
+SGD_API int sgd_kernel_sample(const void* logits, int dtype, int64_t ld, int rows, int vocab, float scale, int top_k, double top_p,
+                              double min_p, const float* uniforms, const int32_t* row_ids, int row_id, int32_t* ids,
+                              float* logprobs, void* stream);
+
+/*
+ * out[r, :] = scale * table[ids[r], :], rounded once from fp32 (out of fp16's range: inf); zeros where ids[r] is not in [0, vocab)
+ * (padding).  table [vocab, d] of type dtype, rows ld elements apart; ids int32 [rows]; out [rows, d] of type
+ * out_dtype, rows ld_out elements apart; both aligned to their elements alone.  1 <= d <= 2^20.  out must not overlap
+ * the table or the ids (SGD_ERR_ARG).
+ */
+SGD_API int sgd_kernel_embedding(const void* table, int dtype, int64_t ld, int vocab, int d, const int32_t* ids, int rows, float scale,
+                                 void* out, int out_dtype, int64_t ld_out, void* stream);
+
+/* Bytes of workspace of sgd_kernel_embedding_grad. */
+SGD_API int sgd_kernel_embedding_grad_workspace(int rows, int vocab, int d, int64_t* bytes);
+
+/*
+ * Gradient of sgd_kernel_embedding's table: with S[t] = scale * sum of grad[r, :] over the rows r with ids[r] = t, in fp32 and in
+ * one order (that of the rows, and of groups of 16 to 64 rows sorted by token for tokens with many),
+ *   accumulate = 0: dtable[t, :] = S[t] for every t in [0, vocab), zeros for tokens without a row;
+ *   accumulate = 1: dtable[t, :] += S[t] for the tokens that have rows; the others are neither read nor written;
+ * each rounded once from fp32.  Rows whose id is not in [0, vocab) are left out, and not read.
+ * grad [rows, d] of type grad_dtype, rows ld_grad elements apart; dtable [vocab, d] of type dtable_dtype, rows ld
+ * elements apart; both aligned to their elements alone.  1 <= d <= 2^20.  workspace: 16-byte aligned, of the size that
+ * sgd_kernel_embedding_grad_workspace gives (else SGD_ERR_ARG); what it holds before and after means nothing.  Calls
+ * and replays that may overlap need one each.  dtable must not overlap another argument (SGD_ERR_ARG).  Results are the same
+ * on every run.
+ */
+SGD_API int sgd_kernel_embedding_grad(const void* grad, int grad_dtype, int64_t ld_grad, const int32_t* ids, int rows, int vocab,
+                                      int d, float scale, int accumulate, void* dtable, int dtable_dtype, int64_t ld,
+                                      void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Bytes of workspace of sgd_kernel_norm_grad (rows_per_batch: 0 without a modulation). */
+SGD_API int sgd_kernel_norm_grad_workspace(int rows, int d, int rows_per_batch, int64_t* bytes);
+
+/*
+ * Backward pass of sgd_kernel_norm.  With xhat = (h - mean) rstd of a row (no mean for SGD_NORM_RMS), n = xhat g + b and
+ * out = n (1 + scale) + shift as there, and dout = dL / dout:
+ *   dn = dout (1 + scale), dx = dn g,
+ *   dh fp32 [rows, d] = rstd (dx - mean(dx) - xhat mean(dx xhat)) + residual, without mean(dx) for SGD_NORM_RMS
+ *     (residual fp32 [rows, d], NULL: 0: what reaches h past the branch; dh may be residual itself);
+ *   dg fp32 [d] = sum over the rows of dn xhat, db fp32 [d] = sum of dn;
+ *   dshift, dscale fp32 [samples, ld_dmod] = sums over a sample's rows of dout and of dout n.
+ * Any of the outputs may be NULL, but not all; dg needs g, db needs b, dshift and dscale need scale, residual needs dh.
+ * h fp32 [rows, d], dout [rows, d] of type dtype, g, b bf16 [d] or NULL, scale fp32 [samples, ld_mod] or NULL, row r of sample
+ * r / rows_per_batch.  d a multiple of 4, 4 <= d <= 4096; h, dh, residual, dg, db and fp32 dout 16-byte aligned, other dout,
+ * g and b 8-byte aligned.  Sums are fp32 (over 8 rows or more at a time, then over those) and the same on every run.
+ * With rows = 0, dg and db are zeros.  workspace as in sgd_kernel_embedding_grad; none is needed where dh is the only
+ * output.  No output may overlap another argument otherwise (SGD_ERR_ARG for dh on h, dout or residual).
+ */
+SGD_API int sgd_kernel_norm_grad(const float* h, const void* dout, int dtype, int rows, int d, int kind, const void* g,
+                                 const void* b, const float* scale, int ld_mod, int rows_per_batch, float eps,
+                                 const float* residual, float* dh, float* dg, float* db, float* dshift, float* dscale,
+                                 int ld_dmod, void* workspace, int64_t workspace_bytes, void* stream);
 
 /* Device status word shared by all kernels (bounded-wait expiry); returns and clears it. */
 SGD_API int sgd_kernel_status(int* status_host);

@@ -56,7 +56,8 @@ EXPORTED = [
     "sgd_set_exec_mode", "sgd_step_host_async", "sgd_host_wait", "sgd_kernel_gemm_static_ws",
     "sgd_set_policy", "sgd_get_drift", "sgd_selftest_wait_timeout", "sgd_kernel_f16_clamped",
     "sgd_kernel_gemm_stat_slots", "sgd_kernel_attention_hs", "sgd_kernel_dependent_launches", "sgd_kernel_gemm_tile",
-    "sgd_kernel_logprobs", "sgd_kernel_distill", "sgd_sampler_reveal",
+    "sgd_kernel_logprobs", "sgd_kernel_distill", "sgd_sampler_reveal", "sgd_kernel_sample", "sgd_kernel_embedding",
+    "sgd_kernel_embedding_grad", "sgd_kernel_embedding_grad_workspace", "sgd_kernel_norm_grad", "sgd_kernel_norm_grad_workspace",
 ]
 EXEC_JAGGED_GRAPH, EXEC_EAGER, EXEC_PADDED_GRAPH = 0, 1, 2
 POLICY_STATIC, POLICY_DRIFT = 0, 1
@@ -166,6 +167,12 @@ def lib() -> C.CDLL:
             "sgd_kernel_logprobs": (i, [vp, i, i64, i, i, f, vp, i, vp, i, vp, vp, i, vp, vp, vp]),
             "sgd_kernel_distill": (i, [vp, i, i64, i, i, f, vp, vp, i, vp, i, vp, vp, i, i64, vp]),
             "sgd_sampler_reveal": (i, [vp, vp, i64, vp, i64, i, vp, vp, vp, vp, i, i, i, vp]),
+            "sgd_kernel_sample": (i, [vp, i, i64, i, i, f, i, C.c_double, C.c_double, vp, vp, i, vp, vp, vp]),
+            "sgd_kernel_embedding": (i, [vp, i, i64, i, i, vp, i, f, vp, i, i64, vp]),
+            "sgd_kernel_embedding_grad_workspace": (i, [i, i, i, C.POINTER(i64)]),
+            "sgd_kernel_embedding_grad": (i, [vp, i, i64, vp, i, i, i, f, i, vp, i, i64, vp, i64, vp]),
+            "sgd_kernel_norm_grad_workspace": (i, [i, i, i, C.POINTER(i64)]),
+            "sgd_kernel_norm_grad": (i, [vp, vp, i, i, i, i, vp, vp, vp, i, i, f, vp, vp, vp, vp, vp, vp, i, vp, i64, vp]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)
@@ -392,6 +399,144 @@ def sgd_kernel_logprobs(logits, tokens=None, token_logprobs=None, entropy=None, 
                     _tensor(top_logprobs, "top_logprobs", f32, (rows, k), device))
 
 
+def sgd_kernel_sample(logits, uniforms, ids, logprobs=None, scale=1.0, top_k=0, top_p=1.0, min_p=0.0, row_ids=None, row_id=0,
+                      stream=None):
+    """A token drawn from each row of logits [rows, vocab] (any row stride) by two numbers in [0, 1) a row (uniforms
+    float32 [rows, 2]) into ids int32 [rows], and its log-probability (under softmax(scale * logits), whatever is filtered
+    out) into logprobs float32 [rows]: from the top_k likeliest tokens (0: all) that have at least min_p times the
+    likeliest one's probability, and of those from the likeliest that together have the share top_p.  scale is 1 /
+    temperature.  With row_ids (int32 [rows]) only rows whose entry is row_id are read and written."""
+    import torch
+    kind, ld = _rows(logits, "logits")
+    rows, vocab = logits.shape
+    device, i32, f32 = logits.device, torch.int32, torch.float32
+    return _call_on(device, lib().sgd_kernel_sample, "sgd_kernel_sample", stream,
+                    logits.data_ptr(), kind, ld, rows, vocab, scale, _id(top_k, "top_k"), top_p, min_p,
+                    _tensor(uniforms, "uniforms", f32, (rows, 2), device),
+                    _tensor(row_ids, "row_ids", i32, (rows,), device), _id(row_id, "row_id"),
+                    _tensor(ids, "ids", i32, (rows,), device), _tensor(logprobs, "logprobs", f32, (rows,), device))
+
+
+def sgd_kernel_embedding(table, ids, out, scale=1.0, stream=None):
+    """out [rows, d] = scale * table[ids] for table [vocab, d] and ids int32 [rows], table and out of any of the three types and
+    any row stride; zeros where an id is not in the table."""
+    import torch
+    kind, ld = _rows(table, "table")
+    okind, ldo = _rows(out, "out")
+    vocab, d = table.shape
+    rows = out.shape[0]
+    if out.shape[1] != d or out.device != table.device:
+        raise ValueError("out must have the width and the device of table")
+    return _call_on(table.device, lib().sgd_kernel_embedding, "sgd_kernel_embedding", stream,
+                    table.data_ptr(), kind, ld, vocab, d, _tensor(ids, "ids", torch.int32, (rows,), table.device), rows, scale,
+                    out.data_ptr(), okind, ldo)
+
+
+def sgd_kernel_embedding_grad_workspace(rows, vocab, d) -> int:
+    """Bytes of workspace of sgd_kernel_embedding_grad."""
+    n = C.c_int64(0)
+    check(lib().sgd_kernel_embedding_grad_workspace(rows, vocab, d, C.byref(n)), "sgd_kernel_embedding_grad_workspace")
+    return int(n.value)
+
+
+def _workspace(workspace, need, device, stream):
+    """(workspace, bytes): the given one, or one of torch's allocator on the stream the call goes to."""
+    import torch
+    if workspace is None:
+        if stream is None:
+            with torch.cuda.device(device):
+                workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        else:
+            # (an integer handle: torch's allocator has to know which stream uses the memory)
+            st = torch.cuda.ExternalStream(stream, device=device) if isinstance(stream, int) else stream
+            with torch.cuda.device(device), torch.cuda.stream(st):
+                workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        return workspace, need
+    if workspace.device != device or not workspace.is_contiguous():
+        raise ValueError(f"the workspace must be contiguous and on {device}")
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def sgd_kernel_embedding_grad(grad, ids, dtable, scale=1.0, accumulate=False, workspace=None, stream=None):
+    """dtable [vocab, d] = (with accumulate: +=) scale * sum of grad [rows, d] over the rows of each token of ids int32 [rows];
+    both of any of the three types and any row stride.  workspace: a tensor of sgd_kernel_embedding_grad_workspace bytes
+    (None: allocated for the call)."""
+    import torch
+    kind, ld = _rows(grad, "grad")
+    tkind, ldt = _rows(dtable, "dtable")
+    rows, d = grad.shape
+    vocab, device = dtable.shape[0], grad.device
+    if dtable.shape[1] != d or dtable.device != device:
+        raise ValueError("dtable must have the width and the device of grad")
+    at = _tensor(ids, "ids", torch.int32, (rows,), device)
+    need = sgd_kernel_embedding_grad_workspace(rows, vocab, d) if workspace is None else 0
+    ws, n = _workspace(workspace, need, device, stream)
+    return _call_on(device, lib().sgd_kernel_embedding_grad, "sgd_kernel_embedding_grad", stream,
+                    grad.data_ptr(), kind, ld, at, rows, vocab, d, scale, int(accumulate), dtable.data_ptr(), tkind, ldt,
+                    ws.data_ptr(), n)
+
+
+def sgd_kernel_norm_grad_workspace(rows, d, rows_per_batch=0) -> int:
+    """Bytes of workspace of sgd_kernel_norm_grad (rows_per_batch 0: without a modulation)."""
+    n = C.c_int64(0)
+    check(lib().sgd_kernel_norm_grad_workspace(rows, d, rows_per_batch, C.byref(n)), "sgd_kernel_norm_grad_workspace")
+    return int(n.value)
+
+
+def _modulation(t, name, samples, d, device):
+    """(address, row stride) of a float32 [samples, d] tensor with dense rows (one part of a wider modulation, say)."""
+    import torch
+    if t.dtype is not torch.float32:
+        raise TypeError(f"{name} must be torch.float32, not {t.dtype}")
+    if t.shape != (samples, d) or t.device != device:
+        raise ValueError(f"{name} must have the shape {(samples, d)} and be on {device}")
+    if t.stride(1) != 1:
+        raise ValueError(f"the rows of {name} must be dense")
+    return t.data_ptr(), t.stride(0) if samples > 1 else max(t.stride(0), d)
+
+
+def sgd_kernel_norm_grad(dout, h, kind, dh=None, g=None, b=None, scale=None, rows_per_batch=1, eps=1e-6, residual=None, dg=None,
+                         db=None, dshift=None, dscale=None, workspace=None, stream=None):
+    """Backward pass of sgd_kernel_norm on h float32 [rows, d]: from dout [rows, d] (any of the three types) the gradients
+    that are given, dh float32 [rows, d] (plus residual float32 [rows, d], which may be dh), dg and db float32 [d] for
+    g and b bfloat16 [d], dshift and dscale float32 [samples, d] (of one row stride) for the modulation scale float32 [samples, d]
+    of rows_per_batch rows a sample.  workspace: a tensor of sgd_kernel_norm_grad_workspace bytes (None: allocated for
+    the call)."""
+    import torch
+    bf16, f32 = torch.bfloat16, torch.float32
+    if h.dim() != 2 or not h.is_cuda:
+        raise ValueError("h must be a 2-d tensor on a CUDA device")
+    shape, device = h.shape, h.device
+    rows, d = shape
+    code = _dtypes().get(dout.dtype)
+    if code is None:
+        raise TypeError(f"dout must be float16, bfloat16 or float32, not {dout.dtype}")
+    at_scale, ld, at_shift, at_dscale, ldd = None, 0, None, None, 0
+    if scale is None and (dshift is not None or dscale is not None):
+        raise ValueError("dshift and dscale need scale")
+    if scale is not None:
+        if rows_per_batch < 1:
+            raise ValueError("rows_per_batch must be positive")
+        samples = -(-rows // rows_per_batch)
+        at_scale, ld = _modulation(scale, "scale", samples, d, device)
+        if dshift is not None:
+            at_shift, ldd = _modulation(dshift, "dshift", samples, d, device)
+        if dscale is not None:
+            at_dscale, ld2 = _modulation(dscale, "dscale", samples, d, device)
+            if dshift is not None and samples > 1 and ld2 != ldd:
+                raise ValueError("dshift and dscale must have one row stride")
+            ldd = max(ldd, ld2)
+    args = (_tensor(h, "h", f32, shape, device), _tensor(dout, "dout", dout.dtype, shape, device), code, rows, d, kind,
+            _tensor(g, "g", bf16, (d,), device), _tensor(b, "b", bf16, (d,), device), at_scale, ld, rows_per_batch, eps,
+            _tensor(residual, "residual", f32, shape, device), _tensor(dh, "dh", f32, shape, device),
+            _tensor(dg, "dg", f32, (d,), device), _tensor(db, "db", f32, (d,), device), at_shift, at_dscale, ldd)
+    need = 0
+    if workspace is None and (dg is not None or db is not None or ldd):
+        need = sgd_kernel_norm_grad_workspace(rows, d, 0 if scale is None else rows_per_batch)
+    ws, n = _workspace(workspace, need, device, stream) if need or workspace is not None else (None, 0)
+    return _call_on(device, lib().sgd_kernel_norm_grad, "sgd_kernel_norm_grad", stream, *args, _ptr(ws), n)
+
+
 def sgd_kernel_distill(logits, teacher_ids, teacher_logprobs, loss, grad=None, row_weight=None, tail=TAIL_BUCKET,
                        scale=1.0, stream=None):
     """Divergence of logits [rows, vocab] from the teacher's lists [rows, k] (sgd_kernel_logprobs' top_ids and
@@ -519,14 +664,15 @@ class Denoiser:
 
     def step_tokens(self, ids, ids_out, logits, t: float, step: int, cand, score, n_reveal, mask_id: int,
                     by: str = "confidence", scale: float = 1.0, window=None, n_left=None, stream=None, class_ids=None,
-                    ctx=None):
+                    ctx=None, uniforms=None, top_k: int = 0, top_p: float = 1.0, min_p: float = 0.0):
         """One step of a masked-token trajectory (argmax remasking), queued on one stream: the denoiser on ids
         int32 [B, N] (with class_ids int32 [B] and ctx bf16 [B, L, d_ctx] as step takes them) into logits fp16 [B, N, V],
         the best token of every masked position into cand int32 [B, N] with its log-probability (by "confidence") or its
         row's entropy (by "entropy") in score float32 [B, N], and the n_reveal best of them revealed in ids_out
         (which may be ids).  What cand and score hold at other positions stays.  A position whose best token is
-        mask_id itself counts as revealed in n_left, and stays masked.  The arguments are checked before the step is
-        launched (TypeError / ValueError)."""
+        mask_id itself counts as revealed in n_left, and stays masked.  With uniforms float32 [B, N, 2] candidates are drawn
+        (sgd_kernel_sample, with scale, top_k, top_p and min_p) instead of the best.  The arguments are checked before
+        the step is launched (TypeError / ValueError)."""
         import torch
         if by not in ("confidence", "entropy"):
             raise ValueError("by must be confidence or entropy")
@@ -538,6 +684,10 @@ class Denoiser:
         if not 0.0 < C.c_float(scale).value <= C.c_float(MAX_SCALE).value:
             raise ValueError("scale must be positive and at most 2e38")
         _id(mask_id, "mask_id")
+        if uniforms is None and (top_k, top_p, min_p) != (0, 1.0, 0.0):
+            raise ValueError("top_k, top_p and min_p go with uniforms: without, the best token is taken")
+        if not (0 <= _id(top_k, "top_k") and 0.0 < top_p <= 1.0 and 0.0 <= min_p <= 1.0):
+            raise ValueError("top_k must not be negative, top_p be above 0 and at most 1, min_p in 0..1")
         device, i32, f32 = ids.device, torch.int32, torch.float32
         shape = (c.batch, c.n_tokens)
         for x, name, dtype, of in ((ids, "ids", i32, shape), (ids_out, "ids_out", i32, shape), (cand, "cand", i32, shape),
@@ -548,15 +698,22 @@ class Denoiser:
             _tensor(x, name, dtype, of, device)
         _tensor(window, "window", i32, (c.batch, 2), device)
         _tensor(n_left, "n_left", i32, (c.batch,), device)
+        _tensor(uniforms, "uniforms", f32, (*shape, 2), device)
         _tensor(class_ids, "class_ids", i32, (c.batch,), device)
         _tensor(ctx, "ctx", torch.bfloat16, (c.batch, c.ctx_len, c.d_ctx), device)
         if not ids.is_cuda:
             raise ValueError("ids must be on a CUDA device")
         self.step(ids, logits, t, step, class_ids=class_ids, ctx=ctx, stream=stream)
         rows = logits.view(-1, logits.shape[-1])
-        out = dict(top_logprobs=score.view(-1, 1)) if by == "confidence" else dict(entropy=score.view(-1))
-        sgd_kernel_logprobs(rows, top_ids=cand.view(-1, 1), scale=scale, row_ids=ids.view(-1), row_id=mask_id,
-                            stream=stream, **out)
+        which = dict(scale=scale, row_ids=ids.view(-1), row_id=mask_id, stream=stream)
+        if uniforms is None:
+            out = dict(top_logprobs=score.view(-1, 1)) if by == "confidence" else dict(entropy=score.view(-1))
+            sgd_kernel_logprobs(rows, top_ids=cand.view(-1, 1), **out, **which)
+        else:
+            sgd_kernel_sample(rows, uniforms.view(-1, 2), cand.view(-1), logprobs=score.view(-1) if by == "confidence" else None,
+                              top_k=top_k, top_p=top_p, min_p=min_p, **which)
+            if by == "entropy":
+                sgd_kernel_logprobs(rows, entropy=score.view(-1), **which)
         return sgd_sampler_reveal(ids, cand, score, n_reveal, ids_out, mask_id, lowest=by == "entropy", window=window,
                                   n_left=n_left, stream=stream)
 

@@ -2027,6 +2027,141 @@ int sgd_kernel_distill(const void* logits, int dtype, int64_t ld, int rows, int 
   return SGD_OK;
 }
 
+int sgd_kernel_sample(const void* logits, int dtype, int64_t ld, int rows, int vocab, float scale, int top_k, double top_p,
+                      double min_p, const float* uniforms, const int32_t* row_ids, int row_id, int32_t* ids, float* logprobs,
+                      void* stream) {
+  const int rc = check_rows("sample", logits, dtype, ld, rows, vocab, scale);
+  if (rc) return rc;
+  if (rows != 0 && (!uniforms || !ids)) return fail(SGD_ERR_ARG, "sample: null argument");
+  if (top_k < 0) return fail(SGD_ERR_ARG, "sample: top_k is negative");
+  if (!(top_p > 0.0) || top_p > 1.0) return fail(SGD_ERR_ARG, "sample: top_p must be above 0 and at most 1");
+  if (!(min_p >= 0.0) || min_p > 1.0) return fail(SGD_ERR_ARG, "sample: min_p must be in 0..1");
+  if (!al4(uniforms) || !al4(row_ids) || !al4(ids) || !al4(logprobs))
+    return fail(SGD_ERR_ARG, "sample: pointers must be 4-byte aligned");
+  if (rows == 0) return SGD_OK;
+  const SampleParams p{logits, dtype, ld, rows, vocab, scale, top_k, top_p, min_p, uniforms, row_ids, row_id, ids, logprobs};
+  CUDA_TRY(sample_launch(p, static_cast<cudaStream_t>(stream)));
+  return SGD_OK;
+}
+
+namespace {
+
+// Bytes of rows that lie ld elements apart.
+int64_t extent(int rows, int64_t ld, int64_t width, int size) { return rows < 1 ? 0 : ((rows - 1) * ld + width) * size; }
+bool overlap(const void* a, int64_t an, const void* b, int64_t bn) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return a && b && an > 0 && bn > 0 && x < y + static_cast<uintptr_t>(bn) && y < x + static_cast<uintptr_t>(an);
+}
+
+// What the embedding's two operators ask of a matrix.
+int check_matrix(const std::string& name, const void* at, int dtype, int64_t ld, int rows, int d) {
+  if (!at && rows != 0) return fail(SGD_ERR_ARG, name + " is null");
+  if (dtype < SGD_F16 || dtype > SGD_F32) return fail(SGD_ERR_ARG, name + ": unknown element type");
+  if (ld < d) return fail(SGD_ERR_ARG, name + ": rows less than d elements apart");
+  if (ld > (1ll << 40)) return fail(SGD_ERR_SHAPE, name + ": rows too far apart");
+  if (reinterpret_cast<uintptr_t>(at) % elem_size(dtype)) return fail(SGD_ERR_ARG, name + " is misaligned");
+  return SGD_OK;
+}
+int check_sizes(const std::string& name, int rows, int vocab, int d) {
+  if (rows < 0 || vocab < 1 || d < 1) return fail(SGD_ERR_ARG, name + ": rows >= 0, vocab >= 1 and d >= 1 are needed");
+  if (rows > kMaxRows) return fail(SGD_ERR_SHAPE, name + ": more than " + std::to_string(kMaxRows) + " rows");
+  if (d > kMaxColumns) return fail(SGD_ERR_SHAPE, name + ": d is above " + std::to_string(kMaxColumns));
+  return SGD_OK;
+}
+
+}  // namespace
+
+int sgd_kernel_embedding(const void* table, int dtype, int64_t ld, int vocab, int d, const int32_t* ids, int rows, float scale, void* out,
+                         int out_dtype, int64_t ld_out, void* stream) {
+  int rc = check_sizes("embedding", rows, vocab, d);
+  if (!rc) rc = check_matrix("embedding: table", table, dtype, ld, rows ? vocab : 0, d);
+  if (!rc) rc = check_matrix("embedding: out", out, out_dtype, ld_out, rows, d);
+  if (rc) return rc;
+  if (rows != 0 && !ids) return fail(SGD_ERR_ARG, "embedding: null ids");
+  if (!al4(ids)) return fail(SGD_ERR_ARG, "embedding: ids must be 4-byte aligned");
+  const int64_t n = extent(rows, ld_out, d, elem_size(out_dtype));
+  if (overlap(out, n, table, extent(vocab, ld, d, elem_size(dtype))) || overlap(out, n, ids, 4ll * rows))
+    return fail(SGD_ERR_ARG, "embedding: out overlaps an input");
+  if (rows == 0) return SGD_OK;
+  const EmbeddingParams p{table, dtype, ld, vocab, d, ids, rows, scale, out, out_dtype, ld_out};
+  CUDA_TRY(embedding_launch(p, static_cast<cudaStream_t>(stream)));
+  return SGD_OK;
+}
+
+int sgd_kernel_embedding_grad_workspace(int rows, int vocab, int d, int64_t* bytes) {
+  if (!bytes) return fail(SGD_ERR_ARG, "embedding_grad: null argument");
+  const int rc = check_sizes("embedding_grad", rows, vocab, d);
+  if (rc) return rc;
+  *bytes = embedding_grad_bytes(rows, d);
+  return SGD_OK;
+}
+
+int sgd_kernel_embedding_grad(const void* grad, int grad_dtype, int64_t ld_grad, const int32_t* ids, int rows, int vocab, int d,
+                              float scale, int accumulate, void* dtable, int dtable_dtype, int64_t ld, void* workspace,
+                              int64_t workspace_bytes, void* stream) {
+  int rc = check_sizes("embedding_grad", rows, vocab, d);
+  if (!rc) rc = check_matrix("embedding_grad: grad", grad, grad_dtype, ld_grad, rows, d);
+  if (!rc) rc = check_matrix("embedding_grad: dtable", dtable, dtable_dtype, ld, vocab, d);
+  if (rc) return rc;
+  if (rows != 0 && !ids) return fail(SGD_ERR_ARG, "embedding_grad: null ids");
+  if (!al4(ids)) return fail(SGD_ERR_ARG, "embedding_grad: ids must be 4-byte aligned");
+  const int64_t need = embedding_grad_bytes(rows, d);
+  if (rows != 0 && (!workspace || !al16(workspace) || workspace_bytes < need))
+    return fail(SGD_ERR_ARG, "embedding_grad: a 16-byte aligned workspace of " + std::to_string(need) + " bytes is needed");
+  const int64_t n = extent(vocab, ld, d, elem_size(dtable_dtype));
+  if (overlap(dtable, n, grad, extent(rows, ld_grad, d, elem_size(grad_dtype))) || overlap(dtable, n, ids, 4ll * rows) ||
+      overlap(dtable, n, workspace, rows ? need : 0))
+    return fail(SGD_ERR_ARG, "embedding_grad: dtable overlaps another argument");
+  const EmbeddingGradParams p{grad, grad_dtype, ld_grad, ids, rows, vocab, d, scale, accumulate != 0, dtable, dtable_dtype, ld, workspace};
+  CUDA_TRY(embedding_grad_launch(p, static_cast<cudaStream_t>(stream)));
+  return SGD_OK;
+}
+
+int sgd_kernel_norm_grad_workspace(int rows, int d, int rows_per_batch, int64_t* bytes) {
+  if (!bytes) return fail(SGD_ERR_ARG, "norm_grad: null argument");
+  if (rows < 0 || rows > kMaxRows || d < 4 || d % 4 || d > 4096 || rows_per_batch < 0)
+    return fail(SGD_ERR_ARG, "norm_grad: bad sizes (d must be a multiple of 4, <= 4096)");
+  *bytes = norm_grad_bytes(rows, d, rows_per_batch);
+  return SGD_OK;
+}
+
+int sgd_kernel_norm_grad(const float* h, const void* dout, int dtype, int rows, int d, int kind, const void* g, const void* b,
+                         const float* scale, int ld_mod, int rows_per_batch, float eps, const float* residual, float* dh, float* dg,
+                         float* db, float* dshift, float* dscale, int ld_dmod, void* workspace, int64_t workspace_bytes,
+                         void* stream) {
+  if (rows < 0 || d < 4 || d % 4 || d > 4096 || kind < 0 || kind > 2)
+    return fail(SGD_ERR_ARG, "norm_grad: bad arguments (d must be a multiple of 4, <= 4096)");
+  if (rows > kMaxRows) return fail(SGD_ERR_SHAPE, "norm_grad: more than " + std::to_string(kMaxRows) + " rows");
+  if (dtype < SGD_F16 || dtype > SGD_F32) return fail(SGD_ERR_ARG, "norm_grad: unknown element type");
+  if (rows != 0 && (!h || !dout)) return fail(SGD_ERR_ARG, "norm_grad: null argument");
+  if (rows != 0 && !dh && !dg && !db && !dshift && !dscale) return fail(SGD_ERR_ARG, "norm_grad: no output asked for");
+  if ((dg && !g) || (db && !b) || ((dshift || dscale) && !scale && rows != 0) || (residual && !dh))
+    return fail(SGD_ERR_ARG, "norm_grad: dg needs g, db needs b, dshift and dscale need scale, residual needs dh");
+  if (scale && (rows_per_batch < 1 || ld_mod < d || ((dshift || dscale) && ld_dmod < d)))
+    return fail(SGD_ERR_ARG, "norm_grad: a modulation needs rows_per_batch >= 1, ld_mod >= d and ld_dmod >= d");
+  if (!al16(h) || !al16(dh) || !al16(residual) || !al16(dg) || !al16(db) || (reinterpret_cast<uintptr_t>(dout) & (dtype == SGD_F32 ? 15u : 7u)))
+    return fail(SGD_ERR_ARG, "norm_grad: h, dh, residual, dg, db and fp32 dout must be 16-byte, other dout 8-byte aligned");
+  if ((reinterpret_cast<uintptr_t>(g) & 7u) || (reinterpret_cast<uintptr_t>(b) & 7u) || !al4(scale) || !al4(dshift) || !al4(dscale))
+    return fail(SGD_ERR_ARG, "norm_grad: g and b must be 8-byte, the modulation's tensors 4-byte aligned");
+  const int64_t n = 4ll * rows * d;
+  if (overlap(dh, n, h, n) || overlap(dh, n, dout, static_cast<int64_t>(elem_size(dtype)) * rows * d) ||
+      (dh != residual && overlap(dh, n, residual, n)))
+    return fail(SGD_ERR_ARG, "norm_grad: dh overlaps an input without being the residual");
+  const bool sums = dg || db || dshift || dscale;
+  const int64_t need = sums ? norm_grad_bytes(rows, d, scale ? rows_per_batch : 0) : 0;
+  if (need > 0 && (!workspace || !al16(workspace) || workspace_bytes < need))
+    return fail(SGD_ERR_ARG, "norm_grad: a 16-byte aligned workspace of " + std::to_string(need) + " bytes is needed");
+  if (rows == 0) {
+    if (dg) CUDA_TRY(cudaMemsetAsync(dg, 0, sizeof(float) * d, static_cast<cudaStream_t>(stream)));
+    if (db) CUDA_TRY(cudaMemsetAsync(db, 0, sizeof(float) * d, static_cast<cudaStream_t>(stream)));
+    return SGD_OK;
+  }
+  const NormGradParams p{h, dout, dtype, rows, d, kind, B16(g), B16(b), scale, ld_mod, rows_per_batch, eps, residual, dh, dg, db,
+                         dshift, dscale, ld_dmod, workspace};
+  CUDA_TRY(norm_grad_launch(p, static_cast<cudaStream_t>(stream)));
+  return SGD_OK;
+}
+
 int sgd_selftest_wait_timeout(void* stream) {
   int* p = device_status_ptr();
   if (!p) return fail(SGD_ERR_CUDA, "status word unavailable");

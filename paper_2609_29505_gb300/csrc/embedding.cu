@@ -1,0 +1,599 @@
+// Rows of an embedding table, scaled, and the table's gradient.
+//
+//   out[r] = scale table[ids[r]];   dtable[t] = scale sum over {r : ids[r] = t} of grad[r], in the order of r.
+//
+// The gradient goes by the rows sorted by token: every sum has one order, no atomics are added to, and a token with
+// half of the rows (the mask of a masked-token model) is split over as many CTAs as the others.
+//   sort     (token, row) ascending.  Up to kRankRows rows each row counts the rows before it, N^2 comparisons over the
+//            whole GPU in one launch; above, a radix sort (8 bits at a time: histogram, scan, scatter).
+//   sums     CTA (chunk of sorted rows, columns): a run of equal tokens that lies inside the chunk is written
+//            to the table; a run that passes a chunk's border leaves a partial sum per chunk in the workspace.
+//   join     adds the partial sums of such a run in the order of the chunks.
+#include "common.cuh"
+#include "kernels.h"
+
+namespace sgd {
+namespace {
+
+// ----- elements of the three types -----
+
+template <typename T>
+struct Vec {  // 16 bytes
+  static constexpr int kN = 16 / static_cast<int>(sizeof(T));
+};
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(f16 x) { return __half2float(x); }
+__device__ __forceinline__ float to_f32(bf16 x) { return __bfloat162float(x); }
+template <typename T>
+__device__ __forceinline__ T from_f32(float x);
+template <>
+__device__ __forceinline__ float from_f32<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ f16 from_f32<f16>(float x) { return __float2half_rn(x); }
+template <>
+__device__ __forceinline__ bf16 from_f32<bf16>(float x) { return __float2bfloat16_rn(x); }
+
+// N values at p, all of them where VEC (then p is aligned to 16 bytes, or to N elements where those are fewer bytes),
+// else the first n.
+template <bool VEC, int N, typename T>
+__device__ __forceinline__ void load(const T* p, int n, float* f) {
+  if constexpr (VEC) {
+    constexpr int kBytes = N * static_cast<int>(sizeof(T));
+    if constexpr (kBytes >= 16) {
+#pragma unroll
+      for (int i = 0; i < kBytes / 16; ++i) {
+        const uint4 u = reinterpret_cast<const uint4*>(p)[i];
+        const T* e = reinterpret_cast<const T*>(&u);
+#pragma unroll
+        for (int j = 0; j < Vec<T>::kN; ++j) f[i * Vec<T>::kN + j] = to_f32(e[j]);
+      }
+    } else {
+      const uint2 u = *reinterpret_cast<const uint2*>(p);
+      const T* e = reinterpret_cast<const T*>(&u);
+#pragma unroll
+      for (int j = 0; j < N; ++j) f[j] = to_f32(e[j]);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j) f[j] = j < n ? to_f32(p[j]) : 0.f;
+  }
+}
+template <bool VEC, int N, typename T>
+__device__ __forceinline__ void store(T* p, int n, const float* f) {
+  if constexpr (VEC) {
+    constexpr int kBytes = N * static_cast<int>(sizeof(T));
+    if constexpr (kBytes >= 16) {
+#pragma unroll
+      for (int i = 0; i < kBytes / 16; ++i) {
+        uint4 u;
+        T* e = reinterpret_cast<T*>(&u);
+#pragma unroll
+        for (int j = 0; j < Vec<T>::kN; ++j) e[j] = from_f32<T>(f[i * Vec<T>::kN + j]);
+        reinterpret_cast<uint4*>(p)[i] = u;
+      }
+    } else {
+      uint2 u;
+      T* e = reinterpret_cast<T*>(&u);
+#pragma unroll
+      for (int j = 0; j < N; ++j) e[j] = from_f32<T>(f[j]);
+      *reinterpret_cast<uint2*>(p) = u;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (j < n) p[j] = from_f32<T>(f[j]);
+  }
+}
+
+template <typename T>
+bool vectors(const void* p, int64_t ld, int per, int d) {  // rows of whole vectors, each aligned
+  const int64_t bytes = static_cast<int64_t>(sizeof(T)) * per < 16 ? sizeof(T) * per : 16;
+  return reinterpret_cast<uintptr_t>(p) % bytes == 0 && ld * static_cast<int64_t>(sizeof(T)) % bytes == 0 && d % per == 0;
+}
+
+// ----- lookup -----
+
+constexpr int kCols = 8;  // columns of a thread
+
+template <typename TI, typename TO, bool VEC>
+__global__ void __launch_bounds__(256) embedding_kernel(const EmbeddingParams p) {
+  const int per = (p.d + kCols - 1) / kCols;
+  const int64_t all = static_cast<int64_t>(p.rows) * per;
+  const TI* table = static_cast<const TI*>(p.table);
+  TO* out = static_cast<TO*>(p.out);
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < all; i += static_cast<int64_t>(gridDim.x) * 256) {
+    const int r = static_cast<int>(i / per), c = static_cast<int>(i - static_cast<int64_t>(r) * per) * kCols;
+    const int id = p.ids[r];
+    float f[kCols];
+    if (id >= 0 && id < p.vocab) {
+      load<VEC, kCols>(table + static_cast<int64_t>(id) * p.ld + c, p.d - c, f);
+#pragma unroll
+      for (int j = 0; j < kCols; ++j) f[j] *= p.scale;
+    } else {
+#pragma unroll
+      for (int j = 0; j < kCols; ++j) f[j] = 0.f;
+    }
+    store<VEC, kCols>(out + static_cast<int64_t>(r) * p.ld_out + c, p.d - c, f);
+  }
+}
+
+template <typename TI, typename TO>
+cudaError_t lookup(const EmbeddingParams& p, cudaStream_t s) {
+  const int64_t all = static_cast<int64_t>(p.rows) * ((p.d + kCols - 1) / kCols);
+  const int64_t blocks = (all + 255) / 256, most = 1 << 20;
+  const dim3 grid(static_cast<unsigned>(blocks < most ? blocks : most));
+  const bool vec = vectors<TI>(p.table, p.ld, kCols, p.d) && vectors<TO>(p.out, p.ld_out, kCols, p.d);
+  if (vec) embedding_kernel<TI, TO, true><<<grid, 256, 0, s>>>(p);
+  else embedding_kernel<TI, TO, false><<<grid, 256, 0, s>>>(p);
+  return cudaGetLastError();
+}
+template <typename TI>
+cudaError_t lookup_to(const EmbeddingParams& p, cudaStream_t s) {
+  if (p.out_dtype == SGD_F16) return lookup<TI, f16>(p, s);
+  if (p.out_dtype == SGD_BF16) return lookup<TI, bf16>(p, s);
+  return lookup<TI, float>(p, s);
+}
+
+// ----- gradient: a table of zeros -----
+
+template <bool VEC, typename T>
+__global__ void __launch_bounds__(256) zero_kernel(T* table, int64_t ld, int vocab, int d) {
+  constexpr int N = VEC ? Vec<T>::kN : 1;
+  const int per = d / N;
+  const int64_t all = static_cast<int64_t>(vocab) * per;
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < all; i += static_cast<int64_t>(gridDim.x) * 256) {
+    const int64_t r = i / per;
+    T* at = table + r * ld + (i - r * per) * N;
+    if constexpr (VEC) *reinterpret_cast<uint4*>(at) = make_uint4(0, 0, 0, 0);
+    else *at = from_f32<T>(0.f);
+  }
+}
+template <typename T>
+cudaError_t zero(void* table, int64_t ld, int vocab, int d, cudaStream_t s) {
+  T* t = static_cast<T*>(table);
+  const bool vec = vectors<T>(t, ld, Vec<T>::kN, d);
+  const int64_t all = static_cast<int64_t>(vocab) * (vec ? d / Vec<T>::kN : d), blocks = (all + 255) / 256;
+  const dim3 grid(static_cast<unsigned>(blocks < (1 << 20) ? blocks : 1 << 20));
+  if (vec) zero_kernel<true><<<grid, 256, 0, s>>>(t, ld, vocab, d);
+  else zero_kernel<false><<<grid, 256, 0, s>>>(t, ld, vocab, d);
+  return cudaGetLastError();
+}
+
+// ----- gradient: the rows sorted by token -----
+
+constexpr int kRankRows = 8192;  // rows that are sorted by counting
+constexpr int kRankCta = 32;     // of a CTA, 8 threads each
+constexpr int kTile = 2048;      // rows of a CTA of the radix sort: 8 warps, 256 each
+constexpr int kBits = 8, kBins = 1 << kBits;
+
+// A row without a token goes behind all others, as one of the token `vocab`.
+__device__ __forceinline__ uint32_t token_of(const int32_t* ids, int r, int vocab) {
+  const uint32_t t = static_cast<uint32_t>(ids[r]);
+  return min(t, static_cast<uint32_t>(vocab));
+}
+
+// rank of row r = number of rows before it in (token, row)
+__global__ void __launch_bounds__(256) rank_kernel(const int32_t* ids, int rows, int vocab, uint32_t* tokens, int32_t* order) {
+  extern __shared__ uint32_t all[];  // [rows, a multiple of 4], the rest above every token
+  const int padded = (rows + 3) & ~3;
+  for (int i = threadIdx.x; i < padded; i += 256) all[i] = i < rows ? token_of(ids, i, vocab) : 0xFFFFFFFFu;
+  __syncthreads();
+  const int r = blockIdx.x * kRankCta + (threadIdx.x >> 3), part = threadIdx.x & 7;
+  int before = 0;
+  uint32_t mine = 0;
+  if (r < rows) {
+    mine = all[r];
+    for (int i = part * 4; i < padded; i += 32) {
+      const uint4 t = *reinterpret_cast<const uint4*>(all + i);
+      // an equal token counts where its row is smaller
+      before += t.x < mine + (i < r);
+      before += t.y < mine + (i + 1 < r);
+      before += t.z < mine + (i + 2 < r);
+      before += t.w < mine + (i + 3 < r);
+    }
+  }
+#pragma unroll
+  for (int o = 4; o > 0; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
+  if (r < rows && part == 0) {
+    tokens[before] = mine;
+    order[before] = r;
+  }
+}
+
+// Radix sort, one digit: counts per (digit, tile), their exclusive scan, and the stable scatter.  FIRST: the keys are
+// the rows' tokens, and a row is its own index.
+template <bool FIRST>
+__device__ __forceinline__ uint32_t sort_key(const int32_t* ids, const uint32_t* keys, int i, int vocab) {
+  return FIRST ? token_of(ids, i, vocab) : keys[i];
+}
+template <bool FIRST>
+__global__ void __launch_bounds__(256) radix_count_kernel(const int32_t* ids, const uint32_t* keys, int rows, int vocab, int shift,
+                                                          uint32_t* counts) {
+  __shared__ uint32_t hist[kBins];
+  hist[threadIdx.x] = 0;
+  __syncthreads();
+  const int first = blockIdx.x * kTile;
+  for (int i = first + threadIdx.x; i < min(first + kTile, rows); i += 256)
+    atomicAdd(&hist[(sort_key<FIRST>(ids, keys, i, vocab) >> shift) & (kBins - 1)], 1u);
+  __syncthreads();
+  counts[static_cast<int64_t>(threadIdx.x) * gridDim.x + blockIdx.x] = hist[threadIdx.x];
+}
+__global__ void __launch_bounds__(1024) radix_scan_kernel(uint32_t* counts, int n) {
+  __shared__ uint32_t warp_sum[32];
+  __shared__ uint32_t total;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) total = 0;
+  for (int at = 0; at < n; at += 4096) {
+    uint32_t v[4], sum = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int i = at + static_cast<int>(threadIdx.x) * 4 + j;
+      v[j] = i < n ? counts[i] : 0u;
+      sum += v[j];
+    }
+    uint32_t up = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t x = __shfl_up_sync(0xffffffffu, up, o);
+      if (lane >= o) up += x;
+    }
+    if (lane == 31) warp_sum[warp] = up;
+    __syncthreads();
+    if (warp == 0) {
+      const uint32_t mine = warp_sum[lane];
+      uint32_t w = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t x = __shfl_up_sync(0xffffffffu, w, o);
+        if (lane >= o) w += x;
+      }
+      const uint32_t before = total;
+      __syncwarp();
+      warp_sum[lane] = before + w - mine;
+      if (lane == 31) total = before + w;
+    }
+    __syncthreads();
+    uint32_t run = warp_sum[warp] + up - sum;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int i = at + static_cast<int>(threadIdx.x) * 4 + j;
+      if (i < n) counts[i] = run;
+      run += v[j];
+    }
+    __syncthreads();
+  }
+}
+template <bool FIRST>
+__global__ void __launch_bounds__(256) radix_scatter_kernel(const int32_t* ids, const uint32_t* keys, const int32_t* rows_in, int rows,
+                                                            int vocab, int shift, const uint32_t* counts, uint32_t* keys_out,
+                                                            int32_t* rows_out) {
+  __shared__ uint32_t seen[8][kBins];  // of a warp: rows with this digit so far; then where its first one goes
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int i = threadIdx.x; i < 8 * kBins; i += 256) seen[i / kBins][i % kBins] = 0;
+  __syncthreads();
+  const int first = blockIdx.x * kTile + warp * 256;
+  uint32_t key[8], rank[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int i = first + j * 32 + lane;
+    const bool in = i < rows;
+    key[j] = in ? sort_key<FIRST>(ids, keys, i, vocab) : 0u;
+    const uint32_t digit = in ? (key[j] >> shift) & (kBins - 1) : kBins;
+    const uint32_t same = __match_any_sync(0xffffffffu, digit);
+    const uint32_t below = __popc(same & ((1u << lane) - 1u));
+    rank[j] = in ? seen[warp][digit] + below : 0u;
+    __syncwarp();
+    if (in && below == 0) seen[warp][digit] += __popc(same);
+    __syncwarp();
+  }
+  __syncthreads();
+  uint32_t run = counts[static_cast<int64_t>(threadIdx.x) * gridDim.x + blockIdx.x];
+#pragma unroll
+  for (int w = 0; w < 8; ++w) {
+    const uint32_t n = seen[w][threadIdx.x];
+    seen[w][threadIdx.x] = run;
+    run += n;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int i = first + j * 32 + lane;
+    if (i >= rows) continue;
+    const uint32_t at = seen[warp][(key[j] >> shift) & (kBins - 1)] + rank[j];
+    keys_out[at] = key[j];
+    rows_out[at] = FIRST ? i : rows_in[i];
+  }
+}
+
+// ----- gradient: sums of runs -----
+
+constexpr int kSumThreads = 128;
+constexpr int kJoinCols = 128;  // of a CTA that joins: 32 lanes, 4 columns each
+
+struct Plan {
+  int rows, d, chunk, chunks, tiles, pd;  // pd: columns of a row of partial sums
+  int64_t keys, order, keys2, order2, counts, partial, bytes;  // offsets in the workspace
+};
+Plan make_plan(int rows, int d) {
+  Plan q{};
+  q.rows = rows;
+  q.d = d;
+  // rows of a chunk: as many as leave a CTA per SM and more to the columns, and partial sums a small share of the traffic
+  q.chunk = 16;
+  while (q.chunk < 64 && rows / q.chunk > 512) q.chunk *= 2;
+  q.chunks = (rows + q.chunk - 1) / q.chunk;
+  q.tiles = (rows + kTile - 1) / kTile;
+  q.pd = (d + 7) & ~7;
+  int64_t at = 0;
+  auto take = [&](int64_t bytes) {
+    const int64_t here = at;
+    at += (bytes + 255) & ~255ll;
+    return here;
+  };
+  q.keys = take(4ll * rows);
+  q.order = take(4ll * rows);
+  if (rows > kRankRows) {
+    q.keys2 = take(4ll * rows);
+    q.order2 = take(4ll * rows);
+    q.counts = take(4ll * kBins * q.tiles);
+  }
+  q.partial = take(8ll * q.chunks * q.pd);
+  q.bytes = at;
+  return q;
+}
+
+struct SumArgs {
+  const void* grad;
+  int64_t ld_grad;
+  const uint32_t* tokens;
+  const int32_t* order;
+  int rows, vocab, d, chunk, chunks, pd, accumulate;
+  float scale;
+  float* partial;  // [chunks, 2, pd]: of the run that came from the chunk before, of the one that goes on to the next
+  void* dtable;
+  int64_t ld;
+};
+
+// scale sum (+ what is there) to the table
+template <typename TO, bool VEC, int N>
+__device__ __forceinline__ void put(const SumArgs& p, uint32_t token, int c, const float* sum) {
+  TO* at = static_cast<TO*>(p.dtable) + static_cast<int64_t>(token) * p.ld + c;
+  float f[N];
+  if (p.accumulate) {
+    if constexpr (VEC) {
+      // (ordinary loads: the table is written by this kernel)
+      TO v[N];
+      constexpr int kBytes = N * static_cast<int>(sizeof(TO));
+      if constexpr (kBytes >= 16) {
+#pragma unroll
+        for (int i = 0; i < kBytes / 16; ++i) reinterpret_cast<uint4*>(v)[i] = reinterpret_cast<const uint4*>(at)[i];
+      } else {
+        *reinterpret_cast<uint2*>(v) = *reinterpret_cast<const uint2*>(at);
+      }
+#pragma unroll
+      for (int j = 0; j < N; ++j) f[j] = fmaf(p.scale, sum[j], to_f32(v[j]));
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j) f[j] = c + j < p.d ? fmaf(p.scale, sum[j], to_f32(at[j])) : 0.f;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j) f[j] = p.scale * sum[j];
+  }
+  store<VEC, N>(at, p.d - c, f);
+}
+
+template <typename TG, typename TO, bool VEC>
+__global__ void __launch_bounds__(kSumThreads) embedding_sums_kernel(const SumArgs p) {
+  constexpr int N = VEC ? Vec<TG>::kN : 4, kAhead = 8;
+  __shared__ uint32_t tok[64 + 2];
+  __shared__ int32_t row[64];
+  const int first = blockIdx.x * p.chunk, n = min(p.chunk, p.rows - first);
+  // the tokens of the chunk and of its neighbours (none: one that no row has)
+  for (int i = threadIdx.x; i < n + 2; i += kSumThreads) {
+    const int at = first + i - 1;
+    tok[i] = at >= 0 && at < p.rows ? p.tokens[at] : 0xFFFFFFFFu;
+  }
+  for (int i = threadIdx.x; i < n; i += kSumThreads) row[i] = p.order[first + i];
+  __syncthreads();
+  const int c = (blockIdx.y * kSumThreads + threadIdx.x) * N;
+  if (c >= p.d) return;
+  const TG* grad = static_cast<const TG*>(p.grad) + c;
+  float sum[N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) sum[j] = 0.f;
+  bool from_before = tok[1] == tok[0];
+  for (int i0 = 0; i0 < n; i0 += kAhead) {
+    float v[kAhead][N];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (i0 + u < n && tok[i0 + u + 1] < static_cast<uint32_t>(p.vocab))
+        load<VEC, N>(grad + static_cast<int64_t>(row[i0 + u]) * p.ld_grad, p.d - c, v[u]);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int i = i0 + u;
+      if (i >= n) break;
+      const uint32_t t = tok[i + 1];
+      if (t >= static_cast<uint32_t>(p.vocab)) return;  // the rest has no token
+#pragma unroll
+      for (int j = 0; j < N; ++j) sum[j] += v[u][j];
+      const bool ends = tok[i + 2] != t, last = i == n - 1;
+      if (!ends && !last) continue;
+      if (ends && !from_before) {
+        put<TO, VEC, N>(p, t, c, sum);
+      } else {
+        float* at = p.partial + (2 * static_cast<int64_t>(blockIdx.x) + (from_before ? 0 : 1)) * p.pd + c;
+        if constexpr (VEC) {
+#pragma unroll
+          for (int j = 0; j < N; j += 4) *reinterpret_cast<float4*>(at + j) = make_float4(sum[j], sum[j + 1], sum[j + 2], sum[j + 3]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < N; ++j) at[j] = sum[j];  // (a row of partial sums is a multiple of 8 long)
+        }
+      }
+      from_before = false;
+#pragma unroll
+      for (int j = 0; j < N; ++j) sum[j] = 0.f;
+    }
+  }
+}
+
+// Runs that pass a chunk's border: CTA (columns, share of the chunks where such a run begins).
+template <typename TO, bool VEC>
+__global__ void __launch_bounds__(256) embedding_join_kernel(const SumArgs p) {
+  __shared__ int begins[256];
+  __shared__ int n_begins;
+  __shared__ float4 sums[8][32];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int c = blockIdx.x * kJoinCols + lane * 4;
+  const uint32_t vocab = static_cast<uint32_t>(p.vocab);
+  for (int base = blockIdx.y; base < p.chunks; base += 256 * gridDim.y) {
+    if (threadIdx.x == 0) n_begins = 0;
+    __syncthreads();
+    // chunks base, base + gridDim.y, ...: does a run begin here and go on?
+    const int64_t mine = base + static_cast<int64_t>(threadIdx.x) * gridDim.y;
+    if (mine + 1 < p.chunks) {  // the last chunk's runs end with it
+      const int end = (static_cast<int>(mine) + 1) * p.chunk;
+      const uint32_t t = p.tokens[end - 1];
+      bool it = t < vocab && p.tokens[end] == t;
+      if (it) {
+        const int at = static_cast<int>(mine) * p.chunk;
+        it = at == 0 || p.tokens[at - 1] != t;  // (a run that came from before began there)
+      }
+      if (it) begins[atomicAdd(&n_begins, 1)] = static_cast<int>(mine);
+    }
+    __syncthreads();
+    const int n = n_begins;
+    for (int k = 0; k < n; ++k) {
+      const int c0 = begins[k];
+      const uint32_t t = p.tokens[(c0 + 1) * p.chunk - 1];
+      // the last chunk of the run: 32 probes at a time between lo (holds the token first) and hi (does not)
+      int lo = c0 + 1, hi = p.chunks;
+      while (hi - lo > 1) {
+        const int step = (hi - lo + 31) / 32;
+        const int at = lo + (lane + 1) * step;
+        const bool in = at < hi && p.tokens[static_cast<int64_t>(at) * p.chunk] == t;
+        const int more = __popc(__ballot_sync(0xffffffffu, in));  // (tokens ascend: the first ones)
+        const int new_lo = lo + more * step;
+        hi = min(hi, new_lo + step);
+        lo = new_lo;
+      }
+      const int parts = lo - c0 + 1;  // tail of c0, heads of c0 + 1 .. lo
+      const int per = (parts + 7) / 8, a = warp * per, b = min(a + per, parts);
+      float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (c < p.pd) {
+#pragma unroll 8
+        for (int i = a; i < b; ++i) {
+          const int64_t slot = 2 * static_cast<int64_t>(c0 + i) + (i == 0 ? 1 : 0);
+          const float4 x = *reinterpret_cast<const float4*>(p.partial + slot * p.pd + c);
+          s.x += x.x;
+          s.y += x.y;
+          s.z += x.z;
+          s.w += x.w;
+        }
+      }
+      sums[warp][lane] = s;
+      __syncthreads();
+      if (warp == 0 && c < p.d) {
+#pragma unroll
+        for (int w = 1; w < 8; ++w) {
+          const float4 x = sums[w][lane];
+          s.x += x.x;
+          s.y += x.y;
+          s.z += x.z;
+          s.w += x.w;
+        }
+        const float f[4] = {s.x, s.y, s.z, s.w};
+        put<TO, VEC, 4>(p, t, c, f);
+      }
+      __syncthreads();
+    }
+    __syncthreads();
+  }
+}
+
+template <typename TG, typename TO>
+cudaError_t sums(const SumArgs& a, cudaStream_t s) {
+  const bool vec = vectors<TG>(a.grad, a.ld_grad, Vec<TG>::kN, a.d) && vectors<TO>(a.dtable, a.ld, Vec<TG>::kN, a.d);
+  const int n = vec ? Vec<TG>::kN : 4;
+  const dim3 grid(a.chunks, (a.d + kSumThreads * n - 1) / (kSumThreads * n));
+  if (vec) embedding_sums_kernel<TG, TO, true><<<grid, kSumThreads, 0, s>>>(a);
+  else embedding_sums_kernel<TG, TO, false><<<grid, kSumThreads, 0, s>>>(a);
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess || a.chunks < 2) return e;
+  const dim3 join((a.d + kJoinCols - 1) / kJoinCols, a.chunks < 16 ? a.chunks : 16);
+  if (vectors<TO>(a.dtable, a.ld, 4, a.d)) embedding_join_kernel<TO, true><<<join, 256, 0, s>>>(a);
+  else embedding_join_kernel<TO, false><<<join, 256, 0, s>>>(a);
+  return cudaGetLastError();
+}
+template <typename TG>
+cudaError_t sums_to(const SumArgs& a, int dtype, cudaStream_t s) {
+  if (dtype == SGD_F16) return sums<TG, f16>(a, s);
+  if (dtype == SGD_BF16) return sums<TG, bf16>(a, s);
+  return sums<TG, float>(a, s);
+}
+
+cudaError_t sort_rows(const EmbeddingGradParams& p, const Plan& q, char* ws, const uint32_t** tokens, const int32_t** order,
+                      cudaStream_t s) {
+  uint32_t* k0 = reinterpret_cast<uint32_t*>(ws + q.keys);
+  int32_t* r0 = reinterpret_cast<int32_t*>(ws + q.order);
+  if (p.rows <= kRankRows) {
+    rank_kernel<<<(p.rows + kRankCta - 1) / kRankCta, 256, 4 * ((p.rows + 3) & ~3), s>>>(p.ids, p.rows, p.vocab, k0, r0);
+    *tokens = k0;
+    *order = r0;
+    return cudaGetLastError();
+  }
+  uint32_t* k1 = reinterpret_cast<uint32_t*>(ws + q.keys2);
+  int32_t* r1 = reinterpret_cast<int32_t*>(ws + q.order2);
+  uint32_t* counts = reinterpret_cast<uint32_t*>(ws + q.counts);
+  for (int shift = 0; shift < 32 && (shift == 0 || p.vocab >> shift); shift += kBits) {
+    if (shift == 0) radix_count_kernel<true><<<q.tiles, 256, 0, s>>>(p.ids, k0, p.rows, p.vocab, shift, counts);
+    else radix_count_kernel<false><<<q.tiles, 256, 0, s>>>(p.ids, k0, p.rows, p.vocab, shift, counts);
+    radix_scan_kernel<<<1, 1024, 0, s>>>(counts, kBins * q.tiles);
+    if (shift == 0) radix_scatter_kernel<true><<<q.tiles, 256, 0, s>>>(p.ids, k0, r0, p.rows, p.vocab, shift, counts, k1, r1);
+    else radix_scatter_kernel<false><<<q.tiles, 256, 0, s>>>(p.ids, k0, r0, p.rows, p.vocab, shift, counts, k1, r1);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    uint32_t* k = k0;
+    k0 = k1;
+    k1 = k;
+    int32_t* r = r0;
+    r0 = r1;
+    r1 = r;
+  }
+  *tokens = k0;
+  *order = r0;
+  return cudaSuccess;
+}
+
+}  // namespace
+
+int64_t embedding_grad_bytes(int rows, int d) { return make_plan(rows, d).bytes; }
+
+cudaError_t embedding_launch(const EmbeddingParams& p, cudaStream_t s) {
+  if (p.dtype == SGD_F16) return lookup_to<f16>(p, s);
+  if (p.dtype == SGD_BF16) return lookup_to<bf16>(p, s);
+  return lookup_to<float>(p, s);
+}
+
+cudaError_t embedding_grad_launch(const EmbeddingGradParams& p, cudaStream_t s) {
+  if (!p.accumulate) {
+    const cudaError_t e = p.dtable_dtype == SGD_F32 ? zero<float>(p.dtable, p.ld, p.vocab, p.d, s)
+                                                    : zero<f16>(p.dtable, p.ld, p.vocab, p.d, s);  // (0 is 0 in bf16 too)
+    if (e != cudaSuccess) return e;
+  }
+  if (p.rows == 0) return cudaSuccess;
+  const Plan q = make_plan(p.rows, p.d);
+  char* ws = static_cast<char*>(p.workspace);
+  const uint32_t* tokens = nullptr;
+  const int32_t* order = nullptr;
+  const cudaError_t e = sort_rows(p, q, ws, &tokens, &order, s);
+  if (e != cudaSuccess) return e;
+  const SumArgs a{p.grad, p.ld_grad, tokens, order, p.rows, p.vocab, p.d, q.chunk, q.chunks, q.pd, p.accumulate, p.scale,
+                  reinterpret_cast<float*>(ws + q.partial), p.dtable, p.ld};
+  if (p.grad_dtype == SGD_F16) return sums_to<f16>(a, p.dtable_dtype, s);
+  if (p.grad_dtype == SGD_BF16) return sums_to<bf16>(a, p.dtable_dtype, s);
+  return sums_to<float>(a, p.dtable_dtype, s);
+}
+
+}  // namespace sgd

@@ -349,6 +349,77 @@ struct DistillParams {
 };
 cudaError_t distill_launch(const DistillParams& p, cudaStream_t s);
 
+// A token drawn per row of logits (sgd_kernel_sample).
+struct SampleParams {
+  const void* logits;
+  int dtype;
+  int64_t ld;
+  int rows, vocab;
+  float scale;
+  int top_k;  // 0: all
+  double top_p, min_p;
+  const float* uniforms;  // [rows, 2]
+  const int32_t* row_ids;
+  int row_id;
+  int32_t* ids;
+  float* logprobs;
+};
+cudaError_t sample_launch(const SampleParams& p, cudaStream_t s);
+
+// Rows of an embedding table (sgd_kernel_embedding) and its gradient (sgd_kernel_embedding_grad).
+constexpr int kMaxColumns = 1 << 20;
+struct EmbeddingParams {
+  const void* table;
+  int dtype;
+  int64_t ld;
+  int vocab, d;
+  const int32_t* ids;
+  int rows;
+  float scale;
+  void* out;
+  int out_dtype;
+  int64_t ld_out;
+};
+cudaError_t embedding_launch(const EmbeddingParams& p, cudaStream_t s);
+struct EmbeddingGradParams {
+  const void* grad;
+  int grad_dtype;
+  int64_t ld_grad;
+  const int32_t* ids;
+  int rows, vocab, d;
+  float scale;
+  int accumulate;
+  void* dtable;
+  int dtable_dtype;
+  int64_t ld;
+  void* workspace;
+};
+int64_t embedding_grad_bytes(int rows, int d);
+cudaError_t embedding_grad_launch(const EmbeddingGradParams& p, cudaStream_t s);
+
+// Backward pass of a norm (sgd_kernel_norm_grad).
+struct NormGradParams {
+  const float* h;
+  const void* dout;
+  int dtype;
+  int rows, d, kind;
+  const bf16* g;
+  const bf16* b;
+  const float* scale;
+  int ld_mod, rows_per_batch;
+  float eps;
+  const float* residual;
+  float* dh;
+  float* dg;
+  float* db;
+  float* dshift;
+  float* dscale;
+  int ld_dmod;
+  void* workspace;
+};
+int64_t norm_grad_bytes(int rows, int d, int rows_per_batch);  // rows_per_batch 0: no modulation
+cudaError_t norm_grad_launch(const NormGradParams& p, cudaStream_t s);
+
 // Reveal step of the masked-token sampler (sgd_sampler_reveal).
 constexpr int kRevealMaxTokens = 49152;  // a sample's keys in shared memory: 192 KB
 struct RevealParams {
