@@ -1,4 +1,4 @@
-// A token drawn from each row of logits: temperature, top-k, min-p and top-p, from two given random numbers a row.
+// A token drawn from each row of logits: temperature, top-k, min-p and top-p, from two given random numbers.
 //
 // With x = scale z, w_i = e^(x_i - max x), and the tokens in the order (z descending, index ascending):
 //   K1 = the first top_k of the order that have w_i >= min_p;  K = the shortest prefix of K1 with a mass (sum of w)
@@ -12,493 +12,630 @@
 // falls within their error of a border, which is seen, and the masses are taken anew; inside a block, and where a cut is
 // looked for, masses are whole numbers (weight() below): their sums have no error and no order.
 //
-// A row is read once from HBM: warps take a block each and leave its maximum and, where masses are needed, its sum of
-// exponentials against that maximum.  What comes after looks again only at blocks whose maximum reaches a bound on the cut
-// (the k-th largest of maxima for top-k; max + ln(min_p) / scale; (1 - top_p) Z / vocab for top-p, as all tokens below it have
-// less than the share 1 - top_p together), from L2.  What reaches the bound is sorted in shared memory, or, where it is more than
-// kCap tokens, narrowed first by histograms (counts and masses) of the order's integers.
+// A row is read once from HBM: warps take blocks and leave their maxima and, where masses are needed, their sums of
+// exponentials against the maximum (kError below).  What comes after looks, from L2, only at blocks whose maximum reaches
+// a bound zl that the cut cannot be below:
+//   top-k: the k-th largest of the blocks' maxima, for large k a quantile of a sample of the row;  min-p: max + ln(min_p) / scale;
+//   top-p alone: the 64th largest of the maxima where the maxima above it already have the mass; else from the sample (one token of 8
+//   in a histogram of its weights), which also gives a bound zh that the cut is not above.  What is above zh is summed, what lies
+//   between is listed; if the cut is not in between after all (counts and sums tell), the whole row is searched.
+// The cut is found in the list, or the row, by histograms of counts and masses over the order's integers, 1024 bins at a time,
+// down to 256 tokens, which are ranked by comparing all with all.
 //
-// Many rows: a CTA each, several per SM, so that one's search hides behind the others' reading.  Few: a cluster reads a row.
-#include <math.h>
-
-#include "vocab_rows.cuh"
+// Many rows: a CTA each, three per SM, so that one's search hides behind the others' reading.  Few: a cluster reads a row.
+#include "sample.cuh"
 
 namespace sgd {
 namespace {
 
 using namespace rows;
 
-constexpr int kBlock = SGD_SAMPLE_BLOCK;
-constexpr int kPerLane = kBlock / 32;
-constexpr int kCap = 1024;   // tokens that are sorted
-constexpr int kBinBits = 10;
-constexpr int kHist = 1 << kBinBits;
-constexpr int kOne = 43;     // weight() of the row's maximum is 2^43: 2^20.6 of them (a row of 3 MiB) add up in 64 bits
-static_assert(kBlock == 512, "a lane takes 16 tokens");
+constexpr int kSampled = 16384;  // rows from this many tokens on are sampled
+constexpr int kShort = 4;          // blocks of a row that 64 threads take
+constexpr int kQueue = 64;       // tokens of a block that a warp puts side by side
 
-struct Args {
-  SampleParams p;
-  float c, c_lo;    // scale log2(e), as the sum of two floats
-  double drop;      // ln(min_p) / scale: a token at or above max + drop passes (-inf: every token)
-  int n_blocks;
-};
+// Adds a mass to one in shared memory that others add to as well (two 32-bit additions: whole numbers have no order).
+__device__ __forceinline__ void add_shared(uint32_t* lo, uint32_t* hi, uint64_t w) {
+  const uint32_t low = static_cast<uint32_t>(w), was = atomicAdd(lo, low);
+  const uint32_t high = static_cast<uint32_t>(w >> 32) + (was + low < was);
+  if (high) atomicAdd(hi, high);
+}
 
+template <int kThreads>
 struct __align__(16) Shared {
-  uint64_t list[kCap];
-  union {
-    uint64_t cum[kCap];
-    struct {
-      uint32_t count[kHist], lo[kHist], hi[kHist];
-    };
-  };
-  uint64_t pow2[32];
-  uint64_t wide[32];
-  float part[32];
-  uint64_t total, best;
-  double target;
-  int n, found, bad;
-  uint64_t cut, above_w, mass;
-  uint32_t above_n, bin_n, bin;
-  uint32_t groups[256];
-};
-
-// 2^(j / 32) 2^62, j = 0 .. 31
-__constant__ uint64_t kPow2[32] = {
-    0x4000000000000000ull, 0x4166C34C5615D0ECull, 0x42D561B3E6243D8Aull, 0x444C0740496D4294ull,
-    0x45CAE0F1F545EB73ull, 0x47521CC5A2E6A9E0ull, 0x48E1E9B9D588E19Bull, 0x4A7A77D47F7B84B1ull,
-    0x4C1BF828C6DC54B8ull, 0x4DC69CDCEAA72A9Cull, 0x4F7A993048D088D7ull, 0x513821818624B40Cull,
-    0x52FF6B54D8A89C75ull, 0x54D0AD5A753E077Cull, 0x56AC1F752150A563ull, 0x5891FAC0E95612C8ull,
-    0x5A827999FCEF3242ull, 0x5C7DD7A3B17DCF75ull, 0x5E8451CFAC061B5Full, 0x6096266533384A2Bull,
-    0x62B39508AA836D6Full, 0x64DCDEC3371793D1ull, 0x6712460A8FC24072ull, 0x69540EC8F895722Dull,
-    0x6BA27E656B4EB57Aull, 0x6DFDDBCBED791BABull, 0x70666F76154A7089ull, 0x72DC8373BE41A454ull,
-    0x75606373EE921C97ull, 0x77F25CCDEE6D7AE6ull, 0x7A92BE8A92436616ull, 0x7D41D96DB915019Dull,
-};
-
-// Weight 2^((z - m) c) of a logit against the row's maximum m as a whole number, 2^43 for the maximum: exact to about 2^-31
-// relative and half a unit.  z - m = d + dl exactly, (d + dl) c = t + tl to 2^-45; t + tl = n + j / 32 + g with |g| <= 1/64;
-// 2^g - 1 = g ln2 + ... to the fourth power (the fifth is 1.3e-12).
-__device__ __forceinline__ uint64_t weight(float z, float m, const Args& a, const uint64_t* pow2) {
-  const float d = z - m;
-  const float t = __fmul_rn(d, a.c);
-  if (!(t > -48.f)) return 0;
-  const float back = d - z;
-  const float dl = (z - (d - back)) + (-m - back);
-  const float tl = fmaf(d, a.c, -t) + fmaf(d, a.c_lo, dl * a.c);
-  constexpr float kMagic = 393216.f;  // 1.5 2^18: its unit is 1/32
-  const float y = __fadd_rn(t, kMagic);
-  const int k = __float_as_int(y) - __float_as_int(kMagic);
-  const float g = (t - (y - kMagic)) + tl;
-  const float e = g * fmaf(g, fmaf(g, fmaf(g, 0.009618129f, 0.05550411f), 0.24022651f), 0.6931472f);
-  const uint64_t base = pow2[k & 31];
-  const int64_t more = static_cast<int64_t>(static_cast<int32_t>(base >> 32)) * __float2int_rn(e * 4294967296.f);
-  const uint64_t w = base + static_cast<uint64_t>(more);  // 2^62 .. 2^63
-  const int shift = 62 - kOne - (k >> 5);
-  return shift > 62 ? 0 : (w + (1ull << (shift - 1))) >> shift;
-}
-
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float d;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
-  return d;
-}
-constexpr uint32_t kKeyFinite = 0xFF7FFFFFu;  // of the largest finite value
-constexpr uint32_t kKeyNan = 0xFFFFFFFFu;
-constexpr uint64_t kEverything = static_cast<uint64_t>(kKeyNegInf) << 32;  // the place that no token is behind
-
-__device__ __forceinline__ uint64_t warp_sum_u64(uint64_t v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
-}
-__device__ __forceinline__ uint64_t warp_scan_u64(uint64_t v, int lane) {  // inclusive
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const uint64_t x = __shfl_up_sync(0xffffffffu, v, o);
-    if (lane >= o) v += x;
-  }
-  return v;
-}
-
-// A token's place in the order: larger comes first.
-__device__ __forceinline__ uint64_t place(uint32_t key, int i) {
-  return static_cast<uint64_t>(key) << 32 | static_cast<uint32_t>(0xFFFFFFFFu - static_cast<uint32_t>(i));
-}
-__device__ __forceinline__ int index_of(uint64_t place) { return static_cast<int>(0xFFFFFFFFu - static_cast<uint32_t>(place)); }
-
-// Maximum of a block (NaN where it holds one) and its sum of 2^((z - maximum) c).  VEC: rows start at 16-byte boundaries.
-template <typename T, bool VEC>
-__device__ __forceinline__ void load_block(const T* row, int vocab, int b, int lane, float* f) {
-  const int first = b * kBlock;
-  constexpr int E = Elem<T>::kPer;
-  if (VEC && first + kBlock <= vocab) {
-#pragma unroll
-    for (int i = 0; i < kPerLane / E; ++i)
-      unpack(reinterpret_cast<const uint4*>(row + first)[i * 32 + lane], f + i * E, static_cast<const T*>(nullptr));
-  } else {
-#pragma unroll
-    for (int j = 0; j < kPerLane; ++j) {
-      const int e = first + j * 32 + lane;
-      f[j] = e < vocab ? to_f(row[e]) : -kInf;
-    }
-  }
-}
-template <bool SUM>
-__device__ __forceinline__ float2 block_stat(const float* f, float c) {
-  float m = f[0];
-#pragma unroll
-  for (int j = 1; j < kPerLane; ++j) m = max_nan(m, f[j]);
-  const uint32_t key = __reduce_max_sync(0xffffffffu, m != m ? kKeyNan : order_key(m));
-  if (key > kKeyFinite) return make_float2(kNan, kNan);  // NaN or +inf
-  m = key_value(key);
-  if (!SUM || m == -kInf) return make_float2(m, 0.f);
-  float s[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int j = 0; j < kPerLane; ++j) s[j & 3] += ex2_approx(__fmul_rn(f[j] - m, c));
-  return make_float2(m, warp_sum((s[0] + s[1]) + (s[2] + s[3])));
-}
-
-template <typename T, int kThreads>
-struct Row {
   static constexpr int kWarps = kThreads / 32;
-  const Args& a;
+  static constexpr int kCap = 16 * kThreads;  // tokens of the list
+  static constexpr int kHist = 4 * kThreads;  // bins
+  uint64_t list[kCap];
+  uint32_t count[kHist], lo[kHist], hi[kHist];
+  uint64_t small[kThreads], small_w[kThreads];
+  uint64_t queue[kWarps][kQueue];
+  uint64_t pow2[32];
+  uint64_t wide[2][kWarps];
+  float part[kWarps];
+  uint32_t part_n[kWarps];
+  uint32_t groups[kThreads];
+  uint64_t best;
+  uint64_t cut, cut_before, cut_upto;
+  uint64_t above_w;
+  uint32_t above_n, bin_n, bin;
+  int n, found, bad;
+  int edge[4];
+  uint32_t edge_n[2];
+};
+
+struct Cut {
+  uint64_t place;         // of the last token that is kept
+  uint64_t before, upto;  // the kept mass without it and with it
+};
+
+template <typename T, bool VEC, int kThreads>
+struct Row {
+  using Sh = Shared<kThreads>;
+  static constexpr int kWarps = kThreads / 32, kSmall = kThreads, kCap = Sh::kCap, kHist = Sh::kHist;
+  static constexpr int kBinBits = kThreads == 256 ? 10 : 8;
+  static_assert(kHist == 1 << kBinBits, "bins");
+  const SampleArgs& a;
   const T* row;
   const float* max_of;  // [n_blocks] maxima
   uint64_t* mass;       // [n_blocks]
-  Shared& sh;
+  Sh& sh;
   float m;              // the row's maximum
   int warp, lane;
 
-  __device__ uint64_t w_of(float z) const { return weight(z, m, a, sh.pow2); }
+  __device__ __forceinline__ uint64_t w_of(float z) const { return weight(z, m, a, sh.pow2); }
 
-  // f(key, index, value) for the tokens of blocks whose maximum is at least `least`
+  // f(b, its tokens) for the blocks whose maximum is at least `least`, a warp each, with the next one's tokens on their way
   template <typename F>
-  __device__ void each(float least, F f) const {
-    for (int b = warp; b < a.n_blocks; b += kWarps) {
-      if (!(max_of[b] >= least)) continue;
-      float z[kPerLane];
-#pragma unroll
-      for (int j = 0; j < kPerLane; ++j) {
-        const int e = b * kBlock + j * 32 + lane;
-        z[j] = e < a.p.vocab ? to_f(row[e]) : kNan;
-      }
-#pragma unroll
-      for (int j = 0; j < kPerLane; ++j)
-        if (z[j] == z[j]) f(order_key(z[j]), b * kBlock + j * 32 + lane, z[j]);
+  __device__ __forceinline__ void blocks(float least, F f) const {
+    auto next = [&](int b) {
+      while (b < a.n_blocks && !(max_of[b] >= least)) b += kWarps;
+      return b;
+    };
+    int b = next(warp);
+    if (b >= a.n_blocks) return;
+    Raw<T> raw = fetch<T, VEC>(row, a.p.vocab, b, lane);
+    while (b < a.n_blocks) {
+      const int after = next(b + kWarps);
+      Raw<T> ahead;
+      if (after < a.n_blocks) ahead = fetch<T, VEC>(row, a.p.vocab, after, lane);
+      f(b, raw);
+      raw = ahead;
+      b = after;
     }
   }
-
-  // Sum over the CTA; a barrier before and after.
-  __device__ uint64_t cta_sum(uint64_t v) const {
-    v = warp_sum_u64(v);
-    __syncthreads();
-    if (lane == 0) sh.wide[warp] = v;
-    __syncthreads();
-    uint64_t s = 0;
-    for (int i = 0; i < kWarps; ++i) s += sh.wide[i];
-    return s;
-  }
-
-  // Masses of the blocks, of the tokens at or before `cut` in the order.
-  __device__ void masses(uint64_t cut) const {
-    const float least = key_value(static_cast<uint32_t>(cut >> 32));
-    for (int b = warp; b < a.n_blocks; b += kWarps) {
-      uint64_t s = 0;
-      if (max_of[b] >= least) {
-        float z[kPerLane];
+  // f(place, value) for the tokens of a block that are marked in `on` (bit j: the lane's token j), side by side in the lanes where they
+  // are few, else one of each lane at a time
+  template <typename F>
+  __device__ __forceinline__ void marked(int b, const float* z, uint32_t on, F f) const {
+    const int mine = __popc(on);
+    int up = mine;
 #pragma unroll
-        for (int j = 0; j < kPerLane; ++j) {
-          const int e = b * kBlock + j * 32 + lane;
-          z[j] = e < a.p.vocab ? to_f(row[e]) : -kInf;
-        }
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, up, o);
+      if (lane >= o) up += x;
+    }
+    const int all = __shfl_sync(0xffffffffu, up, 31);
+    if (all == 0) return;
+    if (all <= kQueue) {
+      int at = up - mine;
+      if (on) {
 #pragma unroll
         for (int j = 0; j < kPerLane; ++j)
-          if (place(order_key(z[j]), b * kBlock + j * 32 + lane) >= cut) s += w_of(z[j]);
-        s = warp_sum_u64(s);
+          if (on >> j & 1) sh.queue[warp][at++] = place(order_key(z[j]), token_at<T, VEC>(b, lane, j));
       }
-      if (lane == 0) mass[b] = s;
+      __syncwarp();
+      for (int i = lane; i < all; i += 32) f(sh.queue[warp][i], value_of(sh.queue[warp][i]));
+      __syncwarp();
+      return;
     }
-    __syncthreads();
-  }
-
-  // Sorts the n tokens of the list (descending) and leaves the cumulative masses in cum.
-  __device__ void sort(int n) const {
-    if (n <= kThreads) {
-      const uint64_t mine = threadIdx.x < n ? sh.list[threadIdx.x] : 0;
-      int before = 0;
-      if (threadIdx.x < n)
-        for (int i = 0; i < n; ++i) before += sh.list[i] > mine;
-      __syncthreads();
-      if (threadIdx.x < n) sh.list[before] = mine;
-      __syncthreads();
-    } else {
-      int all = kThreads;
-      while (all < n) all *= 2;
-      for (int i = n + threadIdx.x; i < all; i += kThreads) sh.list[i] = 0;
-      __syncthreads();
-      for (int size = 2; size <= all; size *= 2) {
-        for (int step = size / 2; step > 0; step /= 2) {
-          for (int i = threadIdx.x; i < all / 2; i += kThreads) {
-            const int x = 2 * i - (i & (step - 1)), y = x + step;
-            const uint64_t p = sh.list[x], q = sh.list[y];
-            const bool descending = (x & size) == 0;
-            if ((p < q) == descending) {
-              sh.list[x] = q;
-              sh.list[y] = p;
-            }
-          }
-          __syncthreads();
+#pragma unroll 1
+    while (__any_sync(0xffffffffu, on)) {
+      if (on) {
+        const int e = token_at<T, VEC>(b, lane, __ffs(on) - 1);
+        on &= on - 1;
+        if (e < a.p.vocab) {
+          const float x = to_f(row[e]);
+          f(place(order_key(x), e), x);
         }
       }
+      __syncwarp();
     }
-    // inclusive sums, kCap / kThreads neighbours a thread
-    constexpr int kPer = kCap / kThreads;
-    uint64_t w[kPer], s = 0;
+  }
+  // f(place, value) for the row's tokens at or before `from` in the order
+  template <typename F>
+  __device__ __forceinline__ void each(uint64_t from, F f) const {
+    const float least = value_of(from);
+    blocks(least, [&](int b, const Raw<T>& raw) {
+      float z[kPerLane];
+      numbers(raw, z);
+      uint32_t on = 0;
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const int i = threadIdx.x * kPer + j;
-      s += w[j] = i < n ? w_of(key_value(static_cast<uint32_t>(sh.list[i] >> 32))) : 0;
-    }
-    const uint64_t up = warp_scan_u64(s, lane);
-    if (lane == 31) sh.wide[warp] = up;
-    __syncthreads();
-    uint64_t run = up - s;
-    for (int i = 0; i < warp; ++i) run += sh.wide[i];
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const int i = threadIdx.x * kPer + j;
-      run += w[j];
-      if (i < n) sh.cum[i] = run;
-    }
-    __syncthreads();
+      for (int j = 0; j < kPerLane; ++j) on |= (z[j] >= least && token_at<T, VEC>(b, lane, j) < a.p.vocab ? 1u : 0u) << j;
+      marked(b, z, on, [&](uint64_t x, float y) {
+        if (x >= from) f(x, y);
+      });
+    });
   }
 
-  // Tokens with keys lo .. hi into the list; returns how many there are (the list holds the first kCap that came).
-  __device__ int gather(uint32_t lo, uint32_t hi) const {
+  // Sums over the CTA; a barrier before and after.
+  __device__ ulonglong2 cta_sum(uint64_t v, uint64_t w) const {
+    v = warp_sum_u64(v);
+    w = warp_sum_u64(w);
+    __syncthreads();
+    if (lane == 0) {
+      sh.wide[0][warp] = v;
+      sh.wide[1][warp] = w;
+    }
+    __syncthreads();
+    ulonglong2 s = make_ulonglong2(0, 0);
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) {
+      s.x += sh.wide[0][i];
+      s.y += sh.wide[1][i];
+    }
+    return s;
+  }
+  __device__ uint64_t cta_sum(uint64_t v) const { return cta_sum(v, 0).x; }
+
+  // Place in a list of n counted so far (one atomic for the lanes that are here).
+  __device__ __forceinline__ int slot(int* n) const {
+    const uint32_t here = __activemask();
+    const int first = __ffs(here) - 1;
+    int at = 0;
+    if (lane == first) at = atomicAdd(n, __popc(here));
+    return __shfl_sync(here, at, first) + __popc(here & ((1u << lane) - 1u));
+  }
+
+  struct Rest {
+    uint64_t above, tail, error;
+  };
+  // Tokens above zh: their masses by blocks, and in rest->above together; those from zl to zh: into the list, as far as it goes; with
+  // TAIL those below: their mass from fp32 sums, and how far it may be off (`mass` holds the blocks' masses at the call).
+  // Returns how many are from zl to zh.
+  template <bool TAIL>
+  __device__ int bracket(float zl, float zh, Rest* rest) const {
     __syncthreads();
     if (threadIdx.x == 0) sh.n = 0;
     __syncthreads();
-    each(key_value(lo), [&](uint32_t key, int i, float) {
-      if (key >= lo && key <= hi) {
-        const int at = atomicAdd(&sh.n, 1);
-        if (at < kCap) sh.list[at] = place(key, i);
+    uint64_t above = 0, tail = 0, skipped = 0;
+    for (int b = threadIdx.x; b < a.n_blocks; b += kThreads)
+      if (!(max_of[b] >= zl)) {
+        if (TAIL) skipped += mass[b];
+        mass[b] = 0;
+      }
+    blocks(zl, [&](int b, const Raw<T>& raw) {
+      float z[kPerLane];
+      numbers(raw, z);
+      uint32_t on = 0;
+      float low[2] = {0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < kPerLane; ++j) {
+        const bool is = z[j] >= zl;
+        on |= (is ? 1u : 0u) << j;
+        if (TAIL) low[j & 1] += is ? 0.f : ex2_approx(__fmul_rn(z[j] - zl, a.c));
+      }
+      if (zl == -kInf)  // (what is no token is -inf)
+#pragma unroll
+        for (int j = 0; j < kPerLane; ++j)
+          if (token_at<T, VEC>(b, lane, j) >= a.p.vocab) on &= ~(1u << j);
+      uint64_t s = 0;
+      marked(b, z, on, [&](uint64_t x, float y) {
+        if (y > zh) {
+          s += w_of(y);
+        } else {
+          const int at = slot(&sh.n);
+          if (at < kCap) sh.list[at] = x;
+        }
+      });
+      if (__any_sync(0xffffffffu, s != 0)) s = warp_sum_u64(s);
+      const float l = TAIL ? warp_sum(low[0] + low[1]) : 0.f;
+      if (lane == 0) {
+        mass[b] = s;
+        above += s;
+        if (TAIL) tail += block_mass(zl, l, m, a, sh.pow2);
       }
     });
-    __syncthreads();
+    const ulonglong2 both = cta_sum(above, tail);
+    rest->above = both.x;
+    if (TAIL) {
+      // of the tail's sums against zl: 18 u, and three roundings of an exponent t whose mean over the mass S (of zl's weight) is at
+      // most log2(vocab) - log2(S); and tokens below 2^-43
+      skipped = cta_sum(skipped);
+      const float s = static_cast<float>(both.y), spread = s > 0.f ? log2f(a.p.vocab * (static_cast<float>(w_of(zl)) + 1.f) / s) : 0.f;
+      rest->tail = both.y + skipped;
+      rest->error = static_cast<uint64_t>(a.n_blocks) + a.p.vocab +
+                    __double2ull_ru(kError * static_cast<double>(skipped) +
+                                    (20.0 + 2.1 * fmaxf(spread, 0.f)) * 5.9604645e-8 * static_cast<double>(both.y));
+    }
     return sh.n;
   }
 
-  // Number of the first n cumulative masses (plus `above`) that are below `target`.
-  __device__ int below(int n, uint64_t above, double target) const {
+  // Masses of the blocks, of the tokens at or before `cut` in the order; returns the whole.
+  __device__ uint64_t masses(uint64_t cut) const {
+    const float least = value_of(cut);
+    uint64_t all = 0;
     __syncthreads();
-    if (threadIdx.x == 0) sh.found = 0;
+    for (int b = threadIdx.x; b < a.n_blocks; b += kThreads)
+      if (!(max_of[b] >= least)) mass[b] = 0;
+    blocks(least, [&](int b, const Raw<T>& raw) {
+      const uint64_t s = warp_sum_u64(raw_mass<T, VEC>(raw, b, lane, a.p.vocab, cut, m, a, sh.pow2));
+      if (lane == 0) {
+        mass[b] = s;
+        all += s;
+      }
+    });
+    return cta_sum(all);
+  }
+  // Adds the list's tokens that are kept to the blocks' masses.
+  __device__ void add_list(int n, uint64_t cut) const {
     __syncthreads();
-    int k = 0;
-    for (int i = threadIdx.x; i < n; i += kThreads) k += static_cast<double>(above + sh.cum[i]) < target;
-    k = __reduce_add_sync(0xffffffffu, k);
-    if (lane == 0 && k) atomicAdd(&sh.found, k);
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+      const uint64_t x = sh.list[i];
+      if (x < cut) continue;
+      uint32_t* to = reinterpret_cast<uint32_t*>(mass + index_of(x) / kBlock);
+      add_shared(to, to + 1, w_of(value_of(x)));
+    }
     __syncthreads();
-    return sh.found;
   }
 
-  // The last token of the shortest prefix of the order, among the tokens with keys lo .. hi, that has `count` tokens or
-  // (count 0) a mass of at least `target`.  *mass_of: the prefix's mass.
-  __device__ uint64_t find_cut(uint32_t lo, uint32_t hi, uint32_t count, double target, uint64_t* mass_of) const {
-    uint32_t above_n = 0;
-    uint64_t above_w = 0;
-    for (;;) {
-      const int shift = max(0, 32 - __clz(hi - lo) - kBinBits);
+  // Where a cut is looked for: the list, or the row.
+  struct List {
+    static constexpr bool kRow = false;
+    const Row& r;
+    int n;
+    template <typename F>
+    __device__ __forceinline__ void each(uint64_t from, F f) const {
+      for (int i = threadIdx.x; i < n; i += kThreads) {
+        const uint64_t x = r.sh.list[i];
+        if (x >= from) f(x, value_of(x));
+      }
+    }
+  };
+  struct Whole {
+    static constexpr bool kRow = true;
+    const Row& r;
+    template <typename F>
+    __device__ __forceinline__ void each(uint64_t from, F f) const {
+      r.each(from, f);
+    }
+  };
+  __device__ uint64_t sum_of_list(int n, uint64_t from) const {
+    uint64_t s = 0;
+    List{*this, n}.each(from, [&](uint64_t, float z) { s += w_of(z); });
+    return cta_sum(s);
+  }
+
+  // The last token of the shortest prefix of the order, among the tokens of src with places lo .. hi (n at most) and those above them (above_n
+  // tokens with the mass above_w), that has `count` tokens or (count 0) a mass of at least `target`.
+  template <typename S>
+  __device__ Cut find_cut(const S& src, int n, uint64_t lo, uint64_t hi, uint32_t count, uint64_t target, uint32_t above_n,
+                          uint64_t above_w) const {
+    while (n > kSmall) {
+      const int shift = max(0, 64 - __clzll(hi - lo) - kBinBits);
       __syncthreads();
       for (int i = threadIdx.x; i < kHist; i += kThreads) sh.count[i] = sh.lo[i] = sh.hi[i] = 0;
       __syncthreads();
-      each(key_value(lo), [&](uint32_t key, int, float z) {
-        if (key < lo || key > hi) return;
-        const uint32_t bin = (hi - key) >> shift;
-        const uint64_t w = w_of(z);
+      src.each(lo, [&](uint64_t x, float z) {
+        if (x > hi) return;
+        const uint32_t bin = static_cast<uint32_t>((hi - x) >> shift);
         atomicAdd(&sh.count[bin], 1u);
-        const uint32_t low = static_cast<uint32_t>(w), was = atomicAdd(&sh.lo[bin], low);
-        const uint32_t high = static_cast<uint32_t>(w >> 32) + (was + low < was);
-        if (high) atomicAdd(&sh.hi[bin], high);
+        add_shared(&sh.lo[bin], &sh.hi[bin], w_of(z));
       });
       __syncthreads();
-      if (warp == 0) {  // kHist / 32 neighbouring bins a lane
-        constexpr int kPer = kHist / 32;
-        uint32_t n = 0;
-        uint64_t w = 0;
-        for (int j = 0; j < kPer; ++j) {
-          const int i = lane * kPer + j;
-          n += sh.count[i];
-          w += static_cast<uint64_t>(sh.hi[i]) << 32 | sh.lo[i];
-        }
-        uint32_t before_n = n;
-        uint64_t before_w = warp_scan_u64(w, lane) - w;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const uint32_t x = __shfl_up_sync(0xffffffffu, before_n, o);
-          if (lane >= o) before_n += x;
-        }
-        before_n -= n;
-        before_n += above_n;
-        before_w += above_w;
-        auto reached = [&](uint32_t cn, uint64_t cw) { return count ? cn >= count : static_cast<double>(cw) >= target; };
-        // the lane where the target is reached; where rounding leaves none, the last one that holds anything
-        uint32_t lanes = __ballot_sync(0xffffffffu, n > 0 && reached(before_n + n, before_w + w));
-        const uint32_t held = __ballot_sync(0xffffffffu, n > 0);
-        const int which = lanes ? __ffs(lanes) - 1 : 31 - __clz(held);
-        if (lane == which) {
-          int last = 0;
-          uint32_t last_n = 0;
-          uint64_t last_w = 0;
-          for (int j = 0; j < kPer; ++j) {
-            const int i = lane * kPer + j;
-            const uint32_t cn = sh.count[i];
-            const uint64_t cw = static_cast<uint64_t>(sh.hi[i]) << 32 | sh.lo[i];
-            if (cn == 0) continue;
-            last = i;
-            last_n = before_n;
-            last_w = before_w;
-            before_n += cn;
-            before_w += cw;
-            if (reached(before_n, before_w)) break;
-          }
-          sh.bin = last;
-          sh.bin_n = sh.count[last];
-          sh.above_n = last_n;
-          sh.above_w = last_w;
-        }
-      }
-      __syncthreads();
+      pick_bin(count, target, above_n, above_w);
       above_n = sh.above_n;
       above_w = sh.above_w;
-      const uint32_t inside = sh.bin_n;
-      hi -= sh.bin << shift;
-      const uint32_t width = (1u << shift) - 1u;
-      lo = hi - lo > width ? hi - width : lo;
-      if (inside <= kCap) {
-        const int n = gather(lo, hi);
-        sort(n);
-        int k = count ? static_cast<int>(count - above_n) - 1 : below(n, above_w, target);
-        k = min(max(k, 0), n - 1);
-        const uint64_t cut = sh.list[k];
-        *mass_of = above_w + sh.cum[k];
-        __syncthreads();
-        return cut;
-      }
-      if (shift == 0) {  // equal logits alone: the first `take` of them
-        const uint64_t w = w_of(key_value(hi));
-        uint32_t take;
-        if (count) take = count - above_n;
-        else if (w == 0) take = inside;
-        else {
-          const double need = ceil((target - static_cast<double>(above_w)) / static_cast<double>(w));
-          take = need >= inside ? inside : static_cast<uint32_t>(max(need, 1.0));
+      n = sh.bin_n;
+      hi -= static_cast<uint64_t>(sh.bin) << shift;
+      const uint64_t width = (1ull << shift) - 1ull;
+      if (hi - lo > width) lo = hi - width;
+      if constexpr (S::kRow) {
+        if (n <= kCap && n > kSmall) {
+          gather(src, lo, hi, sh.list, kCap);
+          return find_cut(List{*this, n}, n, lo, hi, count, target, above_n, above_w);
         }
-        take = min(max(take, 1u), inside);
-        *mass_of = above_w + w * take;
-        return place(hi, tie(hi, take));
       }
     }
-  }
-
-  // Index of the n-th token (n >= 1) whose key is `key`: counts per block, then inside the block.
-  __device__ int tie(uint32_t key, uint32_t n) const {
-    const float z = key_value(key);
-    for (int b = warp; b < a.n_blocks; b += kWarps) {
-      uint32_t k = 0;
-      if (max_of[b] >= z)
-        for (int j = 0; j < kPerLane; ++j) {
-          const int e = b * kBlock + j * 32 + lane;
-          if (e < a.p.vocab) k += order_key(to_f(row[e])) == key;
+    gather(src, lo, hi, sh.small, kSmall);
+    n = sh.n;
+    const int t = threadIdx.x;
+    const uint64_t x = t < n ? sh.small[t] : 0;
+    const uint64_t w = t < n ? w_of(value_of(x)) : 0;
+    sh.small_w[t] = w;
+    if (t == 0) sh.cut = 0;
+    __syncthreads();
+    uint32_t rank = above_n;
+    uint64_t cum = above_w;
+    if (t < n)
+      for (int i = 0; i < n; ++i)
+        if (sh.small[i] >= x) {
+          ++rank;
+          cum += sh.small_w[i];
         }
-      k = __reduce_add_sync(0xffffffffu, k);
-      if (lane == 0) mass[b] = k;
+    // (where rounding leaves none, the last one)
+    const bool it = t < n && (count ? rank == count : cum >= target && cum - w < target);
+    auto write = [&] {
+      sh.cut = x;
+      sh.cut_before = cum - w;
+      sh.cut_upto = cum;
+    };
+    if (it) write();
+    __syncthreads();
+    const bool none = sh.cut == 0;
+    __syncthreads();
+    if (none && t < n && rank == above_n + n) write();
+    __syncthreads();
+    const Cut cut{sh.cut, sh.cut_before, sh.cut_upto};
+    __syncthreads();
+    return cut;
+  }
+  template <typename S>
+  __device__ void gather(const S& src, uint64_t lo, uint64_t hi, uint64_t* to, int cap) const {
+    __syncthreads();
+    if (threadIdx.x == 0) sh.n = 0;
+    __syncthreads();
+    src.each(lo, [&](uint64_t x, float) {
+      if (x > hi) return;
+      const int at = slot(&sh.n);
+      if (at < cap) to[at] = x;
+    });
+    __syncthreads();
+  }
+  // The histogram's first bin with which the target is reached (where rounding leaves none, the last one that holds anything),
+  // and what is above it.
+  __device__ void pick_bin(uint32_t count, uint64_t target, uint32_t above_n, uint64_t above_w) const {
+    if (warp == 0) {
+      constexpr int kPer = kHist / 32;  // neighbouring bins of a lane
+      uint32_t n = 0;
+      uint64_t w = 0;
+      for (int j = 0; j < kPer; ++j) {
+        const int i = lane * kPer + j;
+        n += sh.count[i];
+        w += static_cast<uint64_t>(sh.hi[i]) << 32 | sh.lo[i];
+      }
+      uint32_t before_n = n;
+      uint64_t before_w = above_w + warp_scan_u64(w, lane) - w;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t x = __shfl_up_sync(0xffffffffu, before_n, o);
+        if (lane >= o) before_n += x;
+      }
+      before_n += above_n - n;
+      auto reached = [&](uint32_t cn, uint64_t cw) { return count ? cn >= count : cw >= target; };
+      const uint32_t lanes = __ballot_sync(0xffffffffu, n > 0 && reached(before_n + n, before_w + w));
+      const uint32_t held = __ballot_sync(0xffffffffu, n > 0);
+      const int which = lanes ? __ffs(lanes) - 1 : 31 - __clz(held);
+      if (lane == which) {
+        for (int j = 0; j < kPer; ++j) {
+          const int i = lane * kPer + j;
+          const uint32_t cn = sh.count[i];
+          if (cn == 0) continue;
+          sh.bin = i;
+          sh.bin_n = cn;
+          sh.above_n = before_n;
+          sh.above_w = before_w;
+          before_n += cn;
+          before_w += static_cast<uint64_t>(sh.hi[i]) << 32 | sh.lo[i];
+          if (reached(before_n, before_w)) break;
+        }
+      }
     }
     __syncthreads();
-    if (threadIdx.x == 0) {
-      uint32_t left = n;
-      int b = 0;
-      while (b < a.n_blocks - 1 && mass[b] < left) left -= static_cast<uint32_t>(mass[b++]);
-      int e = b * kBlock;
-      for (; e < a.p.vocab; ++e)
-        if (order_key(to_f(row[e])) == key && --left == 0) break;
-      sh.found = min(e, a.p.vocab - 1);
-    }
-    __syncthreads();
-    const int at = sh.found;
-    __syncthreads();
-    return at;
   }
 
-  // Lower bound on the key of the top_k-th token: the k-th largest of 256 groups' maxima.
+  // Key of the k-th largest of kThreads groups' maxima (k <= kThreads): at least k tokens have it or more.
   __device__ uint32_t bound_of_k(int k) const {
-    static_assert(kThreads >= 256, "a thread per group");
-    if (k > 256) return 0;
     float g = -kInf;
-    if (threadIdx.x < 256) {
-      for (int b = threadIdx.x; b < a.n_blocks; b += 256) g = fmaxf(g, max_of[b]);
-      sh.groups[threadIdx.x] = order_key(g);
-    }
-    if (threadIdx.x == 0) sh.found = 0;
+    for (int b = threadIdx.x; b < a.n_blocks; b += kThreads) g = fmaxf(g, max_of[b]);
+    const uint32_t mine = order_key(g);
+    sh.groups[threadIdx.x] = mine;
     __syncthreads();
-    if (threadIdx.x < 256) {
-      const uint32_t mine = sh.groups[threadIdx.x];
-      int more = 0;
-      for (int i = 0; i < 256; ++i) {
-        const uint32_t x = sh.groups[i];
-        more += x > mine || (x == mine && i < threadIdx.x);
+    int more = 0;
+#pragma unroll 4
+    for (int i = 0; i < kThreads; i += 4) {
+      const uint4 x = *reinterpret_cast<const uint4*>(sh.groups + i);
+      const int t = threadIdx.x;
+      more += (x.x > mine || (x.x == mine && i < t)) + (x.y > mine || (x.y == mine && i + 1 < t)) +
+              (x.z > mine || (x.z == mine && i + 2 < t)) + (x.w > mine || (x.w == mine && i + 3 < t));
+    }
+    if (more == k - 1) sh.above_n = mine;
+    __syncthreads();
+    const uint32_t key = sh.above_n;
+    __syncthreads();
+    return key;
+  }
+
+  // Weights of a sample of the row, one token of 8 or more, in runs of 8: count[i] of those in the i-th 1/32 of an octave from the
+  // maximum down.  Returns how many were looked at.
+  __device__ int sampled() const {
+    const int vocab = a.p.vocab, runs = max(4, (vocab / 8 + 8 * kThreads - 1) / (8 * kThreads));  // of a thread
+    __syncthreads();
+    for (int i = threadIdx.x; i < kHist; i += kThreads) sh.count[i] = 0;
+    if (threadIdx.x < 2) sh.edge[threadIdx.x] = kHist;
+    __syncthreads();
+    const int64_t all = static_cast<int64_t>(runs) * kThreads;
+    for (int k = 0; k < runs; ++k) {
+      int e = static_cast<int>((static_cast<int64_t>(k) * kThreads + threadIdx.x) * (vocab - 8) / all);
+      float z[8];
+      if (VEC) {
+        e &= ~7;
+#pragma unroll
+        for (int i = 0; i < 8 / Elem<T>::kPer; ++i)
+          unpack(reinterpret_cast<const uint4*>(row + e)[i], z + i * Elem<T>::kPer, static_cast<const T*>(nullptr));
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) z[j] = to_f(row[e + j]);
       }
-      if (more == k - 1) sh.found = static_cast<int>(mine);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) atomicAdd(&sh.count[static_cast<int>(fminf((m - z[j]) * a.c * 32.f, kHist - 1.f))], 1u);
     }
     __syncthreads();
-    return static_cast<uint32_t>(sh.found);
+    return static_cast<int>(8 * all);
+  }
+  // A value that about 1.3 k + 400 tokens reach, from the sample.
+  __device__ float sampled_bound_of_k(int k) const {
+    constexpr int kPer = kHist / kThreads;
+    const int looked = sampled();
+    uint32_t n[kPer], sum = 0;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) n[j] = sum += sh.count[threadIdx.x * kPer + j];
+    uint32_t up = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t x = __shfl_up_sync(0xffffffffu, up, o);
+      if (lane >= o) up += x;
+    }
+    if (lane == 31) sh.part_n[warp] = up;
+    __syncthreads();
+    up -= sum;
+    for (int i = 0; i < warp; ++i) up += sh.part_n[i];
+    const double want = (1.3 * k + 400.0) * looked / a.p.vocab;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+      if (up + n[j] >= want) atomicMin(&sh.edge[0], static_cast<int>(threadIdx.x) * kPer + j + 1);
+    __syncthreads();
+    const int edge = sh.edge[0];
+    return edge >= kHist ? -kInf : m - edge / (32.f * a.c);
+  }
+  // Bounds {zl, zh} on the cut by mass, from the sample: tokens below the cut have the mass `share` (of the maximum's weight)
+  // together.  Nothing is lost where they are wrong but time.
+  __device__ float2 sampled_bounds(double share) const {
+    constexpr int kPer = kHist / kThreads;  // bins of a thread
+    const int looked = sampled();
+    // from the low end: tokens in a thread's bins and below, and their mass
+    uint32_t n[kPer + 1];
+    float f[kPer + 1];
+    n[kPer] = 0;
+    f[kPer] = 0.f;
+#pragma unroll
+    for (int j = kPer - 1; j >= 0; --j) {
+      const int i = threadIdx.x * kPer + j;
+      n[j] = n[j + 1] + sh.count[i];
+      f[j] = f[j + 1] + sh.count[i] * ex2_approx(-(i + 0.5f) / 32.f);
+    }
+    uint32_t up_n = n[0];
+    float up_f = f[0];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t x = __shfl_down_sync(0xffffffffu, up_n, o);
+      const float y = __shfl_down_sync(0xffffffffu, up_f, o);
+      if (lane + o < 32) {
+        up_n += x;
+        up_f += y;
+      }
+    }
+    if (lane == 0) {
+      sh.part_n[warp] = up_n;
+      sh.part[warp] = up_f;
+    }
+    __syncthreads();
+    up_n -= n[0];
+    up_f -= f[0];
+    for (int i = warp + 1; i < kWarps; ++i) {
+      up_n += sh.part_n[i];
+      up_f += sh.part[i];
+    }
+    const float want = static_cast<float>(share * looked / a.p.vocab);
+    // edge 0: the first bin below which (and with it) there is less than 0.95 of the mass; edge 1: 1.05
+#pragma unroll
+    for (int j = kPer - 1; j >= 0; --j) {
+      const float here = f[j] + up_f;
+      const int i = threadIdx.x * kPer + j;
+      if (here <= 0.95f * want) atomicMin(&sh.edge[0], i);
+      if (here <= 1.05f * want) atomicMin(&sh.edge[1], i);
+    }
+    __syncthreads();
+    const int low = sh.edge[0], high = sh.edge[1];
+    // 64 sampled tokens more below, 32 above: 800 of the row, which the list has room for
+    if (threadIdx.x == 0) {
+      sh.edge[2] = kHist;
+      sh.edge[3] = 0;
+      sh.edge_n[0] = sh.edge_n[1] = 0;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const int i = threadIdx.x * kPer + j;
+      if (i == low) sh.edge_n[0] = n[j] + up_n;
+      if (i == high) sh.edge_n[1] = n[j] + up_n;
+    }
+    __syncthreads();
+    const uint32_t n_low = sh.edge_n[0], n_high = sh.edge_n[1];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const int i = threadIdx.x * kPer + j;
+      if (n_low >= 64 && n[j] + up_n <= n_low - 64) atomicMin(&sh.edge[2], i);
+      if (n[j] + up_n >= n_high + 32) atomicMax(&sh.edge[3], i);
+    }
+    __syncthreads();
+    const int zl = sh.edge[2], zh = sh.edge[3];
+    __syncthreads();
+    return make_float2(zl >= kHist ? -kInf : m - zl / (32.f * a.c), zh <= 0 ? kInf : m - zh / (32.f * a.c));
   }
 };
 
 template <typename T, bool VEC, int kThreads>
-__global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const Args a) {
+__global__ void __launch_bounds__(kThreads, kThreads == 256 ? 3 : 12) sample_kernel(const SampleArgs a) {
   constexpr int kWarps = kThreads / 32;
+  using Sh = Shared<kThreads>;
   extern __shared__ __align__(16) unsigned char dynamic[];  // Shared, then [n_blocks] masses and maxima
-  Shared& sh = *reinterpret_cast<Shared*>(dynamic);
+  Sh& sh = *reinterpret_cast<Sh*>(dynamic);
   const SampleParams& p = a.p;
-  uint64_t* mass = reinterpret_cast<uint64_t*>(dynamic + sizeof(Shared));
+  uint64_t* mass = reinterpret_cast<uint64_t*>(dynamic + sizeof(Sh));
   float* max_of = reinterpret_cast<float*>(mass + a.n_blocks);
   const int rank = cluster_rank(), n_ctas = cluster_ctas();
   const int64_t r = blockIdx.x / n_ctas;
   if (p.row_ids && p.row_ids[r] != p.row_id) return;  // the whole cluster
   const T* row = static_cast<const T*>(p.logits) + r * p.ld;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  cluster_arrive();
-  if (threadIdx.x < 32) sh.pow2[threadIdx.x] = kPow2[threadIdx.x];
-  if (threadIdx.x == 0) {
-    sh.bad = 0;
-    sh.best = 0;
-  }
+  if (n_ctas > 1) cluster_arrive();
   const bool by_k = p.top_k > 0 && p.top_k < p.vocab, by_m = a.drop != -HUGE_VAL, by_p = p.top_p < 1.0;
   const bool sums = p.logprobs || !(by_k || by_m);
-  cluster_wait();  // every CTA of the cluster runs: the leader's shared memory may be written
+  const float u0 = p.uniforms[2 * r], u1 = p.uniforms[2 * r + 1];
   {
-    const uint32_t to_max = map_to_rank(smem_u32(max_of), 0), to_mass = map_to_rank(smem_u32(mass), 0);
-    constexpr int kAhead = 2;
+    // two blocks of 16-bit logits, or one of fp32, in hand and as many on their way
+    constexpr int kPair = sizeof(T) == 2 ? 2 : 1;
     const int stride = kWarps * n_ctas;
-    for (int b = warp * n_ctas + rank; b < a.n_blocks; b += kAhead * stride) {
-      float f[kAhead][kPerLane];
+    int b = warp * n_ctas + rank;
+    Raw<T> next[kPair];
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u)
-        if (b + u * stride < a.n_blocks) load_block<T, VEC>(row, p.vocab, b + u * stride, lane, f[u]);
+    for (int u = 0; u < kPair; ++u)
+      if (b + u * stride < a.n_blocks) next[u] = fetch<T, VEC>(row, p.vocab, b + u * stride, lane);
+    if (threadIdx.x < 32) sh.pow2[threadIdx.x] = kPow2[threadIdx.x];
+    if (threadIdx.x == 0) {
+      sh.bad = 0;
+      sh.best = 0;
+    }
+    const uint32_t to_max = map_to_rank(smem_u32(max_of), 0), to_mass = map_to_rank(smem_u32(mass), 0);
+    if (n_ctas > 1) cluster_wait();  // every CTA of the cluster runs: the leader's shared memory may be written
+    for (; b < a.n_blocks; b += kPair * stride) {
+      Raw<T> cur[kPair];
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        const int at = b + u * stride;
-        if (at >= a.n_blocks) break;
-        const float2 s = sums ? block_stat<true>(f[u], a.c) : block_stat<false>(f[u], a.c);
-        if (lane == 0) {
-          st_cluster(to_max + 4 * at, s.x);
-          st_cluster(to_mass + 8 * at, static_cast<uint64_t>(__float_as_uint(s.y)));
+      for (int u = 0; u < kPair; ++u) {
+        cur[u] = next[u];
+        if (b + (kPair + u) * stride < a.n_blocks) next[u] = fetch<T, VEC>(row, p.vocab, b + (kPair + u) * stride, lane);
+      }
+      const float2 st = block_stats<T, kPair>(cur, sums, a.c, lane);
+      const int at = kPair == 2 && lane >= 16 ? b + stride : b;
+      if ((lane == 0 || (kPair == 2 && lane == 16)) && at < a.n_blocks) {
+        if (n_ctas == 1) {
+          max_of[at] = st.x;
+          mass[at] = __float_as_uint(st.y);
+        } else {
+          st_cluster(to_max + 4 * at, st.x);
+          st_cluster(to_mass + 8 * at, static_cast<uint64_t>(__float_as_uint(st.y)));
         }
       }
     }
   }
-  __syncwarp();
-  cluster_sync();
-  if (rank != 0) return;
+  if (n_ctas > 1) {
+    __syncwarp();
+    cluster_sync();
+    if (rank != 0) return;
+  } else {
+    __syncthreads();
+  }
 
   // the row's maximum
   float m = -kInf;
@@ -516,15 +653,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
   for (int i = 0; i < kWarps; ++i) m = fmaxf(m, sh.part[i]);
   if (sh.bad || m == -kInf) {
     // no distribution: the first token of the order
-    uint64_t first = 0;
-    bool nan = false;
-    for (int i = threadIdx.x; i < p.vocab; i += kThreads) {
-      const float z = to_f(row[i]);
-      nan |= z != z || z == kInf;
-      const uint64_t x = place(order_key(z), i);
-      first = x > first ? x : first;
-    }
-    atomicMax(reinterpret_cast<unsigned long long*>(&sh.best), static_cast<unsigned long long>(first));
+    const uint64_t first = first_of_order(row, p.vocab, threadIdx.x, kThreads);
+    if (lane == 0) atomicMax(reinterpret_cast<unsigned long long*>(&sh.best), static_cast<unsigned long long>(first));
     __syncthreads();
     if (threadIdx.x == 0) {
       p.ids[r] = index_of(sh.best);
@@ -533,163 +663,140 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     return;
   }
 
-  const Row<T, kThreads> t{a, row, max_of, mass, sh, m, warp, lane};
+  using R = Row<T, VEC, kThreads>;
+  const R t{a, row, max_of, mass, sh, m, warp, lane};
   // masses of whole blocks from their fp32 sums, and the row's
-  uint64_t all = 0;
+  uint64_t whole = 0;
   if (sums) {
     for (int b = threadIdx.x; b < a.n_blocks; b += kThreads) {
-      const float s = __uint_as_float(static_cast<uint32_t>(mass[b]));
-      const uint64_t x = max_of[b] == -kInf ? 0 : __double2ull_rn(static_cast<double>(s) * static_cast<double>(t.w_of(max_of[b])));
+      const uint64_t x = block_mass(max_of[b], __uint_as_float(static_cast<uint32_t>(mass[b])), m, a, sh.pow2);
       mass[b] = x;
-      all += x;
+      whole += x;
     }
-    all = t.cta_sum(all);
+    whole = t.cta_sum(whole);
   }
-  const double whole = static_cast<double>(all);
 
   uint64_t cut = kEverything;
   bool exact = false;
   if (by_k || by_m || by_p) {
-    uint32_t lo = kKeyNegInf;
-    const uint32_t top = order_key(m);
-    if (by_m) lo = max(lo, order_key(__double2float_ru(static_cast<double>(m) + a.drop)));
-    if (by_k) lo = max(lo, t.bound_of_k(p.top_k));
+    const uint64_t top = static_cast<uint64_t>(order_key(m)) << 32 | 0xFFFFFFFFu;
+    float zl = -kInf, zh = kInf;
+    if (by_m) zl = __double2float_ru(static_cast<double>(m) + a.drop);
+    const float floor_m = zl;
+    if (by_k) {
+      // (as many groups as there are blocks have a maximum)
+      if (p.top_k <= min(a.n_blocks, kThreads)) zl = fmaxf(zl, key_value(t.bound_of_k(p.top_k)));
+      else if (p.vocab >= kSampled) zl = fmaxf(zl, t.sampled_bound_of_k(p.top_k));
+    }
     if (!by_k && !by_m) {
-      // tokens below (1 - top_p) Z / vocab: together below the share 1 - top_p (half a percent aside, for the sums' error)
-      const double least = 0.995 * (1.0 - p.top_p) * (whole * (1.0 / (1ull << kOne))) / p.vocab;
-      const float z = m + static_cast<float>(log(least)) / p.scale - 1e-6f * fabsf(m);
-      lo = max(lo, order_key(z));
-    }
-    if (lo > top) lo = top;
-    int n = t.gather(lo, top);
-    if (n <= kCap) {
-      t.sort(n);
-      int keep = by_k ? min(p.top_k, n) : n;
-      if (by_p) {
-        double target = p.top_p * (by_k || by_m ? static_cast<double>(sh.cum[keep - 1]) : whole);
-        int k = t.below(keep, 0, target);
-        if (!by_k && !by_m) {
-          // is the cut another one within the error of the sums?
-          const int k0 = t.below(keep, 0, target * (1.0 - 4e-6)), k1 = t.below(keep, 0, target * (1.0 + 4e-6));
-          if (k0 != k1) {
-            uint64_t w = 0;
-            t.each(-kInf, [&](uint32_t, int, float z) { w += t.w_of(z); });
-            k = t.below(keep, 0, p.top_p * static_cast<double>(t.cta_sum(w)));
-          }
-        }
-        keep = min(k + 1, keep);
+      // the maxima from the 64th largest on, if they have the mass already
+      const uint32_t key = t.bound_of_k(min(64, (a.n_blocks + 3) / 4));
+      uint64_t s = 0;
+      for (int b = threadIdx.x; b < a.n_blocks; b += kThreads)
+        if (order_key(max_of[b]) >= key) s += t.w_of(max_of[b]);
+      if (static_cast<double>(t.cta_sum(s)) >= p.top_p * static_cast<double>(whole) * (1.0 + kError)) {
+        zl = key_value(key);
+      } else if (p.vocab >= kSampled) {
+        const float2 z = t.sampled_bounds((1.0 - p.top_p) * static_cast<double>(whole) * (1.0 / (1ull << kOne)));
+        zl = z.x;
+        zh = z.y;
+      } else {
+        // tokens below (1 - top_p) Z / vocab have less than the share 1 - top_p together (half a percent aside, for the sums' error)
+        const float least = static_cast<float>(0.995 * (1.0 - p.top_p) / p.vocab) * (static_cast<float>(whole) * (1.f / (1ull << kOne)));
+        zl = m + logf(least) / p.scale - 1e-6f * fabsf(m);
       }
-      cut = sh.list[keep - 1];
-      __syncthreads();
-    } else {
-      cut = static_cast<uint64_t>(lo) << 32;
+    }
+    zl = fminf(zl, m);
+    if (!(zh >= zl)) zh = kInf;
+    typename R::Rest rest{};
+    const bool alone = !by_k && !by_m;
+    int n = alone ? t.template bracket<true>(zl, zh, &rest) : t.template bracket<false>(zl, zh, &rest);
+    if (by_k && n < p.top_k && zl > floor_m) {  // the sample misled
+      zl = floor_m;
+      n = t.template bracket<false>(zl, zh, &rest);
+    }
+    bool listed = n <= R::kCap;
+    const typename R::List list{t, n};
+    const typename R::Whole whole_row{t};
+    uint64_t lo = static_cast<uint64_t>(order_key(zl)) << 32;
+    if (!alone) {
+      cut = lo;
       uint64_t kept = 0;
-      const bool cut_k = by_k && p.top_k < n;
-      if (cut_k) {
-        cut = t.find_cut(lo, top, p.top_k, 0.0, &kept);
-        lo = static_cast<uint32_t>(cut >> 32);
+      if (by_k && p.top_k < n) {
+        const Cut k = listed ? t.find_cut(list, n, lo, top, p.top_k, 0, 0, 0) : t.find_cut(whole_row, n, lo, top, p.top_k, 0, 0, 0);
+        lo = cut = k.place;
+        kept = k.upto;
+      } else if (by_p) {
+        kept = listed ? t.sum_of_list(n, lo) : t.masses(lo);
       }
       if (by_p) {
-        if (!cut_k) {
-          const float least = by_k || by_m ? key_value(lo) : -kInf;
-          t.each(least, [&](uint32_t, int, float z) {
-            if (z >= least) kept += t.w_of(z);
-          });
-          kept = t.cta_sum(kept);
+        const uint64_t target = __double2ull_ru(p.top_p * static_cast<double>(kept));
+        // (a search of the row leaves what it found last in the list)
+        cut = listed ? t.find_cut(list, n, lo, top, 0, target, 0, 0).place : t.find_cut(whole_row, n, lo, top, 0, target, 0, 0).place;
+      }
+    } else {
+      const uint64_t hi = zh < m ? static_cast<uint64_t>(order_key(zh)) << 32 | 0xFFFFFFFFu : top;
+      const uint64_t above = rest.above, upto = listed ? above + t.sum_of_list(n, lo) : above;
+      // the row's mass is known but for the error of the tail's
+      uint64_t total = upto + rest.tail, error = rest.error;
+      for (bool sure = false;; sure = true) {
+        const uint64_t target = __double2ull_ru(p.top_p * static_cast<double>(total));
+        if (listed && above + error < target && target + error <= upto) {
+          const Cut k = t.find_cut(list, n, lo, hi, 0, target, 0, above);
+          cut = k.place;
+          if (sure || (target > k.before + error && k.upto >= target + error)) break;
+        } else if (sure) {
+          listed = false;
+          cut = t.find_cut(whole_row, p.vocab, kEverything, top, 0, target, 0, 0).place;
+          break;
         }
-        uint64_t unused;
-        cut = t.find_cut(lo, top, 0, p.top_p * static_cast<double>(kept), &unused);
+        // within the error of another cut, or not between the bounds: the row's mass anew (the blocks' masses above zh have to be kept)
+        uint64_t s = 0;
+        t.blocks(-kInf, [&](int b, const Raw<T>& raw) { s += raw_mass<T, VEC>(raw, b, lane, p.vocab, kEverything, m, a, sh.pow2); });
+        total = t.cta_sum(s);
+        error = 0;
       }
     }
-    __syncthreads();
-    t.masses(cut);
+    if (listed) t.add_list(n, cut);
+    else t.masses(cut);
     exact = true;
   }
 
-  // the block
-  const float u0 = p.uniforms[2 * r], u1 = p.uniforms[2 * r + 1];
+  __syncthreads();
   for (;;) {
-    __syncthreads();
     if (warp == 0) {
-      const int per = (a.n_blocks + 31) / 32, from = min(lane * per, a.n_blocks), to = min(from + per, a.n_blocks);
-      uint64_t s = 0;
-      for (int b = from; b < to; ++b) s += mass[b];
-      const uint64_t up = warp_scan_u64(s, lane), total = __shfl_sync(0xffffffffu, up, 31);
-      const double target = static_cast<double>(fminf(fmaxf(u0, 0.f), 1.f)) * static_cast<double>(total);
-      const uint32_t above = __ballot_sync(0xffffffffu, s > 0 && static_cast<double>(up) > target), held = __ballot_sync(0xffffffffu, s > 0);
-      const int which = above ? __ffs(above) - 1 : 31 - __clz(held);
-      if (lane == which) {
-        uint64_t before = up - s, cum = before;
-        int b = from;
-        for (int i = from; i < to; ++i) {
-          if (mass[i] == 0) continue;
-          b = i;
-          before = cum;
-          cum += mass[i];
-          if (static_cast<double>(cum) > target) break;
-        }
-        // fp32 sums are off by 37 2^-24 = 2.2e-6 relative at most (a term by 2^-22 and three roundings of its exponent, at most 9 in
-        // the mean; 8 sums): a border by half of that of the whole
-        const double error = exact ? 0.0 : 1.2e-6 * static_cast<double>(total);
-        const bool sure = exact || ((before == 0 || target - static_cast<double>(before) > error) &&
-                                    (cum == total || static_cast<double>(cum) - target > error));
-        sh.found = sure ? b : -1;
-      }
+      const int b = pick_block(mass, a.n_blocks, u0, exact, lane);
+      if (b >= 0) draw_token<T, VEC>(a, row, r, b, u1, cut, m, whole, sh.pow2, lane);
+      if (lane == 0) sh.found = b;
     }
+    if (exact) return;
     __syncthreads();
-    if (sh.found >= 0) break;
+    if (sh.found >= 0) return;
     t.masses(kEverything);
     exact = true;
   }
-  if (warp != 0) return;
-  // the token: 16 neighbours a lane
-  const int first = sh.found * kBlock + lane * kPerLane;
-  uint64_t s = 0;
-#pragma unroll 4
-  for (int j = 0; j < kPerLane; ++j) {
-    const float z = first + j < p.vocab ? to_f(row[first + j]) : -kInf;
-    if (place(order_key(z), first + j) >= cut) s += t.w_of(z);
-  }
-  const uint64_t up = warp_scan_u64(s, lane), total = __shfl_sync(0xffffffffu, up, 31);
-  const double target = static_cast<double>(fminf(fmaxf(u1, 0.f), 1.f)) * static_cast<double>(total);
-  const uint32_t above = __ballot_sync(0xffffffffu, s > 0 && static_cast<double>(up) > target), held = __ballot_sync(0xffffffffu, s > 0);
-  const int which = above ? __ffs(above) - 1 : (held ? 31 - __clz(held) : 0);
-  if (lane != which) return;
-  uint64_t cum = up - s;
-  int id = first;
-  float z_id = -kInf;
-  for (int j = 0; j < kPerLane; ++j) {
-    const float z = first + j < p.vocab ? to_f(row[first + j]) : -kInf;
-    const uint64_t w = place(order_key(z), first + j) >= cut ? t.w_of(z) : 0;
-    if (w == 0) continue;
-    id = first + j;
-    z_id = z;
-    cum += w;
-    if (static_cast<double>(cum) > target) break;
-  }
-  p.ids[r] = id;
-  if (p.logprobs) p.logprobs[r] = (z_id - m) * p.scale - logf(static_cast<float>(whole * (1.0 / (1ull << kOne))));
 }
 
-template <typename T, bool VEC>
-cudaError_t launch_rows(const Args& a, cudaStream_t s) {
+template <typename T, bool VEC, int kThreads>
+cudaError_t launch_rows(const SampleArgs& a, cudaStream_t s) {
   // few rows: a cluster reads a row, down to a block or two per warp
-  Launch l{1, 0, 256};
+  Launch l{1, 0, kThreads};
   while (l.cluster < kMaxCluster && static_cast<int64_t>(a.p.rows) * l.cluster < num_sms() && a.n_blocks / l.cluster > 8) l.cluster *= 2;
-  return launch<&sample_kernel<T, VEC, 256>>(a.p.rows, l, sizeof(Shared) + 12 * static_cast<size_t>(a.n_blocks), s, a);
+  return launch<&sample_kernel<T, VEC, kThreads>>(a.p.rows, l, sizeof(Shared<kThreads>) + 12 * static_cast<size_t>(a.n_blocks), s, a);
 }
 template <typename T>
-cudaError_t launch_type(const Args& a, cudaStream_t s) {
+cudaError_t launch_type(const SampleArgs& a, cudaStream_t s) {
   const bool vec = reinterpret_cast<uintptr_t>(a.p.logits) % 16 == 0 && (a.p.rows == 1 || a.p.ld * static_cast<int64_t>(sizeof(T)) % 16 == 0);
-  return vec ? launch_rows<T, true>(a, s) : launch_rows<T, false>(a, s);
+  if (a.n_blocks <= kShort) return vec ? launch_rows<T, true, 64>(a, s) : launch_rows<T, false, 64>(a, s);
+  return vec ? launch_rows<T, true, 256>(a, s) : launch_rows<T, false, 256>(a, s);
 }
 
 }  // namespace
 
 cudaError_t sample_launch(const SampleParams& p, cudaStream_t s) {
   const double c = static_cast<double>(p.scale) * 1.4426950408889634073599;
-  Args a{p, static_cast<float>(c), 0.f, p.min_p > 0.0 ? log(p.min_p) / static_cast<double>(p.scale) : -HUGE_VAL,
-         (p.vocab + kBlock - 1) / kBlock};
+  SampleArgs a{p, static_cast<float>(c), 0.f, p.min_p > 0.0 ? log(p.min_p) / static_cast<double>(p.scale) : -HUGE_VAL,
+               (p.vocab + kBlock - 1) / kBlock, device_status_ptr()};
   a.c_lo = static_cast<float>(c - static_cast<double>(a.c));
   if (p.dtype == SGD_F16) return launch_type<f16>(a, s);
   if (p.dtype == SGD_BF16) return launch_type<bf16>(a, s);
