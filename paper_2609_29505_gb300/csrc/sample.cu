@@ -23,17 +23,92 @@
 // down to 256 tokens, which are ranked by comparing all with all.
 //
 // Many rows: a CTA each, three per SM, so that one's search hides behind the others' reading.  Few: a cluster reads a row.
-#include "sample.cuh"
+#include <math.h>
+
+#include "vocab_rows.cuh"
 
 namespace sgd {
 namespace {
 
 using namespace rows;
 
+constexpr int kBlock = SGD_SAMPLE_BLOCK;
+constexpr int kPerLane = kBlock / 32;
+constexpr int kShort = 4;        // blocks of a row that 64 threads take
 constexpr int kSampled = 16384;  // rows from this many tokens on are sampled
-constexpr int kShort = 4;          // blocks of a row that 64 threads take
-constexpr int kQueue = 64;       // tokens of a block that a warp puts side by side
+constexpr int kOne = 43;         // weight() of the row's maximum is 2^43: 2^20.6 of them (a row of 3 MiB) add up in 64 bits
+static_assert(kBlock == 512, "a lane takes 16 tokens");
 
+// A block's sum in fp32 is off by at most this much of it (u = 2^-24): a term by 4 u (ex2.approx) and three roundings of its exponent,
+// ln2 3 |t| u, whose mean over the block's mass is at most ln2 3 log2(512) u = 18.7 u; 10 u from being added up, 2 u as a
+// multiple of 2^-22: 35 u.
+constexpr double kError = 2.2e-6;
+
+struct SampleArgs {
+  SampleParams p;
+  float c, c_lo;    // scale log2(e), as the sum of two floats
+  double drop;      // ln(min_p) / scale: a token at or above max + drop passes (-inf: every token)
+  int n_blocks;
+};
+
+// 2^(j / 32) 2^62, j = 0 .. 31
+__constant__ uint64_t kPow2[32] = {
+    0x4000000000000000ull, 0x4166C34C5615D0ECull, 0x42D561B3E6243D8Aull, 0x444C0740496D4294ull,
+    0x45CAE0F1F545EB73ull, 0x47521CC5A2E6A9E0ull, 0x48E1E9B9D588E19Bull, 0x4A7A77D47F7B84B1ull,
+    0x4C1BF828C6DC54B8ull, 0x4DC69CDCEAA72A9Cull, 0x4F7A993048D088D7ull, 0x513821818624B40Cull,
+    0x52FF6B54D8A89C75ull, 0x54D0AD5A753E077Cull, 0x56AC1F752150A563ull, 0x5891FAC0E95612C8ull,
+    0x5A827999FCEF3242ull, 0x5C7DD7A3B17DCF75ull, 0x5E8451CFAC061B5Full, 0x6096266533384A2Bull,
+    0x62B39508AA836D6Full, 0x64DCDEC3371793D1ull, 0x6712460A8FC24072ull, 0x69540EC8F895722Dull,
+    0x6BA27E656B4EB57Aull, 0x6DFDDBCBED791BABull, 0x70666F76154A7089ull, 0x72DC8373BE41A454ull,
+    0x75606373EE921C97ull, 0x77F25CCDEE6D7AE6ull, 0x7A92BE8A92436616ull, 0x7D41D96DB915019Dull,
+};
+
+// Weight 2^((z - m) c) of a logit against the row's maximum m as a whole number, 2^43 for the maximum: exact to about 2^-31
+// relative and half a unit.  z - m = d + dl exactly, (d + dl) c = t + tl to 2^-45; t + tl = n + j / 32 + g with |g| <= 1/64;
+// 2^g - 1 = g ln2 + ... to the fourth power (the fifth is 1.3e-12).
+__device__ __forceinline__ uint64_t weight(float z, float m, const SampleArgs& a, const uint64_t* pow2) {
+  const float d = z - m;
+  const float t = __fmul_rn(d, a.c);
+  if (!(t > -48.f)) return 0;
+  const float back = d - z;
+  const float dl = (z - (d - back)) + (-m - back);
+  const float tl = fmaf(d, a.c, -t) + fmaf(d, a.c_lo, dl * a.c);
+  constexpr float kMagic = 393216.f;  // 1.5 2^18: its unit is 1/32
+  const float y = __fadd_rn(t, kMagic);
+  const int k = __float_as_int(y) - __float_as_int(kMagic);
+  const float g = (t - (y - kMagic)) + tl;
+  const float e = g * fmaf(g, fmaf(g, fmaf(g, 0.009618129f, 0.05550411f), 0.24022651f), 0.6931472f);
+  const uint64_t base = pow2[k & 31];
+  const int64_t more = static_cast<int64_t>(static_cast<int32_t>(base >> 32)) * __float2int_rn(e * 4294967296.f);
+  const uint64_t w = base + static_cast<uint64_t>(more);  // 2^62 .. 2^63
+  const int shift = 62 - kOne - (k >> 5);
+  return shift > 62 ? 0 : (w + (1ull << (shift - 1))) >> shift;
+}
+
+constexpr uint64_t kEverything = static_cast<uint64_t>(kKeyNegInf) << 32;  // the place that no token is behind
+
+__device__ __forceinline__ uint64_t warp_sum_u64(uint64_t v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+__device__ __forceinline__ uint64_t warp_scan_u64(uint64_t v, int lane) {  // inclusive
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint64_t x = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += x;
+  }
+  return v;
+}
+// The whole number that a mass is above where it is above u total (u as a multiple of 2^-63).
+__device__ __forceinline__ uint64_t share_of(float u, uint64_t total) {
+  u = fmaxf(u, 0.f);
+  return u >= 1.f ? total : __umul64hi(total, __float2ull_rd(u * 9223372036854775808.f) << 1);
+}
+// The mass s 2^-22 w of a block, s its sum in [1, 512] against its maximum, whose weight is w.
+__device__ __forceinline__ uint64_t times(float s, uint64_t w) {
+  return __umul64hi(w << 10, static_cast<uint64_t>(__float2uint_rn(s * 4194304.f)) << 32);
+}
 // Adds a mass to one in shared memory that others add to as well (two 32-bit additions: whole numbers have no order).
 __device__ __forceinline__ void add_shared(uint32_t* lo, uint32_t* hi, uint64_t w) {
   const uint32_t low = static_cast<uint32_t>(w), was = atomicAdd(lo, low);
@@ -41,25 +116,168 @@ __device__ __forceinline__ void add_shared(uint32_t* lo, uint32_t* hi, uint64_t 
   if (high) atomicAdd(hi, high);
 }
 
-template <int kThreads>
+// A token's place in the order: larger comes first.
+__device__ __forceinline__ uint64_t place(uint32_t key, int i) {
+  return static_cast<uint64_t>(key) << 32 | static_cast<uint32_t>(0xFFFFFFFFu - static_cast<uint32_t>(i));
+}
+__device__ __forceinline__ int index_of(uint64_t x) { return static_cast<int>(0xFFFFFFFFu - static_cast<uint32_t>(x)); }
+__device__ __forceinline__ float value_of(uint64_t x) { return key_value(static_cast<uint32_t>(x >> 32)); }
+
+// ----- a block in a warp's registers -----
+
+// VEC: rows start at 16-byte boundaries, and a lane's tokens are those of its vectors; else every 32nd token.
+template <typename T, bool VEC>
+__device__ __forceinline__ int token_at(int b, int lane, int j) {
+  constexpr int E = Elem<T>::kPer;
+  return b * kBlock + (VEC ? (j / E * 32 + lane) * E + j % E : j * 32 + lane);
+}
+template <typename T>
+struct Raw {
+  static constexpr int kN = kPerLane / Elem<T>::kPer;
+  uint4 v[kN];
+};
+// (no token: -inf)
+template <typename T, bool VEC>
+__device__ __forceinline__ Raw<T> fetch(const T* row, int vocab, int b, int lane) {
+  Raw<T> r;
+  if (VEC && (b + 1) * kBlock <= vocab) {
+#pragma unroll
+    for (int i = 0; i < Raw<T>::kN; ++i) r.v[i] = reinterpret_cast<const uint4*>(row + static_cast<int64_t>(b) * kBlock)[i * 32 + lane];
+  } else {
+    T* e = reinterpret_cast<T*>(r.v);
+#pragma unroll
+    for (int j = 0; j < kPerLane; ++j) {
+      const int at = token_at<T, VEC>(b, lane, j);
+      e[j] = at < vocab ? row[at] : neg_inf<T>();
+    }
+  }
+  return r;
+}
+template <typename T>
+__device__ __forceinline__ void numbers(const Raw<T>& r, float* z) {
+#pragma unroll
+  for (int i = 0; i < Raw<T>::kN; ++i) unpack(r.v[i], z + i * Elem<T>::kPer, static_cast<const T*>(nullptr));
+}
+
+// Largest value of a lane's tokens; NaN where there is one.
+__device__ __forceinline__ float raw_max(const Raw<float>& r) {
+  float z[kPerLane];
+  numbers(r, z);
+  float m = z[0];
+#pragma unroll
+  for (int j = 1; j + 1 < kPerLane; j += 2) asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(m), "f"(z[j]), "f"(z[j + 1]));
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(m), "f"(z[kPerLane - 1]));
+  return m;
+}
+template <typename P, typename T>
+__device__ __forceinline__ float packed_max(const Raw<T>& r) {
+  const P* p = reinterpret_cast<const P*>(r.v);
+  P m = p[0];
+#pragma unroll
+  for (int j = 1; j < kPerLane / 2; ++j) m = __hmax2_nan(m, p[j]);
+  const float a = to_f(m.x), b = to_f(m.y);
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
+__device__ __forceinline__ float raw_max(const Raw<f16>& r) { return packed_max<__half2>(r); }
+__device__ __forceinline__ float raw_max(const Raw<bf16>& r) { return packed_max<__nv_bfloat162>(r); }
+
+__device__ __forceinline__ float warp_max_nan(float m) {
+  float d;
+  asm volatile("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(d) : "f"(m));
+  return d;
+}
+
+// Sum over a lane's tokens of 2^((z - m) c).
+template <typename T>
+__device__ __forceinline__ float raw_sum(const Raw<T>& r, float m, float c) {
+  const uint64_t m2 = pack_f32x2(-m, -m), c2 = pack_f32x2(c, c), none = pack_f32x2(-0.f, -0.f);
+  uint64_t s[2] = {pack_f32x2(0.f, 0.f), pack_f32x2(0.f, 0.f)};
+  float z[kPerLane];
+  numbers(r, z);
+#pragma unroll
+  for (int j = 0; j < kPerLane; j += 2) {
+    // (one rounding each: a product is not contracted into the difference)
+    const uint64_t t = fma_f32x2(add_f32x2(pack_f32x2(z[j], z[j + 1]), m2), c2, none);
+    s[j / 2 & 1] = add_f32x2(s[j / 2 & 1], pack_f32x2(ex2_approx(lo_f32x2(t)), ex2_approx(hi_f32x2(t))));
+  }
+  return sum_f32x2(add_f32x2(s[0], s[1]));
+}
+
+// Maxima and sums of two blocks (or of one), in lanes 0 .. 15 those of the first (or in all): the maximum is NaN where it is not
+// below +inf; the sum of 2^((z - maximum) c) is 0 where there is no token, and where SUMS is not.
+template <typename T, int kPair>
+__device__ __forceinline__ float2 block_stats(const Raw<T>* r, bool sums, float c, int lane) {
+  float m[kPair], s[kPair];
+#pragma unroll
+  for (int u = 0; u < kPair; ++u) m[u] = warp_max_nan(raw_max(r[u]));
+#pragma unroll
+  for (int u = 0; u < kPair; ++u) s[u] = sums ? raw_sum(r[u], m[u], c) : 0.f;
+  float v = s[0], most = m[0];
+  if (kPair == 2) {
+    const bool second = lane >= 16;
+    const float give = second ? s[0] : s[kPair - 1];
+    v = (second ? s[kPair - 1] : s[0]) + __shfl_xor_sync(0xffffffffu, give, 16);
+    if (second) most = m[kPair - 1];
+  } else {
+    v += __shfl_xor_sync(0xffffffffu, v, 16);
+  }
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return make_float2(most < kInf ? most : kNan, most == -kInf ? 0.f : v);
+}
+// A lane's share of a block's mass, of the tokens at or before `cut` in the order.
+template <typename T, bool VEC>
+__device__ __forceinline__ uint64_t raw_mass(const Raw<T>& r, int b, int lane, int vocab, uint64_t cut, float m, const SampleArgs& a,
+                                             const uint64_t* pow2) {
+  float z[kPerLane];
+  numbers(r, z);
+  uint64_t s = 0;
+#pragma unroll
+  for (int j = 0; j < kPerLane; ++j)  // (no token: -inf, of weight 0)
+    if (place(order_key(z[j]), token_at<T, VEC>(b, lane, j)) >= cut) s += weight(z[j], m, a, pow2);
+  return s;
+}
+
+// The largest place of what a thread's lanes see of the row.
+template <typename T>
+__device__ __forceinline__ uint64_t first_of_order(const T* row, int vocab, int threads) {
+  uint64_t first = 0;
+  for (int i = threadIdx.x; i < vocab; i += threads) {
+    const uint64_t x = place(order_key(to_f(row[i])), i);
+    first = x > first ? x : first;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const uint64_t x = __shfl_xor_sync(0xffffffffu, first, o);
+    first = x > first ? x : first;
+  }
+  return first;
+}
+
+constexpr int kQueue = 96;  // tokens that a warp puts side by side: 32 wait at most, and 64 join them
+
+template <int kThreads, bool FILTER>
 struct __align__(16) Shared {
   static constexpr int kWarps = kThreads / 32;
-  static constexpr int kCap = 16 * kThreads;  // tokens of the list
-  static constexpr int kHist = 4 * kThreads;  // bins
+  static constexpr int kCap = FILTER ? 16 * kThreads : 2;  // tokens of the list
+  static constexpr int kHist = FILTER ? 4 * kThreads : 2;  // bins
+  static constexpr int kTeam = FILTER ? kThreads : 4;
   uint64_t list[kCap];
   uint32_t count[kHist], lo[kHist], hi[kHist];
-  uint64_t small[kThreads], small_w[kThreads];
-  uint64_t queue[kWarps][kQueue];
+  uint64_t small[kTeam], small_w[kTeam];
+  int queue[kWarps][FILTER ? kQueue : 2];
+  uint32_t groups[kTeam];
   uint64_t pow2[32];
   uint64_t wide[2][kWarps];
   float part[kWarps];
   uint32_t part_n[kWarps];
-  uint32_t groups[kThreads];
   uint64_t best;
   uint64_t cut, cut_before, cut_upto;
   uint64_t above_w;
   uint32_t above_n, bin_n, bin;
-  int n, found, bad;
+  int n, found, bad, n_live;
   int edge[4];
   uint32_t edge_n[2];
 };
@@ -69,94 +287,22 @@ struct Cut {
   uint64_t before, upto;  // the kept mass without it and with it
 };
 
-template <typename T, bool VEC, int kThreads>
+template <typename T, bool VEC, int kThreads, bool FILTER>
 struct Row {
-  using Sh = Shared<kThreads>;
-  static constexpr int kWarps = kThreads / 32, kSmall = kThreads, kCap = Sh::kCap, kHist = Sh::kHist;
+  using Sh = Shared<kThreads, FILTER>;
+  static constexpr int kWarps = kThreads / 32, kHist = Sh::kHist;
   static constexpr int kBinBits = kThreads == 256 ? 10 : 8;
-  static_assert(kHist == 1 << kBinBits, "bins");
+  static_assert(!FILTER || kHist == 1 << kBinBits, "bins");
   const SampleArgs& a;
   const T* row;
   const float* max_of;  // [n_blocks] maxima
   uint64_t* mass;       // [n_blocks]
+  uint16_t* live;       // [n_blocks] (FILTER: blocks that are looked at)
   Sh& sh;
   float m;              // the row's maximum
   int warp, lane;
 
   __device__ __forceinline__ uint64_t w_of(float z) const { return weight(z, m, a, sh.pow2); }
-
-  // f(b, its tokens) for the blocks whose maximum is at least `least`, a warp each, with the next one's tokens on their way
-  template <typename F>
-  __device__ __forceinline__ void blocks(float least, F f) const {
-    auto next = [&](int b) {
-      while (b < a.n_blocks && !(max_of[b] >= least)) b += kWarps;
-      return b;
-    };
-    int b = next(warp);
-    if (b >= a.n_blocks) return;
-    Raw<T> raw = fetch<T, VEC>(row, a.p.vocab, b, lane);
-    while (b < a.n_blocks) {
-      const int after = next(b + kWarps);
-      Raw<T> ahead;
-      if (after < a.n_blocks) ahead = fetch<T, VEC>(row, a.p.vocab, after, lane);
-      f(b, raw);
-      raw = ahead;
-      b = after;
-    }
-  }
-  // f(place, value) for the tokens of a block that are marked in `on` (bit j: the lane's token j), side by side in the lanes where they
-  // are few, else one of each lane at a time
-  template <typename F>
-  __device__ __forceinline__ void marked(int b, const float* z, uint32_t on, F f) const {
-    const int mine = __popc(on);
-    int up = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int x = __shfl_up_sync(0xffffffffu, up, o);
-      if (lane >= o) up += x;
-    }
-    const int all = __shfl_sync(0xffffffffu, up, 31);
-    if (all == 0) return;
-    if (all <= kQueue) {
-      int at = up - mine;
-      if (on) {
-#pragma unroll
-        for (int j = 0; j < kPerLane; ++j)
-          if (on >> j & 1) sh.queue[warp][at++] = place(order_key(z[j]), token_at<T, VEC>(b, lane, j));
-      }
-      __syncwarp();
-      for (int i = lane; i < all; i += 32) f(sh.queue[warp][i], value_of(sh.queue[warp][i]));
-      __syncwarp();
-      return;
-    }
-#pragma unroll 1
-    while (__any_sync(0xffffffffu, on)) {
-      if (on) {
-        const int e = token_at<T, VEC>(b, lane, __ffs(on) - 1);
-        on &= on - 1;
-        if (e < a.p.vocab) {
-          const float x = to_f(row[e]);
-          f(place(order_key(x), e), x);
-        }
-      }
-      __syncwarp();
-    }
-  }
-  // f(place, value) for the row's tokens at or before `from` in the order
-  template <typename F>
-  __device__ __forceinline__ void each(uint64_t from, F f) const {
-    const float least = value_of(from);
-    blocks(least, [&](int b, const Raw<T>& raw) {
-      float z[kPerLane];
-      numbers(raw, z);
-      uint32_t on = 0;
-#pragma unroll
-      for (int j = 0; j < kPerLane; ++j) on |= (z[j] >= least && token_at<T, VEC>(b, lane, j) < a.p.vocab ? 1u : 0u) << j;
-      marked(b, z, on, [&](uint64_t x, float y) {
-        if (x >= from) f(x, y);
-      });
-    });
-  }
 
   // Sums over the CTA; a barrier before and after.
   __device__ ulonglong2 cta_sum(uint64_t v, uint64_t w) const {
@@ -176,7 +322,130 @@ struct Row {
     }
     return s;
   }
-  __device__ uint64_t cta_sum(uint64_t v) const { return cta_sum(v, 0).x; }
+  __device__ uint64_t cta_sum(uint64_t v) const {
+    v = warp_sum_u64(v);
+    __syncthreads();
+    if (lane == 0) sh.wide[0][warp] = v;
+    __syncthreads();
+    uint64_t s = 0;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) s += sh.wide[0][i];
+    return s;
+  }
+  // Inclusive sum over the CTA's threads in their order, and the whole; a barrier before and after.
+  __device__ uint64_t cta_scan(uint64_t v, uint64_t* whole) const {
+    v = warp_scan_u64(v, lane);
+    __syncthreads();
+    if (lane == 31) sh.wide[0][warp] = v;
+    __syncthreads();
+    uint64_t all = 0;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) {
+      if (i < warp) v += sh.wide[0][i];
+      all += sh.wide[0][i];
+    }
+    *whole = all;
+    return v;
+  }
+
+  // f(b, its tokens) for the blocks whose maximum is at least `least`, a warp each, with the next one's tokens on their way; g(b)
+  // for the others, a thread each.
+  template <typename F, typename G>
+  __device__ __forceinline__ void blocks(float least, F f, G g) const {
+    __syncthreads();
+    if (threadIdx.x == 0) sh.n_live = 0;
+    __syncthreads();
+    for (int b0 = 0; b0 < a.n_blocks; b0 += kThreads) {
+      const int b = b0 + threadIdx.x;
+      const bool is = b < a.n_blocks && max_of[b] >= least;
+      const uint32_t hit = __ballot_sync(0xffffffffu, is);
+      int at = 0;
+      if (lane == 0 && hit) at = atomicAdd(&sh.n_live, __popc(hit));
+      at = __shfl_sync(0xffffffffu, at, 0);
+      if (is) live[at + __popc(hit & ((1u << lane) - 1u))] = static_cast<uint16_t>(b);
+      else if (b < a.n_blocks) g(b);
+    }
+    __syncthreads();
+    const int n = sh.n_live;
+    if (warp >= n) return;
+    Raw<T> raw = fetch<T, VEC>(row, a.p.vocab, live[warp], lane);
+#pragma unroll 1
+    for (int i = warp; i < n; i += kWarps) {
+      Raw<T> ahead;
+      if (i + kWarps < n) ahead = fetch<T, VEC>(row, a.p.vocab, live[i + kWarps], lane);
+      f(live[i], raw);
+      raw = ahead;
+    }
+  }
+  // Tokens of block b that are at least `least`, one bit each.
+  __device__ __forceinline__ uint32_t marks(int b, const Raw<T>& raw, float least) const {
+    float z[kPerLane];
+    numbers(raw, z);
+    uint32_t on = 0;
+#pragma unroll
+    for (int j = 0; j < kPerLane; ++j) on |= z[j] >= least ? 1u << j : 0u;
+    if (least == -kInf && (b + 1) * kBlock > a.p.vocab)  // (what is no token is -inf)
+#pragma unroll
+      for (int j = 0; j < kPerLane; ++j)
+        if (token_at<T, VEC>(b, lane, j) >= a.p.vocab) on &= ~(1u << j);
+    return on;
+  }
+  // f(token, value) for the marked tokens of the blocks that a warp looks at, 32 at a time: they wait in the warp's queue for more.
+  struct Queue {
+    int* at;
+    int n = 0;
+  };
+  template <typename F>
+  __device__ __forceinline__ void drain(Queue& q, int least, F f) const {
+    int done = 0;
+    __syncwarp();
+    for (; q.n - done >= least; done += 32) {
+      const int i = done + lane;
+      if (i < q.n) {
+        const int e = q.at[i];
+        f(e, to_f(row[e]));
+      }
+      __syncwarp();
+    }
+    if (done >= q.n) {
+      q.n = 0;
+      return;
+    }
+    if (done) {  // what is left moves to the front
+      const int i = done + lane;
+      const int e = i < q.n ? q.at[i] : 0;
+      __syncwarp();
+      if (i < q.n) q.at[lane] = e;
+      q.n -= done;
+      __syncwarp();
+    }
+  }
+  template <typename F>
+  __device__ __forceinline__ void marked(Queue& q, int b, uint32_t on, F f) const {
+#pragma unroll 1
+    for (;;) {
+      const uint32_t here = __ballot_sync(0xffffffffu, on != 0);
+      if (!here) return;
+      if (on) {
+        q.at[q.n + __popc(here & ((1u << lane) - 1u))] = token_at<T, VEC>(b, lane, __ffs(on) - 1);
+        on &= on - 1;
+      }
+      q.n += __popc(here);
+      if (q.n > kQueue - 32) drain(q, 32, f);
+    }
+  }
+  // f(place, value) for the row's tokens at or before `from` in the order
+  template <typename F>
+  __device__ __forceinline__ void each(uint64_t from, F f) const {
+    const float least = value_of(from);
+    Queue q{sh.queue[warp]};
+    auto g = [&](int e, float z) {
+      const uint64_t x = place(order_key(z), e);
+      if (x >= from) f(x, z);
+    };
+    blocks(least, [&](int b, const Raw<T>& raw) { marked(q, b, marks(b, raw, least), g); }, [](int) {});
+    drain(q, 1, g);
+  }
 
   // Place in a list of n counted so far (one atomic for the lanes that are here).
   __device__ __forceinline__ int slot(int* n) const {
@@ -187,85 +456,71 @@ struct Row {
     return __shfl_sync(here, at, first) + __popc(here & ((1u << lane) - 1u));
   }
 
-  struct Rest {
-    uint64_t above, tail, error;
-  };
-  // Tokens above zh: their masses by blocks, and in rest->above together; those from zl to zh: into the list, as far as it goes; with
-  // TAIL those below: their mass from fp32 sums, and how far it may be off (`mass` holds the blocks' masses at the call).
-  // Returns how many are from zl to zh.
-  template <bool TAIL>
-  __device__ int bracket(float zl, float zh, Rest* rest) const {
-    __syncthreads();
+  // Tokens above zh: their masses by blocks, and in out->x together; those from zl to zh: into the list, as far as it goes, their mass in
+  // out->y.  Returns how many these are.
+  __device__ int bracket(float zl, float zh, ulonglong2* out) const {
     if (threadIdx.x == 0) sh.n = 0;
-    __syncthreads();
-    uint64_t above = 0, tail = 0, skipped = 0;
-    for (int b = threadIdx.x; b < a.n_blocks; b += kThreads)
-      if (!(max_of[b] >= zl)) {
-        if (TAIL) skipped += mass[b];
-        mass[b] = 0;
+    for (int b = threadIdx.x; b < a.n_blocks; b += kThreads) mass[b] = 0;
+    uint64_t above = 0, inside = 0;
+    Queue q{sh.queue[warp]};
+    auto f = [&](int e, float z) {
+      const uint64_t w = w_of(z);
+      if (z > zh) {
+        above += w;
+        uint32_t* to = reinterpret_cast<uint32_t*>(mass + e / kBlock);
+        add_shared(to, to + 1, w);
+      } else {
+        inside += w;
+        const int at = slot(&sh.n);
+        if (at < Sh::kCap) sh.list[at] = place(order_key(z), e);
       }
-    blocks(zl, [&](int b, const Raw<T>& raw) {
-      float z[kPerLane];
-      numbers(raw, z);
-      uint32_t on = 0;
-      float low[2] = {0.f, 0.f};
-#pragma unroll
-      for (int j = 0; j < kPerLane; ++j) {
-        const bool is = z[j] >= zl;
-        on |= (is ? 1u : 0u) << j;
-        if (TAIL) low[j & 1] += is ? 0.f : ex2_approx(__fmul_rn(z[j] - zl, a.c));
-      }
-      if (zl == -kInf)  // (what is no token is -inf)
-#pragma unroll
-        for (int j = 0; j < kPerLane; ++j)
-          if (token_at<T, VEC>(b, lane, j) >= a.p.vocab) on &= ~(1u << j);
-      uint64_t s = 0;
-      marked(b, z, on, [&](uint64_t x, float y) {
-        if (y > zh) {
-          s += w_of(y);
-        } else {
-          const int at = slot(&sh.n);
-          if (at < kCap) sh.list[at] = x;
-        }
-      });
-      if (__any_sync(0xffffffffu, s != 0)) s = warp_sum_u64(s);
-      const float l = TAIL ? warp_sum(low[0] + low[1]) : 0.f;
-      if (lane == 0) {
-        mass[b] = s;
-        above += s;
-        if (TAIL) tail += block_mass(zl, l, m, a, sh.pow2);
-      }
-    });
-    const ulonglong2 both = cta_sum(above, tail);
-    rest->above = both.x;
-    if (TAIL) {
-      // of the tail's sums against zl: 18 u, and three roundings of an exponent t whose mean over the mass S (of zl's weight) is at
-      // most log2(vocab) - log2(S); and tokens below 2^-43
-      skipped = cta_sum(skipped);
-      const float s = static_cast<float>(both.y), spread = s > 0.f ? log2f(a.p.vocab * (static_cast<float>(w_of(zl)) + 1.f) / s) : 0.f;
-      rest->tail = both.y + skipped;
-      rest->error = static_cast<uint64_t>(a.n_blocks) + a.p.vocab +
-                    __double2ull_ru(kError * static_cast<double>(skipped) +
-                                    (20.0 + 2.1 * fmaxf(spread, 0.f)) * 5.9604645e-8 * static_cast<double>(both.y));
-    }
+    };
+    blocks(zl, [&](int b, const Raw<T>& raw) { marked(q, b, marks(b, raw, zl), f); }, [](int) {});
+    drain(q, 1, f);
+    *out = cta_sum(above, inside);
     return sh.n;
+  }
+  // Mass of the tokens below zl from fp32 sums, and how far it may be off.
+  __device__ ulonglong2 tail(float zl) const {
+    uint64_t sum = 0;
+    const uint64_t w = w_of(zl);
+    blocks(-kInf,
+           [&](int, const Raw<T>& raw) {
+             float z[kPerLane], s[2] = {0.f, 0.f};
+             numbers(raw, z);
+#pragma unroll
+             for (int j = 0; j < kPerLane; ++j) s[j & 1] += z[j] >= zl ? 0.f : ex2_approx(__fmul_rn(z[j] - zl, a.c));
+             const float all = warp_sum(s[0] + s[1]);
+             if (lane == 0) sum += times(all, w);
+           },
+           [](int) {});
+    sum = cta_sum(sum);
+    // 18 u, and three roundings of an exponent t whose mean over the mass S (of zl's weight) is at most log2(vocab) - log2(S); half
+    // a unit of zl's weight's 2^-22 a block, and tokens below 2^-43
+    const float wf = static_cast<float>(w) + 1.f, spread = sum > 0 ? fmaxf(log2f(a.p.vocab * wf / static_cast<float>(sum)), 0.f) : 0.f;
+    return make_ulonglong2(sum, static_cast<uint64_t>(a.p.vocab) + a.n_blocks * (1 + (w >> 22)) +
+                                    __double2ull_ru((20.0 + 2.1 * spread) * 5.9604645e-8 * static_cast<double>(sum)));
   }
 
   // Masses of the blocks, of the tokens at or before `cut` in the order; returns the whole.
   __device__ uint64_t masses(uint64_t cut) const {
-    const float least = value_of(cut);
     uint64_t all = 0;
-    __syncthreads();
-    for (int b = threadIdx.x; b < a.n_blocks; b += kThreads)
-      if (!(max_of[b] >= least)) mass[b] = 0;
-    blocks(least, [&](int b, const Raw<T>& raw) {
-      const uint64_t s = warp_sum_u64(raw_mass<T, VEC>(raw, b, lane, a.p.vocab, cut, m, a, sh.pow2));
-      if (lane == 0) {
-        mass[b] = s;
-        all += s;
-      }
-    });
+    blocks(value_of(cut),
+           [&](int b, const Raw<T>& raw) {
+             const uint64_t s = warp_sum_u64(raw_mass<T, VEC>(raw, b, lane, a.p.vocab, cut, m, a, sh.pow2));
+             if (lane == 0) {
+               mass[b] = s;
+               all += s;
+             }
+           },
+           [&](int b) { mass[b] = 0; });
     return cta_sum(all);
+  }
+  // The row's mass.
+  __device__ uint64_t total() const {
+    uint64_t s = 0;
+    blocks(-kInf, [&](int b, const Raw<T>& raw) { s += raw_mass<T, VEC>(raw, b, lane, a.p.vocab, kEverything, m, a, sh.pow2); }, [](int) {});
+    return cta_sum(s);
   }
   // Adds the list's tokens that are kept to the blocks' masses.
   __device__ void add_list(int n, uint64_t cut) const {
@@ -277,6 +532,65 @@ struct Row {
       add_shared(to, to + 1, w_of(value_of(x)));
     }
     __syncthreads();
+  }
+
+  // The first block whose cumulative mass is above u0 of the whole; -1 where the masses' error (`exact`: none) leaves it open.
+  __device__ int pick_block(float u0, bool exact) const {
+    const int per = (a.n_blocks + kThreads - 1) / kThreads, from = min(static_cast<int>(threadIdx.x) * per, a.n_blocks),
+              to = min(from + per, a.n_blocks);
+    uint64_t s = 0, total;
+    for (int b = from; b < to; ++b) s += mass[b];
+    const uint64_t up = cta_scan(s, &total), target = share_of(u0, total);
+    if (s > 0 && (target < total ? up > target && up - s <= target : up == total)) {
+      uint64_t before = up - s, cum = before;
+      int found = from;
+      for (int i = from; i < to; ++i) {
+        const uint64_t w = mass[i];
+        if (w == 0) continue;
+        found = i;
+        before = cum;
+        cum += w;
+        if (cum > target) break;
+      }
+      // (errors e of the masses before a border, kError at most, move it by e u (1 - u) of the whole, and those behind it as much)
+      if (!exact) {
+        const uint64_t error = static_cast<uint64_t>(static_cast<float>(0.5 * kError) * static_cast<float>(total));
+        if ((before != 0 && target <= before + error) || (cum != total && cum <= target + error)) found = -1;
+      }
+      sh.found = found;
+    }
+    __syncthreads();
+    return sh.found;
+  }
+  // The first token of block b whose cumulative mass, of the tokens at or before `cut`, is above u1 of the block's.
+  __device__ void draw_token(int64_t r, int b, float u1, uint64_t cut, uint64_t whole) const {
+    const SampleParams& p = a.p;
+    constexpr int kPer = kBlock / kThreads;
+    const int first = b * kBlock + threadIdx.x * kPer;
+    float z[kPer];
+    uint64_t w[kPer], s = 0, total;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) z[j] = first + j < p.vocab ? to_f(row[first + j]) : -kInf;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) s += w[j] = place(order_key(z[j]), first + j) >= cut ? w_of(z[j]) : 0;
+    const uint64_t up = cta_scan(s, &total), target = share_of(u1, total);
+    if (s > 0 && (target < total ? up > target && up - s <= target : up == total)) {
+      uint64_t cum = up - s;
+      int id = first;
+      float z_id = z[0];
+      bool done = false;
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) {
+        if (w[j] != 0 && !done) {
+          id = first + j;
+          z_id = z[j];
+          cum += w[j];
+          done = cum > target;
+        }
+      }
+      p.ids[r] = id;
+      if (p.logprobs) p.logprobs[r] = (z_id - m) * p.scale - logf(static_cast<float>(whole) * (1.f / (1ull << kOne)));
+    }
   }
 
   // Where a cut is looked for: the list, or the row.
@@ -300,18 +614,13 @@ struct Row {
       r.each(from, f);
     }
   };
-  __device__ uint64_t sum_of_list(int n, uint64_t from) const {
-    uint64_t s = 0;
-    List{*this, n}.each(from, [&](uint64_t, float z) { s += w_of(z); });
-    return cta_sum(s);
-  }
 
   // The last token of the shortest prefix of the order, among the tokens of src with places lo .. hi (n at most) and those above them (above_n
   // tokens with the mass above_w), that has `count` tokens or (count 0) a mass of at least `target`.
   template <typename S>
   __device__ Cut find_cut(const S& src, int n, uint64_t lo, uint64_t hi, uint32_t count, uint64_t target, uint32_t above_n,
                           uint64_t above_w) const {
-    while (n > kSmall) {
+    while (n > kThreads) {
       const int shift = max(0, 64 - __clzll(hi - lo) - kBinBits);
       __syncthreads();
       for (int i = threadIdx.x; i < kHist; i += kThreads) sh.count[i] = sh.lo[i] = sh.hi[i] = 0;
@@ -331,13 +640,13 @@ struct Row {
       const uint64_t width = (1ull << shift) - 1ull;
       if (hi - lo > width) lo = hi - width;
       if constexpr (S::kRow) {
-        if (n <= kCap && n > kSmall) {
-          gather(src, lo, hi, sh.list, kCap);
+        if (n <= Sh::kCap && n > kThreads) {
+          gather(src, lo, hi, sh.list, Sh::kCap);
           return find_cut(List{*this, n}, n, lo, hi, count, target, above_n, above_w);
         }
       }
     }
-    gather(src, lo, hi, sh.small, kSmall);
+    gather(src, lo, hi, sh.small, kThreads);
     n = sh.n;
     const int t = threadIdx.x;
     const uint64_t x = t < n ? sh.small[t] : 0;
@@ -454,24 +763,36 @@ struct Row {
     for (int i = threadIdx.x; i < kHist; i += kThreads) sh.count[i] = 0;
     if (threadIdx.x < 2) sh.edge[threadIdx.x] = kHist;
     __syncthreads();
-    const int64_t all = static_cast<int64_t>(runs) * kThreads;
-    for (int k = 0; k < runs; ++k) {
-      int e = static_cast<int>((static_cast<int64_t>(k) * kThreads + threadIdx.x) * (vocab - 8) / all);
-      float z[8];
-      if (VEC) {
-        e &= ~7;
+    const int all = runs * kThreads;
+    const float step = static_cast<float>(vocab - 8) / static_cast<float>(all), c32 = a.c * 32.f;
+    constexpr int kAhead = 4, kV = 8 / Elem<T>::kPer;  // loads on their way
+    for (int k0 = 0; k0 < runs; k0 += kAhead) {
+      uint4 v[kAhead][kV];
 #pragma unroll
-        for (int i = 0; i < 8 / Elem<T>::kPer; ++i)
-          unpack(reinterpret_cast<const uint4*>(row + e)[i], z + i * Elem<T>::kPer, static_cast<const T*>(nullptr));
-      } else {
+      for (int u = 0; u < kAhead; ++u) {
+        if (k0 + u >= runs) break;
+        const int e = min(static_cast<int>(((k0 + u) * kThreads + threadIdx.x) * step), vocab - 8);
+        if (VEC) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) z[j] = to_f(row[e + j]);
+          for (int i = 0; i < kV; ++i) v[u][i] = reinterpret_cast<const uint4*>(row + (e & ~7))[i];
+        } else {
+          T* t = reinterpret_cast<T*>(v[u]);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) t[j] = row[e + j];
+        }
       }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) atomicAdd(&sh.count[static_cast<int>(fminf((m - z[j]) * a.c * 32.f, kHist - 1.f))], 1u);
+      for (int u = 0; u < kAhead; ++u) {
+        if (k0 + u >= runs) break;
+        float z[8];
+#pragma unroll
+        for (int i = 0; i < kV; ++i) unpack(v[u][i], z + i * Elem<T>::kPer, static_cast<const T*>(nullptr));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) atomicAdd(&sh.count[static_cast<int>(fminf((m - z[j]) * c32, kHist - 1.f))], 1u);
+      }
     }
     __syncthreads();
-    return static_cast<int>(8 * all);
+    return 8 * all;
   }
   // A value that about 1.3 k + 400 tokens reach, from the sample.
   __device__ float sampled_bound_of_k(int k) const {
@@ -575,23 +896,24 @@ struct Row {
   }
 };
 
-template <typename T, bool VEC, int kThreads>
-__global__ void __launch_bounds__(kThreads, kThreads == 256 ? 3 : 12) sample_kernel(const SampleArgs a) {
+template <typename T, bool VEC, int kThreads, bool FILTER>
+__global__ void __launch_bounds__(kThreads, (FILTER ? 768 : 1024) / kThreads) sample_kernel(const SampleArgs a) {
   constexpr int kWarps = kThreads / 32;
-  using Sh = Shared<kThreads>;
-  extern __shared__ __align__(16) unsigned char dynamic[];  // Shared, then [n_blocks] masses and maxima
+  using Sh = Shared<kThreads, FILTER>;
+  extern __shared__ __align__(16) unsigned char dynamic[];  // Shared, then [n_blocks] masses, maxima, and numbers
   Sh& sh = *reinterpret_cast<Sh*>(dynamic);
   const SampleParams& p = a.p;
   uint64_t* mass = reinterpret_cast<uint64_t*>(dynamic + sizeof(Sh));
   float* max_of = reinterpret_cast<float*>(mass + a.n_blocks);
+  uint16_t* live = reinterpret_cast<uint16_t*>(max_of + a.n_blocks);
   const int rank = cluster_rank(), n_ctas = cluster_ctas();
   const int64_t r = blockIdx.x / n_ctas;
   if (p.row_ids && p.row_ids[r] != p.row_id) return;  // the whole cluster
   const T* row = static_cast<const T*>(p.logits) + r * p.ld;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (n_ctas > 1) cluster_arrive();
-  const bool by_k = p.top_k > 0 && p.top_k < p.vocab, by_m = a.drop != -HUGE_VAL, by_p = p.top_p < 1.0;
-  const bool sums = p.logprobs || !(by_k || by_m);
+  const bool by_k = FILTER && p.top_k > 0 && p.top_k < p.vocab, by_m = FILTER && a.drop != -HUGE_VAL, by_p = FILTER && p.top_p < 1.0;
+  const bool sums = !FILTER || p.logprobs || !(by_k || by_m);
   const float u0 = p.uniforms[2 * r], u1 = p.uniforms[2 * r + 1];
   {
     // two blocks of 16-bit logits, or one of fp32, in hand and as many on their way
@@ -653,7 +975,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 3 : 12) sample_ker
   for (int i = 0; i < kWarps; ++i) m = fmaxf(m, sh.part[i]);
   if (sh.bad || m == -kInf) {
     // no distribution: the first token of the order
-    const uint64_t first = first_of_order(row, p.vocab, threadIdx.x, kThreads);
+    const uint64_t first = first_of_order(row, p.vocab, kThreads);
     if (lane == 0) atomicMax(reinterpret_cast<unsigned long long*>(&sh.best), static_cast<unsigned long long>(first));
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -663,13 +985,13 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 3 : 12) sample_ker
     return;
   }
 
-  using R = Row<T, VEC, kThreads>;
-  const R t{a, row, max_of, mass, sh, m, warp, lane};
+  using R = Row<T, VEC, kThreads, FILTER>;
+  const R t{a, row, max_of, mass, live, sh, m, warp, lane};
   // masses of whole blocks from their fp32 sums, and the row's
   uint64_t whole = 0;
   if (sums) {
     for (int b = threadIdx.x; b < a.n_blocks; b += kThreads) {
-      const uint64_t x = block_mass(max_of[b], __uint_as_float(static_cast<uint32_t>(mass[b])), m, a, sh.pow2);
+      const uint64_t x = times(__uint_as_float(static_cast<uint32_t>(mass[b])), t.w_of(max_of[b]));
       mass[b] = x;
       whole += x;
     }
@@ -678,7 +1000,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 3 : 12) sample_ker
 
   uint64_t cut = kEverything;
   bool exact = false;
-  if (by_k || by_m || by_p) {
+  if constexpr (FILTER) {
     const uint64_t top = static_cast<uint64_t>(order_key(m)) << 32 | 0xFFFFFFFFu;
     float zl = -kInf, zh = kInf;
     if (by_m) zl = __double2float_ru(static_cast<double>(m) + a.drop);
@@ -708,14 +1030,15 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 3 : 12) sample_ker
     }
     zl = fminf(zl, m);
     if (!(zh >= zl)) zh = kInf;
-    typename R::Rest rest{};
+    ulonglong2 sum;
     const bool alone = !by_k && !by_m;
-    int n = alone ? t.template bracket<true>(zl, zh, &rest) : t.template bracket<false>(zl, zh, &rest);
+    int n = t.bracket(zl, zh, &sum);
     if (by_k && n < p.top_k && zl > floor_m) {  // the sample misled
       zl = floor_m;
-      n = t.template bracket<false>(zl, zh, &rest);
+      __syncthreads();
+      n = t.bracket(zl, zh, &sum);
     }
-    bool listed = n <= R::kCap;
+    bool listed = n <= Sh::kCap;
     const typename R::List list{t, n};
     const typename R::Whole whole_row{t};
     uint64_t lo = static_cast<uint64_t>(order_key(zl)) << 32;
@@ -727,7 +1050,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 3 : 12) sample_ker
         lo = cut = k.place;
         kept = k.upto;
       } else if (by_p) {
-        kept = listed ? t.sum_of_list(n, lo) : t.masses(lo);
+        kept = sum.y;
       }
       if (by_p) {
         const uint64_t target = __double2ull_ru(p.top_p * static_cast<double>(kept));
@@ -736,25 +1059,29 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 3 : 12) sample_ker
       }
     } else {
       const uint64_t hi = zh < m ? static_cast<uint64_t>(order_key(zh)) << 32 | 0xFFFFFFFFu : top;
-      const uint64_t above = rest.above, upto = listed ? above + t.sum_of_list(n, lo) : above;
-      // the row's mass is known but for the error of the tail's
-      uint64_t total = upto + rest.tail, error = rest.error;
-      for (bool sure = false;; sure = true) {
+      // The row's mass: from the fp32 sums; where the cut depends on their error, from fp32 sums of the tail alone; where it still does, anew.
+      const uint64_t above = sum.x, upto = sum.x + sum.y;
+      uint64_t total = whole, error = static_cast<uint64_t>(kError * static_cast<double>(whole)) + a.n_blocks;
+      for (int level = 0;; ++level) {
         const uint64_t target = __double2ull_ru(p.top_p * static_cast<double>(total));
         if (listed && above + error < target && target + error <= upto) {
           const Cut k = t.find_cut(list, n, lo, hi, 0, target, 0, above);
           cut = k.place;
-          if (sure || (target > k.before + error && k.upto >= target + error)) break;
-        } else if (sure) {
+          if (level == 2 || (target > k.before + error && k.upto >= target + error)) break;
+        } else if (level == 2) {
           listed = false;
           cut = t.find_cut(whole_row, p.vocab, kEverything, top, 0, target, 0, 0).place;
           break;
         }
-        // within the error of another cut, or not between the bounds: the row's mass anew (the blocks' masses above zh have to be kept)
-        uint64_t s = 0;
-        t.blocks(-kInf, [&](int b, const Raw<T>& raw) { s += raw_mass<T, VEC>(raw, b, lane, p.vocab, kEverything, m, a, sh.pow2); });
-        total = t.cta_sum(s);
-        error = 0;
+        if (level == 0 && listed) {
+          const ulonglong2 rest = t.tail(zl);
+          total = upto + rest.x;
+          error = rest.y;
+        } else {
+          total = t.total();
+          error = 0;
+          level = 1;
+        }
       }
     }
     if (listed) t.add_list(n, cut);
@@ -763,32 +1090,33 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 3 : 12) sample_ker
   }
 
   __syncthreads();
-  for (;;) {
-    if (warp == 0) {
-      const int b = pick_block(mass, a.n_blocks, u0, exact, lane);
-      if (b >= 0) draw_token<T, VEC>(a, row, r, b, u1, cut, m, whole, sh.pow2, lane);
-      if (lane == 0) sh.found = b;
-    }
-    if (exact) return;
-    __syncthreads();
-    if (sh.found >= 0) return;
+  int b = t.pick_block(u0, exact);
+  if (b < 0) {
     t.masses(kEverything);
-    exact = true;
+    b = t.pick_block(u0, true);
   }
+  t.draw_token(r, b, u1, cut, whole);
 }
 
-template <typename T, bool VEC, int kThreads>
+template <typename T, bool VEC, int kThreads, bool FILTER>
 cudaError_t launch_rows(const SampleArgs& a, cudaStream_t s) {
   // few rows: a cluster reads a row, down to a block or two per warp
   Launch l{1, 0, kThreads};
   while (l.cluster < kMaxCluster && static_cast<int64_t>(a.p.rows) * l.cluster < num_sms() && a.n_blocks / l.cluster > 8) l.cluster *= 2;
-  return launch<&sample_kernel<T, VEC, kThreads>>(a.p.rows, l, sizeof(Shared<kThreads>) + 12 * static_cast<size_t>(a.n_blocks), s, a);
+  const size_t smem = sizeof(Shared<kThreads, FILTER>) + 14 * static_cast<size_t>(a.n_blocks);
+  return launch<&sample_kernel<T, VEC, kThreads, FILTER>>(a.p.rows, l, smem, s, a);
+}
+template <typename T, bool VEC>
+cudaError_t launch_vec(const SampleArgs& a, cudaStream_t s) {
+  const SampleParams& p = a.p;
+  if ((p.top_k > 0 && p.top_k < p.vocab) || p.min_p > 0.0 || p.top_p < 1.0)
+    return a.n_blocks <= kShort ? launch_rows<T, VEC, 64, true>(a, s) : launch_rows<T, VEC, 256, true>(a, s);
+  return a.n_blocks <= kShort ? launch_rows<T, VEC, 64, false>(a, s) : launch_rows<T, VEC, 256, false>(a, s);
 }
 template <typename T>
 cudaError_t launch_type(const SampleArgs& a, cudaStream_t s) {
   const bool vec = reinterpret_cast<uintptr_t>(a.p.logits) % 16 == 0 && (a.p.rows == 1 || a.p.ld * static_cast<int64_t>(sizeof(T)) % 16 == 0);
-  if (a.n_blocks <= kShort) return vec ? launch_rows<T, true, 64>(a, s) : launch_rows<T, false, 64>(a, s);
-  return vec ? launch_rows<T, true, 256>(a, s) : launch_rows<T, false, 256>(a, s);
+  return vec ? launch_vec<T, true>(a, s) : launch_vec<T, false>(a, s);
 }
 
 }  // namespace
@@ -796,7 +1124,7 @@ cudaError_t launch_type(const SampleArgs& a, cudaStream_t s) {
 cudaError_t sample_launch(const SampleParams& p, cudaStream_t s) {
   const double c = static_cast<double>(p.scale) * 1.4426950408889634073599;
   SampleArgs a{p, static_cast<float>(c), 0.f, p.min_p > 0.0 ? log(p.min_p) / static_cast<double>(p.scale) : -HUGE_VAL,
-               (p.vocab + kBlock - 1) / kBlock, device_status_ptr()};
+               (p.vocab + kBlock - 1) / kBlock};
   a.c_lo = static_cast<float>(c - static_cast<double>(a.c));
   if (p.dtype == SGD_F16) return launch_type<f16>(a, s);
   if (p.dtype == SGD_BF16) return launch_type<bf16>(a, s);
