@@ -34,7 +34,7 @@ using namespace rows;
 
 constexpr int kBlock = SGD_SAMPLE_BLOCK;
 constexpr int kPerLane = kBlock / 32;
-constexpr int kShort = 4;        // blocks of a row that 64 threads take
+constexpr int kShort = 4;        // blocks of a row that 128 threads take
 constexpr int kSampled = 16384;  // rows from this many tokens on are sampled
 constexpr int kOne = 43;         // weight() of the row's maximum is 2^43: 2^20.6 of them (a row of 3 MiB) add up in 64 bits
 static_assert(kBlock == 512, "a lane takes 16 tokens");
@@ -114,6 +114,12 @@ __device__ __forceinline__ void add_shared(uint32_t* lo, uint32_t* hi, uint64_t 
   const uint32_t low = static_cast<uint32_t>(w), was = atomicAdd(lo, low);
   const uint32_t high = static_cast<uint32_t>(w >> 32) + (was + low < was);
   if (high) atomicAdd(hi, high);
+}
+
+// A barrier of the kThreads threads that take a row.
+template <int kThreads>
+__device__ __forceinline__ void team_sync() {
+  asm volatile("barrier.cta.sync.aligned 1, %0;" ::"n"(kThreads) : "memory");
 }
 
 // A token's place in the order: larger comes first.
@@ -291,7 +297,7 @@ template <typename T, bool VEC, int kThreads, bool FILTER>
 struct Row {
   using Sh = Shared<kThreads, FILTER>;
   static constexpr int kWarps = kThreads / 32, kHist = Sh::kHist;
-  static constexpr int kBinBits = kThreads == 256 ? 10 : 8;
+  static constexpr int kBinBits = kThreads == 256 ? 10 : 9;
   static_assert(!FILTER || kHist == 1 << kBinBits, "bins");
   const SampleArgs& a;
   const T* row;
@@ -308,12 +314,12 @@ struct Row {
   __device__ ulonglong2 cta_sum(uint64_t v, uint64_t w) const {
     v = warp_sum_u64(v);
     w = warp_sum_u64(w);
-    __syncthreads();
+    team_sync<kThreads>();
     if (lane == 0) {
       sh.wide[0][warp] = v;
       sh.wide[1][warp] = w;
     }
-    __syncthreads();
+    team_sync<kThreads>();
     ulonglong2 s = make_ulonglong2(0, 0);
 #pragma unroll
     for (int i = 0; i < kWarps; ++i) {
@@ -324,9 +330,9 @@ struct Row {
   }
   __device__ uint64_t cta_sum(uint64_t v) const {
     v = warp_sum_u64(v);
-    __syncthreads();
+    team_sync<kThreads>();
     if (lane == 0) sh.wide[0][warp] = v;
-    __syncthreads();
+    team_sync<kThreads>();
     uint64_t s = 0;
 #pragma unroll
     for (int i = 0; i < kWarps; ++i) s += sh.wide[0][i];
@@ -335,9 +341,9 @@ struct Row {
   // Inclusive sum over the CTA's threads in their order, and the whole; a barrier before and after.
   __device__ uint64_t cta_scan(uint64_t v, uint64_t* whole) const {
     v = warp_scan_u64(v, lane);
-    __syncthreads();
+    team_sync<kThreads>();
     if (lane == 31) sh.wide[0][warp] = v;
-    __syncthreads();
+    team_sync<kThreads>();
     uint64_t all = 0;
 #pragma unroll
     for (int i = 0; i < kWarps; ++i) {
@@ -352,9 +358,9 @@ struct Row {
   // for the others, a thread each.
   template <typename F, typename G>
   __device__ __forceinline__ void blocks(float least, F f, G g) const {
-    __syncthreads();
+    team_sync<kThreads>();
     if (threadIdx.x == 0) sh.n_live = 0;
-    __syncthreads();
+    team_sync<kThreads>();
     for (int b0 = 0; b0 < a.n_blocks; b0 += kThreads) {
       const int b = b0 + threadIdx.x;
       const bool is = b < a.n_blocks && max_of[b] >= least;
@@ -365,7 +371,7 @@ struct Row {
       if (is) live[at + __popc(hit & ((1u << lane) - 1u))] = static_cast<uint16_t>(b);
       else if (b < a.n_blocks) g(b);
     }
-    __syncthreads();
+    team_sync<kThreads>();
     const int n = sh.n_live;
     if (warp >= n) return;
     Raw<T> raw = fetch<T, VEC>(row, a.p.vocab, live[warp], lane);
@@ -456,50 +462,66 @@ struct Row {
     return __shfl_sync(here, at, first) + __popc(here & ((1u << lane) - 1u));
   }
 
-  // Tokens above zh: their masses by blocks, and in out->x together; those from zl to zh: into the list, as far as it goes, their mass in
-  // out->y.  Returns how many these are.
-  __device__ int bracket(float zl, float zh, ulonglong2* out) const {
+  struct Rest {
+    uint64_t inside, tail, error;
+  };
+  // Tokens from zl to zh: into the list, as far as it goes, and their mass in rest->inside.  Returns how many these are.
+  // With TAIL: the mass of those below, from fp32 sums, and how far it may be off; the blocks' masses, which `mass` holds at the call, lose
+  // it.  Else: `mass` is cleared.
+  template <bool TAIL>
+  __device__ int bracket(float zl, float zh, Rest* rest) const {
     if (threadIdx.x == 0) sh.n = 0;
-    for (int b = threadIdx.x; b < a.n_blocks; b += kThreads) mass[b] = 0;
-    uint64_t above = 0, inside = 0;
+    uint64_t inside = 0, tail = 0, skipped = 0;
+    const uint64_t w_zl = TAIL ? w_of(zl) : 0;
     Queue q{sh.queue[warp]};
     auto f = [&](int e, float z) {
-      const uint64_t w = w_of(z);
-      if (z > zh) {
-        above += w;
-        uint32_t* to = reinterpret_cast<uint32_t*>(mass + e / kBlock);
-        add_shared(to, to + 1, w);
-      } else {
-        inside += w;
-        const int at = slot(&sh.n);
-        if (at < Sh::kCap) sh.list[at] = place(order_key(z), e);
-      }
+      inside += w_of(z);
+      const int at = slot(&sh.n);
+      if (at < Sh::kCap) sh.list[at] = place(order_key(z), e);
     };
-    blocks(zl, [&](int b, const Raw<T>& raw) { marked(q, b, marks(b, raw, zl), f); }, [](int) {});
-    drain(q, 1, f);
-    *out = cta_sum(above, inside);
-    return sh.n;
-  }
-  // Mass of the tokens below zl from fp32 sums, and how far it may be off.
-  __device__ ulonglong2 tail(float zl) const {
-    uint64_t sum = 0;
-    const uint64_t w = w_of(zl);
-    blocks(-kInf,
-           [&](int, const Raw<T>& raw) {
-             float z[kPerLane], s[2] = {0.f, 0.f};
-             numbers(raw, z);
+    blocks(zl,
+           [&](int b, const Raw<T>& raw) {
+             if constexpr (TAIL) {
+               float z[kPerLane], s[2] = {0.f, 0.f};
+               numbers(raw, z);
+               uint32_t on = 0;
 #pragma unroll
-             for (int j = 0; j < kPerLane; ++j) s[j & 1] += z[j] >= zl ? 0.f : ex2_approx(__fmul_rn(z[j] - zl, a.c));
-             const float all = warp_sum(s[0] + s[1]);
-             if (lane == 0) sum += times(all, w);
+               for (int j = 0; j < kPerLane; ++j) {
+                 const bool low = z[j] < zl;
+                 s[j & 1] += low ? ex2_approx(__fmul_rn(z[j] - zl, a.c)) : 0.f;
+                 on |= !low && z[j] <= zh ? 1u << j : 0u;
+               }
+               if (zl == -kInf) on = marks(b, raw, zl);
+               marked(q, b, on, f);
+               const float all = warp_sum(s[0] + s[1]);
+               if (lane == 0) {
+                 const uint64_t w = times(all, w_zl);
+                 tail += w;
+                 mass[b] -= w;
+               }
+             } else {
+               marked(q, b, marks(b, raw, zl), f);
+               if (lane == 0) mass[b] = 0;
+             }
            },
-           [](int) {});
-    sum = cta_sum(sum);
-    // 18 u, and three roundings of an exponent t whose mean over the mass S (of zl's weight) is at most log2(vocab) - log2(S); half
-    // a unit of zl's weight's 2^-22 a block, and tokens below 2^-43
-    const float wf = static_cast<float>(w) + 1.f, spread = sum > 0 ? fmaxf(log2f(a.p.vocab * wf / static_cast<float>(sum)), 0.f) : 0.f;
-    return make_ulonglong2(sum, static_cast<uint64_t>(a.p.vocab) + a.n_blocks * (1 + (w >> 22)) +
-                                    __double2ull_ru((20.0 + 2.1 * spread) * 5.9604645e-8 * static_cast<double>(sum)));
+           [&](int b) {
+             if (TAIL) skipped += mass[b];
+             mass[b] = 0;
+           });
+    drain(q, 1, f);
+    const ulonglong2 sum = cta_sum(inside, tail);
+    rest->inside = sum.x;
+    if constexpr (TAIL) {
+      skipped = cta_sum(skipped);
+      // the sums against zl: 18 u, and three roundings of an exponent t whose mean over the mass S (of zl's weight) is at most log2(vocab) -
+      // log2(S); half a unit of 2^-22 of zl's weight a block, and tokens below 2^-43
+      const float wf = static_cast<float>(w_zl) + 1.f;
+      const float spread = sum.y > 0 ? fmaxf(log2f(a.p.vocab * wf / static_cast<float>(sum.y)), 0.f) : 0.f;
+      rest->tail = sum.y + skipped;
+      rest->error = static_cast<uint64_t>(a.p.vocab) + a.n_blocks * (1 + (w_zl >> 22)) +
+                    __double2ull_ru((20.0 + 2.1 * spread) * 5.9604645e-8 * static_cast<double>(sum.y) + kError * static_cast<double>(skipped));
+    }
+    return sh.n;
   }
 
   // Masses of the blocks, of the tokens at or before `cut` in the order; returns the whole.
@@ -516,50 +538,63 @@ struct Row {
            [&](int b) { mass[b] = 0; });
     return cta_sum(all);
   }
-  // The row's mass.
-  __device__ uint64_t total() const {
-    uint64_t s = 0;
-    blocks(-kInf, [&](int b, const Raw<T>& raw) { s += raw_mass<T, VEC>(raw, b, lane, a.p.vocab, kEverything, m, a, sh.pow2); }, [](int) {});
-    return cta_sum(s);
+  // The row's mass, and that of the tokens below zl.
+  __device__ ulonglong2 total(float zl) const {
+    uint64_t s = 0, low = 0;
+    blocks(-kInf,
+           [&](int, const Raw<T>& raw) {
+             float z[kPerLane];
+             numbers(raw, z);
+#pragma unroll
+             for (int j = 0; j < kPerLane; ++j) {
+               const uint64_t w = w_of(z[j]);
+               s += w;
+               if (z[j] < zl) low += w;
+             }
+           },
+           [](int) {});
+    return cta_sum(s, low);
   }
-  // Adds the list's tokens that are kept to the blocks' masses.
+  // Adds the list's tokens that are kept to the blocks' masses, or (OUT) takes the others out of them.
+  template <bool OUT>
   __device__ void add_list(int n, uint64_t cut) const {
-    __syncthreads();
+    team_sync<kThreads>();
     for (int i = threadIdx.x; i < n; i += kThreads) {
       const uint64_t x = sh.list[i];
-      if (x < cut) continue;
+      if (OUT ? x >= cut : x < cut) continue;
       uint32_t* to = reinterpret_cast<uint32_t*>(mass + index_of(x) / kBlock);
-      add_shared(to, to + 1, w_of(value_of(x)));
+      const uint64_t w = w_of(value_of(x));
+      add_shared(to, to + 1, OUT ? 0 - w : w);
     }
-    __syncthreads();
+    team_sync<kThreads>();
   }
 
-  // The first block whose cumulative mass is above u0 of the whole; -1 where the masses' error (`exact`: none) leaves it open.
-  __device__ int pick_block(float u0, bool exact) const {
+  // (a block without a token that is kept may be left with less than nothing by the fp32 sums)
+  static __device__ __forceinline__ uint64_t positive(uint64_t w) { return static_cast<int64_t>(w) < 0 ? 0 : w; }
+
+  // The first block whose cumulative mass is above u0 of the whole; -1 where the error of the cumulative masses against their whole's share
+  // leaves it open.
+  __device__ int pick_block(float u0, uint64_t error) const {
     const int per = (a.n_blocks + kThreads - 1) / kThreads, from = min(static_cast<int>(threadIdx.x) * per, a.n_blocks),
               to = min(from + per, a.n_blocks);
     uint64_t s = 0, total;
-    for (int b = from; b < to; ++b) s += mass[b];
+    for (int b = from; b < to; ++b) s += positive(mass[b]);
     const uint64_t up = cta_scan(s, &total), target = share_of(u0, total);
     if (s > 0 && (target < total ? up > target && up - s <= target : up == total)) {
       uint64_t before = up - s, cum = before;
       int found = from;
       for (int i = from; i < to; ++i) {
-        const uint64_t w = mass[i];
+        const uint64_t w = positive(mass[i]);
         if (w == 0) continue;
         found = i;
         before = cum;
         cum += w;
         if (cum > target) break;
       }
-      // (errors e of the masses before a border, kError at most, move it by e u (1 - u) of the whole, and those behind it as much)
-      if (!exact) {
-        const uint64_t error = static_cast<uint64_t>(static_cast<float>(0.5 * kError) * static_cast<float>(total));
-        if ((before != 0 && target <= before + error) || (cum != total && cum <= target + error)) found = -1;
-      }
+      if (error && ((before != 0 && target <= before + error) || (cum != total && cum <= target + error))) found = -1;
       sh.found = found;
     }
-    __syncthreads();
+    team_sync<kThreads>();
     return sh.found;
   }
   // The first token of block b whose cumulative mass, of the tokens at or before `cut`, is above u1 of the block's.
@@ -622,16 +657,16 @@ struct Row {
                           uint64_t above_w) const {
     while (n > kThreads) {
       const int shift = max(0, 64 - __clzll(hi - lo) - kBinBits);
-      __syncthreads();
+      team_sync<kThreads>();
       for (int i = threadIdx.x; i < kHist; i += kThreads) sh.count[i] = sh.lo[i] = sh.hi[i] = 0;
-      __syncthreads();
+      team_sync<kThreads>();
       src.each(lo, [&](uint64_t x, float z) {
         if (x > hi) return;
         const uint32_t bin = static_cast<uint32_t>((hi - x) >> shift);
         atomicAdd(&sh.count[bin], 1u);
         add_shared(&sh.lo[bin], &sh.hi[bin], w_of(z));
       });
-      __syncthreads();
+      team_sync<kThreads>();
       pick_bin(count, target, above_n, above_w);
       above_n = sh.above_n;
       above_w = sh.above_w;
@@ -653,7 +688,7 @@ struct Row {
     const uint64_t w = t < n ? w_of(value_of(x)) : 0;
     sh.small_w[t] = w;
     if (t == 0) sh.cut = 0;
-    __syncthreads();
+    team_sync<kThreads>();
     uint32_t rank = above_n;
     uint64_t cum = above_w;
     if (t < n)
@@ -670,26 +705,26 @@ struct Row {
       sh.cut_upto = cum;
     };
     if (it) write();
-    __syncthreads();
+    team_sync<kThreads>();
     const bool none = sh.cut == 0;
-    __syncthreads();
+    team_sync<kThreads>();
     if (none && t < n && rank == above_n + n) write();
-    __syncthreads();
+    team_sync<kThreads>();
     const Cut cut{sh.cut, sh.cut_before, sh.cut_upto};
-    __syncthreads();
+    team_sync<kThreads>();
     return cut;
   }
   template <typename S>
   __device__ void gather(const S& src, uint64_t lo, uint64_t hi, uint64_t* to, int cap) const {
-    __syncthreads();
+    team_sync<kThreads>();
     if (threadIdx.x == 0) sh.n = 0;
-    __syncthreads();
+    team_sync<kThreads>();
     src.each(lo, [&](uint64_t x, float) {
       if (x > hi) return;
       const int at = slot(&sh.n);
       if (at < cap) to[at] = x;
     });
-    __syncthreads();
+    team_sync<kThreads>();
   }
   // The histogram's first bin with which the target is reached (where rounding leaves none, the last one that holds anything),
   // and what is above it.
@@ -730,28 +765,34 @@ struct Row {
         }
       }
     }
-    __syncthreads();
+    team_sync<kThreads>();
   }
 
-  // Key of the k-th largest of kThreads groups' maxima (k <= kThreads): at least k tokens have it or more.
+  // A key that at least k tokens have or more: the k-th largest of the maxima of kThreads groups (k <= kThreads) of blocks, or of tokens.
+  // (Without its last bits, whose place the group's number takes: no two are equal.)
+  template <bool TOKENS>
   __device__ uint32_t bound_of_k(int k) const {
+    constexpr uint32_t kLow = kThreads - 1;
     float g = -kInf;
-    for (int b = threadIdx.x; b < a.n_blocks; b += kThreads) g = fmaxf(g, max_of[b]);
-    const uint32_t mine = order_key(g);
+    if (TOKENS) {
+#pragma unroll 8
+      for (int i = threadIdx.x; i < a.p.vocab; i += kThreads) g = fmaxf(g, to_f(row[i]));
+    } else {
+      for (int b = threadIdx.x; b < a.n_blocks; b += kThreads) g = fmaxf(g, max_of[b]);
+    }
+    const uint32_t mine = (order_key(g) & ~kLow) | threadIdx.x;
     sh.groups[threadIdx.x] = mine;
-    __syncthreads();
+    team_sync<kThreads>();
     int more = 0;
-#pragma unroll 4
+#pragma unroll 8
     for (int i = 0; i < kThreads; i += 4) {
       const uint4 x = *reinterpret_cast<const uint4*>(sh.groups + i);
-      const int t = threadIdx.x;
-      more += (x.x > mine || (x.x == mine && i < t)) + (x.y > mine || (x.y == mine && i + 1 < t)) +
-              (x.z > mine || (x.z == mine && i + 2 < t)) + (x.w > mine || (x.w == mine && i + 3 < t));
+      more += (x.x > mine) + (x.y > mine) + (x.z > mine) + (x.w > mine);
     }
-    if (more == k - 1) sh.above_n = mine;
-    __syncthreads();
-    const uint32_t key = sh.above_n;
-    __syncthreads();
+    if (more == k - 1) sh.above_n = mine & ~kLow;
+    team_sync<kThreads>();
+    const uint32_t key = max(sh.above_n, kKeyNegInf);
+    team_sync<kThreads>();
     return key;
   }
 
@@ -759,10 +800,10 @@ struct Row {
   // maximum down.  Returns how many were looked at.
   __device__ int sampled() const {
     const int vocab = a.p.vocab, runs = max(4, (vocab / 8 + 8 * kThreads - 1) / (8 * kThreads));  // of a thread
-    __syncthreads();
+    team_sync<kThreads>();
     for (int i = threadIdx.x; i < kHist; i += kThreads) sh.count[i] = 0;
     if (threadIdx.x < 2) sh.edge[threadIdx.x] = kHist;
-    __syncthreads();
+    team_sync<kThreads>();
     const int all = runs * kThreads;
     const float step = static_cast<float>(vocab - 8) / static_cast<float>(all), c32 = a.c * 32.f;
     constexpr int kAhead = 4, kV = 8 / Elem<T>::kPer;  // loads on their way
@@ -791,7 +832,7 @@ struct Row {
         for (int j = 0; j < 8; ++j) atomicAdd(&sh.count[static_cast<int>(fminf((m - z[j]) * c32, kHist - 1.f))], 1u);
       }
     }
-    __syncthreads();
+    team_sync<kThreads>();
     return 8 * all;
   }
   // A value that about 1.3 k + 400 tokens reach, from the sample.
@@ -808,14 +849,14 @@ struct Row {
       if (lane >= o) up += x;
     }
     if (lane == 31) sh.part_n[warp] = up;
-    __syncthreads();
+    team_sync<kThreads>();
     up -= sum;
     for (int i = 0; i < warp; ++i) up += sh.part_n[i];
     const double want = (1.3 * k + 400.0) * looked / a.p.vocab;
 #pragma unroll
     for (int j = 0; j < kPer; ++j)
       if (up + n[j] >= want) atomicMin(&sh.edge[0], static_cast<int>(threadIdx.x) * kPer + j + 1);
-    __syncthreads();
+    team_sync<kThreads>();
     const int edge = sh.edge[0];
     return edge >= kHist ? -kInf : m - edge / (32.f * a.c);
   }
@@ -850,7 +891,7 @@ struct Row {
       sh.part_n[warp] = up_n;
       sh.part[warp] = up_f;
     }
-    __syncthreads();
+    team_sync<kThreads>();
     up_n -= n[0];
     up_f -= f[0];
     for (int i = warp + 1; i < kWarps; ++i) {
@@ -866,7 +907,7 @@ struct Row {
       if (here <= 0.95f * want) atomicMin(&sh.edge[0], i);
       if (here <= 1.05f * want) atomicMin(&sh.edge[1], i);
     }
-    __syncthreads();
+    team_sync<kThreads>();
     const int low = sh.edge[0], high = sh.edge[1];
     // 64 sampled tokens more below, 32 above: 800 of the row, which the list has room for
     if (threadIdx.x == 0) {
@@ -874,14 +915,14 @@ struct Row {
       sh.edge[3] = 0;
       sh.edge_n[0] = sh.edge_n[1] = 0;
     }
-    __syncthreads();
+    team_sync<kThreads>();
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
       const int i = threadIdx.x * kPer + j;
       if (i == low) sh.edge_n[0] = n[j] + up_n;
       if (i == high) sh.edge_n[1] = n[j] + up_n;
     }
-    __syncthreads();
+    team_sync<kThreads>();
     const uint32_t n_low = sh.edge_n[0], n_high = sh.edge_n[1];
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
@@ -889,9 +930,9 @@ struct Row {
       if (n_low >= 64 && n[j] + up_n <= n_low - 64) atomicMin(&sh.edge[2], i);
       if (n[j] + up_n >= n_high + 32) atomicMax(&sh.edge[3], i);
     }
-    __syncthreads();
+    team_sync<kThreads>();
     const int zl = sh.edge[2], zh = sh.edge[3];
-    __syncthreads();
+    team_sync<kThreads>();
     return make_float2(zl >= kHist ? -kInf : m - zl / (32.f * a.c), zh <= 0 ? kInf : m - zh / (32.f * a.c));
   }
 };
@@ -919,11 +960,11 @@ __global__ void __launch_bounds__(kThreads, (FILTER ? 768 : 1024) / kThreads) sa
     // two blocks of 16-bit logits, or one of fp32, in hand and as many on their way
     constexpr int kPair = sizeof(T) == 2 ? 2 : 1;
     const int stride = kWarps * n_ctas;
-    int b = warp * n_ctas + rank;
+    int i = warp * n_ctas + rank;
     Raw<T> next[kPair];
 #pragma unroll
     for (int u = 0; u < kPair; ++u)
-      if (b + u * stride < a.n_blocks) next[u] = fetch<T, VEC>(row, p.vocab, b + u * stride, lane);
+      if (i + u * stride < a.n_blocks) next[u] = fetch<T, VEC>(row, p.vocab, i + u * stride, lane);
     if (threadIdx.x < 32) sh.pow2[threadIdx.x] = kPow2[threadIdx.x];
     if (threadIdx.x == 0) {
       sh.bad = 0;
@@ -931,16 +972,17 @@ __global__ void __launch_bounds__(kThreads, (FILTER ? 768 : 1024) / kThreads) sa
     }
     const uint32_t to_max = map_to_rank(smem_u32(max_of), 0), to_mass = map_to_rank(smem_u32(mass), 0);
     if (n_ctas > 1) cluster_wait();  // every CTA of the cluster runs: the leader's shared memory may be written
-    for (; b < a.n_blocks; b += kPair * stride) {
+    for (; i < a.n_blocks; i += kPair * stride) {
       Raw<T> cur[kPair];
 #pragma unroll
       for (int u = 0; u < kPair; ++u) {
         cur[u] = next[u];
-        if (b + (kPair + u) * stride < a.n_blocks) next[u] = fetch<T, VEC>(row, p.vocab, b + (kPair + u) * stride, lane);
+        if (i + (kPair + u) * stride < a.n_blocks) next[u] = fetch<T, VEC>(row, p.vocab, i + (kPair + u) * stride, lane);
       }
       const float2 st = block_stats<T, kPair>(cur, sums, a.c, lane);
-      const int at = kPair == 2 && lane >= 16 ? b + stride : b;
-      if ((lane == 0 || (kPair == 2 && lane == 16)) && at < a.n_blocks) {
+      const int mine = kPair == 2 && lane >= 16 ? i + stride : i;
+      if ((lane == 0 || (kPair == 2 && lane == 16)) && mine < a.n_blocks) {
+        const int at = mine;
         if (n_ctas == 1) {
           max_of[at] = st.x;
           mass[at] = __float_as_uint(st.y);
@@ -956,7 +998,7 @@ __global__ void __launch_bounds__(kThreads, (FILTER ? 768 : 1024) / kThreads) sa
     cluster_sync();
     if (rank != 0) return;
   } else {
-    __syncthreads();
+    team_sync<kThreads>();
   }
 
   // the row's maximum
@@ -970,14 +1012,14 @@ __global__ void __launch_bounds__(kThreads, (FILTER ? 768 : 1024) / kThreads) sa
   m = key_value(__reduce_max_sync(0xffffffffu, order_key(m)));
   if (lane == 0) sh.part[warp] = m;
   if (bad) sh.bad = 1;
-  __syncthreads();
+  team_sync<kThreads>();
 #pragma unroll
   for (int i = 0; i < kWarps; ++i) m = fmaxf(m, sh.part[i]);
   if (sh.bad || m == -kInf) {
     // no distribution: the first token of the order
     const uint64_t first = first_of_order(row, p.vocab, kThreads);
     if (lane == 0) atomicMax(reinterpret_cast<unsigned long long*>(&sh.best), static_cast<unsigned long long>(first));
-    __syncthreads();
+    team_sync<kThreads>();
     if (threadIdx.x == 0) {
       p.ids[r] = index_of(sh.best);
       if (p.logprobs) p.logprobs[r] = sh.bad ? kNan : -kInf;
@@ -999,24 +1041,29 @@ __global__ void __launch_bounds__(kThreads, (FILTER ? 768 : 1024) / kThreads) sa
   }
 
   uint64_t cut = kEverything;
-  bool exact = false;
+  uint64_t pick_error = 0;
   if constexpr (FILTER) {
     const uint64_t top = static_cast<uint64_t>(order_key(m)) << 32 | 0xFFFFFFFFu;
     float zl = -kInf, zh = kInf;
     if (by_m) zl = __double2float_ru(static_cast<double>(m) + a.drop);
     const float floor_m = zl;
     if (by_k) {
-      // (as many groups as there are blocks have a maximum)
-      if (p.top_k <= min(a.n_blocks, kThreads)) zl = fmaxf(zl, key_value(t.bound_of_k(p.top_k)));
+      // (as many groups of blocks as there are blocks have a maximum)
+      if (p.top_k <= min(a.n_blocks, kThreads)) zl = fmaxf(zl, key_value(t.template bound_of_k<false>(p.top_k)));
       else if (p.vocab >= kSampled) zl = fmaxf(zl, t.sampled_bound_of_k(p.top_k));
+      else if (p.top_k <= kThreads) zl = fmaxf(zl, key_value(t.template bound_of_k<true>(p.top_k)));
     }
     if (!by_k && !by_m) {
       // the maxima from the 64th largest on, if they have the mass already
-      const uint32_t key = t.bound_of_k(min(64, (a.n_blocks + 3) / 4));
       uint64_t s = 0;
-      for (int b = threadIdx.x; b < a.n_blocks; b += kThreads)
-        if (order_key(max_of[b]) >= key) s += t.w_of(max_of[b]);
-      if (static_cast<double>(t.cta_sum(s)) >= p.top_p * static_cast<double>(whole) * (1.0 + kError)) {
+      uint32_t key = 0;
+      if (a.n_blocks >= 16) {
+        key = t.template bound_of_k<false>(min(64, a.n_blocks / 4));
+        for (int b = threadIdx.x; b < a.n_blocks; b += kThreads)
+          if (order_key(max_of[b]) >= key) s += t.w_of(max_of[b]);
+        s = t.cta_sum(s);
+      }
+      if (static_cast<double>(s) >= p.top_p * static_cast<double>(whole) * (1.0 + kError)) {
         zl = key_value(key);
       } else if (p.vocab >= kSampled) {
         const float2 z = t.sampled_bounds((1.0 - p.top_p) * static_cast<double>(whole) * (1.0 / (1ull << kOne)));
@@ -1030,13 +1077,14 @@ __global__ void __launch_bounds__(kThreads, (FILTER ? 768 : 1024) / kThreads) sa
     }
     zl = fminf(zl, m);
     if (!(zh >= zl)) zh = kInf;
-    ulonglong2 sum;
+    typename R::Rest rest{};
     const bool alone = !by_k && !by_m;
-    int n = t.bracket(zl, zh, &sum);
+    team_sync<kThreads>();
+    int n = alone ? t.template bracket<true>(zl, zh, &rest) : t.template bracket<false>(zl, zh, &rest);
     if (by_k && n < p.top_k && zl > floor_m) {  // the sample misled
       zl = floor_m;
-      __syncthreads();
-      n = t.bracket(zl, zh, &sum);
+      team_sync<kThreads>();
+      n = t.template bracket<false>(zl, zh, &rest);
     }
     bool listed = n <= Sh::kCap;
     const typename R::List list{t, n};
@@ -1050,7 +1098,7 @@ __global__ void __launch_bounds__(kThreads, (FILTER ? 768 : 1024) / kThreads) sa
         lo = cut = k.place;
         kept = k.upto;
       } else if (by_p) {
-        kept = sum.y;
+        kept = rest.inside;
       }
       if (by_p) {
         const uint64_t target = __double2ull_ru(p.top_p * static_cast<double>(kept));
@@ -1058,42 +1106,46 @@ __global__ void __launch_bounds__(kThreads, (FILTER ? 768 : 1024) / kThreads) sa
         cut = listed ? t.find_cut(list, n, lo, top, 0, target, 0, 0).place : t.find_cut(whole_row, n, lo, top, 0, target, 0, 0).place;
       }
     } else {
+      // What is not kept has at most the share 1 - top_p of the row's mass T: the tail, and the list from its end on.  The mass of the list that
+      // is kept is then at least tail + list - (1 - top_p) T, which is off by the tail's error and, little, by T's.
       const uint64_t hi = zh < m ? static_cast<uint64_t>(order_key(zh)) << 32 | 0xFFFFFFFFu : top;
-      // The row's mass: from the fp32 sums; where the cut depends on their error, from fp32 sums of the tail alone; where it still does, anew.
-      const uint64_t above = sum.x, upto = sum.x + sum.y;
-      uint64_t total = whole, error = static_cast<uint64_t>(kError * static_cast<double>(whole)) + a.n_blocks;
-      for (int level = 0;; ++level) {
-        const uint64_t target = __double2ull_ru(p.top_p * static_cast<double>(total));
-        if (listed && above + error < target && target + error <= upto) {
-          const Cut k = t.find_cut(list, n, lo, hi, 0, target, 0, above);
+      uint64_t total = whole, error = rest.error + __double2ull_ru((1.0 - p.top_p) * kError * static_cast<double>(whole));
+      bool sure = false;
+      for (;;) {
+        const uint64_t out = __double2ull_rd((1.0 - p.top_p) * static_cast<double>(total)), held = rest.tail + rest.inside;
+        if (listed && out + error < held && held - out + error <= rest.inside) {
+          const uint64_t target = held - out;
+          const Cut k = t.find_cut(list, n, lo, hi, 0, target, 0, 0);
           cut = k.place;
-          if (level == 2 || (target > k.before + error && k.upto >= target + error)) break;
-        } else if (level == 2) {
+          if (sure || (target > k.before + error && k.upto >= target + error)) break;
+        }
+        if (sure) {
           listed = false;
-          cut = t.find_cut(whole_row, p.vocab, kEverything, top, 0, target, 0, 0).place;
+          cut = t.find_cut(whole_row, p.vocab, kEverything, top, 0, __double2ull_ru(p.top_p * static_cast<double>(total)), 0, 0).place;
           break;
         }
-        if (level == 0 && listed) {
-          const ulonglong2 rest = t.tail(zl);
-          total = upto + rest.x;
-          error = rest.y;
-        } else {
-          total = t.total();
-          error = 0;
-          level = 1;
-        }
+        // within the error of another cut, or not between the bounds: both anew
+        const ulonglong2 sums_anew = t.total(zl);
+        total = sums_anew.x;
+        rest.tail = sums_anew.y;
+        error = 0;
+        sure = true;
       }
     }
-    if (listed) t.add_list(n, cut);
-    else t.masses(cut);
-    exact = true;
+    if (!listed) t.masses(cut);
+    else if (alone) t.template add_list<true>(n, cut);
+    else t.template add_list<false>(n, cut);
+    pick_error = listed && alone ? 2 * (rest.error + static_cast<uint64_t>(kError * static_cast<double>(whole))) : 0;
+  } else {
+    // (errors e of the masses before a border, kError at most, move it by e u (1 - u) of the whole, and those behind it as much)
+    pick_error = 1 + static_cast<uint64_t>(0.5 * kError * static_cast<double>(whole));
   }
 
-  __syncthreads();
-  int b = t.pick_block(u0, exact);
+  team_sync<kThreads>();
+  int b = t.pick_block(u0, pick_error);
   if (b < 0) {
-    t.masses(kEverything);
-    b = t.pick_block(u0, true);
+    t.masses(cut);
+    b = t.pick_block(u0, 0);
   }
   t.draw_token(r, b, u1, cut, whole);
 }
@@ -1110,8 +1162,8 @@ template <typename T, bool VEC>
 cudaError_t launch_vec(const SampleArgs& a, cudaStream_t s) {
   const SampleParams& p = a.p;
   if ((p.top_k > 0 && p.top_k < p.vocab) || p.min_p > 0.0 || p.top_p < 1.0)
-    return a.n_blocks <= kShort ? launch_rows<T, VEC, 64, true>(a, s) : launch_rows<T, VEC, 256, true>(a, s);
-  return a.n_blocks <= kShort ? launch_rows<T, VEC, 64, false>(a, s) : launch_rows<T, VEC, 256, false>(a, s);
+    return a.n_blocks <= kShort ? launch_rows<T, VEC, 128, true>(a, s) : launch_rows<T, VEC, 256, true>(a, s);
+  return a.n_blocks <= kShort ? launch_rows<T, VEC, 128, false>(a, s) : launch_rows<T, VEC, 256, false>(a, s);
 }
 template <typename T>
 cudaError_t launch_type(const SampleArgs& a, cudaStream_t s) {
