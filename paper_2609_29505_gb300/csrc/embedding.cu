@@ -5,9 +5,10 @@
 // The gradient goes by the rows sorted by token: every sum has one order, no atomics are added to, and a token with
 // half of the rows (the mask of a masked-token model) is split over as many CTAs as the others.
 //   sort     (token, row) ascending.  Up to kRankRows rows each row counts the rows before it, N^2 comparisons over the
-//            whole GPU in one launch; above, a radix sort (8 bits at a time: histogram, scan, scatter).
+//            whole GPU in one launch; above, a radix sort (8 bits at a time: histogram, then a stable scatter).
 //   sums     CTA (chunk of sorted rows, columns): a run of equal tokens that lies inside the chunk is written
-//            to the table; a run that passes a chunk's border leaves a partial sum per chunk in the workspace.
+//            to the table; a run that passes a chunk's border leaves a partial sum per chunk in the workspace.  Beside them,
+//            unless they are kept, CTAs that clear the rows of the tokens that do not occur: a range of the table each.
 //   join     adds the partial sums of such a run in the order of the chunks.
 #include "common.cuh"
 #include "kernels.h"
@@ -93,38 +94,54 @@ bool vectors(const void* p, int64_t ld, int per, int d) {  // rows of whole vect
 
 // ----- lookup -----
 
-constexpr int kCols = 8;  // columns of a thread
+constexpr int kCols = 8;      // columns of a thread
+constexpr int kRowsAhead = 4;  // of its rows, a grid's height apart: their loads are on their way together
 
 template <typename TI, typename TO, bool VEC>
-__global__ void __launch_bounds__(256) embedding_kernel(const EmbeddingParams p) {
-  const int per = (p.d + kCols - 1) / kCols;
-  const int64_t all = static_cast<int64_t>(p.rows) * per;
-  const TI* table = static_cast<const TI*>(p.table);
-  TO* out = static_cast<TO*>(p.out);
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < all; i += static_cast<int64_t>(gridDim.x) * 256) {
-    const int r = static_cast<int>(i / per), c = static_cast<int>(i - static_cast<int64_t>(r) * per) * kCols;
-    const int id = p.ids[r];
-    float f[kCols];
-    if (id >= 0 && id < p.vocab) {
-      load<VEC, kCols>(table + static_cast<int64_t>(id) * p.ld + c, p.d - c, f);
+__global__ void __launch_bounds__(128) embedding_kernel(const EmbeddingParams p) {
+  const int c = (blockIdx.x * 128 + threadIdx.x) * kCols;
+  if (c >= p.d) return;
+  const TI* table = static_cast<const TI*>(p.table) + c;
+  TO* out = static_cast<TO*>(p.out) + c;
+  for (int64_t r0 = blockIdx.y; r0 < p.rows; r0 += static_cast<int64_t>(kRowsAhead) * gridDim.y) {
+    int id[kRowsAhead];
 #pragma unroll
-      for (int j = 0; j < kCols; ++j) f[j] *= p.scale;
-    } else {
-#pragma unroll
-      for (int j = 0; j < kCols; ++j) f[j] = 0.f;
+    for (int u = 0; u < kRowsAhead; ++u) {
+      const int64_t r = r0 + static_cast<int64_t>(u) * gridDim.y;
+      id[u] = r < p.rows ? p.ids[r] : -1;
     }
-    store<VEC, kCols>(out + static_cast<int64_t>(r) * p.ld_out + c, p.d - c, f);
+    float f[kRowsAhead][kCols];
+#pragma unroll
+    for (int u = 0; u < kRowsAhead; ++u) {
+      if (id[u] >= 0 && id[u] < p.vocab) {
+        load<VEC, kCols>(table + static_cast<int64_t>(id[u]) * p.ld, p.d - c, f[u]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < kCols; ++j) f[u][j] = 0.f;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kRowsAhead; ++u) {
+      const int64_t r = r0 + static_cast<int64_t>(u) * gridDim.y;
+      if (r >= p.rows) break;
+#pragma unroll
+      for (int j = 0; j < kCols; ++j) f[u][j] *= p.scale;
+      store<VEC, kCols>(out + r * p.ld_out, p.d - c, f[u]);
+    }
   }
 }
 
 template <typename TI, typename TO>
 cudaError_t lookup(const EmbeddingParams& p, cudaStream_t s) {
-  const int64_t all = static_cast<int64_t>(p.rows) * ((p.d + kCols - 1) / kCols);
-  const int64_t blocks = (all + 255) / 256, most = 1 << 20;
-  const dim3 grid(static_cast<unsigned>(blocks < most ? blocks : most));
+  // a row per thread where that leaves SMs idle otherwise, up to kRowsAhead
+  const int across = (p.d + 128 * kCols - 1) / (128 * kCols);
+  int high = (p.rows + kRowsAhead - 1) / kRowsAhead;
+  const int fill = (8 * num_sms() + across - 1) / across;
+  if (high < fill) high = p.rows < fill ? p.rows : fill;
+  const dim3 grid(across, high < 65535 ? high : 65535);
   const bool vec = vectors<TI>(p.table, p.ld, kCols, p.d) && vectors<TO>(p.out, p.ld_out, kCols, p.d);
-  if (vec) embedding_kernel<TI, TO, true><<<grid, 256, 0, s>>>(p);
-  else embedding_kernel<TI, TO, false><<<grid, 256, 0, s>>>(p);
+  if (vec) embedding_kernel<TI, TO, true><<<grid, 128, 0, s>>>(p);
+  else embedding_kernel<TI, TO, false><<<grid, 128, 0, s>>>(p);
   return cudaGetLastError();
 }
 template <typename TI>
@@ -134,36 +151,13 @@ cudaError_t lookup_to(const EmbeddingParams& p, cudaStream_t s) {
   return lookup<TI, float>(p, s);
 }
 
-// ----- gradient: a table of zeros -----
-
-template <bool VEC, typename T>
-__global__ void __launch_bounds__(256) zero_kernel(T* table, int64_t ld, int vocab, int d) {
-  constexpr int N = VEC ? Vec<T>::kN : 1;
-  const int per = d / N;
-  const int64_t all = static_cast<int64_t>(vocab) * per;
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < all; i += static_cast<int64_t>(gridDim.x) * 256) {
-    const int64_t r = i / per;
-    T* at = table + r * ld + (i - r * per) * N;
-    if constexpr (VEC) *reinterpret_cast<uint4*>(at) = make_uint4(0, 0, 0, 0);
-    else *at = from_f32<T>(0.f);
-  }
-}
-template <typename T>
-cudaError_t zero(void* table, int64_t ld, int vocab, int d, cudaStream_t s) {
-  T* t = static_cast<T*>(table);
-  const bool vec = vectors<T>(t, ld, Vec<T>::kN, d);
-  const int64_t all = static_cast<int64_t>(vocab) * (vec ? d / Vec<T>::kN : d), blocks = (all + 255) / 256;
-  const dim3 grid(static_cast<unsigned>(blocks < (1 << 20) ? blocks : 1 << 20));
-  if (vec) zero_kernel<true><<<grid, 256, 0, s>>>(t, ld, vocab, d);
-  else zero_kernel<false><<<grid, 256, 0, s>>>(t, ld, vocab, d);
-  return cudaGetLastError();
-}
-
 // ----- gradient: the rows sorted by token -----
 
 constexpr int kRankRows = 8192;  // rows that are sorted by counting
-constexpr int kRankCta = 32;     // of a CTA, 8 threads each
-constexpr int kTile = 2048;      // rows of a CTA of the radix sort: 8 warps, 256 each
+constexpr int kRankCta = 16;     // of a CTA, 16 threads each
+constexpr int kTile = 1024;      // rows of a CTA of the radix sort at a time: 8 warps, 128 each
+constexpr int kMaxTiles = 256;   // CTAs: more rows are more at a time
+constexpr int kSteps = kTile / 256;
 constexpr int kBits = 8, kBins = 1 << kBits;
 
 // A row without a token goes behind all others, as one of the token `vocab`.
@@ -178,12 +172,13 @@ __global__ void __launch_bounds__(256) rank_kernel(const int32_t* ids, int rows,
   const int padded = (rows + 3) & ~3;
   for (int i = threadIdx.x; i < padded; i += 256) all[i] = i < rows ? token_of(ids, i, vocab) : 0xFFFFFFFFu;
   __syncthreads();
-  const int r = blockIdx.x * kRankCta + (threadIdx.x >> 3), part = threadIdx.x & 7;
+  const int r = blockIdx.x * kRankCta + (threadIdx.x >> 4), part = threadIdx.x & 15;
   int before = 0;
   uint32_t mine = 0;
   if (r < rows) {
     mine = all[r];
-    for (int i = part * 4; i < padded; i += 32) {
+    #pragma unroll 4
+    for (int i = part * 4; i < padded; i += 64) {
       const uint4 t = *reinterpret_cast<const uint4*>(all + i);
       // an equal token counts where its row is smaller
       before += t.x < mine + (i < r);
@@ -193,7 +188,7 @@ __global__ void __launch_bounds__(256) rank_kernel(const int32_t* ids, int rows,
     }
   }
 #pragma unroll
-  for (int o = 4; o > 0; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
+  for (int o = 8; o > 0; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
   if (r < rows && part == 0) {
     tokens[before] = mine;
     order[before] = r;
@@ -206,123 +201,106 @@ template <bool FIRST>
 __device__ __forceinline__ uint32_t sort_key(const int32_t* ids, const uint32_t* keys, int i, int vocab) {
   return FIRST ? token_of(ids, i, vocab) : keys[i];
 }
+// (A CTA takes `times` tiles, one after another.)
 template <bool FIRST>
-__global__ void __launch_bounds__(256) radix_count_kernel(const int32_t* ids, const uint32_t* keys, int rows, int vocab, int shift,
+__global__ void __launch_bounds__(256) radix_count_kernel(const int32_t* ids, const uint32_t* keys, int rows, int times, int vocab, int shift,
                                                           uint32_t* counts) {
   __shared__ uint32_t hist[kBins];
   hist[threadIdx.x] = 0;
   __syncthreads();
-  const int first = blockIdx.x * kTile;
-  for (int i = first + threadIdx.x; i < min(first + kTile, rows); i += 256)
-    atomicAdd(&hist[(sort_key<FIRST>(ids, keys, i, vocab) >> shift) & (kBins - 1)], 1u);
+  const int64_t first = static_cast<int64_t>(blockIdx.x) * times * kTile, end = min(first + static_cast<int64_t>(times) * kTile, static_cast<int64_t>(rows));
+  for (int64_t i = first + threadIdx.x; i < end; i += 256)
+    atomicAdd(&hist[(sort_key<FIRST>(ids, keys, static_cast<int>(i), vocab) >> shift) & (kBins - 1)], 1u);
   __syncthreads();
-  counts[static_cast<int64_t>(threadIdx.x) * gridDim.x + blockIdx.x] = hist[threadIdx.x];
-}
-__global__ void __launch_bounds__(1024) radix_scan_kernel(uint32_t* counts, int n) {
-  __shared__ uint32_t warp_sum[32];
-  __shared__ uint32_t total;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (threadIdx.x == 0) total = 0;
-  for (int at = 0; at < n; at += 4096) {
-    uint32_t v[4], sum = 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int i = at + static_cast<int>(threadIdx.x) * 4 + j;
-      v[j] = i < n ? counts[i] : 0u;
-      sum += v[j];
-    }
-    uint32_t up = sum;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const uint32_t x = __shfl_up_sync(0xffffffffu, up, o);
-      if (lane >= o) up += x;
-    }
-    if (lane == 31) warp_sum[warp] = up;
-    __syncthreads();
-    if (warp == 0) {
-      const uint32_t mine = warp_sum[lane];
-      uint32_t w = mine;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t x = __shfl_up_sync(0xffffffffu, w, o);
-        if (lane >= o) w += x;
-      }
-      const uint32_t before = total;
-      __syncwarp();
-      warp_sum[lane] = before + w - mine;
-      if (lane == 31) total = before + w;
-    }
-    __syncthreads();
-    uint32_t run = warp_sum[warp] + up - sum;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int i = at + static_cast<int>(threadIdx.x) * 4 + j;
-      if (i < n) counts[i] = run;
-      run += v[j];
-    }
-    __syncthreads();
-  }
+  counts[blockIdx.x * kBins + threadIdx.x] = hist[threadIdx.x];
 }
 template <bool FIRST>
-__global__ void __launch_bounds__(256) radix_scatter_kernel(const int32_t* ids, const uint32_t* keys, const int32_t* rows_in, int rows,
+__global__ void __launch_bounds__(256) radix_scatter_kernel(const int32_t* ids, const uint32_t* keys, const int32_t* rows_in, int rows, int times,
                                                             int vocab, int shift, const uint32_t* counts, uint32_t* keys_out,
                                                             int32_t* rows_out) {
   __shared__ uint32_t seen[8][kBins];  // of a warp: rows with this digit so far; then where its first one goes
+  __shared__ uint32_t warp_sum[8];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int i = threadIdx.x; i < 8 * kBins; i += 256) seen[i / kBins][i % kBins] = 0;
-  __syncthreads();
-  const int first = blockIdx.x * kTile + warp * 256;
-  uint32_t key[8], rank[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const int i = first + j * 32 + lane;
-    const bool in = i < rows;
-    key[j] = in ? sort_key<FIRST>(ids, keys, i, vocab) : 0u;
-    const uint32_t digit = in ? (key[j] >> shift) & (kBins - 1) : kBins;
-    const uint32_t same = __match_any_sync(0xffffffffu, digit);
-    const uint32_t below = __popc(same & ((1u << lane) - 1u));
-    rank[j] = in ? seen[warp][digit] + below : 0u;
-    __syncwarp();
-    if (in && below == 0) seen[warp][digit] += __popc(same);
-    __syncwarp();
+  // where this CTA's rows of digit threadIdx.x go: behind all smaller digits, and the CTAs before it
+  uint32_t before = 0, all = 0;
+#pragma unroll 8
+  for (int i = 0; i < static_cast<int>(gridDim.x); ++i) {
+    const uint32_t n = counts[i * kBins + threadIdx.x];
+    if (i < static_cast<int>(blockIdx.x)) before += n;
+    all += n;
   }
-  __syncthreads();
-  uint32_t run = counts[static_cast<int64_t>(threadIdx.x) * gridDim.x + blockIdx.x];
+  uint32_t up = all;
 #pragma unroll
-  for (int w = 0; w < 8; ++w) {
-    const uint32_t n = seen[w][threadIdx.x];
-    seen[w][threadIdx.x] = run;
-    run += n;
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t x = __shfl_up_sync(0xffffffffu, up, o);
+    if (lane >= o) up += x;
   }
+  if (lane == 31) warp_sum[warp] = up;
   __syncthreads();
+  uint32_t run = up - all + before;
+  for (int w = 0; w < warp; ++w) run += warp_sum[w];
+  for (int k = 0; k < times; ++k) {
+    const int64_t first = (static_cast<int64_t>(blockIdx.x) * times + k) * kTile + warp * (kTile / 8);
+    __syncthreads();
+    for (int i = threadIdx.x; i < 8 * kBins; i += 256) seen[i / kBins][i % kBins] = 0;
+    __syncthreads();
+    uint32_t key[kSteps], rank[kSteps];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const int i = first + j * 32 + lane;
-    if (i >= rows) continue;
-    const uint32_t at = seen[warp][(key[j] >> shift) & (kBins - 1)] + rank[j];
-    keys_out[at] = key[j];
-    rows_out[at] = FIRST ? i : rows_in[i];
+    for (int j = 0; j < kSteps; ++j) {
+      const int64_t i = first + j * 32 + lane;
+      key[j] = i < rows ? sort_key<FIRST>(ids, keys, static_cast<int>(i), vocab) : 0u;
+    }
+#pragma unroll
+    for (int j = 0; j < kSteps; ++j) {
+      const bool in = first + j * 32 + lane < rows;
+      const uint32_t digit = in ? (key[j] >> shift) & (kBins - 1) : kBins;
+      const uint32_t same = __match_any_sync(0xffffffffu, digit);
+      const uint32_t below = __popc(same & ((1u << lane) - 1u));
+      rank[j] = in ? seen[warp][digit] + below : 0u;
+      __syncwarp();
+      if (in && below == 0) seen[warp][digit] += __popc(same);
+      __syncwarp();
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+      const uint32_t n = seen[w][threadIdx.x];
+      seen[w][threadIdx.x] = run;
+      run += n;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kSteps; ++j) {
+      const int64_t i = first + j * 32 + lane;
+      if (i >= rows) continue;
+      const uint32_t at = seen[warp][(key[j] >> shift) & (kBins - 1)] + rank[j];
+      keys_out[at] = key[j];
+      rows_out[at] = FIRST ? static_cast<int32_t>(i) : rows_in[i];
+    }
   }
 }
 
 // ----- gradient: sums of runs -----
 
 constexpr int kSumThreads = 128;
+constexpr int kMaxChunk = 32;   // rows of a chunk
 constexpr int kJoinCols = 128;  // of a CTA that joins: 32 lanes, 4 columns each
 
 struct Plan {
-  int rows, d, chunk, chunks, tiles, pd;  // pd: columns of a row of partial sums
+  int rows, d, chunk, chunks, tiles, times, pd;  // pd: columns of a row of partial sums
   int64_t keys, order, keys2, order2, counts, partial, bytes;  // offsets in the workspace
 };
 Plan make_plan(int rows, int d) {
   Plan q{};
   q.rows = rows;
   q.d = d;
-  // rows of a chunk: as many as leave a CTA per SM and more to the columns, and partial sums a small share of the traffic
-  q.chunk = 16;
-  while (q.chunk < 64 && rows / q.chunk > 512) q.chunk *= 2;
+  // Rows of a chunk: few enough that every SM has some CTAs, and as many as make partial sums a small share of the traffic.
+  const int64_t across = (d + 1023) / 1024;
+  q.chunk = 8;
+  while (q.chunk < kMaxChunk && rows / q.chunk * across > 2048) q.chunk *= 2;
   q.chunks = (rows + q.chunk - 1) / q.chunk;
-  q.tiles = (rows + kTile - 1) / kTile;
+  q.times = (rows + kTile * kMaxTiles - 1) / (kTile * kMaxTiles);
+  q.tiles = static_cast<int>((static_cast<int64_t>(rows) + static_cast<int64_t>(kTile) * q.times - 1) / (static_cast<int64_t>(kTile) * q.times));
   q.pd = (d + 7) & ~7;
   int64_t at = 0;
   auto take = [&](int64_t bytes) {
@@ -349,6 +327,7 @@ struct SumArgs {
   const int32_t* order;
   int rows, vocab, d, chunk, chunks, pd, accumulate;
   float scale;
+  int fill, fill_rows;  // CTAs (in x) that clear a range of so many tokens each
   float* partial;  // [chunks, 2, pd]: of the run that came from the chunk before, of the one that goes on to the next
   void* dtable;
   int64_t ld;
@@ -383,12 +362,64 @@ __device__ __forceinline__ void put(const SumArgs& p, uint32_t token, int c, con
   store<VEC, N>(at, p.d - c, f);
 }
 
+constexpr int kZeros = 16384;     // bytes of zeros in shared memory, which copies to the table start from
+constexpr int kFillRows = 1024;   // tokens of a range, at most
+
+// Clears the rows of the tokens [first, first + n) that do not occur.
+template <typename TO, bool VEC>
+__device__ __forceinline__ void clear_rows(const SumArgs& p, int first, int n, uint4* zeros, uint32_t* here) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int i = threadIdx.x; i < kFillRows / 32; i += kSumThreads) here[i] = 0;
+  if (VEC)
+    for (int i = threadIdx.x; i < kZeros / 16; i += kSumThreads) zeros[i] = make_uint4(0, 0, 0, 0);
+  // the first sorted row with a token of the range: 32 probes at a time between lo (before it) and hi
+  int lo = -1, hi = p.rows;
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 31) / 32, at = lo + (lane + 1) * step;
+    const bool before = at < hi && p.tokens[at] < static_cast<uint32_t>(first);
+    const int more = __popc(__ballot_sync(0xffffffffu, before));
+    const int new_lo = lo + more * step;
+    hi = min(hi, new_lo + step);
+    lo = new_lo;
+  }
+  if (VEC) fence_proxy_async_smem();
+  __syncthreads();
+  for (int i = lo + 1 + static_cast<int>(threadIdx.x); i < p.rows; i += kSumThreads) {
+    const uint32_t t = p.tokens[i] - first;
+    if (t >= static_cast<uint32_t>(n)) break;
+    if (i == lo + 1 || p.tokens[i - 1] - first != t) atomicOr(&here[t >> 5], 1u << (t & 31));
+  }
+  __syncthreads();
+  TO* table = static_cast<TO*>(p.dtable);
+  for (int i = warp; i < n; i += kSumThreads / 32) {
+    if (here[i >> 5] >> (i & 31) & 1) continue;
+    TO* at = table + static_cast<int64_t>(first + i) * p.ld;
+    if constexpr (VEC) {
+      const int64_t bytes = static_cast<int64_t>(p.d) * sizeof(TO);
+      for (int64_t o = static_cast<int64_t>(lane) * kZeros; o < bytes; o += 32 * kZeros)
+        bulk_store(reinterpret_cast<char*>(at) + o, zeros, static_cast<uint32_t>(min(bytes - o, static_cast<int64_t>(kZeros))));
+    } else {
+      for (int c = lane; c < p.d; c += 32) at[c] = from_f32<TO>(0.f);
+    }
+  }
+  if (VEC) bulk_store_wait();  // the zeros stay until they are read
+}
+
 template <typename TG, typename TO, bool VEC>
 __global__ void __launch_bounds__(kSumThreads) embedding_sums_kernel(const SumArgs p) {
+  extern __shared__ __align__(16) uint4 zeros[];
+  __shared__ uint32_t here[kFillRows / 32];
+  if (static_cast<int>(blockIdx.x) < p.fill) {
+    const int64_t first = (static_cast<int64_t>(blockIdx.x) * gridDim.y + blockIdx.y) * p.fill_rows;
+    if (first < p.vocab)
+      clear_rows<TO, VEC>(p, static_cast<int>(first), static_cast<int>(min(static_cast<int64_t>(p.fill_rows), p.vocab - first)), zeros, here);
+    return;
+  }
+  const int chunk = blockIdx.x - p.fill;
   constexpr int N = VEC ? Vec<TG>::kN : 4, kAhead = 8;
-  __shared__ uint32_t tok[64 + 2];
-  __shared__ int32_t row[64];
-  const int first = blockIdx.x * p.chunk, n = min(p.chunk, p.rows - first);
+  __shared__ uint32_t tok[kMaxChunk + 2];
+  __shared__ int32_t row[kMaxChunk];
+  const int first = chunk * p.chunk, n = min(p.chunk, p.rows - first);
   // the tokens of the chunk and of its neighbours (none: one that no row has)
   for (int i = threadIdx.x; i < n + 2; i += kSumThreads) {
     const int at = first + i - 1;
@@ -422,7 +453,7 @@ __global__ void __launch_bounds__(kSumThreads) embedding_sums_kernel(const SumAr
       if (ends && !from_before) {
         put<TO, VEC, N>(p, t, c, sum);
       } else {
-        float* at = p.partial + (2 * static_cast<int64_t>(blockIdx.x) + (from_before ? 0 : 1)) * p.pd + c;
+        float* at = p.partial + (2 * static_cast<int64_t>(chunk) + (from_before ? 0 : 1)) * p.pd + c;
         if constexpr (VEC) {
 #pragma unroll
           for (int j = 0; j < N; j += 4) *reinterpret_cast<float4*>(at + j) = make_float4(sum[j], sum[j + 1], sum[j + 2], sum[j + 3]);
@@ -513,15 +544,18 @@ __global__ void __launch_bounds__(256) embedding_join_kernel(const SumArgs p) {
 }
 
 template <typename TG, typename TO>
-cudaError_t sums(const SumArgs& a, cudaStream_t s) {
-  const bool vec = vectors<TG>(a.grad, a.ld_grad, Vec<TG>::kN, a.d) && vectors<TO>(a.dtable, a.ld, Vec<TG>::kN, a.d);
+cudaError_t sums(SumArgs a, cudaStream_t s) {
+  const bool vec = vectors<TG>(a.grad, a.ld_grad, Vec<TG>::kN, a.d) && vectors<TO>(a.dtable, a.ld, Vec<TG>::kN, a.d) && vectors<TO>(a.dtable, a.ld, Vec<TO>::kN, a.d);
   const int n = vec ? Vec<TG>::kN : 4;
-  const dim3 grid(a.chunks, (a.d + kSumThreads * n - 1) / (kSumThreads * n));
-  if (vec) embedding_sums_kernel<TG, TO, true><<<grid, kSumThreads, 0, s>>>(a);
-  else embedding_sums_kernel<TG, TO, false><<<grid, kSumThreads, 0, s>>>(a);
+  const int across = (a.d + kSumThreads * n - 1) / (kSumThreads * n);
+  a.fill = (a.fill + across - 1) / across;
+  const dim3 grid(a.fill + a.chunks, across);
+  const size_t smem = vec && a.fill ? kZeros : 0;
+  if (vec) embedding_sums_kernel<TG, TO, true><<<grid, kSumThreads, smem, s>>>(a);
+  else embedding_sums_kernel<TG, TO, false><<<grid, kSumThreads, smem, s>>>(a);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess || a.chunks < 2) return e;
-  const dim3 join((a.d + kJoinCols - 1) / kJoinCols, a.chunks < 16 ? a.chunks : 16);
+  const dim3 join((a.d + kJoinCols - 1) / kJoinCols, a.chunks < 256 ? a.chunks : 256);
   if (vectors<TO>(a.dtable, a.ld, 4, a.d)) embedding_join_kernel<TO, true><<<join, 256, 0, s>>>(a);
   else embedding_join_kernel<TO, false><<<join, 256, 0, s>>>(a);
   return cudaGetLastError();
@@ -547,11 +581,10 @@ cudaError_t sort_rows(const EmbeddingGradParams& p, const Plan& q, char* ws, con
   int32_t* r1 = reinterpret_cast<int32_t*>(ws + q.order2);
   uint32_t* counts = reinterpret_cast<uint32_t*>(ws + q.counts);
   for (int shift = 0; shift < 32 && (shift == 0 || p.vocab >> shift); shift += kBits) {
-    if (shift == 0) radix_count_kernel<true><<<q.tiles, 256, 0, s>>>(p.ids, k0, p.rows, p.vocab, shift, counts);
-    else radix_count_kernel<false><<<q.tiles, 256, 0, s>>>(p.ids, k0, p.rows, p.vocab, shift, counts);
-    radix_scan_kernel<<<1, 1024, 0, s>>>(counts, kBins * q.tiles);
-    if (shift == 0) radix_scatter_kernel<true><<<q.tiles, 256, 0, s>>>(p.ids, k0, r0, p.rows, p.vocab, shift, counts, k1, r1);
-    else radix_scatter_kernel<false><<<q.tiles, 256, 0, s>>>(p.ids, k0, r0, p.rows, p.vocab, shift, counts, k1, r1);
+    if (shift == 0) radix_count_kernel<true><<<q.tiles, 256, 0, s>>>(p.ids, k0, p.rows, q.times, p.vocab, shift, counts);
+    else radix_count_kernel<false><<<q.tiles, 256, 0, s>>>(p.ids, k0, p.rows, q.times, p.vocab, shift, counts);
+    if (shift == 0) radix_scatter_kernel<true><<<q.tiles, 256, 0, s>>>(p.ids, k0, r0, p.rows, q.times, p.vocab, shift, counts, k1, r1);
+    else radix_scatter_kernel<false><<<q.tiles, 256, 0, s>>>(p.ids, k0, r0, p.rows, q.times, p.vocab, shift, counts, k1, r1);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     uint32_t* k = k0;
@@ -577,20 +610,21 @@ cudaError_t embedding_launch(const EmbeddingParams& p, cudaStream_t s) {
 }
 
 cudaError_t embedding_grad_launch(const EmbeddingGradParams& p, cudaStream_t s) {
-  if (!p.accumulate) {
-    const cudaError_t e = p.dtable_dtype == SGD_F32 ? zero<float>(p.dtable, p.ld, p.vocab, p.d, s)
-                                                    : zero<f16>(p.dtable, p.ld, p.vocab, p.d, s);  // (0 is 0 in bf16 too)
-    if (e != cudaSuccess) return e;
-  }
-  if (p.rows == 0) return cudaSuccess;
+  if (p.rows == 0 && p.accumulate) return cudaSuccess;
   const Plan q = make_plan(p.rows, p.d);
   char* ws = static_cast<char*>(p.workspace);
   const uint32_t* tokens = nullptr;
   const int32_t* order = nullptr;
-  const cudaError_t e = sort_rows(p, q, ws, &tokens, &order, s);
-  if (e != cudaSuccess) return e;
+  if (p.rows > 0) {
+    const cudaError_t e = sort_rows(p, q, ws, &tokens, &order, s);
+    if (e != cudaSuccess) return e;
+  }
+  // ranges of the table: several per SM
+  int fill_rows = (p.vocab + 8 * num_sms() - 1) / (8 * num_sms());
+  fill_rows = fill_rows < 4 ? 4 : (fill_rows > kFillRows ? kFillRows : fill_rows);
+  const int fill = p.accumulate ? 0 : (p.vocab + fill_rows - 1) / fill_rows;
   const SumArgs a{p.grad, p.ld_grad, tokens, order, p.rows, p.vocab, p.d, q.chunk, q.chunks, q.pd, p.accumulate, p.scale,
-                  reinterpret_cast<float*>(ws + q.partial), p.dtable, p.ld};
+                  fill, fill_rows, reinterpret_cast<float*>(ws + q.partial), p.dtable, p.ld};
   if (p.grad_dtype == SGD_F16) return sums_to<f16>(a, p.dtable_dtype, s);
   if (p.grad_dtype == SGD_BF16) return sums_to<bf16>(a, p.dtable_dtype, s);
   return sums_to<float>(a, p.dtable_dtype, s);

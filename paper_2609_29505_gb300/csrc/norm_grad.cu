@@ -14,17 +14,20 @@
 namespace sgd {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kCtas = 304;         // two for each SM of a GB300
-constexpr int kRowsPerPart = 8;    // of a sample that several groups share, at least
+constexpr int kVec = 2;            // of a thread: vectors of 4 columns
+constexpr int kSms = 152;          // of a GB300
+constexpr int kRowsPerPart = 3;    // of a sample that several groups share, at least
 constexpr int kColsPerCta = 32;    // of the second kernel: 8 threads of 4 columns, 32 shares of the sums
 
-// Threads of a row: 16 columns each, at most.
+// Threads of a row: 8 columns each, at most.
 int group_of(int d) {
   int g = 32;
-  while (g * 16 < d) g *= 2;
+  while (g * 4 * kVec < d) g *= 2;
   return g;
 }
+// CTAs of 256 threads, or of a row's 512; per SM
+constexpr int threads_of(int group) { return group > 256 ? group : 256; }
+constexpr int ctas_per_sm(int group) { return group > 256 ? 1 : 3; }
 
 struct Plan {
   int group, groups;  // threads of a row; rows at a time in a CTA
@@ -36,19 +39,20 @@ struct Plan {
 Plan make_plan(int rows, int d, int per) {
   Plan q{};
   q.group = group_of(d);
-  q.groups = kThreads / q.group;
+  q.groups = threads_of(q.group) / q.group;
+  const int most_ctas = ctas_per_sm(q.group) * kSms;
   if (per <= 0) {
     q.per = rows;
     q.samples = 1;
     q.ctas = (rows + q.groups - 1) / q.groups;
-    if (q.ctas > kCtas) q.ctas = kCtas;
+    if (q.ctas > most_ctas) q.ctas = most_ctas;
     q.parts = q.units = q.ctas;
     return q;
   }
   q.per = per;
   q.samples = (rows + per - 1) / per;
   const int longest = per < rows ? per : rows;
-  q.parts = (kCtas * q.groups + q.samples - 1) / q.samples;
+  q.parts = (most_ctas * q.groups + q.samples - 1) / q.samples;
   const int most = (longest + kRowsPerPart - 1) / kRowsPerPart;
   if (q.parts > most) q.parts = most;
   q.part = (longest + q.parts - 1) / q.parts;
@@ -56,7 +60,7 @@ Plan make_plan(int rows, int d, int per) {
   const int64_t units = static_cast<int64_t>(q.samples) * q.parts;
   q.units = static_cast<int>(units);
   q.ctas = static_cast<int>((units + q.groups - 1) / q.groups);
-  if (q.ctas > kCtas) q.ctas = kCtas;
+  if (q.ctas > most_ctas) q.ctas = most_ctas;
   return q;
 }
 
@@ -116,8 +120,9 @@ __device__ __forceinline__ float3 group_sum(float3 v, float (*red)[3], int warp_
 }
 
 template <typename T, int G, bool MOD, bool PARAMS>
-__global__ void __launch_bounds__(kThreads, 2) norm_grad_kernel(const Args a) {
-  constexpr int NV = 4, kGroups = kThreads / G, kGroupWarps = G / 32;
+__global__ void __launch_bounds__(threads_of(G), ctas_per_sm(G)) norm_grad_kernel(const Args a) {
+  constexpr int NV = kVec, kThreads = threads_of(G), kGroups = kThreads / G, kGroupWarps = G / 32;
+  using Raw = typename Four<T>::Raw;
   __shared__ float red[2][kThreads / 32][3];
   const NormGradParams& p = a.p;
   const int tid = threadIdx.x % G, grp = threadIdx.x / G, nv = p.d >> 2;
@@ -141,24 +146,37 @@ __global__ void __launch_bounds__(kThreads, 2) norm_grad_kernel(const Args a) {
 #pragma unroll
   for (int j = 0; j < NV; ++j) A[j] = B[j] = sc[j] = make_float4(0.f, 0.f, 0.f, 0.f);
 
-  auto row_of = [&](int row) {
-    const int64_t at = static_cast<int64_t>(row) * p.d;
-    const float4* hr = reinterpret_cast<const float4*>(p.h + at);
-    const typename Four<T>::Raw* dr = reinterpret_cast<const typename Four<T>::Raw*>(static_cast<const T*>(p.dout) + at);
-    const float4* rr = reinterpret_cast<const float4*>(p.residual ? p.residual + at : nullptr);
-    float4 x[NV], dx[NV], res[NV];
-    typename Four<T>::Raw raw[NV];
+  // a row's h, dout and residual: the next one's are on their way while a row is worked on
+  float4 h_next[NV], res_next[NV];
+  Raw raw_next[NV];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    h_next[j] = res_next[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+    raw_next[j] = Raw{};
+  }
+  auto load = [&](int64_t row) {
+    const int64_t at = row * p.d;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int i = tid + j * G;
-      x[j] = res[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-      raw[j] = typename Four<T>::Raw{};
       if (i < nv) {
-        x[j] = hr[i];
-        raw[j] = dr[i];
-        if (rr) res[j] = rr[i];
+        h_next[j] = reinterpret_cast<const float4*>(p.h + at)[i];
+        raw_next[j] = reinterpret_cast<const Raw*>(static_cast<const T*>(p.dout) + at)[i];
+        if (p.residual) res_next[j] = reinterpret_cast<const float4*>(p.residual + at)[i];
       }
     }
+  };
+  // row `row`, which has been loaded; `next` is loaded (-1: none)
+  auto row_of = [&](int64_t row, int64_t next) {
+    float4 x[NV], dx[NV], res[NV];
+    Raw raw[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      x[j] = h_next[j];
+      raw[j] = raw_next[j];
+      res[j] = res_next[j];
+    }
+    if (next >= 0) load(next);
     float mean = 0.f;
     if (centred) {
       float s = 0.f;
@@ -211,7 +229,7 @@ __global__ void __launch_bounds__(kThreads, 2) norm_grad_kernel(const Args a) {
         v.y = fmaf(rstd, dx[j].y - m1 - x[j].y * m2, res[j].y);
         v.z = fmaf(rstd, dx[j].z - m1 - x[j].z * m2, res[j].z);
         v.w = fmaf(rstd, dx[j].w - m1 - x[j].w * m2, res[j].w);
-        reinterpret_cast<float4*>(p.dh + at)[i] = v;
+        reinterpret_cast<float4*>(p.dh + row * p.d)[i] = v;
       }
     }
   };
@@ -230,7 +248,8 @@ __global__ void __launch_bounds__(kThreads, 2) norm_grad_kernel(const Args a) {
         if (i < p.d) sc[j] = make_float4(scale[i], scale[i + 1], scale[i + 2], scale[i + 3]);
         if (PARAMS) A[j] = B[j] = make_float4(0.f, 0.f, 0.f, 0.f);
       }
-      for (int64_t r = from; r < to; ++r) row_of(static_cast<int>(r));
+      load(from);
+      for (int64_t r = from; r < to; ++r) row_of(r, r + 1 < to ? r + 1 : -1);
       if (PARAMS) {
         float4* out = reinterpret_cast<float4*>(a.sums + 2 * static_cast<int64_t>(u) * p.d);
 #pragma unroll
@@ -245,10 +264,13 @@ __global__ void __launch_bounds__(kThreads, 2) norm_grad_kernel(const Args a) {
     }
     return;
   }
-  for (int64_t r = blockIdx.x * kGroups + grp; r < p.rows; r += static_cast<int64_t>(gridDim.x) * kGroups) row_of(static_cast<int>(r));
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kGroups;
+  int64_t r = blockIdx.x * kGroups + grp;
+  if (r < p.rows) load(r);
+  for (; r < p.rows; r += step) row_of(r, r + step < p.rows ? r + step : -1);
   if (!PARAMS) return;
   // the groups' sums, in their order
-  __shared__ float4 joined[kGroups > 1 ? 2 : 1][kGroups > 1 ? 4 * G : 1];
+  __shared__ float4 joined[kGroups > 1 ? 2 : 1][kGroups > 1 ? NV * G : 1];
   if constexpr (kGroups > 1) {
     for (int k = 0; k < kGroups; ++k) {
       if (grp == k) {
@@ -336,7 +358,7 @@ __global__ void __launch_bounds__(256) norm_grad_sums_kernel(const Args a) {
 
 template <typename T, int G>
 void rows_of(const Args& a, bool params, cudaStream_t s) {
-  const dim3 grid(a.q.ctas), block(kThreads);
+  const dim3 grid(a.q.ctas), block(threads_of(G));
   if (a.p.scale) {
     if (params) norm_grad_kernel<T, G, true, true><<<grid, block, 0, s>>>(a);
     else norm_grad_kernel<T, G, true, false><<<grid, block, 0, s>>>(a);
@@ -350,7 +372,8 @@ void rows_of_type(const Args& a, bool params, cudaStream_t s) {
   if (a.q.group == 32) rows_of<T, 32>(a, params, s);
   else if (a.q.group == 64) rows_of<T, 64>(a, params, s);
   else if (a.q.group == 128) rows_of<T, 128>(a, params, s);
-  else rows_of<T, 256>(a, params, s);
+  else if (a.q.group == 256) rows_of<T, 256>(a, params, s);
+  else rows_of<T, 512>(a, params, s);
 }
 
 }  // namespace
