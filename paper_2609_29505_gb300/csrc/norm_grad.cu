@@ -8,29 +8,41 @@
 // db = sum over samples of (1 + scale) A, dg = the same of B.  A group of threads takes a row at a time, keeps its columns'
 // A and B in registers over all of its rows, and leaves them in the workspace; a second kernel adds them up in a fixed
 // order.  The statistics are taken anew from h, which has to be read for xhat anyway.
+#include <atomic>
+
 #include "common.cuh"
 #include "kernels.h"
 
 namespace sgd {
 namespace {
 
-constexpr int kVec = 2;            // of a thread: vectors of 4 columns
-constexpr int kSms = 152;          // of a GB300
-constexpr int kRowsPerPart = 3;    // of a sample that several groups share, at least
+constexpr int kThreads = 256;
+constexpr int kSms = 152;        // of a GB300
+constexpr int kRowsPerPart = 3;  // of a sample that several groups share, at least
 constexpr int kColsPerCta = 32;    // of the second kernel: 8 threads of 4 columns, 32 shares of the sums
 
-// Threads of a row: 8 columns each, at most.
-int group_of(int d) {
+// Threads of a row: vectors of 4 columns each, two at most, and four in rows of more than 2048 (`wide`): 4096 columns with a residual are
+// 40 us per 4096 rows with 256 threads a row and two CTAs per SM, 57 with 512 and one, whose barriers nothing hides.
+struct Group {
+  int threads;
+  bool wide;
+};
+Group group_of(int d) {
+  if (d > 2048) return {256, true};
   int g = 32;
-  while (g * 4 * kVec < d) g *= 2;
-  return g;
+  while (g * 8 < d) g *= 2;
+  return {g, false};
 }
-// CTAs of 256 threads, or of a row's 512; per SM
-constexpr int threads_of(int group) { return group > 256 ? group : 256; }
-constexpr int ctas_per_sm(int group) { return group > 256 ? 1 : 3; }
+constexpr int vectors_of(bool wide) { return wide ? 4 : 2; }
+constexpr int ctas_per_sm(bool wide) { return wide ? 2 : 3; }
+// Narrow rows: how many a group has in hand or on their way, and bytes of shared memory: theirs, and two rows of dh.
+constexpr int kStages = 2;
+constexpr int smem_of(bool wide, int elem) { return wide ? 0 : kThreads * 2 * (kStages * (32 + 4 * elem) + 32); }
+static_assert(3 * (smem_of(false, 4) + 9 * 1024) <= 226 * 1024, "shared memory");
 
 struct Plan {
   int group, groups;  // threads of a row; rows at a time in a CTA
+  bool wide;
   int per, samples;   // rows of a sample
   int parts, part;    // shares of a sample, rows of one
   int ctas, units;    // units: sums in the workspace
@@ -38,9 +50,11 @@ struct Plan {
 // per 0: no modulation (one sample; a CTA's groups join their sums)
 Plan make_plan(int rows, int d, int per) {
   Plan q{};
-  q.group = group_of(d);
-  q.groups = threads_of(q.group) / q.group;
-  const int most_ctas = ctas_per_sm(q.group) * kSms;
+  const Group g = group_of(d);
+  q.group = g.threads;
+  q.wide = g.wide;
+  q.groups = kThreads / q.group;
+  const int most_ctas = ctas_per_sm(q.wide) * kSms;
   if (per <= 0) {
     q.per = rows;
     q.samples = 1;
@@ -86,6 +100,11 @@ __device__ __forceinline__ float4 numbers(uint2 u, const f16*) {
   return make_float4(a.x, a.y, c.x, c.y);
 }
 
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void* dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(smem_u32(dst)), "l"(__cvta_generic_to_global(src)), "n"(BYTES) : "memory");
+}
+
 struct Args {
   NormGradParams p;
   Plan q;
@@ -119,9 +138,9 @@ __device__ __forceinline__ float3 group_sum(float3 v, float (*red)[3], int warp_
   return v;
 }
 
-template <typename T, int G, bool MOD, bool PARAMS>
-__global__ void __launch_bounds__(threads_of(G), ctas_per_sm(G)) norm_grad_kernel(const Args a) {
-  constexpr int NV = kVec, kThreads = threads_of(G), kGroups = kThreads / G, kGroupWarps = G / 32;
+template <typename T, int G, bool WIDE, bool MOD, bool PARAMS>
+__global__ void __launch_bounds__(kThreads, ctas_per_sm(WIDE)) norm_grad_kernel(const Args a) {
+  constexpr int NV = vectors_of(WIDE), kGroups = kThreads / G, kGroupWarps = G / 32;
   using Raw = typename Four<T>::Raw;
   __shared__ float red[2][kThreads / 32][3];
   const NormGradParams& p = a.p;
@@ -146,43 +165,84 @@ __global__ void __launch_bounds__(threads_of(G), ctas_per_sm(G)) norm_grad_kerne
 #pragma unroll
   for (int j = 0; j < NV; ++j) A[j] = B[j] = sc[j] = make_float4(0.f, 0.f, 0.f, 0.f);
 
-  // a row's h, dout and residual: the next one's are on their way while a row is worked on
-  float4 h_next[NV], res_next[NV];
-  Raw raw_next[NV];
+  // Narrow rows: h, dout and residual come by asynchronous copies into places that their thread alone reads; dh leaves from one of two rows in
+  // shared memory, by a bulk copy that the group's first thread starts behind the next row's first barrier.
+  extern __shared__ __align__(128) float4 dynamic[];
+  constexpr int kPlaces = NV * kThreads;
+  float4* h_in = dynamic + threadIdx.x;                 // [kStages][NV][kThreads]
+  float4* res_in = h_in + kStages * kPlaces;            // the same
+  float4* out = dynamic + 2 * kStages * kPlaces + grp * 2 * NV * G;  // [2][NV * G] of the group
+  Raw* raw_in = reinterpret_cast<Raw*>(dynamic + 2 * kStages * kPlaces + 2 * kPlaces) + threadIdx.x;
+  auto load = [&](int64_t row, int stage) {  // (row -1: none)
+    if (row >= 0) {
+      const int64_t at = row * p.d;
 #pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    h_next[j] = res_next[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-    raw_next[j] = Raw{};
-  }
-  auto load = [&](int64_t row) {
-    const int64_t at = row * p.d;
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int i = tid + j * G;
-      if (i < nv) {
-        h_next[j] = reinterpret_cast<const float4*>(p.h + at)[i];
-        raw_next[j] = reinterpret_cast<const Raw*>(static_cast<const T*>(p.dout) + at)[i];
-        if (p.residual) res_next[j] = reinterpret_cast<const float4*>(p.residual + at)[i];
+      for (int j = 0; j < NV; ++j) {
+        const int i = tid + j * G, to = stage * kPlaces + j * kThreads;
+        if (i < nv) {
+          copy_async<16>(h_in + to, reinterpret_cast<const float4*>(p.h + at) + i);
+          copy_async<sizeof(Raw)>(raw_in + to, reinterpret_cast<const Raw*>(static_cast<const T*>(p.dout) + at) + i);
+          if (p.residual) copy_async<16>(res_in + to, reinterpret_cast<const float4*>(p.residual + at) + i);
+        }
       }
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  // row `row`, which has been loaded; `next` is loaded (-1: none)
-  auto row_of = [&](int64_t row, int64_t next) {
+  // what lies behind the row's end, or has no residual, is 0
+#pragma unroll
+  for (int k = 0; k < (WIDE ? 0 : kStages * NV); ++k) {
+    const bool behind = tid + k % NV * G >= nv;
+    if (behind) {
+      h_in[k * kThreads] = make_float4(0.f, 0.f, 0.f, 0.f);
+      raw_in[k * kThreads] = Raw{};
+    }
+    if (behind || !p.residual) res_in[k * kThreads] = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  int64_t stored = -1;  // row of dh that waits to be copied
+  int flip_out = 0;
+  auto store = [&] {  // behind a barrier of the group
+    if (stored >= 0 && tid == 0) {
+      bulk_store(p.dh + stored * p.d, out + (flip_out ^ 1) * NV * G, static_cast<uint32_t>(p.d) * 4);
+      asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
+    stored = -1;
+  };
+  // the first barrier of a row: the dh before the last has been read from shared memory, so that its place is free
+  auto first_total = [&](float3 v) {
+    if (WIDE) return total(v);
+    if (tid == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+    v = total(v);
+    if (G == 32) __syncwarp();
+    store();
+    return v;
+  };
+  auto row_of = [&](int64_t row, int stage) {
     float4 x[NV], dx[NV], res[NV];
     Raw raw[NV];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      x[j] = h_next[j];
-      raw[j] = raw_next[j];
-      res[j] = res_next[j];
+      if constexpr (WIDE) {
+        const int i = tid + j * G;
+        x[j] = res[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+        raw[j] = Raw{};
+        if (i < nv) {
+          x[j] = reinterpret_cast<const float4*>(p.h + row * p.d)[i];
+          raw[j] = reinterpret_cast<const Raw*>(static_cast<const T*>(p.dout) + row * p.d)[i];
+          if (p.residual) res[j] = reinterpret_cast<const float4*>(p.residual + row * p.d)[i];
+        }
+      } else {
+        const int at = stage * kPlaces + j * kThreads;
+        x[j] = h_in[at];
+        raw[j] = raw_in[at];
+        res[j] = res_in[at];
+      }
     }
-    if (next >= 0) load(next);
     float mean = 0.f;
     if (centred) {
       float s = 0.f;
 #pragma unroll
       for (int j = 0; j < NV; ++j) s += (x[j].x + x[j].y) + (x[j].z + x[j].w);
-      mean = total(make_float3(s, 0.f, 0.f)).x * inv_d;
+      mean = first_total(make_float3(s, 0.f, 0.f)).x * inv_d;
     }
     float3 s = make_float3(0.f, 0.f, 0.f);  // of x^2, dx, dx x
 #pragma unroll
@@ -205,7 +265,7 @@ __global__ void __launch_bounds__(threads_of(G), ctas_per_sm(G)) norm_grad_kerne
       s.y += (dx[j].x + dx[j].y) + (dx[j].z + dx[j].w);
       s.z += (dx[j].x * x[j].x + dx[j].y * x[j].y) + (dx[j].z * x[j].z + dx[j].w * x[j].w);
     }
-    s = total(s);
+    s = centred ? total(s) : first_total(s);
     const float rstd = rsqrtf(s.x * inv_d + p.eps);
     const float m1 = centred ? s.y * inv_d : 0.f, m2 = s.z * inv_d * rstd;
 #pragma unroll
@@ -229,10 +289,42 @@ __global__ void __launch_bounds__(threads_of(G), ctas_per_sm(G)) norm_grad_kerne
         v.y = fmaf(rstd, dx[j].y - m1 - x[j].y * m2, res[j].y);
         v.z = fmaf(rstd, dx[j].z - m1 - x[j].z * m2, res[j].z);
         v.w = fmaf(rstd, dx[j].w - m1 - x[j].w * m2, res[j].w);
-        reinterpret_cast<float4*>(p.dh + row * p.d)[i] = v;
+        if (WIDE) reinterpret_cast<float4*>(p.dh + row * p.d)[i] = v;
+        else out[flip_out * NV * G + i] = v;
       }
     }
+    if (!WIDE && p.dh) {
+      fence_proxy_async_smem();
+      stored = row;
+      flip_out ^= 1;
+    }
   };
+  // rows from, from + step, ... below to
+  auto rows = [&](int64_t from, int64_t to, int64_t step) {
+    if constexpr (WIDE) {
+      for (int64_t r = from; r < to; r += step) row_of(r, 0);
+      return;
+    }
+#pragma unroll
+    for (int k = 0; k < kStages - 1; ++k) load(from + k * step < to ? from + k * step : -1, k);
+    int stage = 0;
+    for (int64_t r = from; r < to; r += step) {
+      const int64_t ahead = r + (kStages - 1) * step;
+      load(ahead < to ? ahead : -1, stage == 0 ? kStages - 1 : stage - 1);
+      asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+      row_of(r, stage);
+      if (++stage == kStages) stage = 0;
+    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+  };
+  auto finish = [&] {  // the last row's dh
+    if (WIDE) return;
+    if (G == 32) __syncwarp();
+    else asm volatile("barrier.cta.sync.aligned %0, %1;" ::"r"(1 + grp), "n"(G) : "memory");
+    store();
+    if (tid == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+  };
+
 
   if (MOD) {
     // a group by itself: a share of a sample's rows at a time
@@ -248,26 +340,24 @@ __global__ void __launch_bounds__(threads_of(G), ctas_per_sm(G)) norm_grad_kerne
         if (i < p.d) sc[j] = make_float4(scale[i], scale[i + 1], scale[i + 2], scale[i + 3]);
         if (PARAMS) A[j] = B[j] = make_float4(0.f, 0.f, 0.f, 0.f);
       }
-      load(from);
-      for (int64_t r = from; r < to; ++r) row_of(r, r + 1 < to ? r + 1 : -1);
+      rows(from, to, 1);
       if (PARAMS) {
-        float4* out = reinterpret_cast<float4*>(a.sums + 2 * static_cast<int64_t>(u) * p.d);
+        float4* sums = reinterpret_cast<float4*>(a.sums + 2 * static_cast<int64_t>(u) * p.d);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
           const int i = tid + j * G;
           if (i < nv) {
-            out[i] = A[j];
-            out[nv + i] = B[j];
+            sums[i] = A[j];
+            sums[nv + i] = B[j];
           }
         }
       }
     }
+    finish();
     return;
   }
-  const int64_t step = static_cast<int64_t>(gridDim.x) * kGroups;
-  int64_t r = blockIdx.x * kGroups + grp;
-  if (r < p.rows) load(r);
-  for (; r < p.rows; r += step) row_of(r, r + step < p.rows ? r + step : -1);
+  rows(static_cast<int64_t>(blockIdx.x) * kGroups + grp, p.rows, static_cast<int64_t>(gridDim.x) * kGroups);
+  finish();
   if (!PARAMS) return;
   // the groups' sums, in their order
   __shared__ float4 joined[kGroups > 1 ? 2 : 1][kGroups > 1 ? NV * G : 1];
@@ -290,13 +380,13 @@ __global__ void __launch_bounds__(threads_of(G), ctas_per_sm(G)) norm_grad_kerne
     }
   }
   if (kGroups > 1 && grp != kGroups - 1) return;
-  float4* out = reinterpret_cast<float4*>(a.sums + 2 * static_cast<int64_t>(blockIdx.x) * p.d);
+  float4* sums = reinterpret_cast<float4*>(a.sums + 2 * static_cast<int64_t>(blockIdx.x) * p.d);
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     const int i = tid + j * G;
     if (i < nv) {
-      out[i] = A[j];
-      out[nv + i] = B[j];
+      sums[i] = A[j];
+      sums[nv + i] = B[j];
     }
   }
 }
@@ -315,7 +405,7 @@ __global__ void __launch_bounds__(256) norm_grad_sums_kernel(const Args a) {
     const int from = all ? 0 : job * a.q.parts, to = all ? a.q.units : from + a.q.parts;
     float4 A = make_float4(0.f, 0.f, 0.f, 0.f), B = A;
     if (i < nv) {
-#pragma unroll 4
+#pragma unroll 8
       for (int u = from + share; u < to; u += 32) {
         const float4* at = reinterpret_cast<const float4*>(a.sums + 2 * static_cast<int64_t>(u) * p.d);
         float4 x = at[i], y = at[nv + i];
@@ -356,24 +446,34 @@ __global__ void __launch_bounds__(256) norm_grad_sums_kernel(const Args a) {
   }
 }
 
-template <typename T, int G>
-void rows_of(const Args& a, bool params, cudaStream_t s) {
-  const dim3 grid(a.q.ctas), block(threads_of(G));
-  if (a.p.scale) {
-    if (params) norm_grad_kernel<T, G, true, true><<<grid, block, 0, s>>>(a);
-    else norm_grad_kernel<T, G, true, false><<<grid, block, 0, s>>>(a);
-  } else {
-    if (params) norm_grad_kernel<T, G, false, true><<<grid, block, 0, s>>>(a);
-    else norm_grad_kernel<T, G, false, false><<<grid, block, 0, s>>>(a);
+template <typename T, int G, bool WIDE, bool MOD, bool PARAMS>
+cudaError_t launch_rows(const Args& a, cudaStream_t s) {
+  constexpr int kSmem = smem_of(WIDE, sizeof(T));
+  // once per kernel and device
+  static std::atomic<uint64_t> ready{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (kSmem > 40 * 1024 && (dev > 63 || !(ready.load() >> dev & 1))) {
+    e = cudaFuncSetAttribute(norm_grad_kernel<T, G, WIDE, MOD, PARAMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    if (e != cudaSuccess) return e;
+    if (dev <= 63) ready.fetch_or(1ull << dev);
   }
+  norm_grad_kernel<T, G, WIDE, MOD, PARAMS><<<a.q.ctas, kThreads, kSmem, s>>>(a);
+  return cudaGetLastError();
+}
+template <typename T, int G, bool WIDE>
+cudaError_t rows_of(const Args& a, bool params, cudaStream_t s) {
+  if (a.p.scale) return params ? launch_rows<T, G, WIDE, true, true>(a, s) : launch_rows<T, G, WIDE, true, false>(a, s);
+  return params ? launch_rows<T, G, WIDE, false, true>(a, s) : launch_rows<T, G, WIDE, false, false>(a, s);
 }
 template <typename T>
-void rows_of_type(const Args& a, bool params, cudaStream_t s) {
-  if (a.q.group == 32) rows_of<T, 32>(a, params, s);
-  else if (a.q.group == 64) rows_of<T, 64>(a, params, s);
-  else if (a.q.group == 128) rows_of<T, 128>(a, params, s);
-  else if (a.q.group == 256) rows_of<T, 256>(a, params, s);
-  else rows_of<T, 512>(a, params, s);
+cudaError_t rows_of_type(const Args& a, bool params, cudaStream_t s) {
+  if (a.q.wide) return rows_of<T, 256, true>(a, params, s);
+  if (a.q.group == 32) return rows_of<T, 32, false>(a, params, s);
+  if (a.q.group == 64) return rows_of<T, 64, false>(a, params, s);
+  if (a.q.group == 128) return rows_of<T, 128, false>(a, params, s);
+  return rows_of<T, 256, false>(a, params, s);
 }
 
 }  // namespace
@@ -385,10 +485,8 @@ int64_t norm_grad_bytes(int rows, int d, int rows_per_batch) {
 cudaError_t norm_grad_launch(const NormGradParams& p, cudaStream_t s) {
   const bool params = p.dg || p.db || p.dshift || p.dscale;
   const Args a{p, make_plan(p.rows, p.d, p.scale ? p.rows_per_batch : 0), static_cast<float*>(p.workspace)};
-  if (p.dtype == SGD_F16) rows_of_type<f16>(a, params, s);
-  else if (p.dtype == SGD_BF16) rows_of_type<bf16>(a, params, s);
-  else rows_of_type<float>(a, params, s);
-  const cudaError_t e = cudaGetLastError();
+  const cudaError_t e = p.dtype == SGD_F16 ? rows_of_type<f16>(a, params, s)
+                        : p.dtype == SGD_BF16 ? rows_of_type<bf16>(a, params, s) : rows_of_type<float>(a, params, s);
   if (e != cudaSuccess || !params) return e;
   const int jobs = 1 + (p.scale && (p.dshift || p.dscale) ? a.q.samples : 0);
   const dim3 grid((p.d + kColsPerCta - 1) / kColsPerCta, jobs < 1024 ? jobs : 1024);
