@@ -412,6 +412,20 @@ __device__ __forceinline__ void put(const SumArgs& p, uint32_t token, int c, con
 constexpr int kZeros = 16384;     // bytes of zeros in shared memory, which copies to the table start from
 constexpr int kFillRows = 1024;   // tokens of a range, at most
 
+// The first of the sorted rows [lo, hi) whose token is `token` or more, hi where there is none: a warp, 32 probes at a time.
+__device__ __forceinline__ int first_row_of(const uint32_t* tokens, int lo, int hi, uint32_t token) {
+  int before = lo - 1;  // lies before it
+  const int lane = threadIdx.x & 31;
+  while (hi - before > 1) {
+    const int step = (hi - before + 31) / 32, at = before + (lane + 1) * step;
+    const bool is = at < hi && tokens[at] < token;
+    const int more = __popc(__ballot_sync(0xffffffffu, is));
+    before += more * step;
+    hi = min(hi, before + step);
+  }
+  return hi;
+}
+
 // Clears the rows of the tokens [first, first + n) that do not occur.
 template <typename TO, bool VEC>
 __device__ __forceinline__ void clear_rows(const SumArgs& p, int first, int n, uint4* zeros, uint32_t* here) {
@@ -419,22 +433,19 @@ __device__ __forceinline__ void clear_rows(const SumArgs& p, int first, int n, u
   for (int i = threadIdx.x; i < kFillRows / 32; i += kSumThreads) here[i] = 0;
   if (VEC)
     for (int i = threadIdx.x; i < kZeros / 16; i += kSumThreads) zeros[i] = make_uint4(0, 0, 0, 0);
-  // the first sorted row with a token of the range: 32 probes at a time between lo (before it) and hi
-  int lo = -1, hi = p.rows;
-  while (hi - lo > 1) {
-    const int step = (hi - lo + 31) / 32, at = lo + (lane + 1) * step;
-    const bool before = at < hi && p.tokens[at] < static_cast<uint32_t>(first);
-    const int more = __popc(__ballot_sync(0xffffffffu, before));
-    const int new_lo = lo + more * step;
-    hi = min(hi, new_lo + step);
-    lo = new_lo;
-  }
+  // the sorted rows of the range, then each token's first one in them
+  const uint32_t from = static_cast<uint32_t>(first);
+  const int lo = first_row_of(p.tokens, 0, p.rows, from), hi = first_row_of(p.tokens, lo, p.rows, from + n);
   if (VEC) fence_proxy_async_smem();
   __syncthreads();
-  for (int i = lo + 1 + static_cast<int>(threadIdx.x); i < p.rows; i += kSumThreads) {
-    const uint32_t t = p.tokens[i] - first;
-    if (t >= static_cast<uint32_t>(n)) break;
-    if (i == lo + 1 || p.tokens[i - 1] - first != t) atomicOr(&here[t >> 5], 1u << (t & 31));
+  for (int i = threadIdx.x; i < n; i += kSumThreads) {
+    int l = lo, h = hi;
+    while (l < h) {
+      const int at = l + (h - l) / 2;
+      if (p.tokens[at] < from + i) l = at + 1;
+      else h = at;
+    }
+    if (l < hi && p.tokens[l] == from + i) atomicOr(&here[i >> 5], 1u << (i & 31));
   }
   __syncthreads();
   TO* table = static_cast<TO*>(p.dtable);
@@ -463,7 +474,7 @@ __global__ void __launch_bounds__(kSumThreads) embedding_sums_kernel(const SumAr
     return;
   }
   const int chunk = blockIdx.x - p.fill;
-  constexpr int N = VEC ? Vec<TG>::kN : 4, kAhead = 8;
+  constexpr int N = VEC ? Vec<TG>::kN : 4, kAhead = VEC ? 16 : 8;  // (a row's 16 bytes as they are, or its numbers)
   __shared__ uint32_t tok[kMaxChunk + 2];
   __shared__ int32_t row[kMaxChunk];
   const int first = chunk * p.chunk, n = min(p.chunk, p.rows - first);
@@ -482,19 +493,29 @@ __global__ void __launch_bounds__(kSumThreads) embedding_sums_kernel(const SumAr
   for (int j = 0; j < N; ++j) sum[j] = 0.f;
   bool from_before = tok[1] == tok[0];
   for (int i0 = 0; i0 < n; i0 += kAhead) {
-    float v[kAhead][N];
+    uint4 raw[VEC ? kAhead : 1];
+    float v[VEC ? 1 : kAhead][N];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u)
-      if (i0 + u < n && tok[i0 + u + 1] < static_cast<uint32_t>(p.vocab))
-        load<VEC, N>(grad + static_cast<int64_t>(row[i0 + u]) * p.ld_grad, p.d - c, v[u]);
+    for (int u = 0; u < kAhead; ++u) {
+      if (i0 + u >= n || tok[i0 + u + 1] >= static_cast<uint32_t>(p.vocab)) continue;
+      const TG* at = grad + static_cast<int64_t>(row[i0 + u]) * p.ld_grad;
+      if constexpr (VEC) raw[u] = *reinterpret_cast<const uint4*>(at);
+      else load<false, N>(at, p.d - c, v[u]);
+    }
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       const int i = i0 + u;
       if (i >= n) break;
       const uint32_t t = tok[i + 1];
       if (t >= static_cast<uint32_t>(p.vocab)) return;  // the rest has no token
+      if constexpr (VEC) {
+        const TG* e = reinterpret_cast<const TG*>(&raw[u]);
 #pragma unroll
-      for (int j = 0; j < N; ++j) sum[j] += v[u][j];
+        for (int j = 0; j < N; ++j) sum[j] += to_f32(e[j]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) sum[j] += v[u][j];
+      }
       const bool ends = tok[i + 2] != t, last = i == n - 1;
       if (!ends && !last) continue;
       if (ends && !from_before) {
@@ -547,6 +568,12 @@ __global__ void __launch_bounds__(256) embedding_join_kernel(const SumArgs p) {
       const uint32_t t = p.tokens[(c0 + 1) * p.chunk - 1];
       // the last chunk of the run: 32 probes at a time between lo (holds the token first) and hi (does not)
       int lo = c0 + 1, hi = p.chunks;
+      {  // most runs end in the next few chunks
+        const int at = lo + lane + 1;
+        const int more = __popc(__ballot_sync(0xffffffffu, at < hi && p.tokens[static_cast<int64_t>(at) * p.chunk] == t));
+        lo += more;
+        if (more < 32) hi = lo + 1;
+      }
       while (hi - lo > 1) {
         const int step = (hi - lo + 31) / 32;
         const int at = lo + (lane + 1) * step;
@@ -602,7 +629,8 @@ cudaError_t sums(SumArgs a, cudaStream_t s) {
   else embedding_sums_kernel<TG, TO, false><<<grid, kSumThreads, smem, s>>>(a);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess || a.chunks < 2) return e;
-  const dim3 join((a.d + kJoinCols - 1) / kJoinCols, a.chunks < 256 ? a.chunks : 256);
+  const int tiles = (a.d + kJoinCols - 1) / kJoinCols, high = (8 * num_sms() + tiles - 1) / tiles;
+  const dim3 join(tiles, a.chunks < high ? a.chunks : high);
   if (vectors<TO>(a.dtable, a.ld, 4, a.d)) embedding_join_kernel<TO, true><<<join, 256, 0, s>>>(a);
   else embedding_join_kernel<TO, false><<<join, 256, 0, s>>>(a);
   return cudaGetLastError();

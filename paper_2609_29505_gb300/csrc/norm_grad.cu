@@ -19,7 +19,8 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kSms = 152;        // of a GB300
 constexpr int kRowsPerPart = 3;  // of a sample that several groups share, at least
-constexpr int kColsPerCta = 32;    // of the second kernel: 8 threads of 4 columns, 32 shares of the sums
+constexpr int kColsPerCta = 16;  // of the second kernel: 4 threads of 4 columns
+constexpr int kShares = 64;      // and as many shares of the sums as there are threads
 
 // Threads of a row: vectors of 4 columns each, two at most, and four in rows of more than 2048 (`wide`): 4096 columns with a residual are
 // 40 us per 4096 rows with 256 threads a row and two CTAs per SM, 57 with 512 and one, whose barriers nothing hides.
@@ -38,6 +39,7 @@ constexpr int ctas_per_sm(bool wide) { return wide ? 2 : 3; }
 // Narrow rows: how many a group has in hand or on their way, and bytes of shared memory: theirs, and two rows of dh.
 constexpr int kStages = 2;
 constexpr int smem_of(bool wide, int elem) { return wide ? 0 : kThreads * 2 * (kStages * (32 + 4 * elem) + 32); }
+static_assert(kColsPerCta == 16 && kShares == 64, "256 threads");
 static_assert(3 * (smem_of(false, 4) + 9 * 1024) <= 226 * 1024, "shared memory");
 
 struct Plan {
@@ -393,9 +395,9 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(WIDE)) norm_grad_kernel(
 
 // The units' sums added up: CTA (columns, sample) for dshift and dscale, CTA (columns, the last one) for dg and db.
 __global__ void __launch_bounds__(256) norm_grad_sums_kernel(const Args a) {
-  __shared__ float4 red[2][32][8];
+  __shared__ float4 red[2][kShares][kColsPerCta / 4];
   const NormGradParams& p = a.p;
-  const int lane = threadIdx.x & 7, share = threadIdx.x >> 3;
+  const int lane = threadIdx.x & 3, share = threadIdx.x >> 2;
   const int i = blockIdx.x * (kColsPerCta / 4) + lane, nv = p.d >> 2;
   const bool modulated = p.scale != nullptr;
   const int samples = modulated && (p.dshift || p.dscale) ? a.q.samples : 0;
@@ -406,7 +408,7 @@ __global__ void __launch_bounds__(256) norm_grad_sums_kernel(const Args a) {
     float4 A = make_float4(0.f, 0.f, 0.f, 0.f), B = A;
     if (i < nv) {
 #pragma unroll 8
-      for (int u = from + share; u < to; u += 32) {
+      for (int u = from + share; u < to; u += kShares) {
         const float4* at = reinterpret_cast<const float4*>(a.sums + 2 * static_cast<int64_t>(u) * p.d);
         float4 x = at[i], y = at[nv + i];
         if (all && modulated) {
@@ -422,8 +424,19 @@ __global__ void __launch_bounds__(256) norm_grad_sums_kernel(const Args a) {
     red[0][share][lane] = A;
     red[1][share][lane] = B;
     __syncthreads();
+    if (share < 8) {
+      for (int k = share + 8; k < kShares; k += 8) {
+        const float4 x = red[0][k][lane], y = red[1][k][lane];
+        A = make_float4(A.x + x.x, A.y + x.y, A.z + x.z, A.w + x.w);
+        B = make_float4(B.x + y.x, B.y + y.y, B.z + y.z, B.w + y.w);
+      }
+      __syncwarp();
+      red[0][share][lane] = A;
+      red[1][share][lane] = B;
+      __syncwarp();
+    }
     if (share == 0 && i < nv) {
-      for (int k = 1; k < 32; ++k) {
+      for (int k = 1; k < 8; ++k) {
         const float4 x = red[0][k][lane], y = red[1][k][lane];
         A = make_float4(A.x + x.x, A.y + x.y, A.z + x.z, A.w + x.w);
         B = make_float4(B.x + y.x, B.y + y.y, B.z + y.z, B.w + y.w);
