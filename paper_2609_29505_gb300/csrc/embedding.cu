@@ -346,7 +346,7 @@ Plan make_plan(int rows, int d) {
   q.chunk = 8;
   while (q.chunk < kMaxChunk && rows / q.chunk * across > 2048) q.chunk *= 2;
   q.chunks = (rows + q.chunk - 1) / q.chunk;
-  q.times = (rows + kTile * kMaxTiles - 1) / (kTile * kMaxTiles);
+  q.times = rows / (kTile * kMaxTiles) + 1;
   q.tiles = static_cast<int>((static_cast<int64_t>(rows) + static_cast<int64_t>(kTile) * q.times - 1) / (static_cast<int64_t>(kTile) * q.times));
   q.pd = (d + 7) & ~7;
   int64_t at = 0;

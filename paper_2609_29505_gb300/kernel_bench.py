@@ -15,6 +15,11 @@ command that the committed ncu summaries under profiles/ were captured from.
     python -m paper_2609_29505_gb300.kernel_bench logprobs --rows 4096 --vocab 126464 --top 32
     python -m paper_2609_29505_gb300.kernel_bench distill --rows 4096 --vocab 126464 --top 32 --grad bf16
     python -m paper_2609_29505_gb300.kernel_bench reveal --batch 16 --tokens 4096
+    python -m paper_2609_29505_gb300.kernel_bench sample --rows 4096 --vocab 126464 --top-p 0.9
+    python -m paper_2609_29505_gb300.kernel_bench trajectory --config llada --T 16 --remask confidence --temperature 0.7 --top-p 0.9
+    python -m paper_2609_29505_gb300.kernel_bench embedding --rows 4096 --d 4096 --vocab 126464
+    python -m paper_2609_29505_gb300.kernel_bench embedding_grad --rows 4096 --d 4096 --vocab 126464 --masked 0.5
+    python -m paper_2609_29505_gb300.kernel_bench norm_grad --rows 4096 --d 4096 --grad bf16
 """
 from __future__ import annotations
 
@@ -190,6 +195,49 @@ def case_distill(a):
     return dict(case="distill", rows=a.rows, vocab=a.vocab, dtype=a.dtype, top=k, grad=a.grad, ms=ms, gbs=bytes_ / ms / 1e6)
 
 
+def _filters(a):
+    return dict(scale=1.0 / a.temperature, top_k=a.top_k, top_p=a.top_p, min_p=a.min_p)
+
+
+def case_sample(a):
+    z = _logits(a)
+    u = torch.rand(a.rows, 2, device="cuda")
+    ids, lp = torch.empty(a.rows, device="cuda", dtype=torch.int32), torch.empty(a.rows, device="cuda")
+    ms = _time(lambda: binding.sgd_kernel_sample(z, u, ids, logprobs=lp, **_filters(a)), a.iters, a.warmup)
+    return dict(case="sample", rows=a.rows, vocab=a.vocab, dtype=a.dtype, ms=ms, gbs=z.numel() * z.element_size() / ms / 1e6, **_filters(a))
+
+
+def _token_ids(a):
+    ids = torch.randint(0, a.vocab, (a.rows,), device="cuda", dtype=torch.int32)
+    ids[: int(a.masked * a.rows)] = a.vocab - 1
+    return ids[torch.randperm(a.rows, device="cuda")]
+
+
+def case_embedding(a):
+    table = torch.randn(a.vocab, a.d, device="cuda").to(DTYPES[a.dtype])
+    ids, out = _token_ids(a), torch.empty(a.rows, a.d, device="cuda", dtype=DTYPES[a.grad or "f32"])
+    ms = _time(lambda: binding.sgd_kernel_embedding(table, ids, out, scale=2.0), a.iters, a.warmup)
+    bytes_ = (ids.unique().numel() * table.element_size() + a.rows * out.element_size()) * a.d
+    return dict(case="embedding", rows=a.rows, d=a.d, vocab=a.vocab, dtype=a.dtype, masked=a.masked, ms=ms, gbs=bytes_ / ms / 1e6)
+
+
+def case_embedding_grad(a):
+    grad = torch.randn(a.rows, a.d, device="cuda").to(DTYPES[a.dtype])
+    ids, table = _token_ids(a), torch.empty(a.vocab, a.d, device="cuda", dtype=DTYPES[a.grad or "f32"])
+    ws = torch.empty(binding.sgd_kernel_embedding_grad_workspace(a.rows, a.vocab, a.d), device="cuda", dtype=torch.uint8)
+    ms = _time(lambda: binding.sgd_kernel_embedding_grad(grad, ids, table, workspace=ws), a.iters, a.warmup)
+    bytes_ = grad.numel() * grad.element_size() + table.numel() * table.element_size()
+    return dict(case="embedding_grad", rows=a.rows, d=a.d, vocab=a.vocab, dtype=a.dtype, masked=a.masked, ms=ms, gbs=bytes_ / ms / 1e6)
+
+
+def case_norm_grad(a):
+    h, dout = torch.randn(a.rows, a.d, device="cuda"), torch.randn(a.rows, a.d, device="cuda").to(DTYPES[a.grad or "f32"])
+    g, dg, res, dh = torch.ones(a.d, device="cuda", dtype=torch.bfloat16), torch.empty(a.d, device="cuda"), torch.randn_like(h), torch.empty_like(h)
+    ws = torch.empty(binding.sgd_kernel_norm_grad_workspace(a.rows, a.d), device="cuda", dtype=torch.uint8)
+    ms = _time(lambda: binding.sgd_kernel_norm_grad(dout, h, 0, dh=dh, g=g, residual=res, dg=dg, workspace=ws), a.iters, a.warmup)
+    return dict(case="norm_grad", rows=a.rows, d=a.d, ms=ms, gbs=(12.0 + dout.element_size()) * h.numel() / ms / 1e6)
+
+
 def case_reveal(a):
     ids = torch.zeros(a.batch, a.tokens, device="cuda", dtype=torch.int32)
     out, score = torch.empty_like(ids), torch.rand(a.batch, a.tokens, device="cuda")
@@ -209,11 +257,18 @@ def _remask(a, cfg, model, logits):
     n = [torch.full((cfg.batch,), (s * cfg.n_tokens) // T - ((s - 1) * cfg.n_tokens) // T, device="cuda", dtype=torch.int32)
          for s in range(1, T + 1)]
 
+    draw = {}
+    if a.temperature != 1.0 or a.top_k or a.top_p < 1.0 or a.min_p:  # candidates are drawn, by numbers of their own at each step
+        draw = _filters(a)
+        numbers = torch.rand(T, *shape, 2, device="cuda")
+
     def run():
         ids.fill_(mask)
         for s in range(1, T + 1):
+            if draw:
+                draw["uniforms"] = numbers[s - 1]
             model.step_tokens(ids, ids, logits, synth.timestep(cfg, s, T), s, cand, score, n[s - 1], mask, by=a.remask,
-                              n_left=left)
+                              n_left=left, **draw)
     return run, left
 
 
@@ -272,7 +327,7 @@ def case_trajectory(a):
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("case", choices=["gemm", "attention", "frozen", "norm", "trajectory", "logprobs", "distill",
-                                     "reveal"])
+                                     "reveal", "sample", "embedding", "embedding_grad", "norm_grad"])
     ap.add_argument("--config", default="dit", help="trajectory: synthetic model config")
     ap.add_argument("--T", type=int, default=0, help="trajectory: horizon (0: the config's)")
     ap.add_argument("--budget", type=float, default=0.5, help="trajectory: layer-step budget")
@@ -305,12 +360,18 @@ def main():
     ap.add_argument("--d", type=int, default=4096)
     ap.add_argument("--caches", type=int, default=8)
     ap.add_argument("--vocab", type=int, default=126464)
-    ap.add_argument("--dtype", default="f16", choices=list(DTYPES), help="logprobs, distill: type of the logits")
+    ap.add_argument("--dtype", default="f16", choices=list(DTYPES), help="type of the logits, the table, or the rows' gradients")
     ap.add_argument("--top", type=int, default=1, help="logprobs: likeliest tokens; distill: length of the lists")
     ap.add_argument("--entropy", action="store_true", help="logprobs: the entropy too")
-    ap.add_argument("--grad", default="", choices=["", *DTYPES], help="distill: type of the gradient (none: the loss alone)")
+    ap.add_argument("--grad", default="", choices=["", *DTYPES], help="distill: type of the gradient (none: the loss alone); embedding, embedding_grad, "
+                    "norm_grad: of the rows that are written, of the table's gradient, of dout")
     ap.add_argument("--remask", default="", choices=["", "confidence", "entropy"],
                     help="trajectory of a token model: positions revealed by the model's own logits")
+    ap.add_argument("--temperature", type=float, default=1.0, help="sample, trajectory: candidates drawn at this temperature")
+    ap.add_argument("--top-k", type=int, default=0, help="sample, trajectory: from this many of the likeliest tokens (0: all)")
+    ap.add_argument("--top-p", type=float, default=1.0, help="sample, trajectory: from the likeliest tokens with this share")
+    ap.add_argument("--min-p", type=float, default=0.0, help="sample, trajectory: from tokens with this share of the likeliest one's")
+    ap.add_argument("--masked", type=float, default=0.0, help="embedding, embedding_grad: share of rows that hold one token")
     ap.add_argument("--iters", type=int, default=20)
     ap.add_argument("--warmup", type=int, default=3)
     ap.add_argument("--graph", action="store_true",
@@ -322,7 +383,8 @@ def main():
     binding.lib()
     res = {"gemm": case_gemm, "attention": case_attention, "frozen": case_frozen,
            "norm": case_norm, "trajectory": case_trajectory, "logprobs": case_logprobs, "distill": case_distill,
-           "reveal": case_reveal}[a.case](a)
+           "reveal": case_reveal, "sample": case_sample, "embedding": case_embedding, "embedding_grad": case_embedding_grad,
+           "norm_grad": case_norm_grad}[a.case](a)
     res["graph"] = a.graph
     res["status"] = binding.sgd_kernel_status()
     print(json.dumps(res))
