@@ -24,6 +24,7 @@
 //
 // Many rows: a CTA each, three per SM, so that one's search hides behind the others' reading.  Few: a cluster reads a row.
 #include <math.h>
+#include <stddef.h>
 
 #include "vocab_rows.cuh"
 
@@ -49,6 +50,7 @@ struct SampleArgs {
   float c, c_lo;    // scale log2(e), as the sum of two floats
   double drop;      // ln(min_p) / scale: a token at or above max + drop passes (-inf: every token)
   int n_blocks;
+  int* status;
 };
 
 // 2^(j / 32) 2^62, j = 0 .. 31
@@ -114,6 +116,16 @@ __device__ __forceinline__ void add_shared(uint32_t* lo, uint32_t* hi, uint64_t 
   const uint32_t low = static_cast<uint32_t>(w), was = atomicAdd(lo, low);
   const uint32_t high = static_cast<uint32_t>(w >> 32) + (was + low < was);
   if (high) atomicAdd(hi, high);
+}
+
+// Additions to the shared memory of another CTA of the cluster.
+__device__ __forceinline__ void add_cluster(uint32_t to, uint64_t v) {
+  asm volatile("red.relaxed.cluster.shared::cluster.add.u64 [%0], %1;" ::"r"(to), "l"(v) : "memory");
+}
+__device__ __forceinline__ int add_cluster(uint32_t to, int v) {
+  int was;
+  asm volatile("atom.relaxed.cluster.shared::cluster.add.u32 %0, [%1], %2;" : "=r"(was) : "r"(to), "r"(v) : "memory");
+  return was;
 }
 
 // A barrier of the kThreads threads that take a row.
@@ -264,17 +276,34 @@ __device__ __forceinline__ uint64_t first_of_order(const T* row, int vocab, int 
 
 constexpr int kQueue = 96;  // tokens that a warp puts side by side: 32 wait at most, and 64 join them
 
+constexpr int kRing = 3;  // tiles of a row on their way or in hand: two blocks (one of fp32) of each warp
+
+// What the first CTA of a cluster asks the others for.
+struct Command {
+  float m, zl, zh;
+  int mode;  // 0: nothing more, 1: a bracket, 2: with the tail
+};
+
 template <int kThreads, bool FILTER>
-struct __align__(16) Shared {
+struct __align__(128) Shared {
   static constexpr int kWarps = kThreads / 32;
   static constexpr int kCap = FILTER ? 16 * kThreads : 2;  // tokens of the list
   static constexpr int kHist = FILTER ? 4 * kThreads : 2;  // bins
   static constexpr int kTeam = FILTER ? kThreads : 4;
-  uint64_t list[kCap];
-  uint32_t count[kHist], lo[kHist], hi[kHist];
-  uint64_t small[kTeam], small_w[kTeam];
+  union {
+    uint4 ring[kRing][kWarps * 2 * kBlock / 8];  // while the row is read
+    struct {
+      uint64_t list[kCap];
+      uint32_t count[kHist], lo[kHist], hi[kHist];
+      uint64_t small[kTeam], small_w[kTeam];
+    };
+  };
+  uint64_t full[kRing], empty[kRing];
+  alignas(16) Command command;
+  uint64_t inside, tail;  // of a cluster's CTAs
+  int abort_flag;
   int queue[kWarps][FILTER ? kQueue : 2];
-  uint32_t groups[kTeam];
+  alignas(16) uint32_t groups[kTeam];  // (read four at a time)
   uint64_t pow2[32];
   uint64_t wide[2][kWarps];
   float part[kWarps];
@@ -465,6 +494,17 @@ struct Row {
   struct Rest {
     uint64_t inside, tail, error;
   };
+  // The tail's mass: `low` from sums against zl, `skipped` from blocks' sums; and how far it may be off.
+  __device__ void tail_error(float zl, uint64_t low, uint64_t skipped, Rest* rest) const {
+    // the sums against zl: 18 u, and three roundings of an exponent t whose mean over the mass S (of zl's weight) is at most log2(vocab) -
+    // log2(S); half a unit of 2^-22 of zl's weight a block, and tokens below 2^-43
+    const uint64_t w_zl = w_of(zl);
+    const float wf = static_cast<float>(w_zl) + 1.f;
+    const float spread = low > 0 ? fmaxf(log2f(a.p.vocab * wf / static_cast<float>(low)), 0.f) : 0.f;
+    rest->tail = low + skipped;
+    rest->error = static_cast<uint64_t>(a.p.vocab) + a.n_blocks * (1 + (w_zl >> 22)) +
+                  __double2ull_ru((20.0 + 2.1 * spread) * 5.9604645e-8 * static_cast<double>(low) + kError * static_cast<double>(skipped));
+  }
   // Tokens from zl to zh: into the list, as far as it goes, and their mass in rest->inside.  Returns how many these are.
   // With TAIL: the mass of those below, from fp32 sums, and how far it may be off; the blocks' masses, which `mass` holds at the call, lose
   // it.  Else: `mass` is cleared.
@@ -512,15 +552,77 @@ struct Row {
     const ulonglong2 sum = cta_sum(inside, tail);
     rest->inside = sum.x;
     if constexpr (TAIL) {
-      skipped = cta_sum(skipped);
-      // the sums against zl: 18 u, and three roundings of an exponent t whose mean over the mass S (of zl's weight) is at most log2(vocab) -
-      // log2(S); half a unit of 2^-22 of zl's weight a block, and tokens below 2^-43
-      const float wf = static_cast<float>(w_zl) + 1.f;
-      const float spread = sum.y > 0 ? fmaxf(log2f(a.p.vocab * wf / static_cast<float>(sum.y)), 0.f) : 0.f;
-      rest->tail = sum.y + skipped;
-      rest->error = static_cast<uint64_t>(a.p.vocab) + a.n_blocks * (1 + (w_zl >> 22)) +
-                    __double2ull_ru((20.0 + 2.1 * spread) * 5.9604645e-8 * static_cast<double>(sum.y) + kError * static_cast<double>(skipped));
+      tail_error(zl, sum.y, cta_sum(skipped), rest);
     }
+    return sh.n;
+  }
+
+  // A cluster's bracket: each CTA takes the blocks that it has read, and sends what it finds to the first one, whose `mass` keeps the blocks'
+  // masses, less the tail's, or is not looked at.
+  template <bool TAIL>
+  __device__ void bracket_share(float zl, float zh, int rank, int n_ctas, int tile) const {
+    const uint32_t to_n = map_to_rank(smem_u32(&sh.n), 0), to_list = map_to_rank(smem_u32(sh.list), 0), to_mass = map_to_rank(smem_u32(mass), 0);
+    uint64_t inside = 0, tail = 0;
+    const uint64_t w_zl = TAIL ? w_of(zl) : 0;
+    Queue q{sh.queue[warp]};
+    auto f = [&](int e, float z) {
+      if (z > zh) return;
+      inside += w_of(z);
+      const uint32_t here = __activemask();
+      const int first = __ffs(here) - 1;
+      int at = 0;
+      if (lane == first) at = add_cluster(to_n, __popc(here));
+      at = __shfl_sync(here, at, first) + __popc(here & ((1u << lane) - 1u));
+      if (at < Sh::kCap) st_cluster(to_list + 8 * at, place(order_key(z), e));
+    };
+    for (int k = rank; k * tile < a.n_blocks; k += n_ctas) {
+      for (int b = k * tile + warp; b < min((k + 1) * tile, a.n_blocks); b += kWarps) {
+        if (!(max_of[b] >= zl)) continue;
+        const Raw<T> raw = fetch<T, VEC>(row, a.p.vocab, b, lane);
+        if (TAIL && zl > -kInf) {
+          float z[kPerLane], s[2] = {0.f, 0.f};
+          numbers(raw, z);
+#pragma unroll
+          for (int j = 0; j < kPerLane; ++j) s[j & 1] += z[j] < zl ? ex2_approx(__fmul_rn(z[j] - zl, a.c)) : 0.f;
+          const float all = warp_sum(s[0] + s[1]);
+          if (lane == 0) {
+            const uint64_t w = times(all, w_zl);
+            tail += w;
+            add_cluster(to_mass + 8 * b, 0 - w);
+          }
+        }
+        marked(q, b, marks(b, raw, zl), f);
+      }
+    }
+    drain(q, 1, f);
+    const ulonglong2 sum = cta_sum(inside, tail);
+    if (threadIdx.x == 0) {
+      add_cluster(map_to_rank(smem_u32(&sh.inside), 0), static_cast<uint64_t>(sum.x));
+      if (TAIL) add_cluster(map_to_rank(smem_u32(&sh.tail), 0), static_cast<uint64_t>(sum.y));
+    }
+  }
+  // ... asked for by the first CTA, which takes its share: as bracket().
+  template <bool TAIL>
+  __device__ int bracket_cluster(float zl, float zh, int n_ctas, int tile, Rest* rest) const {
+    if (threadIdx.x == 0) {
+      sh.n = 0;
+      sh.inside = sh.tail = 0;
+    }
+    uint64_t skipped = 0;
+    for (int b = threadIdx.x; b < a.n_blocks; b += kThreads)
+      if (!TAIL || !(max_of[b] >= zl)) {
+        if (TAIL) skipped += mass[b];
+        mass[b] = 0;
+      }
+    if (static_cast<int>(threadIdx.x) < n_ctas)
+      st_cluster(map_to_rank(smem_u32(&sh.command), threadIdx.x), make_float4(m, zl, zh, __int_as_float(TAIL ? 2 : 1)));
+    __syncwarp();
+    cluster_sync();
+    bracket_share<TAIL>(zl, zh, 0, n_ctas, tile);
+    __syncwarp();
+    cluster_sync();
+    rest->inside = sh.inside;
+    if (TAIL) tail_error(zl, sh.tail, cta_sum(skipped), rest);
     return sh.n;
   }
 
@@ -941,8 +1043,9 @@ template <typename T, bool VEC, int kThreads, bool FILTER>
 __global__ void __launch_bounds__(kThreads, (FILTER ? 768 : 1024) / kThreads) sample_kernel(const SampleArgs a) {
   constexpr int kWarps = kThreads / 32;
   using Sh = Shared<kThreads, FILTER>;
-  extern __shared__ __align__(16) unsigned char dynamic[];  // Shared, then [n_blocks] masses, maxima, and numbers
+  extern __shared__ __align__(128) unsigned char dynamic[];  // Shared, then [n_blocks] masses, maxima, and numbers
   Sh& sh = *reinterpret_cast<Sh*>(dynamic);
+  static_assert(offsetof(Sh, groups) % 16 == 0 && offsetof(Sh, ring) % 16 == 0 && sizeof(Sh) % 16 == 0, "vectors of 16 bytes");
   const SampleParams& p = a.p;
   uint64_t* mass = reinterpret_cast<uint64_t*>(dynamic + sizeof(Sh));
   float* max_of = reinterpret_cast<float*>(mass + a.n_blocks);
@@ -956,47 +1059,130 @@ __global__ void __launch_bounds__(kThreads, (FILTER ? 768 : 1024) / kThreads) sa
   const bool by_k = FILTER && p.top_k > 0 && p.top_k < p.vocab, by_m = FILTER && a.drop != -HUGE_VAL, by_p = FILTER && p.top_p < 1.0;
   const bool sums = !FILTER || p.logprobs || !(by_k || by_m);
   const float u0 = p.uniforms[2 * r], u1 = p.uniforms[2 * r + 1];
-  {
-    // two blocks of 16-bit logits, or one of fp32, in hand and as many on their way
-    constexpr int kPair = sizeof(T) == 2 ? 2 : 1;
-    const int stride = kWarps * n_ctas;
-    int i = warp * n_ctas + rank;
-    Raw<T> next[kPair];
-#pragma unroll
-    for (int u = 0; u < kPair; ++u)
-      if (i + u * stride < a.n_blocks) next[u] = fetch<T, VEC>(row, p.vocab, i + u * stride, lane);
-    if (threadIdx.x < 32) sh.pow2[threadIdx.x] = kPow2[threadIdx.x];
-    if (threadIdx.x == 0) {
-      sh.bad = 0;
-      sh.best = 0;
+  constexpr int kPair = sizeof(T) == 2 ? 2 : 1, kTile = kWarps * kPair;  // blocks of a warp at a time, of the CTA
+  if (threadIdx.x < 32) sh.pow2[threadIdx.x] = kPow2[threadIdx.x];
+  if (threadIdx.x == 0) {
+    sh.bad = 0;
+    sh.best = 0;
+    sh.abort_flag = 0;
+  }
+  const uint32_t to_max = map_to_rank(smem_u32(max_of), 0), to_mass = map_to_rank(smem_u32(mass), 0);
+  auto put = [&](const Raw<T>* cur, int b) {  // blocks b and b + kWarps
+    const float2 st = block_stats<T, kPair>(cur, sums, a.c, lane);
+    const int at = kPair == 2 && lane >= 16 ? b + kWarps : b;
+    if ((lane == 0 || (kPair == 2 && lane == 16)) && at < a.n_blocks) {
+      if (FILTER && rank != 0) max_of[at] = st.x;  // (for this CTA's share of a bracket)
+      if (n_ctas == 1) {
+        max_of[at] = st.x;
+        mass[at] = __float_as_uint(st.y);
+      } else {
+        st_cluster(to_max + 4 * at, st.x);
+        st_cluster(to_mass + 8 * at, static_cast<uint64_t>(__float_as_uint(st.y)));
+      }
     }
-    const uint32_t to_max = map_to_rank(smem_u32(max_of), 0), to_mass = map_to_rank(smem_u32(mass), 0);
+  };
+  const int tiles = (a.n_blocks + kTile - 1) / kTile;
+  if constexpr (VEC) {
+    // Tiles of 16 KB (256 threads) by bulk copies: long stretches of a row at a time.  With loads of the warps' own, 1 KB each, some sizes
+    // of the whole took half as long again as others.
+    constexpr int kTileBytes = kTile * kBlock * static_cast<int>(sizeof(T)), E = Elem<T>::kPer;
+    static_assert(kTileBytes == static_cast<int>(sizeof(sh.ring[0])), "the ring's tiles");
+    volatile int* abort_flag = &sh.abort_flag;
+    const int64_t whole_bytes = static_cast<int64_t>(p.vocab / E) * 16;
+    auto issue = [&](int k) {  // one thread
+      const int64_t from = (static_cast<int64_t>(k) * n_ctas + rank) * kTileBytes;
+      const int64_t left = whole_bytes - from;
+      uint64_t* bar = &sh.full[k % kRing];
+      if (left > 0) {
+        const uint32_t bytes = left < kTileBytes ? static_cast<uint32_t>(left) : kTileBytes;
+        mbar_arrive_expect_tx(bar, bytes);
+        bulk_load(sh.ring[k % kRing], reinterpret_cast<const char*>(row) + from, bytes, bar);
+      } else {
+        mbar_arrive(bar);
+      }
+    };
+    const int mine = tiles > rank ? (tiles - rank + n_ctas - 1) / n_ctas : 0;
+    if (threadIdx.x == 0) {
+      for (int i = 0; i < kRing; ++i) {
+        mbar_init(&sh.full[i], 1);
+        mbar_init(&sh.empty[i], kWarps);
+      }
+      fence_mbar_init();
+      fence_proxy_async_smem();
+      for (int k = 0; k < min(kRing, mine); ++k) issue(k);
+    }
+    team_sync<kThreads>();
     if (n_ctas > 1) cluster_wait();  // every CTA of the cluster runs: the leader's shared memory may be written
-    for (; i < a.n_blocks; i += kPair * stride) {
+    for (int k = 0; k < mine; ++k) {
+      if (threadIdx.x == 0 && k > 0 && k - 1 + kRing < mine) {  // the tile before has been read by all: another into its place
+        if (mbar_wait(&sh.empty[(k - 1) % kRing], ((k - 1) / kRing) & 1, abort_flag, a.status, 71)) issue(k - 1 + kRing);
+        else mbar_arrive(&sh.full[(k - 1) % kRing]);
+      }
+      __syncwarp();
+      // (after an expired wait, which is recorded, the kernel goes on with what is there; no copy lands after the CTA has left)
+      if (!mbar_wait_warp(smem_u32(&sh.full[k % kRing]), (k / kRing) & 1, abort_flag, a.status, 72))
+        mbar_drain(&sh.full[k % kRing], (k / kRing) & 1);
+      const int b = (k * n_ctas + rank) * kTile + warp;
       Raw<T> cur[kPair];
 #pragma unroll
       for (int u = 0; u < kPair; ++u) {
-        cur[u] = next[u];
-        if (i + (kPair + u) * stride < a.n_blocks) next[u] = fetch<T, VEC>(row, p.vocab, i + (kPair + u) * stride, lane);
-      }
-      const float2 st = block_stats<T, kPair>(cur, sums, a.c, lane);
-      const int mine = kPair == 2 && lane >= 16 ? i + stride : i;
-      if ((lane == 0 || (kPair == 2 && lane == 16)) && mine < a.n_blocks) {
-        const int at = mine;
-        if (n_ctas == 1) {
-          max_of[at] = st.x;
-          mass[at] = __float_as_uint(st.y);
-        } else {
-          st_cluster(to_max + 4 * at, st.x);
-          st_cluster(to_mass + 8 * at, static_cast<uint64_t>(__float_as_uint(st.y)));
+        const uint4* from = sh.ring[k % kRing] + (warp + u * kWarps) * (kBlock / E);
+        const int first = (b + u * kWarps) * kBlock;
+        if (first + kBlock <= p.vocab) {
+#pragma unroll
+          for (int i = 0; i < Raw<T>::kN; ++i) cur[u].v[i] = from[i * 32 + lane];
+        } else {  // the row's end: copies bring whole vectors alone
+#pragma unroll
+          for (int i = 0; i < Raw<T>::kN; ++i) {
+            const int e = first + (i * 32 + lane) * E;
+            if (e + E <= p.vocab) {
+              cur[u].v[i] = from[i * 32 + lane];
+            } else {
+              T* t = reinterpret_cast<T*>(&cur[u].v[i]);
+#pragma unroll
+              for (int j = 0; j < E; ++j) t[j] = e + j < p.vocab ? row[e + j] : neg_inf<T>();
+            }
+          }
         }
       }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.empty[k % kRing]);
+      put(cur, b);
+    }
+  } else {
+    if (n_ctas > 1) cluster_wait();
+    int b = rank * kTile + warp;
+    Raw<T> next[kPair];
+#pragma unroll
+    for (int u = 0; u < kPair; ++u)
+      if (b + u * kWarps < a.n_blocks) next[u] = fetch<T, VEC>(row, p.vocab, b + u * kWarps, lane);
+    for (; b < a.n_blocks; b += kTile * n_ctas) {
+      Raw<T> cur[kPair];
+#pragma unroll
+      for (int u = 0; u < kPair; ++u) {
+        const int ahead = b + u * kWarps + kTile * n_ctas;
+        cur[u] = next[u];
+        if (ahead < a.n_blocks) next[u] = fetch<T, VEC>(row, p.vocab, ahead, lane);
+      }
+      put(cur, b);
     }
   }
   if (n_ctas > 1) {
     __syncwarp();
     cluster_sync();
-    if (rank != 0) return;
+    if (rank != 0) {
+      if constexpr (FILTER) {
+        cluster_sync();  // the command has come
+        const Command c = sh.command;
+        if (c.mode == 0) return;
+        const Row<T, VEC, kThreads, FILTER> t{a, row, max_of, mass, live, sh, c.m, warp, lane};
+        if (c.mode == 2) t.template bracket_share<true>(c.zl, c.zh, rank, n_ctas, kTile);
+        else t.template bracket_share<false>(c.zl, c.zh, rank, n_ctas, kTile);
+        __syncwarp();
+        cluster_sync();
+      }
+      return;
+    }
   } else {
     team_sync<kThreads>();
   }
@@ -1016,6 +1202,12 @@ __global__ void __launch_bounds__(kThreads, (FILTER ? 768 : 1024) / kThreads) sa
 #pragma unroll
   for (int i = 0; i < kWarps; ++i) m = fmaxf(m, sh.part[i]);
   if (sh.bad || m == -kInf) {
+    if (FILTER && n_ctas > 1) {
+      if (static_cast<int>(threadIdx.x) < n_ctas)
+        st_cluster(map_to_rank(smem_u32(&sh.command), threadIdx.x), make_float4(0.f, 0.f, 0.f, __int_as_float(0)));
+      __syncwarp();
+      cluster_sync();
+    }
     // no distribution: the first token of the order
     const uint64_t first = first_of_order(row, p.vocab, kThreads);
     if (lane == 0) atomicMax(reinterpret_cast<unsigned long long*>(&sh.best), static_cast<unsigned long long>(first));
@@ -1080,7 +1272,9 @@ __global__ void __launch_bounds__(kThreads, (FILTER ? 768 : 1024) / kThreads) sa
     typename R::Rest rest{};
     const bool alone = !by_k && !by_m;
     team_sync<kThreads>();
-    int n = alone ? t.template bracket<true>(zl, zh, &rest) : t.template bracket<false>(zl, zh, &rest);
+    int n;
+    if (n_ctas > 1) n = alone ? t.template bracket_cluster<true>(zl, zh, n_ctas, kTile, &rest) : t.template bracket_cluster<false>(zl, zh, n_ctas, kTile, &rest);
+    else n = alone ? t.template bracket<true>(zl, zh, &rest) : t.template bracket<false>(zl, zh, &rest);
     if (by_k && n < p.top_k && zl > floor_m) {  // the sample misled
       zl = floor_m;
       team_sync<kThreads>();
@@ -1176,7 +1370,7 @@ cudaError_t launch_type(const SampleArgs& a, cudaStream_t s) {
 cudaError_t sample_launch(const SampleParams& p, cudaStream_t s) {
   const double c = static_cast<double>(p.scale) * 1.4426950408889634073599;
   SampleArgs a{p, static_cast<float>(c), 0.f, p.min_p > 0.0 ? log(p.min_p) / static_cast<double>(p.scale) : -HUGE_VAL,
-               (p.vocab + kBlock - 1) / kBlock};
+               (p.vocab + kBlock - 1) / kBlock, device_status_ptr()};
   a.c_lo = static_cast<float>(c - static_cast<double>(a.c));
   if (p.dtype == SGD_F16) return launch_type<f16>(a, s);
   if (p.dtype == SGD_BF16) return launch_type<bf16>(a, s);
