@@ -1239,12 +1239,16 @@ __global__ void __launch_bounds__(kThreads, (FILTER ? 768 : 1024) / kThreads) sa
     float zl = -kInf, zh = kInf;
     if (by_m) zl = __double2float_ru(static_cast<double>(m) + a.drop);
     const float floor_m = zl;
-    if (by_k) {
+    auto bound_by_k = [&] {
       // (as many groups of blocks as there are blocks have a maximum)
-      if (p.top_k <= min(a.n_blocks, kThreads)) zl = fmaxf(zl, key_value(t.template bound_of_k<false>(p.top_k)));
-      else if (p.vocab >= kSampled) zl = fmaxf(zl, t.sampled_bound_of_k(p.top_k));
-      else if (p.top_k <= kThreads) zl = fmaxf(zl, key_value(t.template bound_of_k<true>(p.top_k)));
-    }
+      if (p.top_k <= min(a.n_blocks, kThreads)) return fmaxf(zl, key_value(t.template bound_of_k<false>(p.top_k)));
+      if (p.vocab >= kSampled) return fmaxf(zl, t.sampled_bound_of_k(p.top_k));
+      if (p.top_k <= kThreads) return fmaxf(zl, key_value(t.template bound_of_k<true>(p.top_k)));
+      return zl;
+    };
+    // (half a percent of the maximum's weight leaves few tokens by itself, as a rule)
+    const bool by_m_first = by_m && p.min_p >= 0.005;
+    if (by_k && !by_m_first) zl = bound_by_k();
     if (!by_k && !by_m) {
       // the maxima from the 64th largest on, if they have the mass already
       uint64_t s = 0;
@@ -1275,10 +1279,15 @@ __global__ void __launch_bounds__(kThreads, (FILTER ? 768 : 1024) / kThreads) sa
     int n;
     if (n_ctas > 1) n = alone ? t.template bracket_cluster<true>(zl, zh, n_ctas, kTile, &rest) : t.template bracket_cluster<false>(zl, zh, n_ctas, kTile, &rest);
     else n = alone ? t.template bracket<true>(zl, zh, &rest) : t.template bracket<false>(zl, zh, &rest);
-    if (by_k && n < p.top_k && zl > floor_m) {  // the sample misled
-      zl = floor_m;
+    if (by_k && by_m_first ? n > Sh::kCap : by_k && n < p.top_k && zl > floor_m) {  // it did not; or the sample misled
+      zl = by_m_first ? bound_by_k() : floor_m;
       team_sync<kThreads>();
       n = t.template bracket<false>(zl, zh, &rest);
+      if (n < p.top_k && zl > floor_m) {
+        zl = floor_m;
+        team_sync<kThreads>();
+        n = t.template bracket<false>(zl, zh, &rest);
+      }
     }
     bool listed = n <= Sh::kCap;
     const typename R::List list{t, n};

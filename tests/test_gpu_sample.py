@@ -157,6 +157,23 @@ def test_every_token_of_a_cut_can_be_drawn(B):
         assert np.abs(count - w / w.sum()).max() <= 2.0 / n
 
 
+@pytest.mark.parametrize("vocab", [3000, 20000, 100000])
+@pytest.mark.parametrize("rows", [1, 9, 200])
+def test_filters_that_leave_many_tokens(B, rows, vocab):
+    """A min-p that leaves more than the list holds, with a top-k and without; a top-k of most of the tokens; flat rows, whose cut
+    by mass is among tens of thousands of nearly equal tokens."""
+    rng = np.random.default_rng(vocab + rows)
+    z1 = np.where(np.arange(rows)[:, None] % 2 == 0, 0.3, 1.0) * rng.standard_normal((rows, vocab))
+    for dtype in ("bf16", "f32"):
+        z = _put(z1, dtype)
+        few = slice(0, min(rows, 9))
+        for i, kw in enumerate([dict(min_p=0.02), dict(min_p=0.01, top_k=40), dict(min_p=0.01, top_k=2000, top_p=0.8), dict(min_p=0.001, top_p=0.9),
+                                dict(top_k=vocab - 7), dict(top_k=vocab // 2, top_p=0.7), dict(top_p=0.3), dict(top_p=0.97), dict(top_k=5000)]):
+            u = _numbers(rows, 20 + i)
+            ids, lp = _draw(B, z, u, **kw)
+            _check((ids[few], lp[few]), z[few], u[few], **kw)
+
+
 @pytest.mark.parametrize("kw", [dict(), dict(top_k=50), dict(top_p=0.9), dict(min_p=0.05)])
 def test_numbers_at_the_ends_and_outside(B, kw):
     z = _put(_logits(8, 3001, 4), "f16")
