@@ -288,7 +288,7 @@ SGD_API int sgd_kernel_distill(const void* logits, int dtype, int64_t ld, int ro
  *     u0 mass(K), and the first token of K in b whose cumulative mass inside b (tokens ascending) is above u1 mass(b);
  *     the last one of positive mass where rounding leaves none.
  * With independent uniform numbers that is a draw from w over K, with the resolution of both.  Masses are compared as
- * 64-bit arithmetic has them (to 2^-30 relative; tokens below 2^-44 of the maximum have none).
+ * sums of whole multiples of 2^-43 of the largest weight, each within 2^-30 of its value (tokens below 2^-44 have none).
  *   ids int32 [rows] = the token;  logprobs fp32 [rows] (NULL: not wanted) = its ln p, p = softmax(x) over all tokens.
  * scale = 1 / temperature, 0 < scale <= 2e38.  top_k >= 0, 0 < top_p <= 1, 0 <= min_p <= 1 (else SGD_ERR_ARG).
  * row_ids, row_id, the rows of logits and their limits as in sgd_kernel_logprobs.  -inf masks a token.  A row without a
@@ -315,7 +315,7 @@ SGD_API int sgd_kernel_embedding_grad_workspace(int rows, int vocab, int d, int6
 
 /*
  * Gradient of sgd_kernel_embedding's table: with S[t] = scale * sum of grad[r, :] over the rows r with ids[r] = t, in fp32 and in
- * one order (that of the rows, and of groups of 16 to 64 rows sorted by token for tokens with many),
+ * one order (that of the rows, and of groups of 8 to 32 rows sorted by token for tokens with many),
  *   accumulate = 0: dtable[t, :] = S[t] for every t in [0, vocab), zeros for tokens without a row;
  *   accumulate = 1: dtable[t, :] += S[t] for the tokens that have rows; the others are neither read nor written;
  * each rounded once from fp32.  Rows whose id is not in [0, vocab) are left out, and not read.
@@ -343,7 +343,7 @@ SGD_API int sgd_kernel_norm_grad_workspace(int rows, int d, int rows_per_batch, 
  * Any of the outputs may be NULL, but not all; dg needs g, db needs b, dshift and dscale need scale, residual needs dh.
  * h fp32 [rows, d], dout [rows, d] of type dtype, g, b bf16 [d] or NULL, scale fp32 [samples, ld_mod] or NULL, row r of sample
  * r / rows_per_batch.  d a multiple of 4, 4 <= d <= 4096; h, dh, residual, dg, db and fp32 dout 16-byte aligned, other dout,
- * g and b 8-byte aligned.  Sums are fp32 (over 8 rows or more at a time, then over those) and the same on every run.
+ * g and b 8-byte aligned.  Sums are fp32 (over a share of the rows at a time, then over the shares) and the same on every run.
  * With rows = 0, dg and db are zeros.  workspace as in sgd_kernel_embedding_grad; none is needed where dh is the only
  * output.  No output may overlap another argument otherwise (SGD_ERR_ARG for dh on h, dout or residual).
  */

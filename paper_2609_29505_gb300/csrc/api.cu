@@ -2112,6 +2112,8 @@ int sgd_kernel_embedding_grad(const void* grad, int grad_dtype, int64_t ld_grad,
   if (overlap(dtable, n, grad, extent(rows, ld_grad, d, elem_size(grad_dtype))) || overlap(dtable, n, ids, 4ll * rows) ||
       overlap(dtable, n, workspace, rows ? need : 0))
     return fail(SGD_ERR_ARG, "embedding_grad: dtable overlaps another argument");
+  if (overlap(workspace, rows ? need : 0, grad, extent(rows, ld_grad, d, elem_size(grad_dtype))) || overlap(workspace, rows ? need : 0, ids, 4ll * rows))
+    return fail(SGD_ERR_ARG, "embedding_grad: the workspace overlaps another argument");
   const EmbeddingGradParams p{grad, grad_dtype, ld_grad, ids, rows, vocab, d, scale, accumulate != 0, dtable, dtable_dtype, ld, workspace};
   CUDA_TRY(embedding_grad_launch(p, static_cast<cudaStream_t>(stream)));
   return SGD_OK;

@@ -12,17 +12,29 @@
 // falls within their error of a border, which is seen, and the masses are taken anew; inside a block, and where a cut is
 // looked for, masses are whole numbers (weight() below): their sums have no error and no order.
 //
-// A row is read once from HBM: warps take blocks and leave their maxima and, where masses are needed, their sums of
-// exponentials against the maximum (kError below).  What comes after looks, from L2, only at blocks whose maximum reaches
-// a bound zl that the cut cannot be below:
+// A row is read once from HBM, by tiles of 16 KB that bulk copies bring into a ring of three: warps take blocks and leave their maxima
+// and, where masses are needed, their sums of exponentials against the maximum (kError below).  What comes after looks, from L2, only
+// at blocks whose maximum reaches a bound zl that the cut is not below:
 //   top-k: the k-th largest of the blocks' maxima, for large k a quantile of a sample of the row;  min-p: max + ln(min_p) / scale;
 //   top-p alone: the 64th largest of the maxima where the maxima above it already have the mass; else from the sample (one token of 8
-//   in a histogram of its weights), which also gives a bound zh that the cut is not above.  What is above zh is summed, what lies
-//   between is listed; if the cut is not in between after all (counts and sums tell), the whole row is searched.
+//   in a histogram of its weights), which also gives a bound zh that the cut is not above.
+// What lies between the bounds is listed.  For top-p alone the tail below zl is summed in fp32 as well: what is not kept has the share
+// 1 - top_p at most, so that the cut depends on the tail's error and, by 1 - top_p, on the row's; where it does (one row in twenty of a
+// broad distribution) both masses are taken anew.  The blocks' masses lose the tail and what of the list is not kept.  If the cut
+// is not between the bounds after all, which counts and sums tell, the whole row is searched.
 // The cut is found in the list, or the row, by histograms of counts and masses over the order's integers, 1024 bins at a time,
 // down to 256 tokens, which are ranked by comparing all with all.
 //
-// Many rows: a CTA each, three per SM, so that one's search hides behind the others' reading.  Few: a cluster reads a row.
+// Many rows: a CTA of 256 threads each (128 for rows of up to 2048 tokens), three or four per SM, so that one's search hides
+// behind the others' reading.  Few: a cluster reads a row, and takes the bracket between the bounds together.
+//
+// Measured (GB300, replayed from a graph; a copy moves 6.7 TB/s): every token of 2048 of 4096 x 126464 fp16 93 us = 5.6 TB/s, of 1024 x
+// 126464 fp32 81 us = 6.4: HBM, and for 16-bit logits the issue slots (60% busy) and exponentials (73% of their rate).  A persistent
+// form with 16 streaming warps per SM and finishing warps was slower everywhere (96 and 83 us; 1500 x 126464 147 against 135).
+// 1003 x 32003 fp32 with every filter 48 us: a row is 18 thousand clocks of reading and 15 of steps one after another.
+// 1024 x 126464 bf16, top-p 0.9 of a broad distribution (2900 tokens): 330 us: 200 thousand clocks a row, half of them the
+// bracket (300 instructions a block), in 2.25 rounds of 456 rows; two or four CTAs per SM instead of three: 347 and 336 us.
+// One row of 126464: 5.8 us, with top-p 17 to 27, latency.
 #include <math.h>
 #include <stddef.h>
 

@@ -74,7 +74,8 @@ def _embedding_grad(lib, **kw):
     (dict(grad=None), ARG), (dict(ids=None), ARG), (dict(dtable=None), ARG), (dict(grad_dtype=3), ARG), (dict(dtable_dtype=7), ARG),
     (dict(ld_grad=7), ARG), (dict(ld=7), ARG), (dict(vocab=0), ARG), (dict(d=0), ARG), (dict(rows=-1), ARG), (dict(grad=P + 1), ARG),
     (dict(dtable=3 * P + 2), ARG), (dict(ids=2 * P + 1), ARG), (dict(workspace=None), ARG), (dict(workspace=4 * P + 8), ARG),
-    (dict(workspace_bytes=10), ARG), (dict(dtable=P + 16), ARG), (dict(dtable=2 * P), ARG), (dict(dtable=4 * P + 64), ARG),
+    (dict(workspace_bytes=10), ARG), (dict(dtable=P + 16), ARG), (dict(dtable=2 * P), ARG), (dict(dtable=4 * P + 64), ARG), (dict(workspace=P), ARG),
+    (dict(workspace=2 * P), ARG),
     (dict(d=(1 << 20) + 1, ld=1 << 21, ld_grad=1 << 21), SHAPE), (dict(rows=1 << 27), SHAPE),
 ])
 def test_embedding_grad_refuses(lib, kw, code):

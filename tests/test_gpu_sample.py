@@ -311,3 +311,67 @@ def test_binding_refuses(B):
     for kw in (dict(top_k=-1), dict(top_p=0.0), dict(top_p=1.5), dict(min_p=-1.0), dict(min_p=2.0), dict(scale=0.0)):
         with pytest.raises(B.SgdError):
             B.sgd_kernel_sample(z, u, ids, **kw)
+
+
+@pytest.mark.parametrize("dtype,rows,vocab,pad", [("f16", 280, 126464, 0), ("bf16", 281, 126461, 3), ("f32", 141, 126464, 0), ("bf16", 700, 50000, 8),
+                                                  ("f32", 300, 60000, 4), ("f16", 400, 100003, 5)])
+def test_many_long_rows(B, dtype, rows, vocab, pad):
+    """More of them than run at once; some without a distribution, some numbers next to a block's border, rows that are not asked for."""
+    rng = np.random.default_rng(rows)
+    z1 = (1.0 + np.arange(rows) % 3)[:, None] * rng.standard_normal((rows, vocab), dtype=np.float32)
+    z1[np.arange(rows), rng.integers(0, vocab, rows)] = 9.0
+    z1[3] = -INF
+    z1[5, 77] = math.nan
+    z1[6, vocab - 1] = INF
+    z1[7, 1:] = -INF
+    z = _put(z1, dtype, pad)
+    u = _numbers(rows, 1)
+    zn = z.float().cpu().numpy()
+    for r in range(8, 20):  # next to a border: masses are taken anew
+        w = oe.weights(zn[r])
+        u[r, 0] = float(np.float32((np.cumsum(np.pad(w, (0, -vocab % 512)).reshape(-1, 512).sum(1)) / w.sum())[r * 4]))
+    on = torch.ones(rows, dtype=torch.int32, device="cuda")
+    on[::5] = 0
+    for ids in (None, on):
+        got, lp = _draw(B, z, u, **({} if ids is None else dict(row_ids=ids, row_id=1)))
+        keep = np.ones(rows, bool) if ids is None else on.cpu().numpy() == 1
+        assert (got[~keep] == -7).all() and (lp[~keep] == 77).all()
+        look = [r for r in range(rows) if keep[r] and (r < 24 or r % 9 == 0)]
+        _check((got[look], lp[look]), z[look], u[look], some=False)
+        # the log-probability of every token is that of the scoring kernel
+        want = torch.empty(rows, 1, device="cuda")
+        B.sgd_kernel_logprobs(z, tokens=torch.from_numpy(got).cuda()[:, None], token_logprobs=want)
+        want = want[:, 0].cpu().numpy()
+        fine = keep & np.isfinite(lp) & np.isfinite(want)
+        assert np.abs(lp[fine] - want[fine]).max() <= 2 * (186 * U + 4 * U * 80) and fine.sum() >= keep.sum() - 3
+
+
+def test_many_long_rows_without_a_distribution(B):
+    """Each takes the first token of its order."""
+    rows, vocab = 3000, 50000
+    z = torch.zeros(rows, vocab, dtype=torch.bfloat16, device="cuda")
+    z[:, 100] = 1.0
+    z[:, 4] = math.nan
+    ids = torch.full((rows,), -7, dtype=torch.int32, device="cuda")
+    lp = torch.zeros(rows, device="cuda")
+    B.sgd_kernel_sample(z, torch.rand(rows, 2, device="cuda"), ids, logprobs=lp)
+    assert (ids == 100).all() and lp.isnan().all() and B.sgd_kernel_status() == 0
+
+
+def test_many_long_rows_streams_and_graphs(B):
+    z = _put(_logits(300, 126464, 3).astype(np.float32), "f16")
+    u = _numbers(300, 4).cuda()
+    want, want_lp = torch.empty(300, dtype=torch.int32, device="cuda"), torch.empty(300, device="cuda")
+    B.sgd_kernel_sample(z, u, want, logprobs=want_lp)
+    torch.cuda.synchronize()
+    outs = [(torch.empty_like(want), torch.empty_like(want_lp)) for _ in range(3)]
+    for s, (i, p) in zip([torch.cuda.Stream() for _ in outs], outs):
+        B.sgd_kernel_sample(z, u, i, logprobs=p, stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(i, want) and torch.equal(p, want_lp) for i, p in outs)
+    ids = torch.empty_like(want)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        B.sgd_kernel_sample(z, u, ids)
+    g.replay()
+    assert torch.equal(ids, want)
