@@ -701,6 +701,23 @@ static const int g_f16_clamp_registered = register_f16_clamp_flag(&f16_clamp_fla
 bool& pdl_flag();
 int64_t& pdl_launches();  // the calling thread's launches with the attribute
 
+// A launch behind another of the same call on the stream, with the attribute whatever pdl_flag() says: both kernels begin with
+// pdl_wait_and_trigger().
+template <typename... KArgs, typename... Args>
+static inline cudaError_t launch_behind(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
 template <typename... KArgs, typename... Args>
 static inline cudaError_t launch_k(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem,
                                    cudaStream_t s, Args... args) {

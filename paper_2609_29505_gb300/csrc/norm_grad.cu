@@ -147,6 +147,7 @@ __device__ __forceinline__ float3 group_sum(float3 v, float (*red)[3], int warp_
 template <typename T, int G, bool WIDE, bool MOD, bool PARAMS>
 __global__ void __launch_bounds__(kThreads, ctas_per_sm(WIDE)) norm_grad_kernel(const Args a) {
   constexpr int NV = vectors_of(WIDE), kGroups = kThreads / G, kGroupWarps = G / 32;
+  pdl_wait_and_trigger();
   using Raw = typename Four<T>::Raw;
   __shared__ float red[2][kThreads / 32][3];
   const NormGradParams& p = a.p;
@@ -400,6 +401,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(WIDE)) norm_grad_kernel(
 // The units' sums added up: CTA (columns, sample) for dshift and dscale, CTA (columns, the last one) for dg and db.
 __global__ void __launch_bounds__(256) norm_grad_sums_kernel(const Args a) {
   __shared__ float4 red[2][kShares][kColsPerCta / 4];
+  pdl_wait_and_trigger();
   const NormGradParams& p = a.p;
   const int lane = threadIdx.x & 3, share = threadIdx.x >> 2;
   const int i = blockIdx.x * (kColsPerCta / 4) + lane, nv = p.d >> 2;
@@ -507,8 +509,7 @@ cudaError_t norm_grad_launch(const NormGradParams& p, cudaStream_t s) {
   if (e != cudaSuccess || !params) return e;
   const int jobs = 1 + (p.scale && (p.dshift || p.dscale) ? a.q.samples : 0);
   const dim3 grid((p.d + kColsPerCta - 1) / kColsPerCta, jobs < 1024 ? jobs : 1024);
-  norm_grad_sums_kernel<<<grid, 256, 0, s>>>(a);
-  return cudaGetLastError();
+  return launch_behind(norm_grad_sums_kernel, grid, dim3(256), 0, s, a);
 }
 
 }  // namespace sgd

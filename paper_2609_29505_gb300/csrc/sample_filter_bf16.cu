@@ -1,0 +1,8 @@
+// Filtered draws of bf16 logits (sample.cu).
+#include "sample_kernel.cuh"
+
+namespace sgd {
+namespace rows {
+template cudaError_t sample_rows<bf16, true>(const SampleArgs&, cudaStream_t);
+}  // namespace rows
+}  // namespace sgd

@@ -122,7 +122,7 @@ def test_gradient(B, rows, vocab, d, dtype, out, accumulate):
 
 
 @pytest.mark.parametrize("hot", [0.0, 0.5, 1.0])
-@pytest.mark.parametrize("rows", [1, 2, 15, 16, 17, 31, 33, 255, 1000, 2049, 4096, 8191, 8192, 8193, 10000, 20481, 70001])
+@pytest.mark.parametrize("rows", [1, 2, 15, 16, 17, 31, 33, 255, 1000, 2049, 4096, 6143, 6144, 6145, 8191, 8192, 8193, 10000, 20481, 70001])
 def test_gradient_of_many_rows(B, rows, hot):
     """Either sort; tokens whose rows fill chunks, end at their borders or pass many of them."""
     for vocab in (3, 700) if rows > 5000 else (1, 3, 255, 256, 257, 70000):

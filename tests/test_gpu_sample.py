@@ -89,7 +89,7 @@ def _check(got, z, u, some=True, **kw):
     assert not some or len(z) < 8 or far * 2 >= len(z)
 
 
-SIZES = [(1, 1), (3, 2), (5, 8), (4, 65), (3, 511), (3, 512), (3, 513), (9, 1000), (3, 1024), (2, 1025), (200, 1000), (1, 4099),
+SIZES = [(1, 1), (3, 2), (5, 8), (4, 65), (3, 511), (3, 512), (3, 513), (9, 1000), (3, 1024), (2, 1025), (200, 1000), (9, 2047), (700, 900), (5, 8192), (5, 8193), (1, 4099),
          (7, 16385), (3, 32003), (1, 126464), (3, 126464), (20, 126464), (160, 20011)]
 FILTERS = [dict(), dict(top_k=1), dict(top_k=50), dict(top_p=0.9), dict(min_p=0.05), dict(top_k=40, top_p=0.8, min_p=0.01),
            dict(top_p=0.95, min_p=0.002), dict(top_k=700), dict(top_k=700, top_p=0.97), dict(top_k=3000, top_p=0.99), dict(min_p=1e-4),
@@ -375,3 +375,35 @@ def test_many_long_rows_streams_and_graphs(B):
         B.sgd_kernel_sample(z, u, ids)
     g.replay()
     assert torch.equal(ids, want)
+
+
+@pytest.mark.parametrize("dtype,vocab", [("f16", 3 << 19), ("f32", 3 << 18), ("bf16", 1000003)])
+def test_longest_rows(B, dtype, vocab):
+    """Rows of 3 MiB, by a cluster and by CTAs of their own; the same rows at odd addresses."""
+    rng = np.random.default_rng(2)
+    z1 = (2.0 * rng.standard_normal((3, vocab), dtype=np.float32))
+    z1[:, rng.integers(0, vocab, 30)] = 10.0 + 4.0 * rng.random(30, dtype=np.float32)
+    z1[2] *= 0.1
+    u = _numbers(3, 8)
+    for offset in (0, 1):
+        z = _put(z1, dtype, offset=offset)
+        for kw in (dict(), dict(top_k=50), dict(top_k=3000), dict(top_p=0.9), dict(min_p=0.01), dict(top_k=40, top_p=0.9, min_p=0.02)):
+            # (NEAR is for 2^17 tokens; half a unit of 2^-43 each, 1.6 million are off by 9e-8)
+            ids, _ = _draw(B, z, u, **kw)
+            for r in range(3):
+                want, _, near = oe.sample(z[r].double().cpu().numpy(), u[r].double().numpy(), **kw)
+                assert ids[r] == want or near <= 12 * NEAR, (kw, r, ids[r], want, near)
+    many = z[:1].expand(700, vocab).contiguous()
+    got, _ = _draw(B, many, u[:1].expand(700, 2).contiguous(), top_p=0.5)
+    assert (got == got[0]).all()
+
+
+@pytest.mark.parametrize("kw", [dict(top_p=1e-300), dict(top_p=1e-12), dict(top_p=1 - 2 ** -53), dict(top_p=1 - 1e-9), dict(min_p=1e-300), dict(min_p=1e-12, top_p=0.5),
+                                dict(top_k=2 ** 31 - 1), dict(top_k=1, top_p=0.5, min_p=1.0)])
+@pytest.mark.parametrize("rows,vocab", [(3, 900), (3, 9000), (2, 50000), (200, 50000)])
+def test_filters_at_their_ends(B, rows, vocab, kw):
+    z = _put(_logits(rows, vocab, 17), "f32")
+    u = _numbers(rows, 5)
+    few = slice(0, min(rows, 9))
+    ids, lp = _draw(B, z, u, **kw)
+    _check((ids[few], lp[few]), z[few], u[few], some=False, **kw)
