@@ -11,9 +11,10 @@
 //            unless they are kept, CTAs that clear the rows of the tokens that do not occur: a range of the table each.
 //   join     adds the partial sums of such a run in the order of the chunks.
 //
-// Measured (GB300; a copy moves 6.7 TB/s): 4096 rows, half of them of one token, for a table of 126464 x 4096 bf16: 190 us, 168 of them sums and
+// Measured (GB300; a copy moves 6.7 TB/s): 4096 rows, half of them of one token, for a table of 126464 x 4096 bf16: 187 us, 167 of them sums and
 // cleared rows (1.07 GB, 6.2 TB/s; a kernel of its own that cleared the table by 16-byte stores took 266 us).  65537 x 1024 for
-// 32003 tokens: 88 us, 54 of them the sums (a thread's 16 rows at once; 8: 84 us), 27 the sort, 15 the join.
+// 32003 tokens: 83 us, 54 of them the sums (a thread's 16 rows at once; 8: 84 us).  The launches of a call overlap their starts and
+// ends (programmatic dependent launch): 88 us without.
 #include <atomic>
 
 #include "common.cuh"

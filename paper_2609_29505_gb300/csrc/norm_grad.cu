@@ -10,8 +10,8 @@
 // order.  The statistics are taken anew from h, which has to be read for xhat anyway.
 //
 // HBM bounds it, and the chain of a row (statistics, two sums, the result) where rows are few: 4096 x 4096 with bf16 dout and a
-// residual 40 us = 5.9 TB/s of 6.7, and 7 us for 304 pairs of sums; 2048 x 1152 modulated, 8 samples: 14 us for 5 rows a
-// group one after another, and 5 us.
+// residual 44.5 us, 39 of them the rows (6.0 TB/s of 6.7), the rest 304 pairs of sums; 2048 x 1152 modulated, 8 samples: 15 us, 14 for 5
+// rows a group one after another.
 #include <atomic>
 
 #include "common.cuh"
