@@ -54,8 +54,9 @@ cudaError_t rows_of_type(const SampleArgs& a, cudaStream_t s) {
 }  // namespace
 
 cudaError_t sample_launch(const SampleParams& p, cudaStream_t s) {
-  const double c = static_cast<double>(p.scale) * 1.4426950408889634073599;
-  SampleArgs a{p, static_cast<float>(c), 0.f, p.min_p > 0.0 ? log(p.min_p) / static_cast<double>(p.scale) : -HUGE_VAL,
+  const float f = p.scale < 0x1p-64f ? 0x1p-64f : 1.f, scale = p.scale / f;
+  const double c = static_cast<double>(scale) * 1.4426950408889634073599;
+  SampleArgs a{p, f, static_cast<float>(c), 0.f, scale, p.min_p > 0.0 ? log(p.min_p) / static_cast<double>(p.scale) : -HUGE_VAL,
                (p.vocab + SGD_SAMPLE_BLOCK - 1) / SGD_SAMPLE_BLOCK, device_status_ptr()};
   a.c_lo = static_cast<float>(c - static_cast<double>(a.c));
   if (p.dtype == SGD_F16) return rows_of_type<f16>(a, s);

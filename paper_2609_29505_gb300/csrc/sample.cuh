@@ -8,7 +8,11 @@ namespace rows {
 
 struct SampleArgs {
   SampleParams p;
-  float c, c_lo;    // scale log2(e), as the sum of two floats
+  // Exponents are (z - m) f c in base 2.  f is 1, or 2^-64 for scales below: there logits may lie as far apart as their type has them, farther
+  // than an fp32 difference holds, and still both have a share; and the product scale log2(e) may have few bits.
+  float f;
+  float c, c_lo;    // scale log2(e) / f, as the sum of two floats
+  float scale;      // scale / f
   double drop;      // ln(min_p) / scale: a token at or above max + drop passes (-inf: every token)
   int n_blocks;
   int* status;

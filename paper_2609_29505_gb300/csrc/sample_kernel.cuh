@@ -38,14 +38,14 @@ static __constant__ uint64_t kPow2[32] = {
 };
 
 // Weight 2^((z - m) c) of a logit against the row's maximum m as a whole number, 2^43 for the maximum: exact to about 2^-31
-// relative and half a unit.  z - m = d + dl exactly, (d + dl) c = t + tl to 2^-45; t + tl = n + j / 32 + g with |g| <= 1/64;
-// 2^g - 1 = g ln2 + ... to the fourth power (the fifth is 1.3e-12).
+// relative and half a unit.  (z - m) f = d + dl exactly, (d + dl) c = t + tl to 2^-45; t + tl = n + j / 32 + g with |g| <= 1/64;
+// 2^g - 1 = g ln2 + ... to the fourth power (the fifth is 1.3e-12).  (With the factor f = 1 an fma is the difference.)
 __device__ __forceinline__ uint64_t weight(float z, float m, const SampleArgs& a, const uint64_t* pow2) {
-  const float d = z - m;
+  const float mf = __fmul_rn(m, a.f), d = fmaf(z, a.f, -mf);
   const float t = __fmul_rn(d, a.c);
   if (!(t > -48.f)) return 0;
-  const float back = d - z;
-  const float dl = (z - (d - back)) + (-m - back);
+  const float back = fmaf(-z, a.f, d);
+  const float dl = fmaf(z, a.f, back - d) + (-mf - back);
   const float tl = fmaf(d, a.c, -t) + fmaf(d, a.c_lo, dl * a.c);
   constexpr float kMagic = 393216.f;  // 1.5 2^18: its unit is 1/32
   const float y = __fadd_rn(t, kMagic);
@@ -179,31 +179,32 @@ __device__ __forceinline__ float warp_max_nan(float m) {
   return d;
 }
 
-// Sum over a lane's tokens of 2^((z - m) c).
+// Sum over a lane's tokens of 2^((z - m) f c).
 template <typename T>
-__device__ __forceinline__ float raw_sum(const Raw<T>& r, float m, float c) {
-  const uint64_t m2 = pack_f32x2(-m, -m), c2 = pack_f32x2(c, c), none = pack_f32x2(-0.f, -0.f);
+__device__ __forceinline__ float raw_sum(const Raw<T>& r, float m, float f, float c) {
+  const float mf = __fmul_rn(m, f);
+  const uint64_t m2 = pack_f32x2(-mf, -mf), f2 = pack_f32x2(f, f), c2 = pack_f32x2(c, c), none = pack_f32x2(-0.f, -0.f);
   uint64_t s[2] = {pack_f32x2(0.f, 0.f), pack_f32x2(0.f, 0.f)};
   float z[kPerLane];
   numbers(r, z);
 #pragma unroll
   for (int j = 0; j < kPerLane; j += 2) {
     // (one rounding each: a product is not contracted into the difference)
-    const uint64_t t = fma_f32x2(add_f32x2(pack_f32x2(z[j], z[j + 1]), m2), c2, none);
+    const uint64_t t = fma_f32x2(fma_f32x2(pack_f32x2(z[j], z[j + 1]), f2, m2), c2, none);
     s[j / 2 & 1] = add_f32x2(s[j / 2 & 1], pack_f32x2(ex2_approx(lo_f32x2(t)), ex2_approx(hi_f32x2(t))));
   }
   return sum_f32x2(add_f32x2(s[0], s[1]));
 }
 
 // Maxima and sums of two blocks (or of one), in lanes 0 .. 15 those of the first (or in all): the maximum is NaN where it is not
-// below +inf; the sum of 2^((z - maximum) c) is 0 where there is no token, and where SUMS is not.
+// below +inf; the sum of 2^((z - maximum) f c) is 0 where there is no token, and where SUMS is not.
 template <typename T, int kPair>
-__device__ __forceinline__ float2 block_stats(const Raw<T>* r, bool sums, float c, int lane) {
+__device__ __forceinline__ float2 block_stats(const Raw<T>* r, bool sums, float f, float c, int lane) {
   float m[kPair], s[kPair];
 #pragma unroll
   for (int u = 0; u < kPair; ++u) m[u] = warp_max_nan(raw_max(r[u]));
 #pragma unroll
-  for (int u = 0; u < kPair; ++u) s[u] = sums ? raw_sum(r[u], m[u], c) : 0.f;
+  for (int u = 0; u < kPair; ++u) s[u] = sums ? raw_sum(r[u], m[u], f, c) : 0.f;
   float v = s[0], most = m[0];
   if (kPair == 2) {
     const bool second = lane >= 16;
@@ -495,12 +496,13 @@ struct Row {
            [&](int b, const Raw<T>& raw) {
              if constexpr (TAIL) {
                float z[kPerLane], s[2] = {0.f, 0.f};
+               const float zf = __fmul_rn(zl, a.f);
                numbers(raw, z);
                uint32_t on = 0;
 #pragma unroll
                for (int j = 0; j < kPerLane; ++j) {
                  const bool low = z[j] < zl;
-                 s[j & 1] += low ? ex2_approx(__fmul_rn(z[j] - zl, a.c)) : 0.f;
+                 s[j & 1] += low ? ex2_approx(__fmul_rn(fmaf(z[j], a.f, -zf), a.c)) : 0.f;
                  on |= !low && z[j] <= zh ? 1u << j : 0u;
                }
                if (zl == -kInf) on = marks(b, raw, zl);
@@ -553,9 +555,10 @@ struct Row {
         const Raw<T> raw = fetch<T, VEC>(row, a.p.vocab, b, lane);
         if (TAIL && zl > -kInf) {
           float z[kPerLane], s[2] = {0.f, 0.f};
+          const float zf = __fmul_rn(zl, a.f);
           numbers(raw, z);
 #pragma unroll
-          for (int j = 0; j < kPerLane; ++j) s[j & 1] += z[j] < zl ? ex2_approx(__fmul_rn(z[j] - zl, a.c)) : 0.f;
+          for (int j = 0; j < kPerLane; ++j) s[j & 1] += z[j] < zl ? ex2_approx(__fmul_rn(fmaf(z[j], a.f, -zf), a.c)) : 0.f;
           const float all = warp_sum(s[0] + s[1]);
           if (lane == 0) {
             const uint64_t w = times(all, w_zl);
@@ -698,7 +701,7 @@ struct Row {
         }
       }
       p.ids[r] = id;
-      if (p.logprobs) p.logprobs[r] = (z_id - m) * p.scale - logf(static_cast<float>(whole) * (1.f / (1ull << kOne)));
+      if (p.logprobs) p.logprobs[r] = fmaf(z_id, a.f, -__fmul_rn(m, a.f)) * a.scale - logf(static_cast<float>(whole) * (1.f / (1ull << kOne)));
     }
   }
 
@@ -879,7 +882,7 @@ struct Row {
     if (threadIdx.x < 2) sh.edge[threadIdx.x] = kHist;
     team_sync<kThreads>();
     const int all = runs * kThreads;
-    const float step = static_cast<float>(vocab - 8) / static_cast<float>(all), c32 = a.c * 32.f;
+    const float step = static_cast<float>(vocab - 8) / static_cast<float>(all), c32 = a.c * 32.f, mf = __fmul_rn(m, a.f);
     constexpr int kAhead = 4, kV = 8 / Elem<T>::kPer;  // loads on their way
     for (int k0 = 0; k0 < runs; k0 += kAhead) {
       uint4 v[kAhead][kV];
@@ -903,12 +906,14 @@ struct Row {
 #pragma unroll
         for (int i = 0; i < kV; ++i) unpack(v[u][i], z + i * Elem<T>::kPer, static_cast<const T*>(nullptr));
 #pragma unroll
-        for (int j = 0; j < 8; ++j) atomicAdd(&sh.count[static_cast<int>(fminf((m - z[j]) * c32, kHist - 1.f))], 1u);
+        for (int j = 0; j < 8; ++j) atomicAdd(&sh.count[static_cast<int>(fminf(fmaf(-z[j], a.f, mf) * c32, kHist - 1.f))], 1u);
       }
     }
     team_sync<kThreads>();
     return 8 * all;
   }
+  // The value that lies bins / 32 of an octave below the maximum (-inf: out of fp32's range).
+  __device__ float below_max(int bins) const { return (__fmul_rn(m, a.f) - bins / (32.f * a.c)) / a.f; }
   // A value that about 1.3 k + 400 tokens reach, from the sample.
   __device__ float sampled_bound_of_k(int k) const {
     constexpr int kPer = kHist / kThreads;
@@ -932,7 +937,7 @@ struct Row {
       if (up + n[j] >= want) atomicMin(&sh.edge[0], static_cast<int>(threadIdx.x) * kPer + j + 1);
     team_sync<kThreads>();
     const int edge = sh.edge[0];
-    return edge >= kHist ? -kInf : m - edge / (32.f * a.c);
+    return edge >= kHist ? -kInf : below_max(edge);
   }
   // Bounds {zl, zh} on the cut by mass, from the sample: tokens below the cut have the mass `share` (of the maximum's weight)
   // together.  Nothing is lost where they are wrong but time.
@@ -1007,7 +1012,7 @@ struct Row {
     team_sync<kThreads>();
     const int zl = sh.edge[2], zh = sh.edge[3];
     team_sync<kThreads>();
-    return make_float2(zl >= kHist ? -kInf : m - zl / (32.f * a.c), zh <= 0 ? kInf : m - zh / (32.f * a.c));
+    return make_float2(zl >= kHist ? -kInf : below_max(zl), zh <= 0 ? kInf : below_max(zh));
   }
 };
 
@@ -1040,7 +1045,7 @@ __global__ void __launch_bounds__(kThreads, (FILTER ? 768 : 1024) / kThreads) sa
   }
   const uint32_t to_max = map_to_rank(smem_u32(max_of), 0), to_mass = map_to_rank(smem_u32(mass), 0);
   auto put = [&](const Raw<T>* cur, int b) {  // blocks b and b + kWarps
-    const float2 st = block_stats<T, kPair>(cur, sums, a.c, lane);
+    const float2 st = block_stats<T, kPair>(cur, sums, a.f, a.c, lane);
     const int at = kPair == 2 && lane >= 16 ? b + kWarps : b;
     if ((lane == 0 || (kPair == 2 && lane == 16)) && at < a.n_blocks) {
       if (FILTER && rank != 0) max_of[at] = st.x;  // (for this CTA's share of a bracket)

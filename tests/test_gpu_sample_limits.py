@@ -1,0 +1,62 @@
+"""sgd_kernel_sample on the GPU where its arithmetic is at its limits: logits as far apart as their type has them, at scales that bring
+them together, against oracle/ends.py in float64 (bounds as in test_gpu_sample.py)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import ends as oe
+from test_gpu_sample import B, FILTERS, _check, _draw, _numbers, _put  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def _wide(rows, vocab, scale, dtype, seed):
+    """Logits whose scaled values lie some units apart, or as far as the type has them; the last row a few far below all others."""
+    top = min(8.0 / scale, 3.3e38 if dtype != "f16" else 6e4)
+    z = np.random.default_rng(seed).uniform(-top, top, (rows, vocab))
+    z[-1, ::3] = -top
+    z[-1, 1::3] = top
+    return z
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [2.0 ** -63, 2.0 ** -64, 2.0 ** -65, 2.0 ** -100, 2.0 ** -118, 1e-38, 1.5e-39, 1e-41, 1e-45])
+def test_differences_beyond_the_type(B, scale, dtype):
+    """Differences of up to 6.6e38, which fp32 does not hold, at scales down to the smallest."""
+    scale = float(np.float32(scale))
+    for rows, vocab in ((5, 3), (9, 700), (5, 5000), (3, 40001)):
+        z = _put(_wide(rows, vocab, scale, dtype, vocab), dtype)
+        for i, kw in enumerate(FILTERS):
+            u = _numbers(rows, i)
+            _check(_draw(B, z, u, scale=scale, **kw), z, u, some=False, scale=scale, **kw)
+
+
+def test_few_and_many_long_rows_at_a_small_scale(B):
+    """By clusters, and by CTAs of their own."""
+    scale = float(np.float32(1e-38))
+    for rows in (1, 12, 300):
+        z = _put(_wide(rows, 60001, scale, "f32", rows), "f32")
+        few = slice(0, min(rows, 6))
+        for i, kw in enumerate(FILTERS):
+            u = _numbers(rows, i)
+            ids, lp = _draw(B, z, u, scale=scale, **kw)
+            _check((ids[few], lp[few]), z[few], u[few], some=False, scale=scale, **kw)
+
+
+@pytest.mark.parametrize("scale", [1e9, 1e37, 2e38])
+@pytest.mark.parametrize("rows", [3, 200])
+def test_large_scales_of_long_rows(B, scale, rows):
+    """All of the mass on the likeliest, or on those that equal it."""
+    rng = np.random.default_rng(rows)
+    z1 = rng.standard_normal((rows, 30011))
+    z1[1::2] = np.round(z1[1::2])
+    z = _put(z1, "f32")
+    few = slice(0, min(rows, 6))
+    for i, kw in enumerate(FILTERS):
+        u = _numbers(rows, i)
+        ids, lp = _draw(B, z, u, scale=scale, **kw)
+        zn = z[few].double().cpu().numpy()
+        for r in range(len(zn)):
+            want, want_lp, near = oe.sample(zn[r], u[r].double().numpy(), scale=scale, **kw)
+            assert 0 <= ids[r] < 30011 and (near <= 9e-9 or ids[r] == want), (i, r)
+            assert near <= 9e-9 or abs(lp[r] - want_lp) <= 1e-4
