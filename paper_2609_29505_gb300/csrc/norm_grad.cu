@@ -69,9 +69,10 @@ Plan make_plan(int rows, int d, int per) {
     q.parts = q.units = q.ctas;
     return q;
   }
+  if (per > rows) per = rows;  // one sample (whatever period says so: rows + per stays in 32 bits)
   q.per = per;
   q.samples = (rows + per - 1) / per;
-  const int longest = per < rows ? per : rows;
+  const int longest = per;
   q.parts = (most_ctas * q.groups + q.samples - 1) / q.samples;
   const int most = (longest + kRowsPerPart - 1) / kRowsPerPart;
   if (q.parts > most) q.parts = most;

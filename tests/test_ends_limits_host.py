@@ -1,0 +1,27 @@
+"""The operators at a token model's two ends at the limits of their arguments, as far as no device is needed."""
+import ctypes as C
+
+import pytest
+
+from paper_2609_29505_gb300 import binding
+
+OK = binding.SGD_OK
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2609_29505_gb300 import build
+    build.build()
+    return binding.lib()
+
+
+@pytest.mark.parametrize("rows,d", [(1, 4), (64, 64), (65, 1152), (5000, 4096), ((1 << 27) - 1, 4)])
+def test_norm_grad_workspace_of_one_sample(lib, rows, d):
+    """Every period that holds all rows means one sample, up to the largest integer."""
+    n = C.c_int64(0)
+    assert lib.sgd_kernel_norm_grad_workspace(rows, d, rows, C.byref(n)) == OK
+    want = n.value
+    assert want > 0
+    for per in (rows + 1, 2 ** 31 - 1, 2 ** 31 - 48, 2 ** 31 - rows, 2 ** 31 - rows + 1):
+        assert lib.sgd_kernel_norm_grad_workspace(rows, d, min(per, 2 ** 31 - 1), C.byref(n)) == OK
+        assert n.value == want, per
