@@ -477,9 +477,9 @@ def sgd_kernel_embedding_grad(grad, ids, dtable, scale=1.0, accumulate=False, wo
 
 
 def sgd_kernel_norm_grad_workspace(rows, d, rows_per_batch=0) -> int:
-    """Bytes of workspace of sgd_kernel_norm_grad (rows_per_batch 0: without a modulation)."""
+    """Bytes of workspace of sgd_kernel_norm_grad (rows_per_batch 0: without a modulation; any number from rows on: one sample)."""
     n = C.c_int64(0)
-    check(lib().sgd_kernel_norm_grad_workspace(rows, d, rows_per_batch, C.byref(n)), "sgd_kernel_norm_grad_workspace")
+    check(lib().sgd_kernel_norm_grad_workspace(rows, d, min(rows_per_batch, 2 ** 31 - 1), C.byref(n)), "sgd_kernel_norm_grad_workspace")
     return int(n.value)
 
 
@@ -517,6 +517,7 @@ def sgd_kernel_norm_grad(dout, h, kind, dh=None, g=None, b=None, scale=None, row
     if scale is not None:
         if rows_per_batch < 1:
             raise ValueError("rows_per_batch must be positive")
+        rows_per_batch = min(rows_per_batch, max(rows, 1))  # (a longer period is one sample too, and may pass 32 bits)
         samples = -(-rows // rows_per_batch)
         at_scale, ld = _modulation(scale, "scale", samples, d, device)
         if dshift is not None:

@@ -25,3 +25,5 @@ def test_norm_grad_workspace_of_one_sample(lib, rows, d):
     for per in (rows + 1, 2 ** 31 - 1, 2 ** 31 - 48, 2 ** 31 - rows, 2 ** 31 - rows + 1):
         assert lib.sgd_kernel_norm_grad_workspace(rows, d, min(per, 2 ** 31 - 1), C.byref(n)) == OK
         assert n.value == want, per
+    for per in (2 ** 31, 2 ** 32 + 1, 2 ** 40):
+        assert binding.sgd_kernel_norm_grad_workspace(rows, d, per) == want
