@@ -736,9 +736,9 @@ cudaError_t embedding_grad_launch(const EmbeddingGradParams& p, cudaStream_t s) 
     if (e != cudaSuccess) return e;
   }
   // ranges of the table: several per SM
-  int fill_rows = (p.vocab + 8 * num_sms() - 1) / (8 * num_sms());
-  fill_rows = fill_rows < 4 ? 4 : (fill_rows > kFillRows ? kFillRows : fill_rows);
-  const int fill = p.accumulate ? 0 : (p.vocab + fill_rows - 1) / fill_rows;
+  const int64_t vocab = p.vocab, share = (vocab + 8 * num_sms() - 1) / (8 * num_sms());
+  const int fill_rows = share < 4 ? 4 : (share > kFillRows ? kFillRows : static_cast<int>(share));
+  const int fill = p.accumulate ? 0 : static_cast<int>((vocab + fill_rows - 1) / fill_rows);
   const SumArgs a{p.grad, p.ld_grad, tokens, order, p.rows, p.vocab, p.d, q.chunk, q.chunks, q.pd, p.accumulate, p.scale,
                   fill, fill_rows, reinterpret_cast<float*>(ws + q.partial), p.dtable, p.ld};
   if (p.grad_dtype == SGD_F16) return sums_to<f16>(a, p.dtable_dtype, s);
