@@ -448,7 +448,10 @@ def _workspace(workspace, need, device, stream):
                 workspace = torch.empty(need, dtype=torch.uint8, device=device)
         else:
             # (an integer handle: torch's allocator has to know which stream uses the memory)
-            st = torch.cuda.ExternalStream(stream, device=device) if isinstance(stream, int) else stream
+            # (and the default stream's handle is 0, of which ExternalStream makes another stream)
+            st = stream
+            if isinstance(stream, int):
+                st = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
             with torch.cuda.device(device), torch.cuda.stream(st):
                 workspace = torch.empty(need, dtype=torch.uint8, device=device)
         return workspace, need

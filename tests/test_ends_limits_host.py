@@ -2,6 +2,7 @@
 import ctypes as C
 
 import pytest
+import torch
 
 from paper_2609_29505_gb300 import binding
 
@@ -27,3 +28,23 @@ def test_norm_grad_workspace_of_one_sample(lib, rows, d):
         assert n.value == want, per
     for per in (2 ** 31, 2 ** 32 + 1, 2 ** 40):
         assert binding.sgd_kernel_norm_grad_workspace(rows, d, per) == want
+
+
+@pytest.mark.parametrize("handle,want", [(0, "default"), (7, "external 7"), ("an object", "an object")])
+def test_workspace_of_a_call_belongs_to_its_stream(monkeypatch, handle, want):
+    """torch's allocator gives memory to the next user of the stream that it was allocated on: that has to be the call's."""
+    import contextlib
+    on, got = [], []
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda h, device=None: f"external {h}" if h else "a stream of the pool")
+    monkeypatch.setattr(torch.cuda, "default_stream", lambda device=None: "default")
+    monkeypatch.setattr(torch.cuda, "device", lambda d: contextlib.nullcontext())
+
+    @contextlib.contextmanager
+    def stream(s):
+        on.append(s)
+        yield
+        on.pop()
+    monkeypatch.setattr(torch.cuda, "stream", stream)
+    monkeypatch.setattr(torch, "empty", lambda n, **kw: got.append((n, on[-1])))
+    assert binding._workspace(None, 64, torch.device("cuda:0"), handle)[1] == 64
+    assert got == [(64, want)]

@@ -31,3 +31,22 @@ def test_gradient_of_the_longest_table(B, vocab, dtype):
     out = torch.full((7, 1), 9.0, dtype=dtype, device="cuda")
     B.sgd_kernel_embedding(table, ids, out)
     assert out[:, 0].tolist() == [15.0, 6.0, 27.0, 15.0, 0.0, 27.0, 21.0]
+
+
+@pytest.mark.parametrize("which", ["none", "handle", "object", "other"])
+def test_workspace_of_a_call_belongs_to_its_stream(B, which):
+    """Memory that torch's allocator hands out again is ordered behind the call only on the stream that it was allocated on."""
+    other = torch.cuda.Stream()
+    stream = {"none": None, "handle": 0, "object": torch.cuda.default_stream(), "other": other.cuda_stream}[which]
+    want = other.cuda_stream if which == "other" else 0
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()  # (else the inputs come to lie in a large segment that an earlier test left, and the workspace beside them)
+    # (a workspace of 17 MB: larger than what is left over of a segment of torch's allocator)
+    grad, ids = torch.ones(1 << 16, 1024, device="cuda"), torch.zeros(1 << 16, dtype=torch.int32, device="cuda")
+    table = torch.empty(4, 1024, device="cuda")
+    before = {s["address"] for s in torch.cuda.memory_snapshot()}
+    B.sgd_kernel_embedding_grad(grad, ids, table, stream=stream)
+    new = [s["stream"] for s in torch.cuda.memory_snapshot() if s["address"] not in before]
+    torch.cuda.synchronize()
+    assert new and all(s == want for s in new)
+    assert (table[0] == 1 << 16).all() and (table[1:] == 0).all()
