@@ -319,8 +319,13 @@ def _tensor(t, name, dtype, shape, device):
     raise ValueError(f"{name} must be contiguous")
 
 
+def _size(rows, width, name):
+    if rows >= 2 ** 31 or width >= 2 ** 31:
+        raise ValueError(f"{name} has more rows or columns than a 32-bit integer holds")
+
+
 def _id(value, name):
-    """A token id as the library has it: ctypes would cut one of more than 32 bits down to another."""
+    """A token id or a size as the library has it: ctypes would cut one of more than 32 bits down to another."""
     if not -2 ** 31 <= value < 2 ** 31:
         raise ValueError(f"{name} must be a 32-bit integer")
     return value
@@ -334,6 +339,7 @@ def _rows(t, name):
     if t.dim() != 2 or not t.is_cuda:
         raise ValueError(f"{name} must be a 2-d tensor on a CUDA device")
     rows, vocab = t.shape
+    _size(rows, vocab, name)
     ld, step = t.stride()
     if step != 1 and vocab > 1:
         raise ValueError(f"the rows of {name} must be dense")
@@ -435,7 +441,7 @@ def sgd_kernel_embedding(table, ids, out, scale=1.0, stream=None):
 def sgd_kernel_embedding_grad_workspace(rows, vocab, d) -> int:
     """Bytes of workspace of sgd_kernel_embedding_grad."""
     n = C.c_int64(0)
-    check(lib().sgd_kernel_embedding_grad_workspace(rows, vocab, d, C.byref(n)), "sgd_kernel_embedding_grad_workspace")
+    check(lib().sgd_kernel_embedding_grad_workspace(_id(rows, "rows"), _id(vocab, "vocab"), _id(d, "d"), C.byref(n)), "sgd_kernel_embedding_grad_workspace")
     return int(n.value)
 
 
@@ -482,7 +488,7 @@ def sgd_kernel_embedding_grad(grad, ids, dtable, scale=1.0, accumulate=False, wo
 def sgd_kernel_norm_grad_workspace(rows, d, rows_per_batch=0) -> int:
     """Bytes of workspace of sgd_kernel_norm_grad (rows_per_batch 0: without a modulation; any number from rows on: one sample)."""
     n = C.c_int64(0)
-    check(lib().sgd_kernel_norm_grad_workspace(rows, d, min(rows_per_batch, 2 ** 31 - 1), C.byref(n)), "sgd_kernel_norm_grad_workspace")
+    check(lib().sgd_kernel_norm_grad_workspace(_id(rows, "rows"), _id(d, "d"), min(rows_per_batch, 2 ** 31 - 1), C.byref(n)), "sgd_kernel_norm_grad_workspace")
     return int(n.value)
 
 
@@ -511,6 +517,7 @@ def sgd_kernel_norm_grad(dout, h, kind, dh=None, g=None, b=None, scale=None, row
         raise ValueError("h must be a 2-d tensor on a CUDA device")
     shape, device = h.shape, h.device
     rows, d = shape
+    _size(rows, d, "h")
     code = _dtypes().get(dout.dtype)
     if code is None:
         raise TypeError(f"dout must be float16, bfloat16 or float32, not {dout.dtype}")

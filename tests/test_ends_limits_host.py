@@ -48,3 +48,38 @@ def test_workspace_of_a_call_belongs_to_its_stream(monkeypatch, handle, want):
     monkeypatch.setattr(torch, "empty", lambda n, **kw: got.append((n, on[-1])))
     assert binding._workspace(None, 64, torch.device("cuda:0"), handle)[1] == 64
     assert got == [(64, want)]
+
+
+class _Shape:
+    """What the checks see of a tensor on a device, without its memory."""
+    is_cuda, device, dtype = True, torch.device("cuda:0"), torch.float16
+
+    def __init__(self, *shape, dtype=torch.float16):
+        self.shape, self.dtype = torch.Size(shape), dtype
+
+    def dim(self):
+        return len(self.shape)
+
+    def stride(self):
+        return (self.shape[1], 1)
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        raise AssertionError("the address is not asked for")
+
+
+def test_sizes_of_more_than_32_bits_are_refused():
+    """The library's sizes are 32 bits: a table of 2^32 + 3 rows would be one of 3."""
+    many, wide, few = _Shape(2 ** 32 + 3, 1), _Shape(2, 2 ** 32 + 3), _Shape(4, 1)
+    ids = _Shape(4, dtype=torch.int32)
+    for call in (lambda: binding.sgd_kernel_sample(many, None, None), lambda: binding.sgd_kernel_sample(wide, None, None),
+                 lambda: binding.sgd_kernel_logprobs(many), lambda: binding.sgd_kernel_embedding(many, ids, few),
+                 lambda: binding.sgd_kernel_embedding(few, ids, many), lambda: binding.sgd_kernel_embedding_grad(few, ids, many),
+                 lambda: binding.sgd_kernel_embedding_grad(many, ids, few), lambda: binding.sgd_kernel_norm_grad(many, many, 0, dh=many),
+                 lambda: binding.sgd_kernel_norm_grad(few, wide, 0), lambda: binding.sgd_kernel_embedding_grad_workspace(2 ** 32 + 1, 8, 8),
+                 lambda: binding.sgd_kernel_embedding_grad_workspace(1, 2 ** 31, 8), lambda: binding.sgd_kernel_embedding_grad_workspace(1, 8, 2 ** 33),
+                 lambda: binding.sgd_kernel_norm_grad_workspace(2 ** 32 + 1, 8), lambda: binding.sgd_kernel_norm_grad_workspace(1, 2 ** 32 + 8)):
+        with pytest.raises(ValueError, match="32-bit"):
+            call()
