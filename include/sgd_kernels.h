@@ -20,6 +20,8 @@
  * sgd_sampler_reveal); and, for programs that train a token model's ends on that gradient, its embedding with the table's
  * gradient and the norms' backward pass.
  *
+ * Where an output must not overlap an argument, matrices may lie between one another's rows if they have one row stride.
+ *
  * All pointers are device pointers; all calls are asynchronous on `stream`
  * (a cudaStream_t) and return an sgd_status (sgd.h).  Arguments are validated on
  * the host (SGD_ERR_ARG / SGD_ERR_SHAPE); nothing is launched on a validation error.

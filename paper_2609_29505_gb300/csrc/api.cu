@@ -16,6 +16,7 @@
 #include <cstdio>
 #include <cstring>
 #include <functional>
+#include <initializer_list>
 #include <map>
 #include <memory>
 #include <mutex>
@@ -2027,6 +2028,40 @@ int sgd_kernel_distill(const void* logits, int dtype, int64_t ld, int rows, int 
   return SGD_OK;
 }
 
+namespace {
+
+// Memory of an argument: rows of `width` bytes, `stride` bytes apart (the products pass 64 bits for the largest rows and strides).
+using Wide = __int128;
+struct Span {
+  Wide at, rows, width, stride;
+};
+Span matrix(const void* at, int64_t rows, int64_t ld, int64_t width, int size) {
+  const Wide from = static_cast<Wide>(reinterpret_cast<uintptr_t>(at));
+  if (!at || rows < 1 || width < 1) return {from, 0, 0, 1};
+  if (ld == width || rows == 1) return {from, 1, static_cast<Wide>(rows) * width * size, 1};  // one piece
+  return {from, rows, static_cast<Wide>(width) * size, static_cast<Wide>(ld) * size};
+}
+Span vector(const void* at, int64_t n, int size = 4) { return matrix(at, 1, n, n, size); }
+// Whether two have a byte in common; matrices of different strides, whether what lies between their first and last bytes has.
+bool overlap(const Span& a, const Span& b) {
+  if (a.rows == 0 || b.rows == 0) return false;
+  if (a.at >= b.at + (b.rows - 1) * b.stride + b.width || b.at >= a.at + (a.rows - 1) * a.stride + a.width) return false;
+  if (a.rows > 1 && b.rows > 1 && a.stride != b.stride) return true;
+  // rows i of a and j of b have one where (i - j) S lies between d - a.width and d + b.width
+  const Wide S = a.rows > 1 ? a.stride : b.stride, d = b.at - a.at, from = d - a.width;
+  Wide k = from >= 0 ? from / S + 1 : -((-from + S - 1) / S) + 1;
+  if (k < 1 - b.rows) k = 1 - b.rows;
+  return k < a.rows && k * S < d + b.width;
+}
+using Spans = std::initializer_list<Span>;
+bool overlaps_any(const Span& a, const Spans& others) {
+  for (const Span& b : others)
+    if (overlap(a, b)) return true;
+  return false;
+}
+
+}  // namespace
+
 int sgd_kernel_sample(const void* logits, int dtype, int64_t ld, int rows, int vocab, float scale, int top_k, double top_p,
                       double min_p, const float* uniforms, const int32_t* row_ids, int row_id, int32_t* ids, float* logprobs,
                       void* stream) {
@@ -2045,13 +2080,6 @@ int sgd_kernel_sample(const void* logits, int dtype, int64_t ld, int rows, int v
 }
 
 namespace {
-
-// Bytes of rows that lie ld elements apart.
-int64_t extent(int rows, int64_t ld, int64_t width, int size) { return rows < 1 ? 0 : ((rows - 1) * ld + width) * size; }
-bool overlap(const void* a, int64_t an, const void* b, int64_t bn) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return a && b && an > 0 && bn > 0 && x < y + static_cast<uintptr_t>(bn) && y < x + static_cast<uintptr_t>(an);
-}
 
 // What the embedding's two operators ask of a matrix.
 int check_matrix(const std::string& name, const void* at, int dtype, int64_t ld, int rows, int d) {
@@ -2079,8 +2107,8 @@ int sgd_kernel_embedding(const void* table, int dtype, int64_t ld, int vocab, in
   if (rc) return rc;
   if (rows != 0 && !ids) return fail(SGD_ERR_ARG, "embedding: null ids");
   if (!al4(ids)) return fail(SGD_ERR_ARG, "embedding: ids must be 4-byte aligned");
-  const int64_t n = extent(rows, ld_out, d, elem_size(out_dtype));
-  if (overlap(out, n, table, extent(vocab, ld, d, elem_size(dtype))) || overlap(out, n, ids, 4ll * rows))
+  const Spans inputs = {matrix(table, vocab, ld, d, elem_size(dtype)), vector(ids, rows)};
+  if (overlaps_any(matrix(out, rows, ld_out, d, elem_size(out_dtype)), inputs))
     return fail(SGD_ERR_ARG, "embedding: out overlaps an input");
   if (rows == 0) return SGD_OK;
   const EmbeddingParams p{table, dtype, ld, vocab, d, ids, rows, scale, out, out_dtype, ld_out};
@@ -2108,11 +2136,10 @@ int sgd_kernel_embedding_grad(const void* grad, int grad_dtype, int64_t ld_grad,
   const int64_t need = embedding_grad_bytes(rows, d);
   if (rows != 0 && (!workspace || !al16(workspace) || workspace_bytes < need))
     return fail(SGD_ERR_ARG, "embedding_grad: a 16-byte aligned workspace of " + std::to_string(need) + " bytes is needed");
-  const int64_t n = extent(vocab, ld, d, elem_size(dtable_dtype));
-  if (overlap(dtable, n, grad, extent(rows, ld_grad, d, elem_size(grad_dtype))) || overlap(dtable, n, ids, 4ll * rows) ||
-      overlap(dtable, n, workspace, rows ? need : 0))
-    return fail(SGD_ERR_ARG, "embedding_grad: dtable overlaps another argument");
-  if (overlap(workspace, rows ? need : 0, grad, extent(rows, ld_grad, d, elem_size(grad_dtype))) || overlap(workspace, rows ? need : 0, ids, 4ll * rows))
+  const Spans inputs = {matrix(grad, rows, ld_grad, d, elem_size(grad_dtype)), vector(ids, rows)};
+  const Span out = matrix(dtable, vocab, ld, d, elem_size(dtable_dtype)), ws = vector(workspace, rows ? need : 0, 1);
+  if (overlaps_any(out, inputs) || overlap(out, ws)) return fail(SGD_ERR_ARG, "embedding_grad: dtable overlaps another argument");
+  if (overlaps_any(ws, inputs))
     return fail(SGD_ERR_ARG, "embedding_grad: the workspace overlaps another argument");
   const EmbeddingGradParams p{grad, grad_dtype, ld_grad, ids, rows, vocab, d, scale, accumulate != 0, dtable, dtable_dtype, ld, workspace};
   CUDA_TRY(embedding_grad_launch(p, static_cast<cudaStream_t>(stream)));
@@ -2145,10 +2172,9 @@ int sgd_kernel_norm_grad(const float* h, const void* dout, int dtype, int rows, 
     return fail(SGD_ERR_ARG, "norm_grad: h, dh, residual, dg, db and fp32 dout must be 16-byte, other dout 8-byte aligned");
   if ((reinterpret_cast<uintptr_t>(g) & 7u) || (reinterpret_cast<uintptr_t>(b) & 7u) || !al4(scale) || !al4(dshift) || !al4(dscale))
     return fail(SGD_ERR_ARG, "norm_grad: g and b must be 8-byte, the modulation's tensors 4-byte aligned");
-  const int64_t n = 4ll * rows * d;
-  if (overlap(dh, n, h, n) || overlap(dh, n, dout, static_cast<int64_t>(elem_size(dtype)) * rows * d) ||
-      (dh != residual && overlap(dh, n, residual, n)))
-    return fail(SGD_ERR_ARG, "norm_grad: dh overlaps an input without being the residual");
+  const int64_t n = static_cast<int64_t>(rows) * d;
+  const Spans inputs = {vector(h, n), vector(dout, n, elem_size(dtype)), vector(dh == residual ? nullptr : residual, n)};
+  if (overlaps_any(vector(dh, n), inputs)) return fail(SGD_ERR_ARG, "norm_grad: dh overlaps an input without being the residual");
   const bool sums = dg || db || dshift || dscale;
   const int64_t need = sums ? norm_grad_bytes(rows, d, scale ? rows_per_batch : 0) : 0;
   if (need > 0 && (!workspace || !al16(workspace) || workspace_bytes < need))

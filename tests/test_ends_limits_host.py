@@ -6,7 +6,8 @@ import torch
 
 from paper_2609_29505_gb300 import binding
 
-OK = binding.SGD_OK
+OK, ARG = binding.SGD_OK, binding.SGD_ERR_ARG
+P = 1 << 20  # an address that nothing reads
 
 
 @pytest.fixture(scope="module")
@@ -83,3 +84,16 @@ def test_sizes_of_more_than_32_bits_are_refused():
                  lambda: binding.sgd_kernel_norm_grad_workspace(2 ** 32 + 1, 8), lambda: binding.sgd_kernel_norm_grad_workspace(1, 2 ** 32 + 8)):
         with pytest.raises(ValueError, match="32-bit"):
             call()
+
+
+def _embedding(lib, **kw):
+    a = dict(table=P, dtype=1, ld=8, vocab=4, d=8, ids=P << 8, rows=2, scale=1.0, out=(P << 8) + 4, out_dtype=2, ld_out=8, stream=None)
+    a.update(kw)
+    return lib.sgd_kernel_embedding(*a.values())
+
+
+def test_overlaps_of_the_largest_matrices(lib):
+    """Extents that pass 64 bits: of 2^31 - 1 rows, 2^40 fp32 values apart."""
+    huge = dict(table=P, dtype=2, ld=1 << 40, vocab=2 ** 31 - 1, d=8, ids=P >> 1)
+    for row in (1, 3, 1 << 20):
+        assert _embedding(lib, **huge, rows=1, out=P + (row << 42) + 16) == ARG and b"overlaps" in lib.sgd_last_error()

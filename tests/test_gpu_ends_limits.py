@@ -50,3 +50,26 @@ def test_workspace_of_a_call_belongs_to_its_stream(B, which):
     torch.cuda.synchronize()
     assert new and all(s == want for s in new)
     assert (table[0] == 1 << 16).all() and (table[1:] == 0).all()
+
+
+def test_matrices_between_one_anothers_rows(B):
+    """Columns of one buffer: the rows looked up beside the table, the table's gradient beside the rows', a modulation's gradients beside it."""
+    gen = torch.Generator().manual_seed(2)
+    both = torch.randn(40, 96, generator=gen).cuda()
+    table, out, rest = both[:, :32], both[:30, 32:64], both[:, 64:].clone()
+    ids = torch.randint(0, 40, (30,), generator=gen, dtype=torch.int32).cuda()
+    before = table.clone()
+    B.sgd_kernel_embedding(table, ids, out, scale=2.0)
+    assert torch.equal(out, 2.0 * before[ids.long()]) and torch.equal(table, before) and torch.equal(both[:, 64:], rest)
+    grad, dtable = both[:30, 32:64], both[:, 64:]
+    want = torch.zeros(40, 32, device="cuda", dtype=torch.float64).index_add_(0, ids.long(), grad.double())
+    B.sgd_kernel_embedding_grad(grad, ids, dtable)
+    # (30 rows at most of a token, each sum rounded to 2^-24 of magnitudes of at most 30 times the largest)
+    assert (dtable.double() - want).abs().max() <= 30 * 30 * 2.0 ** -24 * float(grad.abs().max()) and torch.equal(table, before)
+    x, want = _run(B, 50, 64, "f32", "ln_plain", per=20, seed=4)
+    mod = torch.full((3, 200), 7.0, device="cuda")
+    mod[:, 4:68] = x.pop("scale")
+    dh = torch.empty_like(x["h"])
+    B.sgd_kernel_norm_grad(kind=2, rows_per_batch=20, scale=mod[:, 4:68], dh=dh, dshift=mod[:, 68:132], dscale=mod[:, 132:196], **x)
+    assert torch.equal(dh, want["dh"]) and torch.equal(mod[:, 68:132], want["dshift"]) and torch.equal(mod[:, 132:196], want["dscale"])
+    assert (mod[:, :4] == 7).all() and (mod[:, 196:] == 7).all()
