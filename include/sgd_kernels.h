@@ -296,7 +296,7 @@ SGD_API int sgd_kernel_distill(const void* logits, int dtype, int64_t ld, int ro
  * row_ids, row_id, the rows of logits and their limits as in sgd_kernel_logprobs.  -inf masks a token.  A row without a
  * distribution takes the first token of the order: one of -inf alone token 0 with ln p = -inf, one that holds NaN
  * (which ranks with -inf) or +inf its ln p = NaN.
- * No output may overlap an input or the other output.  No workspace: calls on several streams and replays of captured
+ * No output may overlap an input or the other output (SGD_ERR_ARG).  No workspace: calls on several streams and replays of captured
  * ones may overlap.  Results are the same on every run.
  */
 SGD_API int sgd_kernel_sample(const void* logits, int dtype, int64_t ld, int rows, int vocab, float scale, int top_k, double top_p,

@@ -2073,6 +2073,9 @@ int sgd_kernel_sample(const void* logits, int dtype, int64_t ld, int rows, int v
   if (!(min_p >= 0.0) || min_p > 1.0) return fail(SGD_ERR_ARG, "sample: min_p must be in 0..1");
   if (!al4(uniforms) || !al4(row_ids) || !al4(ids) || !al4(logprobs))
     return fail(SGD_ERR_ARG, "sample: pointers must be 4-byte aligned");
+  const Spans inputs = {matrix(logits, rows, ld, vocab, elem_size(dtype)), vector(uniforms, 2ll * rows), vector(row_ids, rows)};
+  if (overlaps_any(vector(ids, rows), inputs) || overlaps_any(vector(logprobs, rows), inputs) || overlap(vector(ids, rows), vector(logprobs, rows)))
+    return fail(SGD_ERR_ARG, "sample: an output overlaps another argument");
   if (rows == 0) return SGD_OK;
   const SampleParams p{logits, dtype, ld, rows, vocab, scale, top_k, top_p, min_p, uniforms, row_ids, row_id, ids, logprobs};
   CUDA_TRY(sample_launch(p, static_cast<cudaStream_t>(stream)));

@@ -86,6 +86,24 @@ def test_sizes_of_more_than_32_bits_are_refused():
             call()
 
 
+def _sample(lib, **kw):
+    a = dict(logits=P, dtype=0, ld=64, rows=8, vocab=60, scale=1.0, top_k=0, top_p=1.0, min_p=0.0, uniforms=2 * P, row_ids=3 * P, row_id=0,
+             ids=4 * P, logprobs=5 * P, stream=None)
+    a.update(kw)
+    return lib.sgd_kernel_sample(*a.values())
+
+
+@pytest.mark.parametrize("name", ["ids", "logprobs"])
+@pytest.mark.parametrize("at", [P, P + 4, P + 7 * 128 + 116, 2 * P, 2 * P + 60, 3 * P, 3 * P - 28, 3 * P + 28, P + 7 * 128 - 4])
+def test_sample_refuses_overlaps(lib, name, at):
+    assert _sample(lib, **{name: at}) == ARG and b"overlaps" in lib.sgd_last_error()
+
+
+def test_sample_refuses_outputs_that_overlap(lib):
+    for at in (4 * P, 4 * P + 28, 4 * P - 28):
+        assert _sample(lib, logprobs=at) == ARG and b"overlaps" in lib.sgd_last_error()
+
+
 def _embedding(lib, **kw):
     a = dict(table=P, dtype=1, ld=8, vocab=4, d=8, ids=P << 8, rows=2, scale=1.0, out=(P << 8) + 4, out_dtype=2, ld_out=8, stream=None)
     a.update(kw)
