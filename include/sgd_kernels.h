@@ -347,7 +347,7 @@ SGD_API int sgd_kernel_norm_grad_workspace(int rows, int d, int rows_per_batch, 
  * r / rows_per_batch.  d a multiple of 4, 4 <= d <= 4096; h, dh, residual, dg, db and fp32 dout 16-byte aligned, other dout,
  * g and b 8-byte aligned.  Sums are fp32 (over a share of the rows at a time, then over the shares) and the same on every run.
  * With rows = 0, dg and db are zeros.  workspace as in sgd_kernel_embedding_grad; none is needed where dh is the only
- * output.  No output may overlap another argument otherwise (SGD_ERR_ARG for dh on h, dout or residual).
+ * output.  Otherwise no output, nor the workspace, may overlap another argument (SGD_ERR_ARG).
  */
 SGD_API int sgd_kernel_norm_grad(const float* h, const void* dout, int dtype, int rows, int d, int kind, const void* g,
                                  const void* b, const float* scale, int ld_mod, int rows_per_batch, float eps,

@@ -2175,13 +2175,22 @@ int sgd_kernel_norm_grad(const float* h, const void* dout, int dtype, int rows, 
     return fail(SGD_ERR_ARG, "norm_grad: h, dh, residual, dg, db and fp32 dout must be 16-byte, other dout 8-byte aligned");
   if ((reinterpret_cast<uintptr_t>(g) & 7u) || (reinterpret_cast<uintptr_t>(b) & 7u) || !al4(scale) || !al4(dshift) || !al4(dscale))
     return fail(SGD_ERR_ARG, "norm_grad: g and b must be 8-byte, the modulation's tensors 4-byte aligned");
-  const int64_t n = static_cast<int64_t>(rows) * d;
-  const Spans inputs = {vector(h, n), vector(dout, n, elem_size(dtype)), vector(dh == residual ? nullptr : residual, n)};
+  const int64_t n = static_cast<int64_t>(rows) * d, samples = scale && rows > 0 ? (rows - 1) / rows_per_batch + 1 : 0;
+  const Spans inputs = {vector(h, n), vector(dout, n, elem_size(dtype)), vector(g, d, 2), vector(b, d, 2),
+                         matrix(scale, samples, ld_mod, d, 4), vector(dh == residual ? nullptr : residual, n)};
   if (overlaps_any(vector(dh, n), inputs)) return fail(SGD_ERR_ARG, "norm_grad: dh overlaps an input without being the residual");
+  const Spans outputs = {vector(dh, n), vector(dg, d), vector(db, d), matrix(dshift, samples, ld_dmod, d, 4), matrix(dscale, samples, ld_dmod, d, 4)};
+  for (const Span* o = outputs.begin() + 1; o != outputs.end(); ++o) {
+    bool clash = overlaps_any(*o, inputs);
+    for (const Span* other = outputs.begin(); other != o; ++other) clash |= overlap(*o, *other);
+    if (clash) return fail(SGD_ERR_ARG, "norm_grad: an output overlaps another argument");
+  }
   const bool sums = dg || db || dshift || dscale;
   const int64_t need = sums ? norm_grad_bytes(rows, d, scale ? rows_per_batch : 0) : 0;
   if (need > 0 && (!workspace || !al16(workspace) || workspace_bytes < need))
     return fail(SGD_ERR_ARG, "norm_grad: a 16-byte aligned workspace of " + std::to_string(need) + " bytes is needed");
+  const Span ws = vector(workspace, need, 1);
+  if (overlaps_any(ws, inputs) || overlaps_any(ws, outputs)) return fail(SGD_ERR_ARG, "norm_grad: the workspace overlaps another argument");
   if (rows == 0) {
     if (dg) CUDA_TRY(cudaMemsetAsync(dg, 0, sizeof(float) * d, static_cast<cudaStream_t>(stream)));
     if (db) CUDA_TRY(cudaMemsetAsync(db, 0, sizeof(float) * d, static_cast<cudaStream_t>(stream)));

@@ -1,5 +1,6 @@
 """The operators at a token model's two ends at the limits of their arguments, as far as no device is needed."""
 import ctypes as C
+import random
 
 import pytest
 import torch
@@ -102,6 +103,50 @@ def test_sample_refuses_overlaps(lib, name, at):
 def test_sample_refuses_outputs_that_overlap(lib):
     for at in (4 * P, 4 * P + 28, 4 * P - 28):
         assert _sample(lib, logprobs=at) == ARG and b"overlaps" in lib.sgd_last_error()
+
+
+def _norm_grad(lib, **kw):
+    a = dict(h=P, dout=2 * P, dtype=1, rows=6, d=8, kind=1, g=3 * P, b=4 * P, scale=5 * P, ld_mod=16, rows_per_batch=2, eps=1e-6,
+             residual=6 * P, dh=7 * P, dg=8 * P, db=9 * P, dshift=10 * P, dscale=11 * P, ld_dmod=16, workspace=12 * P, workspace_bytes=1 << 16,
+             stream=None)
+    a.update(kw)
+    return lib.sgd_kernel_norm_grad(*a.values())
+
+
+@pytest.mark.parametrize("name,at", [
+    ("dg", P), ("dg", P + 176), ("dg", 2 * P + 80), ("dg", 3 * P), ("db", 4 * P - 16), ("dg", 5 * P), ("dg", 6 * P), ("dg", 7 * P + 176), ("db", 8 * P + 16),
+    ("dshift", P), ("dshift", 5 * P), ("dshift", 5 * P + 28), ("dshift", 7 * P), ("dshift", 8 * P), ("dscale", 10 * P), ("dscale", 10 * P + 28),
+    ("dscale", 10 * P - 28), ("dscale", 3 * P), ("dh", 3 * P), ("dh", 5 * P), ("dh", 4 * P), ("dh", 8 * P - 32),
+    ("workspace", P), ("workspace", 2 * P), ("workspace", 3 * P), ("workspace", 5 * P + 128), ("workspace", 6 * P), ("workspace", 7 * P),
+    ("workspace", 8 * P), ("workspace", 10 * P + 64), ("workspace", 11 * P),
+])
+def test_norm_grad_refuses_overlaps(lib, name, at):
+    assert _norm_grad(lib, **{name: at}) == ARG and b"overlap" in lib.sgd_last_error()
+
+
+def test_overlaps_of_matrices(lib):
+    """dshift and scale as parts of one memory: refused where they have a byte in common, and where their strides differ and their
+    extents meet.  (Without a workspace: what is not refused for the overlap is for that, and nothing is launched.)"""
+    rng = random.Random(3)
+    seen = {True: 0, False: 0}
+    for _ in range(3000):
+        rows, d = rng.randint(1, 7), 4 * rng.randint(1, 4)
+        per = rng.randint(1, 3)
+        samples = -(-rows // per)
+        ld = d + rng.choice([0, 1, 3, d, 2 * d])
+        ld2 = ld if rng.random() < 0.7 else d + rng.choice([0, 2, d])
+        at = 5 * P + 4 * rng.randint(-samples * ld - 3, samples * ld + 3)
+        a = {5 * P + 4 * (i * ld + j) for i in range(samples) for j in range(d)}
+        b = {at + 4 * (i * ld2 + j) for i in range(samples) for j in range(d)}
+        want = bool(a & b)
+        if ld != ld2 and ld != d and ld2 != d and samples > 1:
+            want = max(min(a), min(b)) <= min(max(a), max(b))
+        got = _norm_grad(lib, rows=rows, d=d, rows_per_batch=per, ld_mod=ld, ld_dmod=ld2, dshift=at, dscale=None, workspace=None)
+        assert got == ARG
+        assert (b"overlaps" in lib.sgd_last_error()) == want, (rows, d, per, ld, ld2, at)
+        assert want or b"workspace" in lib.sgd_last_error()
+        seen[want] += 1
+    assert min(seen.values()) > 300
 
 
 def _embedding(lib, **kw):
