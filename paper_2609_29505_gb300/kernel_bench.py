@@ -196,7 +196,7 @@ def case_distill(a):
 
 
 def _filters(a):
-    return dict(scale=1.0 / a.temperature, top_k=a.top_k, top_p=a.top_p, min_p=a.min_p)
+    return dict(scale=1.0 if a.temperature is None else 1.0 / a.temperature, top_k=a.top_k, top_p=a.top_p, min_p=a.min_p)
 
 
 def case_sample(a):
@@ -258,7 +258,7 @@ def _remask(a, cfg, model, logits):
          for s in range(1, T + 1)]
 
     draw = {}
-    if a.temperature != 1.0 or a.top_k or a.top_p < 1.0 or a.min_p:  # candidates are drawn, by numbers of their own at each step
+    if a.temperature is not None or a.top_k or a.top_p < 1.0 or a.min_p:  # candidates are drawn, by numbers of their own at each step
         draw = _filters(a)
         numbers = torch.rand(T, *shape, 2, device="cuda")
 
@@ -367,7 +367,8 @@ def main():
                     "norm_grad: of the rows that are written, of the table's gradient, of dout")
     ap.add_argument("--remask", default="", choices=["", "confidence", "entropy"],
                     help="trajectory of a token model: positions revealed by the model's own logits")
-    ap.add_argument("--temperature", type=float, default=1.0, help="sample, trajectory: candidates drawn at this temperature")
+    ap.add_argument("--temperature", type=float, default=None,
+                    help="sample, trajectory: candidates drawn at this temperature (none given: at 1, a trajectory only with a filter)")
     ap.add_argument("--top-k", type=int, default=0, help="sample, trajectory: from this many of the likeliest tokens (0: all)")
     ap.add_argument("--top-p", type=float, default=1.0, help="sample, trajectory: from the likeliest tokens with this share")
     ap.add_argument("--min-p", type=float, default=0.0, help="sample, trajectory: from tokens with this share of the likeliest one's")
