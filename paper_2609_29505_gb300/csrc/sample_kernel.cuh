@@ -56,7 +56,7 @@ __device__ __forceinline__ uint64_t weight(float z, float m, const SampleArgs& a
   const int64_t more = static_cast<int64_t>(static_cast<int32_t>(base >> 32)) * __float2int_rn(e * 4294967296.f);
   const uint64_t w = base + static_cast<uint64_t>(more);  // 2^62 .. 2^63
   const int shift = 62 - kOne - (k >> 5);
-  return shift > 62 ? 0 : (w + (1ull << (shift - 1))) >> shift;
+  return shift > 63 ? 0 : (w + (1ull << (shift - 1))) >> shift;
 }
 
 constexpr uint64_t kEverything = static_cast<uint64_t>(kKeyNegInf) << 32;  // the place that no token is behind

@@ -60,3 +60,18 @@ def test_large_scales_of_long_rows(B, scale, rows):
             want, want_lp, near = oe.sample(zn[r], u[r].double().numpy(), scale=scale, **kw)
             assert 0 <= ids[r] < 30011 and (near <= 9e-9 or ids[r] == want), (i, r)
             assert near <= 9e-9 or abs(lp[r] - want_lp) <= 1e-4
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("vocab", [2, 1500, 20000])
+def test_smallest_masses(B, vocab, dtype):
+    """Beside one token of weight 1, all others at 2^-43.9 (rounded to the unit 2^-43) or 2^-44.1 (none): at the number 1 the last token of
+    positive mass is drawn."""
+    for power, want in ((-43.1, vocab - 1), (-43.5, vocab - 1), (-43.9, vocab - 1), (-44.1, 0), (-44.5, 0), (-47.0, 0), (-60.0, 0)):
+        z1 = np.full((1, vocab), power * np.log(2.0))  # (fp16 has steps of 2^-6 there, 0.02 in base 2)
+        z1[0, 0] = 0.0
+        z = _put(z1, dtype)
+        u = torch.ones(1, 2)
+        for kw in (dict(), dict(min_p=1e-14), dict(top_k=vocab - 1) if vocab > 2 else dict()):
+            ids, _ = _draw(B, z, u, **kw)
+            assert ids[0] == (min(want, vocab - 2) if "top_k" in kw else want), (power, kw)
