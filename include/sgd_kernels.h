@@ -290,7 +290,7 @@ SGD_API int sgd_kernel_distill(const void* logits, int dtype, int64_t ld, int ro
  *     u0 mass(K), and the first token of K in b whose cumulative mass inside b (tokens ascending) is above u1 mass(b);
  *     the last one of positive mass where rounding leaves none.
  * With independent uniform numbers that is a draw from w over K, with the resolution of both.  Masses are compared as
- * sums of whole multiples of 2^-43 of the largest weight, each within 2^-30 of its value (tokens below 2^-44 have none).
+ * sums of whole multiples of 2^-43 of the largest weight, each within 2^-29 of its value and half of one (tokens below 2^-44 have none).
  *   ids int32 [rows] = the token;  logprobs fp32 [rows] (NULL: not wanted) = its ln p, p = softmax(x) over all tokens.
  * scale = 1 / temperature, 0 < scale <= 2e38.  top_k >= 0, 0 < top_p <= 1, 0 <= min_p <= 1 (else SGD_ERR_ARG).
  * row_ids, row_id, the rows of logits and their limits as in sgd_kernel_logprobs.  -inf masks a token.  A row without a

@@ -37,8 +37,9 @@ static __constant__ uint64_t kPow2[32] = {
     0x75606373EE921C97ull, 0x77F25CCDEE6D7AE6ull, 0x7A92BE8A92436616ull, 0x7D41D96DB915019Dull,
 };
 
-// Weight 2^((z - m) c) of a logit against the row's maximum m as a whole number, 2^43 for the maximum: exact to about 2^-31
-// relative and half a unit.  (z - m) f = d + dl exactly, (d + dl) c = t + tl to 2^-45; t + tl = n + j / 32 + g with |g| <= 1/64;
+// Weight 2^((z - m) c) of a logit against the row's maximum m as a whole number, 2^43 for the maximum: off by 2^-29
+// of itself and half a unit at most.  (Roundings of g, of the polynomial's last sum, of its product and of that as a whole number: at most 1.4, 1, 1
+// and 0.25 of 2^-31, and 0.1 of the rest; 2^-29.36 is the most that has been seen.)  (z - m) f = d + dl exactly, (d + dl) c = t + tl to 2^-45; t + tl = n + j / 32 + g with |g| <= 1/64;
 // 2^g - 1 = g ln2 + ... to the fourth power (the fifth is 1.3e-12).  (With the factor f = 1 an fma is the difference.)
 __device__ __forceinline__ uint64_t weight(float z, float m, const SampleArgs& a, const uint64_t* pow2) {
   const float mf = __fmul_rn(m, a.f), d = fmaf(z, a.f, -mf);

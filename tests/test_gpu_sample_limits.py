@@ -6,6 +6,7 @@ import torch
 
 from oracle import ends as oe
 from test_gpu_sample import B, FILTERS, _check, _draw, _numbers, _put  # noqa: F401
+from test_sample_weights_host import UNIT, bound, weight
 
 pytestmark = pytest.mark.gpu
 
@@ -75,3 +76,26 @@ def test_smallest_masses(B, vocab, dtype):
         for kw in (dict(), dict(min_p=1e-14), dict(top_k=vocab - 1) if vocab > 2 else dict()):
             ids, _ = _draw(B, z, u, **kw)
             assert ids[0] == (min(want, vocab - 2) if "top_k" in kw else want), (power, kw)
+
+
+@pytest.mark.parametrize("third", [False, True])
+@pytest.mark.parametrize("scale", [1.0, 1e-38])
+def test_masses_are_within_the_headers_bound(B, scale, third):
+    """Two tokens of weights 1 and w: at a share of 1 / (1 + w') the second is kept for a mass above w', so that shares on both sides of
+    the bound show whether the mass lies within it.  Half of the logits are those whose restated mass is off by the most."""
+    scale = float(np.float32(scale))
+    rng = np.random.default_rng(4)
+    x = (-rng.uniform(0.01, min(10.0, 3.3e38 * scale), 200000) / scale).astype(np.float32)
+    exact, _, _ = weight(x, 0.0, scale)
+    w = np.exp(x.astype(np.longdouble) * np.longdouble(scale))
+    off = np.abs(exact * np.longdouble(UNIT) / w - 1)
+    worst = np.argsort(-off.astype(np.float64))[:60]
+    u = torch.tensor([[0.0, 1.0 - 2.0 ** -24]]).cuda()
+    ids = torch.empty(1, dtype=torch.int32, device="cuda")
+    for i in [*worst, *range(60)]:
+        z = torch.tensor([[0.0, x[i], -np.inf][:3 if third else 2]], device="cuda")
+        for sign, kept in ((1, 0), (-1, 1)):
+            edge = w[i] * (1 + sign * np.longdouble(bound())) + sign * UNIT / 2
+            p = float(1 / (1 + edge)) * (1 - sign * 2.0 ** -51)
+            B.sgd_kernel_sample(z, u, ids, top_k=2 if third else 0, top_p=p, scale=scale)
+            assert int(ids) == kept, (float(x[i]), sign)
