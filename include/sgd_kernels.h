@@ -305,9 +305,9 @@ SGD_API int sgd_kernel_sample(const void* logits, int dtype, int64_t ld, int row
 
 /*
  * out[r, :] = scale * table[ids[r], :], rounded once from fp32 (out of fp16's range: inf); zeros where ids[r] is not in [0, vocab)
- * (padding).  table [vocab, d] of type dtype, rows ld elements apart; ids int32 [rows]; out [rows, d] of type
- * out_dtype, rows ld_out elements apart; both aligned to their elements alone.  1 <= d <= 2^20.  out must not overlap
- * the table or the ids (SGD_ERR_ARG).
+ * (padding; a model's own stem, SGD_STEM_EMBED, takes the table's first or last row there).  table [vocab, d] of type dtype, rows
+ * ld elements apart; ids int32 [rows]; out [rows, d] of type out_dtype, rows ld_out elements apart; both aligned to their
+ * elements alone.  1 <= d <= 2^20.  out must not overlap the table or the ids (SGD_ERR_ARG).
  */
 SGD_API int sgd_kernel_embedding(const void* table, int dtype, int64_t ld, int vocab, int d, const int32_t* ids, int rows, float scale,
                                  void* out, int out_dtype, int64_t ld_out, void* stream);

@@ -425,7 +425,7 @@ def sgd_kernel_sample(logits, uniforms, ids, logprobs=None, scale=1.0, top_k=0, 
 
 def sgd_kernel_embedding(table, ids, out, scale=1.0, stream=None):
     """out [rows, d] = scale * table[ids] for table [vocab, d] and ids int32 [rows], table and out of any of the three types and
-    any row stride; zeros where an id is not in the table."""
+    any row stride; zeros where an id is not in the table (a Denoiser's stem takes the first or last row there)."""
     import torch
     kind, ld = _rows(table, "table")
     okind, ldo = _rows(out, "out")
