@@ -160,3 +160,16 @@ def test_overlaps_of_the_largest_matrices(lib):
     huge = dict(table=P, dtype=2, ld=1 << 40, vocab=2 ** 31 - 1, d=8, ids=P >> 1)
     for row in (1, 3, 1 << 20):
         assert _embedding(lib, **huge, rows=1, out=P + (row << 42) + 16) == ARG and b"overlaps" in lib.sgd_last_error()
+
+
+@pytest.mark.parametrize("rows,d,chunk", [(1, 1, 8), (17, 300, 8), (1000, 4096, 8), (4000, 1024, 8), (4103, 4096, 8), (4104, 4096, 16), (8207, 4096, 16),
+                                          (8208, 4096, 32), (16391, 1024, 8), (16392, 1024, 16), (32783, 64, 16), (32784, 64, 32), (65537, 1024, 32),
+                                          (1 << 20, 64, 32), (6144, 64, 8), (6145, 64, 8)])
+def test_embedding_grad_workspace(lib, rows, d, chunk):
+    """Tokens and order, twice above the 6144 rows that are sorted by counting, with 1 KB of counts per 1024 rows there; two rows of partial sums
+    per chunk of 8, 16 or 32 rows: the largest that leaves 2048 pieces of 1024 columns, or 8."""
+    n = C.c_int64(0)
+    assert lib.sgd_kernel_embedding_grad_workspace(rows, 1000, d, C.byref(n)) == OK
+    sums = 8 * -(-rows // chunk) * (-(-d // 8) * 8)
+    sort = 8 * rows if rows <= 6144 else 16 * rows
+    assert sums + sort <= n.value <= sums + sort + (0 if rows <= 6144 else rows + 1024) + 6 * 256

@@ -99,3 +99,30 @@ def test_masses_are_within_the_headers_bound(B, scale, third):
             p = float(1 / (1 + edge)) * (1 - sign * 2.0 ** -51)
             B.sgd_kernel_sample(z, u, ids, top_k=2 if third else 0, top_p=p, scale=scale)
             assert int(ids) == kept, (float(x[i]), sign)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("vocab", [700, 5000, 40000])
+def test_cuts_among_equal_logits(B, vocab, dtype):
+    """Shares that fall between two tokens of equal weight: the cut goes by the token."""
+    z = np.zeros((8, vocab))
+    z[4:] = -2.5
+    z = _put(z, dtype)
+    for i, kw in enumerate([dict(top_p=0.37), dict(top_p=0.9), dict(min_p=1.0, top_p=0.7), dict(top_k=600, top_p=0.61),
+                            dict(min_p=0.3, top_p=0.93, top_k=499)]):
+        k = min(kw.get("top_k", vocab), vocab)
+        n = round(kw["top_p"] * k)  # the share of n tokens and 0.4 of another: n + 1 are kept
+        kw["top_p"] = (n + 0.4) / k
+        mask, near = oe.kept(z[0].double().cpu().numpy(), **kw)
+        assert mask.sum() == n + 1 and mask[:n + 1].all() and near > 9e-9
+        u = _numbers(8, i)
+        u[0] = u[4] = 1.0 - 2.0 ** -24  # the last one that is kept
+        ids, lp = _draw(B, z, u, **kw)
+        assert ids[0] == n and ids[4] == n
+        far = 0
+        for r in range(8):
+            want, _, near = oe.sample(z[r].double().cpu().numpy(), u[r].double().numpy(), **kw)
+            if near > 9e-9:
+                far += 1
+                assert ids[r] == want
+        assert far >= 7
