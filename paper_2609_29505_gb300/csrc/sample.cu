@@ -28,13 +28,14 @@
 // Many rows: a CTA of 256 threads each (64 or 128 for short rows), three or four per SM, so that one's search hides
 // behind the others' reading.  Few: a cluster reads a row, and takes the bracket between the bounds together.
 //
-// Measured (GB300, replayed from a graph; a copy moves 6.7 TB/s): every token of 2048 of 4096 x 126464 fp16 92 us = 5.6 TB/s, of 1024 x
+// Measured (GB300, replayed from a graph; a copy moves 6.7 TB/s): every token of 2048 of 4096 x 126464 fp16 93 us = 5.6 TB/s (over other
+// buffers of the same size up to 156, where a copy and the scoring kernel take as long as everywhere: not known why), of 1024 x
 // 126464 fp32 81 us = 6.4: HBM, and for 16-bit logits the issue slots (60% busy) and exponentials (73% of their rate).  A persistent
 // form with 16 streaming warps per SM and finishing warps was slower everywhere (96 and 83 us; 1500 x 126464 147 against 135).
-// 1003 x 32003 fp32 with every filter 47 us: a row is 18 thousand clocks of reading and 15 of steps one after another.
-// 1024 x 126464 bf16, top-p 0.9 of a broad distribution (2900 tokens): 330 us: 200 thousand clocks a row, half of them the
+// 1003 x 32003 fp32 with every filter 46 us: a row is 18 thousand clocks of reading and 15 of steps one after another.
+// 1024 x 126464 bf16, top-p 0.9 of a broad distribution (2900 tokens): 336 us: 200 thousand clocks a row, half of them the
 // bracket (300 instructions a block), in 2.25 rounds of 456 rows; two or four CTAs per SM instead of three: 347 and 336 us.
-// One row of 126464: 5.8 us, with top-p 17 to 27, latency.
+// One row of 126464: 5.8 us, with top-p 17 to 30, latency; 634 where tens of thousands of tokens are kept, which the row is searched for.
 #include <math.h>
 
 #include "sample.cuh"
