@@ -319,9 +319,11 @@ def _tensor(t, name, dtype, shape, device):
     raise ValueError(f"{name} must be contiguous")
 
 
-def _size(rows, width, name):
-    if rows >= 2 ** 31 or width >= 2 ** 31:
-        raise ValueError(f"{name} has more rows or columns than a 32-bit integer holds")
+_MOST = 2 ** 31 - 1  # rows, columns
+
+
+def _too_many(name):
+    raise ValueError(f"{name} has more rows or columns than a 32-bit integer holds")
 
 
 def _id(value, name):
@@ -339,7 +341,8 @@ def _rows(t, name):
     if t.dim() != 2 or not t.is_cuda:
         raise ValueError(f"{name} must be a 2-d tensor on a CUDA device")
     rows, vocab = t.shape
-    _size(rows, vocab, name)
+    if rows > _MOST or vocab > _MOST:
+        _too_many(name)
     ld, step = t.stride()
     if step != 1 and vocab > 1:
         raise ValueError(f"the rows of {name} must be dense")
@@ -517,7 +520,8 @@ def sgd_kernel_norm_grad(dout, h, kind, dh=None, g=None, b=None, scale=None, row
         raise ValueError("h must be a 2-d tensor on a CUDA device")
     shape, device = h.shape, h.device
     rows, d = shape
-    _size(rows, d, "h")
+    if rows > _MOST or d > _MOST:
+        _too_many("h")
     code = _dtypes().get(dout.dtype)
     if code is None:
         raise TypeError(f"dout must be float16, bfloat16 or float32, not {dout.dtype}")

@@ -2030,25 +2030,33 @@ int sgd_kernel_distill(const void* logits, int dtype, int64_t ld, int rows, int 
 
 namespace {
 
-// Memory of an argument: rows of `width` bytes, `stride` bytes apart (the products pass 64 bits for the largest rows and strides).
-using Wide = __int128;
+// Memory of an argument: rows of `width` bytes, `stride` bytes apart; `end` is where the last one ends, or the largest address.
 struct Span {
-  Wide at, rows, width, stride;
+  uintptr_t at, end;
+  int64_t rows, width, stride;
 };
 Span matrix(const void* at, int64_t rows, int64_t ld, int64_t width, int size) {
-  const Wide from = static_cast<Wide>(reinterpret_cast<uintptr_t>(at));
-  if (!at || rows < 1 || width < 1) return {from, 0, 0, 1};
-  if (ld == width || rows == 1) return {from, 1, static_cast<Wide>(rows) * width * size, 1};  // one piece
-  return {from, rows, static_cast<Wide>(width) * size, static_cast<Wide>(ld) * size};
+  if (!at || rows < 1 || width < 1) return {0, 0, 0, 0, 1};
+  if (ld == width || rows == 1) {  // one piece
+    width *= rows;
+    rows = 1;
+    ld = width;
+  }
+  Span s{reinterpret_cast<uintptr_t>(at), 0, rows, width * size, ld * size};
+  uintptr_t n;
+  if (__builtin_mul_overflow(static_cast<uintptr_t>(rows - 1), static_cast<uintptr_t>(s.stride), &n) ||
+      __builtin_add_overflow(n, static_cast<uintptr_t>(s.width), &n) || __builtin_add_overflow(n, s.at, &s.end))
+    s.end = UINTPTR_MAX;
+  return s;
 }
 Span vector(const void* at, int64_t n, int size = 4) { return matrix(at, 1, n, n, size); }
 // Whether two have a byte in common; matrices of different strides, whether what lies between their first and last bytes has.
 bool overlap(const Span& a, const Span& b) {
-  if (a.rows == 0 || b.rows == 0) return false;
-  if (a.at >= b.at + (b.rows - 1) * b.stride + b.width || b.at >= a.at + (a.rows - 1) * a.stride + a.width) return false;
+  if (a.at >= b.end || b.at >= a.end) return false;
   if (a.rows > 1 && b.rows > 1 && a.stride != b.stride) return true;
   // rows i of a and j of b have one where (i - j) S lies between d - a.width and d + b.width
-  const Wide S = a.rows > 1 ? a.stride : b.stride, d = b.at - a.at, from = d - a.width;
+  using Wide = __int128;
+  const Wide S = a.rows > 1 ? a.stride : b.stride, d = static_cast<Wide>(b.at) - static_cast<Wide>(a.at), from = d - a.width;
   Wide k = from >= 0 ? from / S + 1 : -((-from + S - 1) / S) + 1;
   if (k < 1 - b.rows) k = 1 - b.rows;
   return k < a.rows && k * S < d + b.width;
